@@ -3,7 +3,8 @@
  *
  * The library quantizes token activations with token-group scales (DSTG) whose clip
  * radius is projected by two bounds (DCRP), quantizes weights per output channel, and
- * runs the W4A4 linear layer on the 4-bit codes.
+ * runs the W4A4 linear layer on the 4-bit codes.  Beside them stand a linear layer on 8-bit floating point
+ * codes with its quantizers, and the norm and rotation of queries and keys that follows a qkv layer.
  *
  * Conventions shared by every call
  *   - Unless a parameter is marked HOST, pointers are DEVICE pointers owned by the caller.
@@ -20,7 +21,7 @@
  *   - The library allocates no device memory.  tdq_quant_linear_host creates two streams and
  *     a few events per device on first use and keeps them for the life of the process; no
  *     other call creates CUDA objects.
- *   - Non-finite inputs (NaN, Inf) give unspecified codes; they never fault.
+ *   - Non-finite inputs (NaN, Inf) give unspecified 4-bit codes (the 8-bit calls say what they give); they never fault.
  *
  * Notation (the paper's): M = B*N tokens, C = I input channels, O output channels,
  * g group size, K = C_pad / g groups per token with C_pad = g * ceil(C / g),
@@ -46,7 +47,7 @@ typedef enum {
     TDQ_ERR_DEVICE_TIMEOUT = 6  /* a bounded device-side wait ran out (see workspace status) */
 } tdq_status;
 
-typedef enum { TDQ_F32 = 0, TDQ_BF16 = 1, TDQ_F16 = 2 /* outputs of the linear layer only */ } tdq_dtype;
+typedef enum { TDQ_F32 = 0, TDQ_BF16 = 1, TDQ_F16 = 2 /* of the 4-bit calls only the linear layer's outputs */ } tdq_dtype;
 
 /* Which DCRP bounds take part in the projection (Algorithm S1 step 4; the ablation
  * variants of Table S6).  Both = COD-TDQ, neither = DSTG only. */
@@ -267,6 +268,83 @@ tdq_status tdq_w4a4_linear_static(const uint8_t* xcodes, const float* xscale, co
                                   const float* wscale, const float* bias, int64_t M, int64_t I_pad, int64_t O,
                                   int32_t group_size, void* y, tdq_dtype y_dtype, int64_t y_row_stride,
                                   int32_t wait, void* cuda_stream);
+
+/*
+ * The 8-bit floating point layer, for layers that do not stand four bits (the paper has no counterpart): E4M3 codes with a
+ * float32 scale for each block of 128 channels of a token, and of 128 x 128 of a weight matrix.
+ *
+ * Quantizer of activations.  For token m and block k (channels 128k .. 128k+127, zeros behind C):
+ *   a = max(max |x|, 2^-64);  scale = a / 448;  r = 448 / a;  code = E4M3(x r)   (each operation in binary32, the codes
+ *   nearest even, at most 448 in magnitude).  A block with a NaN or an infinity gets scale NaN and codes NaN.
+ *   x       [B*N rows, C], float32, bf16 or fp16, rows row_stride_elems apart (>= C).  x and row pitch on the 16-byte grid
+ *           are read with vector loads, anything else element by element; the results are the same.
+ *   codes   [B*N, C_pad] bytes, C_pad = 128 ceil(C/128), 16-byte aligned; the codes behind C are 0 (NaN in a NaN block).
+ *   scale   [B*N, C_pad/128] float32.
+ * B*N == 0 is a no-op.  TDQ_ERR_UNSUPPORTED for 2^36 elements or more.
+ */
+tdq_status tdq_quantize_act_fp8(const void* x, tdq_dtype x_dtype, int64_t B, int64_t N, int64_t C,
+                                int64_t row_stride_elems, uint8_t* codes, float* scale, void* cuda_stream);
+
+/*
+ * Quantizer of weights: the same formula over blocks of 128 output channels x 128 input channels.
+ *   w       [O, I] row-major, contiguous, float32, bf16 or fp16.
+ *   wcodes  [O, I_pad] bytes, I_pad = 128 ceil(I/128), 16-byte aligned, codes behind I as above.
+ *   wscale  [ceil(O/128), I_pad/128] float32.
+ */
+tdq_status tdq_quantize_weight_fp8(const void* w, tdq_dtype w_dtype, int64_t O, int64_t I, uint8_t* wcodes,
+                                   float* wscale, void* cuda_stream);
+
+/*
+ * The linear layer on E4M3 codes, on the tensor cores' 8-bit floating point instructions:
+ *   y[m,o] = bias[o] + sum_k xscale[m,k] wscale[o/128,k] sum_{i in block k} x[m,i] w[o,i]
+ *   The sum over a block is the tensor core's, in binary32; across blocks acc = fma(sum, fl(xscale wscale), acc) in binary32, in
+ *   order of k, or in up to eight parts of consecutive blocks that are added in order (few tokens).  The same call gives the same bits.
+ *   xcodes [M, I_pad], xscale [M, I_pad/128], wcodes [O, I_pad], wscale [ceil(O/128), I_pad/128], bias NULL or [O] float32.
+ *   I_pad a multiple of 128.  Codes are any E4M3 bytes; a NaN code or scale makes the outputs it reaches NaN.
+ *   y      [M, O], y_dtype (float32, bf16 or fp16, rounded to nearest even from the float32 result), rows y_row_stride elements
+ *          apart (>= O).  Rows on the 16-byte grid are stored by the copy engine, others element by element.
+ *   workspace  at least tdq_fp8_linear_workspace_bytes(), 16-byte aligned: the status word that tdq_workspace_status() reads.  The call
+ *              clears it; one workspace must not be shared by calls that overlap in time.
+ * Alignment: xcodes, wcodes 16 bytes.
+ */
+tdq_status tdq_fp8_linear(const uint8_t* xcodes, const float* xscale, const uint8_t* wcodes, const float* wscale,
+                          const float* bias, int64_t M, int64_t I_pad, int64_t O, void* y, tdq_dtype y_dtype,
+                          int64_t y_row_stride, void* workspace, size_t workspace_bytes, void* cuda_stream);
+size_t tdq_fp8_linear_workspace_bytes(int64_t M, int64_t I_pad, int64_t O);
+
+/*
+ * What follows a qkv layer (the paper has no counterpart): the norm of every query and key head and the rotation by the token's positions,
+ * in one pass, in place or into other buffers.  For head x of D = head_dim channels, R = rotary_dim <= D (even):
+ *   with TDQ_ROPE_NORM   n_i = x_i w_i / sqrt(mean_j x_j^2 + eps)   (w == 1 where weight is NULL), else n = x;
+ *   pair i < R/2 is channels (i, i + R/2), with TDQ_ROPE_ADJACENT (2i, 2i+1):   t = positions[m, axis[i]] freq[i],
+ *   (n_a, n_b) -> (n_a cos t - n_b sin t, n_b cos t + n_a sin t);   channels from R on are n.
+ *   Angles are binary64 up to the fraction of a turn; everything else is binary32, rounded once when stored.
+ *   q, k       either may be NULL or have no heads.  Element (m, h, i) of x is x[m row_stride + h head_stride + i], of out
+ *              likewise; heads and rows of out must not overlap each other.  out == x (with the same strides) works in place;
+ *              otherwise out overlaps neither x, and the two outs do not overlap.  weight NULL or [D] float32.  A qkv matrix of the
+ *              linear layer is x = its first query or key channel, row_stride its pitch, head_stride D.
+ *   dtype      of x and out: float32, bf16 or fp16.
+ *   positions  [M, n_axes] int64;  freq [R/2] float64, radians per position;  axis [R/2] int32, the column of positions that
+ *              turns the pair (a number outside 0 .. n_axes-1 counts as the last column).  Unused when R == 0.
+ *   Pointers and strides on the 16-byte grid with D a multiple of 16 (float32: 8), R/2 of 8 (4) and D <= 512 (256) take the
+ *   vector kernel, anything else a slower general one.  M == 0 is a no-op.
+ */
+#define TDQ_ROPE_NORM 1u
+#define TDQ_ROPE_ADJACENT 2u
+typedef struct {
+    int32_t head_dim, rotary_dim, n_axes;
+    uint32_t flags;
+    float eps;
+} tdq_rope_params;
+typedef struct {
+    const void* x;
+    void* out;
+    const float* weight;
+    int64_t heads, row_stride, head_stride, out_row_stride, out_head_stride;   /* strides in elements */
+} tdq_rope_heads;
+tdq_status tdq_qk_norm_rope(const tdq_rope_heads* q /* HOST */, const tdq_rope_heads* k /* HOST */, tdq_dtype dtype,
+                            int64_t M, const tdq_rope_params* p /* HOST */, const int64_t* positions,
+                            const double* freq, const int32_t* axis, void* cuda_stream);
 
 /* Bytes of workspace tdq_w4a4_linear / tdq_quant_linear_fused need for this problem. */
 size_t tdq_linear_workspace_bytes(int64_t M, int64_t I_pad, int64_t O, int32_t group_size);

@@ -28,12 +28,23 @@ ENABLE_C1, ENABLE_C2, POW2_STEP = 1, 2, 4
 EXPORTS = ["tdq_default_act_params", "tdq_quantize_act", "tdq_quantize_weight", "tdq_w4a4_linear",
            "tdq_quant_linear_fused", "tdq_quant_linear_host", "tdq_quantize_act_nchw", "tdq_quantize_act_fixed", "tdq_w4a4_linear_pow2", "tdq_linear_workspace_bytes",
            "tdq_workspace_status", "tdq_status_string", "tdq_kernel_launch_count", "tdq_w4a4_linear_static",
-           "tdq_quantize_status", "tdq_selftest_wait_timeout", "tdq_fold_output_affine", "tdq_measure_mma_clocks"]
+           "tdq_quantize_status", "tdq_selftest_wait_timeout", "tdq_fold_output_affine", "tdq_measure_mma_clocks",
+           "tdq_quantize_act_fp8", "tdq_quantize_weight_fp8", "tdq_fp8_linear", "tdq_fp8_linear_workspace_bytes", "tdq_qk_norm_rope"]
 
 
 class ActParams(ctypes.Structure):
     _fields_ = [("group_size", ctypes.c_int32), ("tau", ctypes.c_float), ("zr", ctypes.c_float),
                 ("base_percentile", ctypes.c_float), ("flags", ctypes.c_uint32)]
+
+
+class RopeParams(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("n_axes", ctypes.c_int32),
+                ("flags", ctypes.c_uint32), ("eps", ctypes.c_float)]
+
+
+class RopeHeads(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("out", ctypes.c_void_p), ("weight", ctypes.c_void_p)] + [
+        (n, ctypes.c_int64) for n in ("heads", "row_stride", "head_stride", "out_row_stride", "out_head_stride")]
 
 
 _i64, _i32, _vp, _sz = ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p, ctypes.c_size_t
@@ -74,6 +85,17 @@ _lib.tdq_fold_output_affine.argtypes = [_vp, _vp, _vp, _vp, _i64, _vp, _vp, _vp]
 _lib.tdq_fold_output_affine.restype = ctypes.c_int
 _lib.tdq_measure_mma_clocks.argtypes = [_i32, _i32, _vp, _sz, ctypes.POINTER(ctypes.c_double), _vp]
 _lib.tdq_measure_mma_clocks.restype = ctypes.c_int
+_lib.tdq_quantize_act_fp8.argtypes = [_vp, ctypes.c_int, _i64, _i64, _i64, _i64, _vp, _vp, _vp]
+_lib.tdq_quantize_act_fp8.restype = ctypes.c_int
+_lib.tdq_quantize_weight_fp8.argtypes = [_vp, ctypes.c_int, _i64, _i64, _vp, _vp, _vp]
+_lib.tdq_quantize_weight_fp8.restype = ctypes.c_int
+_lib.tdq_fp8_linear.argtypes = [_vp, _vp, _vp, _vp, _vp, _i64, _i64, _i64, _vp, ctypes.c_int, _i64, _vp, _sz, _vp]
+_lib.tdq_fp8_linear.restype = ctypes.c_int
+_lib.tdq_fp8_linear_workspace_bytes.argtypes = [_i64, _i64, _i64]
+_lib.tdq_fp8_linear_workspace_bytes.restype = _sz
+_lib.tdq_qk_norm_rope.argtypes = [ctypes.POINTER(RopeHeads), ctypes.POINTER(RopeHeads), ctypes.c_int, _i64, ctypes.POINTER(RopeParams),
+                                  _vp, _vp, _vp, _vp]
+_lib.tdq_qk_norm_rope.restype = ctypes.c_int
 _lib.tdq_status_string.argtypes = [ctypes.c_int]
 _lib.tdq_status_string.restype = ctypes.c_char_p
 _lib.tdq_kernel_launch_count.argtypes = []
@@ -190,6 +212,56 @@ def quant_linear_host(x_host: torch.Tensor, wcodes, wscale, bias=None, params: A
     """tdq_quant_linear_host: x_host [M, C] (CPU, ideally pinned) in, y_host [M, O] (CPU) out.  The device buffers
     the call needs are allocated here.  Returns (y_host, workspace); synchronise the current stream before reading."""
     return _host.quant_linear_host(x_host, wcodes, wscale, bias, params, out_dtype, y_host)
+
+
+def quantize_act_fp8(x: torch.Tensor, *, codes=None, scale=None):
+    """tdq_quantize_act_fp8 on x [..., C] (last dim contiguous, rows equally spaced; float32, bfloat16 or float16).
+
+    Returns (codes float8_e4m3fn [M, C_pad], scale float32 [M, C_pad/128]), C_pad = C rounded up to 128."""
+    return _host.quantize_act_fp8(x, codes, scale)
+
+
+def quantize_weight_fp8(w: torch.Tensor, *, wcodes=None, wscale=None):
+    """tdq_quantize_weight_fp8 on w [O, I].  Returns (wcodes float8_e4m3fn [O, I_pad], wscale [ceil(O/128), I_pad/128])."""
+    return _host.quantize_weight_fp8(w, wcodes, wscale)
+
+
+FP8_WORKSPACE_BYTES = int(_lib.tdq_fp8_linear_workspace_bytes(1, 128, 1))   # of any size of layer
+
+
+def fp8_linear_workspace(device) -> torch.Tensor:
+    return torch.zeros((FP8_WORKSPACE_BYTES,), dtype=torch.uint8, device=device)
+
+
+def fp8_linear(xcodes, xscale, wcodes, wscale, bias=None, *, out_dtype=torch.float32, y=None, workspace=None):
+    """tdq_fp8_linear on codes and scales of quantize_act_fp8 and quantize_weight_fp8 (codes float8_e4m3fn, or uint8 with the same
+    bytes).  Returns y [M, O]."""
+    return _host.fp8_linear(xcodes, xscale, wcodes, wscale, bias, out_dtype, y, workspace)
+
+
+def rope_table(rotary_dim: int, sections=None, base: float = 10000.0, *, restart: bool = False, device="cuda"):
+    """(freq float64 [R/2], axis int32 [R/2]) for qk_norm_rope.
+
+    sections: how many of the R/2 pairs each column of the positions turns, in order (default: one column turns all).  Pair i
+    turns by base^(-2i/R) radians per position; with restart=True the count starts anew in each section, as image models with
+    a frequency range of their own per axis have it: pair j of a section of n by base^(-j/n)."""
+    half = rotary_dim // 2
+    sections = [half] if sections is None else [int(n) for n in sections]
+    if rotary_dim < 0 or rotary_dim % 2 or sum(sections) != half or min(sections, default=0) < 0 or not base > 0:
+        raise ValueError("rotary_dim must be even, base positive, and sections non-negative with sum rotary_dim / 2")
+    axis = torch.tensor([i for i, n in enumerate(sections) for _ in range(n)], dtype=torch.int32)
+    exponent = torch.cat([torch.arange(n, dtype=torch.float64) / max(n, 1) for n in (sections if restart else [half])])
+    return (float(base) ** -exponent).to(device), axis.to(device)
+
+
+def qk_norm_rope(q, k, positions, table, q_weight=None, k_weight=None, *, eps=1e-6, adjacent=False, q_out=None, k_out=None):
+    """tdq_qk_norm_rope on q [M, Hq, D] and k [M, Hk, D] (k may be None; channels adjacent in memory, any row and head stride,
+    so views of a qkv matrix work).
+
+    positions int64 [M, axes] (or [M]); table: rope_table()'s (freq, axis).  eps=None: rotation without the norm.
+    q_out, k_out: pass q and k themselves to work in place; new tensors if None.  Returns (q_out, k_out)."""
+    freq, axis = table
+    return _host.qk_norm_rope(q, k, positions, freq, axis, q_weight, k_weight, eps, adjacent, q_out, k_out)
 
 
 def workspace_status(workspace: torch.Tensor):

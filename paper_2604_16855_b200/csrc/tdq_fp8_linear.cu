@@ -1,0 +1,347 @@
+// tdq_fp8_linear: y[m,o] = bias[o] + sum_k xs[m,k] ws[o/128,k] sum_{i in block k} x[m,i] w[o,i] on E4M3 codes.
+//
+// The sum of a block of 128 channels is four tensor-core instructions (kind::f8f6f4, binary32 accumulator in TMEM); its two scales
+// change from block to block, so each block's sums are taken out of TMEM and added, scaled, to binary32 registers.
+// Two kernels: tiles of 256 x 256 by pairs of CTAs (tdq_fp8_pair.cu) for layers with enough of them, and here the one for few tokens.
+//
+// fp8_split_kernel.  Few tokens: the time is that of reading the weights once, so all SMs have to read, however few rows the output
+// has.  128 output channels are the instruction's 128 rows and NT tokens (16 .. 128) its columns; the contraction is cut in up to eight
+// parts, one CTA of a cluster each, whose sums meet in distributed shared memory and are added there in rank order: no
+// atomics, no workspace, the same bits every time.  Warp 0 loads (tensor maps, 16 KB of weights and the tokens' 128 bytes a stage), warp 1
+// issues, the others scale and add: a thread has one output channel and up to 32 tokens, whose factors xs * ws are laid out
+// in shared memory eight blocks at a time, before they are needed.
+#include "tdq_fp8.cuh"
+#include "tdq_tc.cuh"
+
+namespace tdq {
+
+bool fp8_operand_map(CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int box_rows) {
+    static const TensorMapEncodeFn encode = [] {
+        void* fn = nullptr;
+        cudaDriverEntryPointQueryResult res;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &res) != cudaSuccess || res != cudaDriverEntryPointSuccess)
+            fn = nullptr;
+        return reinterpret_cast<TensorMapEncodeFn>(fn);
+    }();
+    if (!encode) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)cols};
+    const cuuint32_t box[2] = {(cuuint32_t)kFp8Block, (cuuint32_t)box_rows};
+    const cuuint32_t elem_strides[2] = {1u, 1u};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(p), dims, strides, box, elem_strides, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+namespace {
+
+constexpr int kSplitMaxStages = 12;
+constexpr int kSplitMax = 8;                 // CTAs of a cluster
+constexpr int kSplitSlots = 4;               // accumulators in TMEM
+constexpr uint32_t kSplitCtrl = 1024;
+constexpr uint32_t kWBytes = 128 * 128;      // a stage's weights
+constexpr int kChunkF = 8;                   // blocks whose factors are laid out at a time
+constexpr int kSplitWarp0 = 4;               // first adding warp
+
+template <int NT> struct SplitShape {
+    static constexpr int kCols = NT < 32 ? NT : 32;          // tokens per adding thread
+    static constexpr int kWarps = 4 * (NT / kCols);
+    static constexpr int kThreads = (kSplitWarp0 + kWarps) * 32;
+    static constexpr uint32_t kStage = kWBytes + NT * 128;
+    static constexpr uint32_t kTable = kChunkF * kCols * 4;  // a warp's factors
+    static constexpr uint32_t kIdesc = (1u << 4) | ((uint32_t)(NT >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+    static constexpr uint32_t kFixed = kSplitCtrl + 1024 + kWarps * kTable;
+};
+
+struct SplitCtrl {
+    uint64_t full[kSplitMaxStages], empty[kSplitMaxStages];
+    uint64_t tfull[kSplitSlots], tempty[kSplitSlots];
+};
+static_assert(sizeof(Ctrl) + sizeof(SplitCtrl) <= kSplitCtrl, "control block outgrew its reservation");
+
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, uint64_t* bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+
+template <int NT>
+__global__ void __launch_bounds__(SplitShape<NT>::kThreads, NT == 128 ? 1 : 2)
+fp8_split_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap wmap) {
+    using Sh = SplitShape<NT>;
+    constexpr int CW = Sh::kCols;
+    extern __shared__ __align__(128) uint8_t smem_raw[];
+    Ctrl* c = reinterpret_cast<Ctrl*>(smem_raw);             // its abort flag and TMEM address; the barriers are g's
+    SplitCtrl* g = reinterpret_cast<SplitCtrl*>(smem_raw + sizeof(Ctrl));
+    const uint32_t sm_s = smem_u32(smem_raw);
+    const uint32_t ring_s = (sm_s + kSplitCtrl + 1023u) & ~1023u;
+    const uint32_t n_stages = (uint32_t)a.n_stages;
+    const int warp = uniform_warp(), lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kSplitMaxStages; ++i) { mbar_init(&g->full[i], 1); mbar_init(&g->empty[i], 1); }
+        for (int i = 0; i < kSplitSlots; ++i) { mbar_init(&g->tfull[i], 1); mbar_init(&g->tempty[i], Sh::kWarps); }
+        c->abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&c->tmem_base)), "n"(kSplitSlots * NT) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    pdl_wait();
+    pdl_trigger();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0u;
+    const uint32_t tmem_base = c->tmem_base;
+    const uint32_t split = (uint32_t)a.split, rank = split > 1 ? fp8_cluster_rank() : 0u;
+    const uint32_t tile = blockIdx.x / split;                // token tiles of an output tile follow each other: its weights stay in L2
+    const int ot = (int)(tile / (uint32_t)a.tiles_m), tt = (int)(tile - (uint32_t)ot * (uint32_t)a.tiles_m);
+    const int kb0 = (int)((int64_t)a.K * rank / split), n_kb = (int)((int64_t)a.K * (rank + 1) / split) - kb0;
+
+    if (warp == 0) {
+        // ------------------------------------------------------------ loads
+        uint32_t s = 0, ph = 1;
+        for (int i = 0; i < n_kb; ++i) {
+            wait_hot(smem_u32(&g->empty[s]), ph, c, a.status, 5u);
+            if (c->abort_flag) break;
+            if (elect_one()) {
+                const uint32_t dst = ring_s + s * Sh::kStage;
+                mbar_expect_tx(&g->full[s], Sh::kStage);
+                tma_load_2d(dst, &wmap, (kb0 + i) * (int)kFp8Block, ot * 128, &g->full[s]);
+                tma_load_2d(dst + kWBytes, &xmap, (kb0 + i) * (int)kFp8Block, tt * NT, &g->full[s]);
+            }
+            __syncwarp();
+            if (++s == n_stages) { s = 0; ph ^= 1; }
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------ MMA issue
+        uint32_t s = 0, ph = 0;
+        for (int i = 0; i < n_kb; ++i) {
+            const uint32_t slot = (uint32_t)i % kSplitSlots;
+            wait_hot(smem_u32(&g->tempty[slot]), (((uint32_t)i / kSplitSlots) & 1u) ^ 1u, c, a.status, 3u);
+            wait_hot(smem_u32(&g->full[s]), ph, c, a.status, 4u);
+            if (c->abort_flag) break;
+            tc_fence_after();
+            if (elect_one()) {
+                const uint64_t wd = sw_desc(ring_s + s * Sh::kStage), xd = sw_desc(ring_s + s * Sh::kStage + kWBytes);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) mma_f8(tmem_base + slot * NT, wd + 2 * k, xd + 2 * k, Sh::kIdesc, k ? 1u : 0u);
+                mma_commit(smem_u32(&g->empty[s]));
+                mma_commit(smem_u32(&g->tfull[slot]));
+            }
+            __syncwarp();
+            if (++s == n_stages) { s = 0; ph ^= 1; }
+        }
+    } else if (warp >= kSplitWarp0) {
+        // ------------------------------------------------------------ scaled sums
+        const int pw = warp - kSplitWarp0, quarter = warp & 3, cg = pw >> 2;
+        const uint32_t table_s = ring_s + n_stages * Sh::kStage + (uint32_t)pw * Sh::kTable;
+        const int64_t tok = (int64_t)tt * NT + cg * CW + lane;
+        const bool mine = lane < CW && tok < a.M;
+        const float* xs = a.xscale + (mine ? tok * a.K + kb0 : 0);
+        const float* ws = a.wscale + (int64_t)ot * a.K + kb0;
+        float f[kChunkF];
+#pragma unroll
+        for (int q = 0; q < kChunkF; ++q) f[q] = mine && q < n_kb ? __ldg(xs + q) * __ldg(ws + q) : 0.f;
+        uint64_t acc[CW / 2];
+#pragma unroll
+        for (int j = 0; j < CW / 2; ++j) acc[j] = 0ull;
+        uint32_t v[32];
+#pragma unroll
+        for (int q = 0; q < 32; ++q) v[q] = 0u;
+        for (int c0 = 0; c0 < n_kb && !c->abort_flag; c0 += kChunkF) {
+            __syncwarp();
+            if (lane < CW) {
+#pragma unroll
+                for (int q = 0; q < kChunkF; ++q) sts32(table_s + (uint32_t)(q * CW + lane) * 4u, __float_as_uint(f[q]));
+            }
+            __syncwarp();
+#pragma unroll
+            for (int q = 0; q < kChunkF; ++q) {
+                const int kb = c0 + kChunkF + q;
+                f[q] = mine && kb < n_kb ? __ldg(xs + kb) * __ldg(ws + kb) : 0.f;
+            }
+            const int n = min(kChunkF, n_kb - c0);
+#pragma unroll 1
+            for (int q = 0; q < n; ++q) {
+                const uint32_t i = (uint32_t)(c0 + q), slot = i % kSplitSlots;
+                wait_hot(smem_u32(&g->tfull[slot]), (i / kSplitSlots) & 1u, c, a.status, 2u);
+                if (c->abort_flag) break;
+                tc_fence_after();
+                const uint32_t tm = tmem_base + ((uint32_t)(quarter * 32) << 16) + slot * NT + cg * CW;
+                if constexpr (CW == 32) tmem_ld32(tm, v);
+                else tmem_ld16(tm, v);
+                tmem_ld_wait_on(v);
+                tc_fence_before();
+                __syncwarp();
+                mbar_arrive_lane0_s(smem_u32(&g->tempty[slot]), lane);
+#pragma unroll
+                for (int j = 0; j < CW / 4; ++j) {
+                    uint64_t f0, f1;
+                    lds128(table_s + (uint32_t)(q * CW + 4 * j) * 4u, f0, f1);
+                    fma2(acc[2 * j], pack2(v[4 * j], v[4 * j + 1]), f0);
+                    fma2(acc[2 * j + 1], pack2(v[4 * j + 2], v[4 * j + 3]), f1);
+                }
+            }
+        }
+        // the last instruction has read the ring; the sums take its place, token by token
+#pragma unroll
+        for (int j = 0; j < CW / 2; ++j) {
+            float lo, hi;
+            unpack2(acc[j], lo, hi);
+            const uint32_t at = ring_s + ((uint32_t)(cg * CW + 2 * j) * 128u + (uint32_t)(quarter * 32 + lane)) * 4u;
+            sts32(at, __float_as_uint(lo));
+            sts32(at + 512u, __float_as_uint(hi));
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (c->abort_flag) __nanosleep(1000000);                 // a wait gave up: give copies and tensor core a moment
+    if (split > 1) fp8_cluster_sync();
+    const int n_tok = (int)min((int64_t)NT, a.M - (int64_t)tt * NT);
+    const int64_t o0 = (int64_t)ot * 128;
+    for (uint32_t u = rank * Sh::kThreads + threadIdx.x; u < (uint32_t)n_tok * 32u; u += split * Sh::kThreads) {
+        const int64_t o = o0 + (u & 31u) * 4;
+        if (o >= a.O) continue;
+        float r[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (uint32_t p = 0; p < split; ++p) {
+            const float4 q = ld_cluster4(map_to_cta(ring_s + u * 16u, p));
+            r[0] += q.x; r[1] += q.y; r[2] += q.z; r[3] += q.w;
+        }
+        const int left = (int)min((int64_t)4, a.O - o);
+        if (a.bias) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (j < left) r[j] += __ldg(a.bias + o + j);
+        }
+        const int64_t at = ((int64_t)tt * NT + (u >> 5)) * a.y_stride + o;
+        if (a.y_type == TDQ_F32) {
+            float* y = reinterpret_cast<float*>(a.y) + at;
+            if (a.y_vec && left == 4) *reinterpret_cast<float4*>(y) = make_float4(r[0], r[1], r[2], r[3]);
+            else
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (j < left) y[j] = r[j];
+        } else {
+            uint16_t* y = reinterpret_cast<uint16_t*>(a.y) + at;
+            const uint32_t w0 = pack16(r[0], r[1], a.y_type == TDQ_F16), w1 = pack16(r[2], r[3], a.y_type == TDQ_F16);
+            if (a.y_vec && left == 4) *reinterpret_cast<uint2*>(y) = make_uint2(w0, w1);
+            else
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (j < left) y[j] = (uint16_t)((j & 2 ? w1 : w0) >> (16 * (j & 1)));
+        }
+    }
+    if (split > 1) fp8_cluster_sync();                       // no CTA leaves while another reads its sums
+    if (warp == 2)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "n"(kSplitSlots * NT) : "memory");
+}
+
+// The kernel divides the blocks in `split` nearly equal parts; a part costs its blocks and, when there is more than one, about
+// two blocks' time for meeting.
+int choose_split(int64_t tiles, int K, int n_sm) {
+    int best = 1;
+    int64_t best_cost = INT64_MAX;
+    for (int s = 1; s <= kSplitMax && s <= K; ++s) {
+        const int64_t waves = (tiles * s + n_sm - 1) / n_sm;
+        const int64_t cost = waves * ((K + s - 1) / s + (s > 1 ? 2 : 0));
+        if (cost < best_cost) { best_cost = cost; best = s; }
+    }
+    return best;
+}
+
+template <int NT>
+tdq_status launch_split(Fp8Args a, const uint8_t* xcodes, const CUtensorMap& wmap, int n_sm, int dev, cudaStream_t stream) {
+    using Sh = SplitShape<NT>;
+    CUtensorMap xmap;
+    if (!fp8_operand_map(&xmap, xcodes, a.M, (int64_t)a.K * kFp8Block, NT)) return TDQ_ERR_CUDA;
+    const int64_t tiles_m = (a.M + NT - 1) / NT, tiles_n = fp8_blocks(a.O), tiles = tiles_m * tiles_n;
+    if (tiles > (int64_t)INT32_MAX / kSplitMax) return TDQ_ERR_UNSUPPORTED;
+    a.split = choose_split(tiles, a.K, n_sm);
+    a.tiles_m = (int32_t)tiles_m;
+    a.tiles_n = (int32_t)tiles_n;
+    // One CTA per SM with a deep ring while there is an SM for each, else two that share an SM.  Two CTAs of clusters that wait for each
+    // other must both get their TMEM columns (512 in all): at least 77 KB a CTA leaves room for two, and the 512 columns of NT = 128
+    // come with so much shared memory that no other of these CTAs fits beside them.
+    const int per_cta = (tiles * a.split <= n_sm || NT == 128) ? kSmemLimit : 113 * 1024;
+    const int per = (a.K + a.split - 1) / a.split;
+    const int least = ((NT == 128 ? 152 : 77) * 1024 - (int)Sh::kFixed + (int)Sh::kStage - 1) / (int)Sh::kStage;
+    int stages = (per_cta - (int)Sh::kFixed) / (int)Sh::kStage;
+    stages = stages > kSplitMaxStages ? kSplitMaxStages : stages;
+    a.n_stages = stages < per ? stages : per > least ? per : least;
+    const uint32_t smem = Sh::kFixed + (uint32_t)a.n_stages * Sh::kStage;
+    static std::atomic<uint64_t> smem_done{0};
+    if (allow_smem(fp8_split_kernel<NT>, kSmemLimit, smem_done, dev) != cudaSuccess) return TDQ_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(tiles * a.split));
+    cfg.blockDim = dim3(Sh::kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = (unsigned)a.split;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    if (cudaLaunchKernelEx(&cfg, fp8_split_kernel<NT>, a, xmap, wmap) != cudaSuccess) return TDQ_ERR_CUDA;
+    g_launch_count.fetch_add(1, std::memory_order_relaxed);
+    return TDQ_OK;
+}
+
+}  // namespace
+}  // namespace tdq
+
+using namespace tdq;
+
+extern "C" size_t tdq_fp8_linear_workspace_bytes(int64_t, int64_t, int64_t) { return kWorkspaceHeader; }
+
+extern "C" tdq_status tdq_fp8_linear(const uint8_t* xcodes, const float* xscale, const uint8_t* wcodes, const float* wscale, const float* bias,
+                                     int64_t M, int64_t I_pad, int64_t O, void* y, tdq_dtype y_dtype, int64_t y_row_stride, void* workspace,
+                                     size_t workspace_bytes, void* cuda_stream) {
+    if (M < 0 || O < 0 || I_pad <= 0 || I_pad % kFp8Block || y_row_stride < O) return TDQ_ERR_INVALID_ARG;
+    if (y_dtype != TDQ_F32 && y_dtype != TDQ_BF16 && y_dtype != TDQ_F16) return TDQ_ERR_INVALID_ARG;
+    if (M == 0 || O == 0) return TDQ_OK;
+    if (!xcodes || !xscale || !wcodes || !wscale || !y) return TDQ_ERR_INVALID_ARG;
+    if (!workspace || workspace_bytes < kWorkspaceHeader) return TDQ_ERR_WORKSPACE;
+    const uintptr_t esz = y_dtype == TDQ_F32 ? 4 : 2;
+    const auto off = [](const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; };
+    if (off(xcodes, 16) || off(wcodes, 16) || off(workspace, 16) || off(xscale, 4) || off(wscale, 4) || off(bias, 4) || off(y, esz)) return TDQ_ERR_ALIGNMENT;
+    // coordinates of the copies are 32-bit
+    if (M > INT32_MAX - 256 || O > INT32_MAX - 256 || I_pad > INT32_MAX - 256) return TDQ_ERR_UNSUPPORTED;
+    int dev = 0;
+    const int n_sm = current_device_sm_count(&dev);
+    if (n_sm <= 0) return TDQ_ERR_CUDA;
+    Fp8Args a = {};
+    a.xscale = xscale;
+    a.wscale = wscale;
+    a.bias = bias;
+    a.y = y;
+    a.M = M;
+    a.O = O;
+    a.y_stride = y_row_stride;
+    a.K = (int32_t)(I_pad / kFp8Block);
+    a.y_type = y_dtype;
+    a.y_vec = !off(y, 16) && (y_row_stride * (int64_t)esz) % 16 == 0;
+    a.status = reinterpret_cast<uint32_t*>(workspace);
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+    CUtensorMap wmap;
+    if (!fp8_operand_map(&wmap, wcodes, O, I_pad, 128)) return TDQ_ERR_CUDA;
+    if (M > 128 && ((M + 255) / 256) * ((O + 255) / 256) >= n_sm / 4) {
+        CUtensorMap xmap;
+        if (!fp8_operand_map(&xmap, xcodes, M, I_pad, 128)) return TDQ_ERR_CUDA;
+        return launch_fp8_pair(a, xmap, wmap, n_sm, dev, st);
+    }
+    if (M <= 16) return launch_split<16>(a, xcodes, wmap, n_sm, dev, st);
+    if (M <= 32) return launch_split<32>(a, xcodes, wmap, n_sm, dev, st);
+    if (M <= 64) return launch_split<64>(a, xcodes, wmap, n_sm, dev, st);
+    return launch_split<128>(a, xcodes, wmap, n_sm, dev, st);
+}

@@ -1,0 +1,294 @@
+// tdq_quantize_act_fp8, tdq_quantize_weight_fp8: E4M3 codes with a binary32 scale for each block of 128 channels of a token, or of
+// 128 x 128 of a weight matrix.
+//
+//   a = max(max |x|, 2^-64);   scale = fl(a / 448);   r = fl(448 / a);   code = E4M3(fl(x r)), nearest, ties to even
+//
+// Both quotients are IEEE divisions, one of each per block; an element costs one product, so that codes are those of the
+// formula bit for bit.  |x r| <= 448 (1 + 2^-23) rounds to 448 at most.  The floor 2^-64 keeps scale and r normal numbers.
+// A block with a NaN or an infinity gets scale NaN and codes NaN (0x7F): patterns of magnitudes compare as unsigned
+// numbers, with NaN above infinity above everything finite, so the maximum carries them along.
+//
+// Bound by HBM: 2 (4) bytes in and 1 out an element, the input read once.  A block of a token is eight threads of sixteen
+// channels each (16-byte loads, a 16-byte store, three shuffles for the maximum); rows off the 16-byte grid are read by a warp per
+// block, four channels a thread.  A weight block stays in the registers of 256 threads between its maximum and its codes.
+#include "tdq_fp8.cuh"
+
+namespace tdq {
+namespace {
+
+constexpr int kThreadsA = 256;
+constexpr int kThreadsW = 256;
+
+template <int DT> struct Elem { using T = uint16_t; };   // DT: tdq_dtype
+template <> struct Elem<TDQ_F32> { using T = float; };
+
+template <int DT>
+__device__ __forceinline__ float widen(typename Elem<DT>::T v) {
+    if constexpr (DT == TDQ_F32) return v;
+    else if constexpr (DT == TDQ_BF16) return __uint_as_float((uint32_t)v << 16);
+    else return __half2float(__ushort_as_half(v));
+}
+// bit pattern of the larger magnitude of two words' elements, and of a word's own (as binary32)
+template <int DT>
+__device__ __forceinline__ uint32_t max_abs(uint32_t m, uint32_t w) {
+    if constexpr (DT == TDQ_F32) return max(m, w & 0x7fffffffu);
+    else return __vmaxu2(m, w & 0x7fff7fffu);
+}
+template <int DT>
+__device__ __forceinline__ uint32_t max_bits(uint32_t m) {
+    if constexpr (DT == TDQ_F32) return m;
+    else return __float_as_uint(widen<DT>((uint16_t)max(m & 0xffffu, m >> 16)));
+}
+// scale and reciprocal of a block whose largest magnitude has this pattern
+__device__ __forceinline__ void block_scale(uint32_t bits, float& scale, float& r) {
+    const float a = fmaxf(__uint_as_float(bits), kFp8Smallest);
+    scale = __fdiv_rn(a, kFp8Max);
+    r = __fdiv_rn(kFp8Max, a);
+    if (bits >= 0x7f800000u) scale = r = __uint_as_float(0x7fffffffu);
+}
+// two elements' codes, the first in the low byte
+__device__ __forceinline__ uint32_t cvt2(float lo, float hi) {
+    uint16_t v;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(v) : "f"(hi), "f"(lo));
+    return v;
+}
+__device__ __forceinline__ uint32_t cvt4(float a, float b, float c, float d, float r) {
+    return cvt2(__fmul_rn(a, r), __fmul_rn(b, r)) | cvt2(__fmul_rn(c, r), __fmul_rn(d, r)) << 16;
+}
+template <int DT>
+__device__ __forceinline__ void widen2(uint32_t w, float& lo, float& hi) {
+    if constexpr (DT == TDQ_BF16) {
+        lo = __uint_as_float(w << 16);
+        hi = __uint_as_float(w & 0xffff0000u);
+    } else {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+        lo = f.x;
+        hi = f.y;
+    }
+}
+// the codes of a 16-byte vector: one word (four binary32) or two (eight 16-bit elements)
+template <int DT>
+__device__ __forceinline__ void codes_of(const uint4& v, float r, uint32_t* out) {
+    if constexpr (DT == TDQ_F32) {
+        out[0] = cvt4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w), r);
+    } else {
+        float a, b, c, d;
+        widen2<DT>(v.x, a, b);
+        widen2<DT>(v.y, c, d);
+        out[0] = cvt4(a, b, c, d, r);
+        widen2<DT>(v.z, a, b);
+        widen2<DT>(v.w, c, d);
+        out[1] = cvt4(a, b, c, d, r);
+    }
+}
+// Elements [0, n) of a 16-byte vector one by one, the rest zero; n <= 0: nothing is read.
+template <int DT>
+__device__ __forceinline__ uint4 load_part(const typename Elem<DT>::T* p, int64_t n) {
+    constexpr int kPer = 16 / (int)sizeof(typename Elem<DT>::T);
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+        if (i < n) {
+            if constexpr (DT == TDQ_F32) w[i] = __float_as_uint(p[i]);
+            else w[i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
+        }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Rows on the 16-byte grid: a thread holds sixteen consecutive channels, eight threads a block of 128.
+template <int DT>
+__global__ void __launch_bounds__(kThreadsA) act_fp8_kernel(const typename Elem<DT>::T* __restrict__ x, uint32_t n_blocks, uint32_t K,
+                                                            int64_t C, int64_t stride, uint4* __restrict__ codes, float* __restrict__ scale) {
+    using T = typename Elem<DT>::T;
+    constexpr int kVecs = (int)sizeof(T);                  // 16-byte vectors a thread reads: 16 elements
+    constexpr int kPer = 16 / (int)sizeof(T);
+    pdl_wait();
+    pdl_trigger();
+    const uint32_t t = blockIdx.x * kThreadsA + threadIdx.x;
+    const uint32_t b = t >> 3;                             // block of 128
+    const bool on = b < n_blocks;
+    const uint32_t m = on ? b / K : 0u, k = on ? b - m * K : 0u;
+    const int64_t c0 = (int64_t)k * kFp8Block + (threadIdx.x & 7) * 16;
+    const T* src = x + (int64_t)m * stride + c0;
+    uint4 v[kVecs];
+    if (on && c0 + 16 <= C) {
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) v[i] = __ldg(reinterpret_cast<const uint4*>(src) + i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) v[i] = load_part<DT>(src + i * kPer, on ? C - c0 - i * kPer : 0);
+    }
+    uint32_t mx = 0;
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+        mx = max_abs<DT>(mx, v[i].x);
+        mx = max_abs<DT>(mx, v[i].y);
+        mx = max_abs<DT>(mx, v[i].z);
+        mx = max_abs<DT>(mx, v[i].w);
+    }
+#pragma unroll
+    for (int d = 1; d < 8; d <<= 1) mx = max_abs<DT>(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+    if (!on) return;
+    float s, r;
+    block_scale(max_bits<DT>(mx), s, r);
+    uint32_t out[4];
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) codes_of<DT>(v[i], r, out + i * (4 / kVecs));
+    codes[t] = make_uint4(out[0], out[1], out[2], out[3]);   // rows of C_pad codes follow each other without a gap
+    if ((threadIdx.x & 7) == 0) scale[b] = s;
+}
+
+// Rows anywhere: a warp takes kRagged blocks, their loads in flight together, a thread four consecutive channels of each.
+constexpr int kRagged = 4;
+template <int DT>
+__global__ void __launch_bounds__(kThreadsA) act_fp8_ragged_kernel(const typename Elem<DT>::T* __restrict__ x, uint32_t n_blocks, uint32_t K,
+                                                                   int64_t C, int64_t stride, uint32_t* __restrict__ codes,
+                                                                   float* __restrict__ scale) {
+    using T = typename Elem<DT>::T;
+    pdl_wait();
+    pdl_trigger();
+    const uint32_t b0 = (blockIdx.x * (kThreadsA / 32) + (threadIdx.x >> 5)) * kRagged;
+    const int lane = threadIdx.x & 31;
+    T v[kRagged][4];
+#pragma unroll
+    for (int i = 0; i < kRagged; ++i) {
+        const uint32_t b = b0 + i < n_blocks ? b0 + i : n_blocks - 1;
+        const uint32_t m = b / K, k = b - m * K;
+        const int64_t c0 = (int64_t)k * kFp8Block + lane * 4;
+        const T* src = x + (int64_t)m * stride + c0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[i][j] = c0 + j < C ? __ldg(src + j) : T(0);
+    }
+#pragma unroll
+    for (int i = 0; i < kRagged; ++i) {
+        if (b0 + i >= n_blocks) return;
+        float f[4];
+        uint32_t mx = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            f[j] = widen<DT>(v[i][j]);
+            mx = max(mx, __float_as_uint(f[j]) & 0x7fffffffu);
+        }
+        mx = __reduce_max_sync(0xffffffffu, mx);
+        float s, r;
+        block_scale(mx, s, r);
+        codes[(int64_t)(b0 + i) * 32 + lane] = cvt4(f[0], f[1], f[2], f[3], r);
+        if (lane == 0) scale[b0 + i] = s;
+    }
+}
+
+// One block of 128 x 128 weights in registers; VEC: rows on the 16-byte grid.
+template <int DT, bool VEC>
+__global__ void __launch_bounds__(kThreadsW) weight_fp8_kernel(const typename Elem<DT>::T* __restrict__ w, int64_t O, int64_t I, int64_t I_pad,
+                                                               uint8_t* __restrict__ codes, float* __restrict__ scale) {
+    using T = typename Elem<DT>::T;
+    constexpr int kPer = 16 / (int)sizeof(T);              // elements of a vector
+    constexpr int kAcross = kFp8Block / kPer;              // vectors of a row of the block
+    constexpr int kRows = kThreadsW / kAcross;             // rows per pass of the thread block
+    constexpr int kPasses = kFp8Block / kRows;
+    __shared__ uint32_t warp_max[kThreadsW / 32];
+    pdl_wait();
+    pdl_trigger();
+    const int64_t col = (int64_t)blockIdx.x * kFp8Block + (threadIdx.x % kAcross) * kPer;
+    const int64_t row0 = (int64_t)blockIdx.y * kFp8Block + threadIdx.x / kAcross;
+    uint4 v[kPasses];
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+        const int64_t row = row0 + i * kRows;
+        const T* src = w + row * I + col;
+        const int64_t n = row < O ? I - col : 0;
+        if (VEC && n >= kPer) v[i] = __ldg(reinterpret_cast<const uint4*>(src));
+        else v[i] = load_part<DT>(src, n);
+    }
+    uint32_t mx = 0;
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+        mx = max_abs<DT>(mx, v[i].x);
+        mx = max_abs<DT>(mx, v[i].y);
+        mx = max_abs<DT>(mx, v[i].z);
+        mx = max_abs<DT>(mx, v[i].w);
+    }
+    mx = __reduce_max_sync(0xffffffffu, max_bits<DT>(mx));
+    if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = mx;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kThreadsW / 32; ++i) mx = max(mx, warp_max[i]);
+    float s, r;
+    block_scale(mx, s, r);
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+        const int64_t row = row0 + i * kRows;
+        if (row >= O) break;
+        uint32_t out[2];
+        codes_of<DT>(v[i], r, out);
+        uint8_t* dst = codes + row * I_pad + col;
+        if constexpr (DT == TDQ_F32) *reinterpret_cast<uint32_t*>(dst) = out[0];
+        else *reinterpret_cast<uint2*>(dst) = make_uint2(out[0], out[1]);
+    }
+    if (threadIdx.x == 0) scale[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = s;
+}
+
+template <int DT>
+cudaError_t launch_act(const void* x, uint32_t n_blocks, uint32_t K, int64_t C, int64_t stride, uint8_t* codes, float* scale, cudaStream_t st) {
+    using T = typename Elem<DT>::T;
+    const T* p = reinterpret_cast<const T*>(x);
+    if (reinterpret_cast<uintptr_t>(x) % 16 == 0 && (stride * (int64_t)sizeof(T)) % 16 == 0)
+        return launch_pdl(act_fp8_kernel<DT>, dim3((n_blocks + kThreadsA / 8 - 1) / (kThreadsA / 8)), dim3(kThreadsA), 0, st, p, n_blocks, K, C, stride,
+                          reinterpret_cast<uint4*>(codes), scale);
+    constexpr uint32_t per = kThreadsA / 32 * kRagged;
+    return launch_pdl(act_fp8_ragged_kernel<DT>, dim3((n_blocks + per - 1) / per), dim3(kThreadsA), 0, st, p, n_blocks, K, C, stride,
+                      reinterpret_cast<uint32_t*>(codes), scale);
+}
+template <int DT>
+cudaError_t launch_weight(const void* w, int64_t O, int64_t I, uint8_t* codes, float* scale, cudaStream_t st) {
+    using T = typename Elem<DT>::T;
+    const T* p = reinterpret_cast<const T*>(w);
+    const int64_t I_pad = fp8_blocks(I) * kFp8Block;
+    const dim3 grid((unsigned)fp8_blocks(I), (unsigned)fp8_blocks(O));
+    if (reinterpret_cast<uintptr_t>(w) % 16 == 0 && (I * (int64_t)sizeof(T)) % 16 == 0)
+        return launch_pdl(weight_fp8_kernel<DT, true>, grid, dim3(kThreadsW), 0, st, p, O, I, I_pad, codes, scale);
+    return launch_pdl(weight_fp8_kernel<DT, false>, grid, dim3(kThreadsW), 0, st, p, O, I, I_pad, codes, scale);
+}
+bool known_dtype(tdq_dtype t) { return t == TDQ_F32 || t == TDQ_BF16 || t == TDQ_F16; }
+
+}  // namespace
+}  // namespace tdq
+
+using namespace tdq;
+
+extern "C" tdq_status tdq_quantize_act_fp8(const void* x, tdq_dtype x_dtype, int64_t B, int64_t N, int64_t C, int64_t row_stride_elems,
+                                           uint8_t* codes, float* scale, void* cuda_stream) {
+    if (!known_dtype(x_dtype) || B < 0 || N < 0 || C <= 0 || row_stride_elems < C) return TDQ_ERR_INVALID_ARG;
+    if (C > INT32_MAX || (N > 0 && B > INT64_MAX / N)) return TDQ_ERR_INVALID_ARG;
+    const int64_t M = B * N, K = fp8_blocks(C);
+    if (M == 0) return TDQ_OK;
+    if (!x || !codes || !scale) return TDQ_ERR_INVALID_ARG;
+    const uintptr_t esz = x_dtype == TDQ_F32 ? 4 : 2;
+    if (reinterpret_cast<uintptr_t>(x) % esz || reinterpret_cast<uintptr_t>(codes) % 16 || reinterpret_cast<uintptr_t>(scale) % 4) return TDQ_ERR_ALIGNMENT;
+    if (M > ((1 << 29) - 1024) / K) return TDQ_ERR_UNSUPPORTED;   // 2^36 elements; the kernels count their threads in 32 bits
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+    const uint32_t n = (uint32_t)(M * K);
+    cudaError_t e;
+    if (x_dtype == TDQ_F32) e = launch_act<TDQ_F32>(x, n, (uint32_t)K, C, row_stride_elems, codes, scale, st);
+    else if (x_dtype == TDQ_BF16) e = launch_act<TDQ_BF16>(x, n, (uint32_t)K, C, row_stride_elems, codes, scale, st);
+    else e = launch_act<TDQ_F16>(x, n, (uint32_t)K, C, row_stride_elems, codes, scale, st);
+    if (e == cudaSuccess) g_launch_count.fetch_add(1, std::memory_order_relaxed);
+    return cuda_status(e);
+}
+
+extern "C" tdq_status tdq_quantize_weight_fp8(const void* w, tdq_dtype w_dtype, int64_t O, int64_t I, uint8_t* wcodes, float* wscale,
+                                              void* cuda_stream) {
+    if (!known_dtype(w_dtype) || O < 0 || I <= 0) return TDQ_ERR_INVALID_ARG;
+    if (O == 0) return TDQ_OK;
+    if (!w || !wcodes || !wscale) return TDQ_ERR_INVALID_ARG;
+    const uintptr_t esz = w_dtype == TDQ_F32 ? 4 : 2;
+    if (reinterpret_cast<uintptr_t>(w) % esz || reinterpret_cast<uintptr_t>(wcodes) % 16 || reinterpret_cast<uintptr_t>(wscale) % 4) return TDQ_ERR_ALIGNMENT;
+    if (O > (int64_t)65535 * kFp8Block || I > INT32_MAX) return TDQ_ERR_UNSUPPORTED;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+    cudaError_t e;
+    if (w_dtype == TDQ_F32) e = launch_weight<TDQ_F32>(w, O, I, wcodes, wscale, st);
+    else if (w_dtype == TDQ_BF16) e = launch_weight<TDQ_BF16>(w, O, I, wcodes, wscale, st);
+    else e = launch_weight<TDQ_F16>(w, O, I, wcodes, wscale, st);
+    if (e == cudaSuccess) g_launch_count.fetch_add(1, std::memory_order_relaxed);
+    return cuda_status(e);
+}

@@ -53,8 +53,8 @@ tdq_dtype dtype_id(const at::Tensor& t) {
     switch (t.scalar_type()) {
         case at::kFloat: return TDQ_F32;
         case at::kBFloat16: return TDQ_BF16;
-        case at::kHalf: return TDQ_F16;   // outputs of the linear layer only; the library refuses it elsewhere
-        default: throw Bad{PyExc_TypeError, "tdq takes float32, bfloat16 or (for outputs) float16 tensors, got " + dtype_name(t.scalar_type())};
+        case at::kHalf: return TDQ_F16;   // the library refuses it where a call does not take it
+        default: throw Bad{PyExc_TypeError, "tdq takes float32, bfloat16 or (where the call says so) float16 tensors, got " + dtype_name(t.scalar_type())};
     }
 }
 at::ScalarType dtype_arg(PyObject* o) {
@@ -368,6 +368,164 @@ PyObject* quant_linear_host(PyObject* const* a) {
     return t;
 }
 
+// ---------------------------------------------------------------------------------------------- 8-bit floating point layer
+
+// A tensor that the caller passed for an output or operand: type, sizes, contiguity, device.
+void check_tensor(const char* name, const at::Tensor& t, std::initializer_list<at::ScalarType> types, at::IntArrayRef sizes, const at::Tensor& on) {
+    bool fits = false;
+    for (at::ScalarType s : types) fits = fits || t.scalar_type() == s;
+    if (!fits) throw Bad{PyExc_TypeError, std::string(name) + " must be " + dtype_name(*types.begin()) + ", got " + dtype_name(t.scalar_type())};
+    if (t.sizes() != sizes) {
+        std::string want, got;
+        for (int64_t n : sizes) want += (want.empty() ? "" : ", ") + std::to_string(n);
+        for (int64_t n : t.sizes()) got += (got.empty() ? "" : ", ") + std::to_string(n);
+        throw Bad{PyExc_ValueError, std::string(name) + " must be of size [" + want + "], got [" + got + "]"};
+    }
+    if (!t.is_contiguous()) throw Bad{PyExc_ValueError, std::string(name) + " must be contiguous"};
+    if (t.device() != on.device()) throw Bad{PyExc_ValueError, std::string(name) + " is on " + t.device().str() + ", not on " + on.device().str()};
+}
+constexpr int64_t kFp8Block = 128;
+int64_t fp8_blocks(int64_t n) { return (n + kFp8Block - 1) / kFp8Block; }
+
+// quantize_act_fp8(x, codes, scale)
+PyObject* quantize_act_fp8(PyObject* const* a) {
+    const at::Tensor& x = tensor(a[0]);
+    const at::Tensor *oc = opt_tensor(a[1]), *os = opt_tensor(a[2]);
+    need_cuda({&x, oc, os});
+    if (x.dim() < 1 || x.size(-1) < 1) throw Bad{PyExc_ValueError, "x must have channels"};
+    const int64_t C = x.size(-1), K = fp8_blocks(C);
+    const at::Tensor x2 = x.dim() == 2 ? x : x.reshape({x.numel() / C, C});
+    const int64_t M = x2.size(0);
+    if (C > 1 && M > 0 && x2.stride(1) != 1) throw Bad{PyExc_ValueError, "the channel axis must be contiguous"};
+    const tdq_dtype dt = dtype_id(x2);
+    if (oc) check_tensor("codes", *oc, {at::kFloat8_e4m3fn, at::kByte}, {M, K * kFp8Block}, x);
+    if (os) check_tensor("scale", *os, {at::kFloat}, {M, K}, x);
+    const at::Tensor codes = oc ? *oc : new_like(x, {M, K * kFp8Block}, at::kFloat8_e4m3fn);
+    const at::Tensor scale = os ? *os : new_like(x, {M, K}, at::kFloat);
+    check(call(x, [&](void* st) {
+              return tdq_quantize_act_fp8(ptr(x2), dt, 1, M, C, M > 1 ? x2.stride(0) : C, ptr<uint8_t>(codes), ptr<float>(scale), st);
+          }), "tdq_quantize_act_fp8");
+    return tuple2(codes, scale);
+}
+
+// quantize_weight_fp8(w, wcodes, wscale)
+PyObject* quantize_weight_fp8(PyObject* const* a) {
+    const at::Tensor& w0 = tensor(a[0]);
+    const at::Tensor *oc = opt_tensor(a[1]), *os = opt_tensor(a[2]);
+    need_cuda({&w0, oc, os});
+    if (w0.dim() != 2 || w0.size(1) < 1) throw Bad{PyExc_ValueError, "w must be a matrix [O, I]"};
+    const at::Tensor w = w0.contiguous();
+    const int64_t O = w.size(0), I = w.size(1), K = fp8_blocks(I), T = fp8_blocks(O);
+    const tdq_dtype dt = dtype_id(w);
+    if (oc) check_tensor("wcodes", *oc, {at::kFloat8_e4m3fn, at::kByte}, {O, K * kFp8Block}, w);
+    if (os) check_tensor("wscale", *os, {at::kFloat}, {T, K}, w);
+    const at::Tensor codes = oc ? *oc : new_like(w, {O, K * kFp8Block}, at::kFloat8_e4m3fn);
+    const at::Tensor scale = os ? *os : new_like(w, {T, K}, at::kFloat);
+    check(call(w, [&](void* st) {
+              return tdq_quantize_weight_fp8(ptr(w), dt, O, I, ptr<uint8_t>(codes), ptr<float>(scale), st);
+          }), "tdq_quantize_weight_fp8");
+    return tuple2(codes, scale);
+}
+
+// fp8_linear(xcodes, xscale, wcodes, wscale, bias, out_dtype, y, workspace)
+PyObject* fp8_linear(PyObject* const* a) {
+    const at::Tensor &xc = tensor(a[0]), &xs = tensor(a[1]), &wc = tensor(a[2]), &ws = tensor(a[3]);
+    const at::Tensor *bias = opt_tensor(a[4]), *oy = opt_tensor(a[6]), *ow = opt_tensor(a[7]);
+    need_cuda({&xc, &xs, &wc, &ws, bias, oy, ow});
+    if (xc.dim() != 2 || wc.dim() != 2) throw Bad{PyExc_ValueError, "xcodes and wcodes must be matrices"};
+    const int64_t M = xc.size(0), I_pad = xc.size(1), O = wc.size(0), K = I_pad / kFp8Block;
+    if (I_pad < 1 || I_pad % kFp8Block) throw Bad{PyExc_ValueError, "the codes' rows must be a multiple of 128 long"};
+    check_tensor("xcodes", xc, {at::kFloat8_e4m3fn, at::kByte}, {M, I_pad}, xc);
+    check_tensor("xscale", xs, {at::kFloat}, {M, K}, xc);
+    check_tensor("wcodes", wc, {at::kFloat8_e4m3fn, at::kByte}, {O, I_pad}, xc);
+    check_tensor("wscale", ws, {at::kFloat}, {fp8_blocks(O), K}, xc);
+    if (bias) check_tensor("bias", *bias, {at::kFloat}, {O}, xc);
+    if (ow) check_tensor("workspace", *ow, {at::kByte}, ow->sizes(), xc);
+    const at::Tensor y = oy ? *oy : new_like(xc, {M, O}, dtype_arg(a[5]));
+    check_y(y, &xc);
+    if (y.size(0) != M || y.size(1) != O) throw Bad{PyExc_ValueError, "y must be of size [" + std::to_string(M) + ", " + std::to_string(O) + "]"};
+    const tdq_dtype dt = dtype_id(y);
+    at::DataPtr own;
+    void* wsp = ow ? ow->data_ptr() : nullptr;
+    size_t wsp_bytes = ow ? (size_t)ow->numel() : 0;
+    if (!ow) {
+        c10::cuda::CUDAGuard guard(xc.device());
+        wsp_bytes = tdq_fp8_linear_workspace_bytes(M, I_pad, O);
+        own = c10::cuda::CUDACachingAllocator::get()->allocate(wsp_bytes);
+        wsp = own.get();
+    }
+    check(call(xc, [&](void* st) {
+              return tdq_fp8_linear(ptr<uint8_t>(xc), ptr<float>(xs), ptr<uint8_t>(wc), ptr<float>(ws), ptr<float>(bias), M, I_pad, O, ptr(y), dt,
+                                    M > 1 ? y.stride(0) : O, wsp, wsp_bytes, st);
+          }), "tdq_fp8_linear");
+    return THPVariable_Wrap(y);
+}
+
+// One side of the rotation: the strides of x and out, both [M, H, D].
+tdq_rope_heads rope_side(const char* name, const at::Tensor& x, const at::Tensor& out, const at::Tensor* weight, int64_t M, int64_t D) {
+    const int64_t H = x.size(1);
+    const auto last = [&](const at::Tensor& t) { return D == 1 || t.numel() == 0 || t.stride(2) == 1; };
+    if (!last(x) || !last(out)) throw Bad{PyExc_ValueError, std::string("the channels of ") + name + " must be adjacent in memory"};
+    if (weight) check_tensor((std::string(name) + "_weight").c_str(), *weight, {at::kFloat}, {D}, x);
+    return {ptr(x), ptr(out), ptr<float>(weight), H, M > 1 ? x.stride(0) : 0, H > 1 ? x.stride(1) : 0, M > 1 ? out.stride(0) : 0, H > 1 ? out.stride(1) : 0};
+}
+
+// qk_norm_rope(q, k, positions, freq, axis, q_weight, k_weight, eps, adjacent, q_out, k_out)  ->  (q_out, k_out)
+PyObject* qk_norm_rope(PyObject* const* a) {
+    const at::Tensor &q = tensor(a[0]), &pos = tensor(a[2]), &freq = tensor(a[3]), &axis = tensor(a[4]);
+    const at::Tensor *k = opt_tensor(a[1]), *qw = opt_tensor(a[5]), *kw = opt_tensor(a[6]), *oq = opt_tensor(a[9]), *ok = opt_tensor(a[10]);
+    need_cuda({&q, k, &pos, &freq, &axis, qw, kw, oq, ok});
+    if (q.dim() != 3 || (k && k->dim() != 3)) throw Bad{PyExc_ValueError, "q and k must be [M, heads, head_dim]"};
+    const int64_t M = q.size(0), D = q.size(2);
+    if (k && (k->size(0) != M || k->size(2) != D || k->scalar_type() != q.scalar_type() || k->device() != q.device()))
+        throw Bad{PyExc_ValueError, "k must agree with q in tokens, head size, type and device"};
+    if (!k && (kw || ok)) throw Bad{PyExc_ValueError, "k_weight and k_out need k"};
+    const tdq_dtype dt = dtype_id(q);
+    tdq_rope_params p = {};
+    if (D > INT32_MAX) throw Bad{PyExc_ValueError, "head_dim is out of range"};
+    p.head_dim = (int32_t)D;
+    check_tensor("freq", freq, {at::kDouble}, {freq.numel()}, q);
+    check_tensor("axis", axis, {at::kInt}, {freq.numel()}, q);
+    if (2 * freq.numel() > D) throw Bad{PyExc_ValueError, "the table has more pairs than half of head_dim"};
+    p.rotary_dim = (int32_t)(2 * freq.numel());
+    if (pos.dim() < 1 || pos.dim() > 2) throw Bad{PyExc_ValueError, "positions must be [M, axes] or [M]"};
+    const int64_t axes = pos.dim() == 2 ? pos.size(1) : 1;
+    if (pos.dim() == 2) check_tensor("positions", pos, {at::kLong}, {M, axes}, q);
+    else check_tensor("positions", pos, {at::kLong}, {M}, q);
+    if (axes > INT32_MAX) throw Bad{PyExc_ValueError, "positions have too many axes"};
+    p.n_axes = (int32_t)axes;
+    if (a[7] != Py_None) {
+        const double eps = PyFloat_AsDouble(a[7]);
+        if (eps == -1.0 && PyErr_Occurred()) throw python_error();
+        p.eps = (float)eps;
+        p.flags |= TDQ_ROPE_NORM;
+    } else if (qw || kw) {
+        throw Bad{PyExc_ValueError, "weights need the norm: eps is None"};
+    }
+    const int adjacent = PyObject_IsTrue(a[8]);
+    if (adjacent < 0) throw python_error();
+    if (adjacent) p.flags |= TDQ_ROPE_ADJACENT;
+    const auto out_of = [&](const char* name, const at::Tensor& x, const at::Tensor* o) {
+        if (!o) return new_like(x, x.sizes(), x.scalar_type());
+        if (o->sizes() != x.sizes() || o->scalar_type() != x.scalar_type() || o->device() != x.device())
+            throw Bad{PyExc_ValueError, std::string(name) + " must agree with its input in sizes, type and device"};
+        return *o;
+    };
+    const at::Tensor q_out = out_of("q_out", q, oq);
+    const at::Tensor k_out = k ? out_of("k_out", *k, ok) : at::Tensor();
+    const tdq_rope_heads hq = rope_side("q", q, q_out, qw, M, D);
+    tdq_rope_heads hk = {};
+    if (k) hk = rope_side("k", *k, k_out, kw, M, D);
+    check(call(q, [&](void* st) {
+              return tdq_qk_norm_rope(&hq, k ? &hk : nullptr, dt, M, &p, ptr<int64_t>(pos), ptr<double>(freq), ptr<int32_t>(axis), st);
+          }), "tdq_qk_norm_rope");
+    if (k) return tuple2(q_out, k_out);
+    PyObject* pq = THPVariable_Wrap(q_out);
+    PyObject* t = pq ? PyTuple_Pack(2, pq, Py_None) : nullptr;
+    Py_XDECREF(pq);
+    return t;
+}
+
 // Argument count, and C++ exceptions as Python ones.
 template <PyObject* (*F)(PyObject* const*), int N>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -395,6 +553,7 @@ PyObject* set_error_class(PyObject*, PyObject* cls) {
 PyMethodDef methods[] = {
     TDQ_ENTRY(quantize_act, 5), TDQ_ENTRY(quantize_act_fixed, 6), TDQ_ENTRY(quantize_act_nchw, 5), TDQ_ENTRY(quantize_weight, 4),
     TDQ_ENTRY(w4a4_linear, 11), TDQ_ENTRY(w4a4_linear_static, 8), TDQ_ENTRY(quant_linear_fused, 8), TDQ_ENTRY(quant_linear_host, 7),
+    TDQ_ENTRY(quantize_act_fp8, 3), TDQ_ENTRY(quantize_weight_fp8, 3), TDQ_ENTRY(fp8_linear, 8), TDQ_ENTRY(qk_norm_rope, 11),
     {"set_error_class", set_error_class, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 #undef TDQ_ENTRY
 

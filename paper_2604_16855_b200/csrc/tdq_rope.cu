@@ -1,0 +1,313 @@
+// tdq_qk_norm_rope: root-mean-square norm of every query and key head and the rotation by the token's positions, in one pass.
+//
+//   r = 1 / sqrt(mean_i x_i^2 + eps);  n_i = x_i (r w_i);   for pair i < R/2:  t = pos[m, axis_i] freq_i,
+//   (n_a, n_b) -> (n_a cos t - n_b sin t,  n_b cos t + n_a sin t);   channels from R on: n_i
+//
+// Angles.  t reaches 10^6 and more, where binary32 has lost the fraction of a turn: the product, the turns and their
+// fraction are binary64 (three operations per pair and token, shared by all heads), and only the fraction of a turn is rounded to
+// binary32 for sincospif.  Sum of squares, norm and rotation are binary32; one rounding at the store.
+//
+// Bound by HBM: every head is read and written once.  A thread owns the two 16-byte vectors of a head whose elements form pairs (halves:
+// one from either half; adjacent: neighbours), so that a head is a power of two of lanes, its sum of squares a few shuffles, and
+// no element passes through another thread: in place is safe.  A thread block takes a few tokens with all their heads: their cosines and sines
+// are computed once, into shared memory, while the heads' loads are in flight.
+#include <cuda_fp16.h>
+
+#include "tdq_common.cuh"
+
+namespace tdq {
+namespace {
+
+constexpr int kMaxWarps = 16;
+
+struct RopeArgs {
+    tdq_rope_heads q, k;
+    const int64_t* pos;
+    const double* freq;
+    const int32_t* axis;
+    int64_t M;
+    int32_t Hq, H;             // query heads, all heads
+    int32_t D, half, n_axes;   // half = R / 2
+    int32_t norm, adjacent;
+    float eps;
+    int32_t tokens, groups;    // per block: tokens; head groups (one warp each) per token
+    int32_t lanes_log2;        // lanes of a head
+};
+
+template <int DT> struct Bits { using T = uint16_t; };
+template <> struct Bits<TDQ_F32> { using T = float; };
+template <int DT>
+__device__ __forceinline__ float to_f(typename Bits<DT>::T v) {
+    if constexpr (DT == TDQ_F32) return v;
+    else if constexpr (DT == TDQ_BF16) return __uint_as_float((uint32_t)v << 16);
+    else return __half2float(__ushort_as_half(v));
+}
+template <int DT>
+__device__ __forceinline__ typename Bits<DT>::T from_f(float v) {
+    if constexpr (DT == TDQ_F32) return v;
+    else if constexpr (DT == TDQ_BF16) return __bfloat16_as_ushort(__float2bfloat16_rn(v));
+    else return __half_as_ushort(__float2half_rn(v));
+}
+template <int DT>
+__device__ __forceinline__ void unpack(const uint4& v, float* f) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (DT == TDQ_F32) {
+            f[i] = __uint_as_float(w[i]);
+        } else if constexpr (DT == TDQ_BF16) {
+            f[2 * i] = __uint_as_float(w[i] << 16);
+            f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        } else {
+            const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+            f[2 * i] = h.x;
+            f[2 * i + 1] = h.y;
+        }
+    }
+}
+template <int DT>
+__device__ __forceinline__ uint4 pack(const float* f) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (DT == TDQ_F32) {
+            w[i] = __float_as_uint(f[i]);
+        } else if constexpr (DT == TDQ_BF16) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t*>(&h);
+        } else {
+            const __half2 h = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// cosine and sine of pair i of token m; an axis outside the positions counts as their last
+__device__ __forceinline__ float2 turn_of(const RopeArgs& a, int64_t m, int i) {
+    const uint32_t ax = min((uint32_t)__ldg(a.axis + i), (uint32_t)a.n_axes - 1u);
+    const double turns = (double)__ldg(reinterpret_cast<const long long*>(a.pos) + m * a.n_axes + ax) * __ldg(a.freq + i) * 0.15915494309189533577;
+    float s, c;
+    sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
+    return make_float2(c, s);
+}
+
+template <int DT, bool ADJ>
+__global__ void __launch_bounds__(kMaxWarps * 32) rope_kernel(const RopeArgs a) {
+    using T = typename Bits<DT>::T;
+    constexpr int V = 16 / (int)sizeof(T);                 // elements of a vector, pairs of a thread
+    extern __shared__ float2 table[];                      // [tokens][half]
+    pdl_wait();
+    pdl_trigger();
+    const int64_t m0 = (int64_t)blockIdx.x * a.tokens;
+    const int n_tok = (int)min((int64_t)a.tokens, a.M - m0);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = blockDim.x >> 5;
+    const int L = 1 << a.lanes_log2, unit = lane & (L - 1), sub = lane >> a.lanes_log2, per_warp = 32 >> a.lanes_log2;
+    const bool has = unit * 2 * V < a.D;
+    const bool turns = unit * V < a.half;                  // a unit of the rotated channels (R is a multiple of 2 V)
+    // element offsets of the thread's two vectors in a head
+    const int e0 = ADJ || !turns ? 2 * unit * V : unit * V, e1 = ADJ || !turns ? e0 + V : a.half + unit * V;
+    bool have_table = false;                               // every warp has an item
+    for (int item = warp; item < a.tokens * a.groups; item += n_warps) {
+        const int tb = item / a.groups, head = (item - tb * a.groups) * per_warp + sub;
+        const bool on = has && tb < n_tok && head < a.H;
+        const bool is_q = head < a.Hq;
+        const tdq_rope_heads& s = is_q ? a.q : a.k;
+        const int64_t m = m0 + tb;
+        const int hh = is_q ? head : head - a.Hq;
+        uint4 v0 = make_uint4(0, 0, 0, 0), v1 = v0;
+        if (on) {
+            const T* p = reinterpret_cast<const T*>(s.x) + m * s.row_stride + hh * s.head_stride;
+            v0 = *reinterpret_cast<const uint4*>(p + e0);
+            v1 = *reinterpret_cast<const uint4*>(p + e1);
+        }
+        if (!have_table) {                                 // the first loads are in flight
+            for (int i = threadIdx.x; i < n_tok * a.half; i += blockDim.x) {
+                const int t = i / a.half;
+                table[i] = turn_of(a, m0 + t, i - t * a.half);
+            }
+            __syncthreads();
+            have_table = true;
+        }
+        float x[V], y[V];
+        unpack<DT>(v0, x);
+        unpack<DT>(v1, y);
+        if (a.norm) {
+            float ss = 0.f;
+#pragma unroll
+            for (int j = 0; j < V; ++j) ss = fmaf(x[j], x[j], fmaf(y[j], y[j], ss));
+            for (int d = 1; d < L; d <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
+            const float r = rsqrtf(ss / (float)a.D + a.eps);
+            if (on && s.weight) {
+#pragma unroll
+                for (int j = 0; j < V; j += 4) {
+                    const float4 w0 = __ldg(reinterpret_cast<const float4*>(s.weight + e0 + j)), w1 = __ldg(reinterpret_cast<const float4*>(s.weight + e1 + j));
+                    x[j] *= r * w0.x; x[j + 1] *= r * w0.y; x[j + 2] *= r * w0.z; x[j + 3] *= r * w0.w;
+                    y[j] *= r * w1.x; y[j + 1] *= r * w1.y; y[j + 2] *= r * w1.z; y[j + 3] *= r * w1.w;
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j) { x[j] *= r; y[j] *= r; }
+            }
+        }
+        if (on) {
+            if (turns) {
+                const float2* cs = table + tb * a.half + unit * V;
+                if constexpr (ADJ) {
+#pragma unroll
+                    for (int j = 0; j < V; j += 2) {
+                        const float2 p = cs[j / 2], q = cs[V / 2 + j / 2];
+                        const float xa = x[j], xb = x[j + 1], ya = y[j], yb = y[j + 1];
+                        x[j] = xa * p.x - xb * p.y;
+                        x[j + 1] = xb * p.x + xa * p.y;
+                        y[j] = ya * q.x - yb * q.y;
+                        y[j + 1] = yb * q.x + ya * q.y;
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        const float2 p = cs[j];
+                        const float xa = x[j], yb = y[j];
+                        x[j] = xa * p.x - yb * p.y;
+                        y[j] = yb * p.x + xa * p.y;
+                    }
+                }
+            }
+            T* p = reinterpret_cast<T*>(s.out) + m * s.out_row_stride + hh * s.out_head_stride;
+            *reinterpret_cast<uint4*>(p + e0) = pack<DT>(x);
+            *reinterpret_cast<uint4*>(p + e1) = pack<DT>(y);
+        }
+    }
+}
+
+// Any head size, stride and alignment: a warp per head, a lane per pair.
+template <int DT>
+__global__ void __launch_bounds__(256) rope_any_kernel(const RopeArgs a) {
+    using T = typename Bits<DT>::T;
+    pdl_wait();
+    pdl_trigger();
+    const int64_t item = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31;
+    const int64_t m = item / a.H;
+    if (m >= a.M) return;
+    const int head = (int)(item - m * a.H);
+    const bool is_q = head < a.Hq;
+    const tdq_rope_heads& s = is_q ? a.q : a.k;
+    const int hh = is_q ? head : head - a.Hq;
+    const T* x = reinterpret_cast<const T*>(s.x) + m * s.row_stride + hh * s.head_stride;
+    T* out = reinterpret_cast<T*>(s.out) + m * s.out_row_stride + hh * s.out_head_stride;
+    float r = 1.f;
+    if (a.norm) {
+        float ss = 0.f;
+        for (int i = lane; i < a.D; i += 32) {
+            const float f = to_f<DT>(x[i]);
+            ss = fmaf(f, f, ss);
+        }
+        for (int d = 1; d < 32; d <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
+        r = rsqrtf(ss / (float)a.D + a.eps);
+    }
+    const float* w = a.norm ? s.weight : nullptr;
+    for (int i = lane; i < a.half; i += 32) {
+        const int ia = a.adjacent ? 2 * i : i, ib = a.adjacent ? 2 * i + 1 : a.half + i;
+        const float na = to_f<DT>(x[ia]) * (w ? r * __ldg(w + ia) : r), nb = to_f<DT>(x[ib]) * (w ? r * __ldg(w + ib) : r);
+        const float2 t = turn_of(a, m, i);
+        out[ia] = from_f<DT>(na * t.x - nb * t.y);
+        out[ib] = from_f<DT>(nb * t.x + na * t.y);
+    }
+    for (int i = 2 * a.half + lane; i < a.D; i += 32) out[i] = from_f<DT>(to_f<DT>(x[i]) * (w ? r * __ldg(w + i) : r));
+}
+
+template <int DT>
+tdq_status launch(RopeArgs a, cudaStream_t st) {
+    using T = typename Bits<DT>::T;
+    constexpr int V = 16 / (int)sizeof(T);
+    const auto fits = [&](const tdq_rope_heads& s) {       // 16-byte vectors everywhere
+        if (s.heads == 0) return true;
+        return reinterpret_cast<uintptr_t>(s.x) % 16 == 0 && reinterpret_cast<uintptr_t>(s.out) % 16 == 0 && reinterpret_cast<uintptr_t>(s.weight) % 16 == 0 &&
+               s.row_stride % V == 0 && s.head_stride % V == 0 && s.out_row_stride % V == 0 && s.out_head_stride % V == 0;
+    };
+    cudaError_t e;
+    // a head of at most 32 lanes, whole vectors on either side of the rotated channels' middle and end
+    if (a.D % (2 * V) == 0 && a.half % V == 0 && a.D <= 64 * V && fits(a.q) && fits(a.k)) {
+        a.lanes_log2 = 0;
+        while ((2 * V << a.lanes_log2) < a.D) ++a.lanes_log2;
+        const int per_warp = 32 >> a.lanes_log2;
+        a.groups = (a.H + per_warp - 1) / per_warp;
+        // about eight warps a block, each with one item; small heads come several tokens at a time
+        a.tokens = a.groups >= 8 ? 1 : 8 / a.groups;
+        const int items = a.tokens * a.groups, warps = items < kMaxWarps ? items : kMaxWarps;
+        const size_t smem = (size_t)a.tokens * a.half * sizeof(float2);   // at most 8 x 256 pairs, 16 KB
+        const int64_t blocks = (a.M + a.tokens - 1) / a.tokens;
+        if (blocks > INT32_MAX) return TDQ_ERR_UNSUPPORTED;
+        e = launch_pdl(a.adjacent ? rope_kernel<DT, true> : rope_kernel<DT, false>, dim3((unsigned)blocks), dim3(warps * 32), smem, st, a);
+    } else {
+        const int64_t blocks = (a.M * a.H + 7) / 8;
+        if (blocks > INT32_MAX) return TDQ_ERR_UNSUPPORTED;
+        e = launch_pdl(rope_any_kernel<DT>, dim3((unsigned)blocks), dim3(256), 0, st, a);
+    }
+    if (e == cudaSuccess) g_launch_count.fetch_add(1, std::memory_order_relaxed);
+    return cuda_status(e);
+}
+
+// null pointers, sizes and element alignment of one side; TDQ_OK when it has no heads
+tdq_status check_heads(const tdq_rope_heads& s, int64_t M, int64_t D, uintptr_t esz) {
+    if (s.heads < 0) return TDQ_ERR_INVALID_ARG;
+    if (s.heads == 0 || M == 0) return TDQ_OK;
+    if (!s.x || !s.out) return TDQ_ERR_INVALID_ARG;
+    if (s.heads > 65536) return TDQ_ERR_UNSUPPORTED;
+    // strides such that no offset passes 63 bits
+    const int64_t limit = (int64_t)1 << 40;
+    const auto wild = [&](int64_t v) { return v < 0 || v > limit; };
+    if (wild(s.row_stride) || wild(s.head_stride) || wild(s.out_row_stride) || wild(s.out_head_stride)) return TDQ_ERR_INVALID_ARG;
+    // heads and rows of the output must not overlap one another
+    const bool many_h = s.heads > 1, many_m = M > 1;
+    if ((many_h && s.out_head_stride < D) || (many_m && s.out_row_stride < D)) return TDQ_ERR_INVALID_ARG;
+    if (many_h && many_m && s.out_row_stride < (s.heads - 1) * s.out_head_stride + D &&
+        (double)s.out_head_stride < (double)(M - 1) * (double)s.out_row_stride + (double)D)
+        return TDQ_ERR_INVALID_ARG;
+    if (s.x == s.out && ((many_m && s.row_stride != s.out_row_stride) || (many_h && s.head_stride != s.out_head_stride))) return TDQ_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(s.x) % esz || reinterpret_cast<uintptr_t>(s.out) % esz || reinterpret_cast<uintptr_t>(s.weight) % 4) return TDQ_ERR_ALIGNMENT;
+    return TDQ_OK;
+}
+
+}  // namespace
+}  // namespace tdq
+
+using namespace tdq;
+
+extern "C" tdq_status tdq_qk_norm_rope(const tdq_rope_heads* q, const tdq_rope_heads* k, tdq_dtype dtype, int64_t M, const tdq_rope_params* p,
+                                       const int64_t* positions, const double* freq, const int32_t* axis, void* cuda_stream) {
+    if (!p || (!q && !k) || M < 0) return TDQ_ERR_INVALID_ARG;
+    if (dtype != TDQ_F32 && dtype != TDQ_BF16 && dtype != TDQ_F16) return TDQ_ERR_INVALID_ARG;
+    if (p->head_dim <= 0 || p->rotary_dim < 0 || p->rotary_dim > p->head_dim || p->rotary_dim % 2) return TDQ_ERR_INVALID_ARG;
+    if (p->flags & ~(uint32_t)(TDQ_ROPE_NORM | TDQ_ROPE_ADJACENT)) return TDQ_ERR_INVALID_ARG;
+    if ((p->flags & TDQ_ROPE_NORM) && !(p->eps >= 0.f)) return TDQ_ERR_INVALID_ARG;
+    if (p->rotary_dim > 0 && p->n_axes <= 0) return TDQ_ERR_INVALID_ARG;
+    if (M > INT32_MAX) return TDQ_ERR_UNSUPPORTED;
+    const uintptr_t esz = dtype == TDQ_F32 ? 4 : 2;
+    RopeArgs a = {};
+    for (int i = 0; i < 2; ++i) {
+        const tdq_rope_heads* s = i ? k : q;
+        if (!s) continue;
+        const tdq_status st = check_heads(*s, M, p->head_dim, esz);
+        if (st != TDQ_OK) return st;
+        (i ? a.k : a.q) = *s;
+    }
+    if (M == 0 || a.q.heads + a.k.heads == 0) return TDQ_OK;
+    if (p->rotary_dim > 0 && (!positions || !freq || !axis)) return TDQ_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(positions) % 8 || reinterpret_cast<uintptr_t>(freq) % 8 || reinterpret_cast<uintptr_t>(axis) % 4) return TDQ_ERR_ALIGNMENT;
+    a.pos = positions;
+    a.freq = freq;
+    a.axis = axis;
+    a.M = M;
+    a.Hq = (int32_t)a.q.heads;
+    a.H = (int32_t)(a.q.heads + a.k.heads);
+    a.D = p->head_dim;
+    a.half = p->rotary_dim / 2;
+    a.n_axes = p->n_axes;
+    a.norm = (p->flags & TDQ_ROPE_NORM) != 0;
+    a.adjacent = (p->flags & TDQ_ROPE_ADJACENT) != 0;
+    a.eps = p->eps;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+    return dtype == TDQ_F32 ? launch<TDQ_F32>(a, st) : dtype == TDQ_BF16 ? launch<TDQ_BF16>(a, st) : launch<TDQ_F16>(a, st);
+}
