@@ -1,0 +1,152 @@
+"""Norm and rotation of queries and keys against the 64-bit form."""
+import pytest
+import torch
+
+import fp8_utils as fu
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def tdq():
+    from paper_2604_16855_b200 import tdq
+    return tdq
+
+
+def _heads(M, H, D, seed, dtype):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn((M, H, D), generator=g) * torch.exp(torch.randn((M, H, 1), generator=g))).to(dtype).cuda()
+
+
+def _case(tdq, M, hq, hk, D, R, axes, dtype, eps=1e-6, adjacent=False, weights=True, far=0, views=None):
+    dt = fu.DT[dtype]
+    q, k = _heads(M, hq, D, 1, dt), _heads(M, hk, D, 2, dt)
+    g = torch.Generator().manual_seed(3)
+    qw = (1 + 0.2 * torch.randn((D,), generator=g)).cuda() if weights and eps is not None else None
+    kw = (1 + 0.2 * torch.randn((D,), generator=g)).cuda() if weights and eps is not None else None
+    pos = torch.randint(-far - 50, far + 50, (M, axes), generator=g).cuda()
+    half = R // 2
+    freq, axis = tdq.rope_table(R, [half // axes + (i < half % axes) for i in range(axes)])
+    if views:
+        q, k = views(q), views(k)
+    qo, ko = tdq.qk_norm_rope(q, k, pos, (freq, axis), qw, kw, eps=eps, adjacent=adjacent)
+    for out, x, w in ((qo, q, qw), (ko, k, kw)):
+        assert out.shape == x.shape and out.dtype == dt and out.is_contiguous()
+        fu.check_rope(out, *fu.rope(x, w, pos, freq, axis.long(), eps, adjacent))
+    tdq.qk_norm_rope(q, k, pos, (freq, axis), qw, kw, eps=eps, adjacent=adjacent, q_out=q, k_out=k)
+    assert torch.equal(q, qo) and torch.equal(k, ko)      # in place: the same bits
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("adjacent", [False, True])
+@pytest.mark.parametrize("D,R", [(2, 2), (1, 0), (3, 2), (16, 16), (32, 32), (40, 40), (64, 64), (64, 32), (80, 80), (80, 40), (96, 96), (128, 128), (128, 64),
+                                 (128, 0), (256, 256), (512, 512), (72, 48), (576, 64), (1030, 1030)])
+def test_head_sizes(tdq, D, R, adjacent, dtype):
+    _case(tdq, 7, 3, 2, D, R, 1, dtype, adjacent=adjacent)
+
+
+@pytest.mark.parametrize("M,hq,hk", [(1, 1, 1), (1, 32, 8), (2, 71, 1), (5, 12, 12), (9, 200, 3), (65, 4, 4), (1000, 6, 1)])
+@pytest.mark.parametrize("D", [64, 128, 72])
+def test_tokens_and_heads(tdq, M, hq, hk, D):
+    _case(tdq, M, hq, hk, D, D, 1, "bf16")
+
+
+@pytest.mark.parametrize("axes", [1, 2, 3, 5])
+@pytest.mark.parametrize("adjacent", [False, True])
+def test_axes(tdq, axes, adjacent):
+    _case(tdq, 33, 4, 2, 128, 128, axes, "fp32", adjacent=adjacent)
+
+
+@pytest.mark.parametrize("D", [64, 72])
+@pytest.mark.parametrize("far", [1 << 17, 1 << 24, 1 << 31])
+def test_far_positions(tdq, far, D):
+    _case(tdq, 50, 2, 2, D, D, 2, "fp32", far=far)
+
+
+@pytest.mark.parametrize("D", [64, 72])
+def test_without_norm_and_without_weights(tdq, D):
+    _case(tdq, 20, 4, 2, D, D, 1, "fp16", eps=None)
+    _case(tdq, 20, 4, 2, D, D, 1, "fp16", weights=False)
+    _case(tdq, 20, 4, 2, D, D, 1, "fp32", eps=0.0)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("gap,shift", [(0, 0), (16, 16), (8, 0), (1, 0), (0, 1), (3, 5)])
+def test_strides_and_alignment(tdq, gap, shift, dtype):
+    def views(x):
+        M, H, D = x.shape
+        v = torch.full((shift + M * (H * (D + gap) + gap),), float("nan"), dtype=x.dtype, device="cuda")[shift:]
+        v = v.as_strided((M, H, D), (H * (D + gap) + gap, D + gap, 1))
+        v.copy_(x)
+        return v
+    _case(tdq, 11, 3, 2, 64, 64, 1, dtype, views=views)
+    _case(tdq, 11, 3, 2, 64, 64, 1, dtype, views=lambda x: x.transpose(0, 1).contiguous().transpose(0, 1))      # head-major
+
+
+def test_zero_heads_of_zeros_and_non_finite_ones(tdq):
+    table, pos = tdq.rope_table(64), torch.arange(4, device="cuda")
+    x = _heads(4, 3, 64, 5, torch.float32)
+    x[1, 1] = 0
+    x[2, 0, 5] = float("nan")
+    x[3, 2, 63] = float("inf")
+    out, none = tdq.qk_norm_rope(x, None, pos, table)
+    assert none is None and (out[1, 1] == 0).all()
+    bad = torch.zeros((4, 3), dtype=torch.bool, device="cuda")
+    bad[2, 0] = bad[3, 2] = True
+    assert torch.isfinite(out[~bad]).all() and out[2, 0].isnan().all() and not torch.isfinite(out[3, 2, [31, 63]]).any()
+    o = torch.zeros((4, 0, 64), device="cuda")
+    qo, ko = tdq.qk_norm_rope(x, o, pos, table)           # a side without heads
+    assert ko.shape == (4, 0, 64) and torch.equal(qo.nan_to_num(), out.nan_to_num())
+    n0 = tdq.kernel_launch_count()
+    qo, ko = tdq.qk_norm_rope(x[:0], o[:0], pos[:0], table)
+    assert qo.shape == (0, 3, 64) and tdq.kernel_launch_count() == n0
+
+
+def test_an_axis_outside_the_positions_is_their_last(tdq):
+    x, pos = _heads(9, 2, 64, 1, torch.float32), torch.randint(0, 99, (9, 3), device="cuda")
+    freq, axis = tdq.rope_table(64, [10, 11, 11])
+    want = tdq.qk_norm_rope(x, None, pos, (freq, axis))[0]
+    for odd in (3, -1, 2 ** 31 - 1, -2 ** 31):
+        assert torch.equal(tdq.qk_norm_rope(x, None, pos, (freq, torch.where(axis == 2, odd, axis).to(torch.int32)))[0], want)
+
+
+def test_refusals_of_the_binding(tdq):
+    x, pos, table = _heads(4, 2, 64, 1, torch.float32), torch.arange(4, device="cuda"), tdq.rope_table(64)
+    n0 = tdq.kernel_launch_count()
+    w = torch.ones(64, device="cuda")
+    for args, kw in [((x[0], None, pos, table), {}), ((x, x[:3], pos, table), {}), ((x, x.half(), pos, table), {}), ((x, None, pos[:3], table), {}),
+                     ((x, None, pos, tdq.rope_table(128)), {}), ((x, None, pos, table, w[:32]), {}), ((x, None, pos, table, w), {"eps": None}),
+                     ((x, None, pos, table, None, w), {}), ((x, None, pos, table), {"q_out": x[:, :1]}), ((x, None, pos, table), {"q_out": x.half()}),
+                     ((x.transpose(1, 2).contiguous().transpose(1, 2), None, pos, table), {}), ((x, None, pos.cpu(), table), {}),
+                     ((x, None, pos, (table[0], table[1][:3])), {}), ((x, None, pos.view(1, 1, 4), table), {})]:
+        with pytest.raises(ValueError):
+            tdq.qk_norm_rope(*args, **kw)
+    for args in [(x.double(), None, pos, table), (x, None, pos.int(), table), (x, None, pos, (table[0].float(), table[1])),
+                 (x, None, pos, (table[0], table[1].long())), (x, None, pos, table, w.half())]:
+        with pytest.raises(TypeError):
+            tdq.qk_norm_rope(*args)
+    for kw in [{"eps": -1.0}, {"q_out": x[:1].expand(4, 2, 64)}]:
+        with pytest.raises(tdq.TdqError) as e:
+            tdq.qk_norm_rope(x, None, pos, table, **kw)
+        assert e.value.code == tdq.ERR_INVALID_ARG
+    assert tdq.kernel_launch_count() == n0
+
+
+@pytest.mark.parametrize("D", [128, 72])
+def test_graph_replay_in_place(tdq, D):
+    q, k = _heads(40, 4, D, 1, torch.bfloat16), _heads(40, 2, D, 2, torch.bfloat16)
+    pos, table = torch.arange(40, device="cuda"), tdq.rope_table(D)
+    qo, ko = torch.empty_like(q), torch.empty_like(k)
+    tdq.qk_norm_rope(q, k, pos, table, q_out=qo, k_out=ko)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            tdq.qk_norm_rope(q, k, pos, table, q_out=qo, k_out=ko)
+    q.copy_(_heads(40, 4, D, 7, torch.bfloat16))
+    pos.add_(1000)
+    graph.replay()
+    torch.cuda.synchronize()
+    want = tdq.qk_norm_rope(q, k, pos, table)
+    assert torch.equal(qo, want[0]) and torch.equal(ko, want[1])
