@@ -49,6 +49,36 @@ __device__ __forceinline__ uint32_t fp8_cluster_rank() {
 __device__ __forceinline__ void fp8_cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// for the kernels that include tdq_tc.cuh first
+#ifdef TDQ_TC_CUH_
+__device__ __forceinline__ bool fp8_try(uint32_t bar_s, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar_s), "r"(parity) : "memory");
+    return ok != 0;
+}
+// Bounded wait of a converged warp on a barrier of its CTA.  try_wait without a time hint: the hardware holds the warp for a while at
+// a time, where the hinted form comes back every 40 clocks (counted: half of all instructions of the pair kernel were the
+// waiting warps').
+__device__ __forceinline__ void fp8_wait_more(uint32_t bar_s, uint32_t parity, Ctrl* c, uint32_t* status, uint32_t code) {
+    const uint32_t t0 = (uint32_t)clock();
+#pragma unroll 1
+    while (!fp8_try(bar_s, parity)) {
+        if (c->abort_flag) return;
+        if ((uint32_t)clock() - t0 > (uint32_t)kTimeoutCycles) {
+            atomicCAS(status, 0u, code | ((uint32_t)blockIdx.x << 8));
+            c->abort_flag = 1;
+            return;
+        }
+    }
+}
+__device__ __forceinline__ void fp8_wait(uint32_t bar_s, uint32_t parity, Ctrl* c, uint32_t* status, uint32_t code) {
+    if (!fp8_try(bar_s, parity)) fp8_wait_more(bar_s, parity, c, status, code);
+}
+#endif
 __device__ __forceinline__ uint32_t map_to_cta(uint32_t saddr, uint32_t rank) {
     uint32_t r;
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(saddr), "r"(rank));

@@ -10,8 +10,8 @@
 // atomics, no workspace, the same bits every time.  Warp 0 loads (tensor maps, 16 KB of weights and the tokens' 128 bytes a stage), warp 1
 // issues, the others scale and add: a thread has one output channel and up to 32 tokens, whose factors xs * ws are laid out
 // in shared memory eight blocks at a time, before they are needed.
-#include "tdq_fp8.cuh"
 #include "tdq_tc.cuh"
+#include "tdq_fp8.cuh"
 
 namespace tdq {
 
@@ -107,7 +107,7 @@ fp8_split_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, cons
         // ------------------------------------------------------------ loads
         uint32_t s = 0, ph = 1;
         for (int i = 0; i < n_kb; ++i) {
-            wait_hot(smem_u32(&g->empty[s]), ph, c, a.status, 5u);
+            fp8_wait(smem_u32(&g->empty[s]), ph, c, a.status, 5u);
             if (c->abort_flag) break;
             if (elect_one()) {
                 const uint32_t dst = ring_s + s * Sh::kStage;
@@ -123,8 +123,8 @@ fp8_split_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, cons
         uint32_t s = 0, ph = 0;
         for (int i = 0; i < n_kb; ++i) {
             const uint32_t slot = (uint32_t)i % kSplitSlots;
-            wait_hot(smem_u32(&g->tempty[slot]), (((uint32_t)i / kSplitSlots) & 1u) ^ 1u, c, a.status, 3u);
-            wait_hot(smem_u32(&g->full[s]), ph, c, a.status, 4u);
+            fp8_wait(smem_u32(&g->tempty[slot]), (((uint32_t)i / kSplitSlots) & 1u) ^ 1u, c, a.status, 3u);
+            fp8_wait(smem_u32(&g->full[s]), ph, c, a.status, 4u);
             if (c->abort_flag) break;
             tc_fence_after();
             if (elect_one()) {
@@ -170,7 +170,7 @@ fp8_split_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, cons
 #pragma unroll 1
             for (int q = 0; q < n; ++q) {
                 const uint32_t i = (uint32_t)(c0 + q), slot = i % kSplitSlots;
-                wait_hot(smem_u32(&g->tfull[slot]), (i / kSplitSlots) & 1u, c, a.status, 2u);
+                fp8_wait(smem_u32(&g->tfull[slot]), (i / kSplitSlots) & 1u, c, a.status, 2u);
                 if (c->abort_flag) break;
                 tc_fence_after();
                 const uint32_t tm = tmem_base + ((uint32_t)(quarter * 32) << 16) + slot * NT + cg * CW;

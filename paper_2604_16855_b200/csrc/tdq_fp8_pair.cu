@@ -7,34 +7,40 @@
 // TMEM columns), filled and drained in turn, so that three quarters of TMEM are in the tensor core's hands while one is read.
 //
 //   warps 0, 3  loads of this CTA's 128 token rows and 128 weight rows (tensor maps, 128-byte swizzle, 16 KB each a stage), signalled to
-//               CTA 0's barrier
-//   warp 1      CTA 0: issues the instructions (cta_group::2, 256 x 128 x 32), commits to both CTAs' barriers
-//   warp 2      allocates TMEM
-//   warps 4-11  scale and add: 32 token rows x 128 columns each in registers (so 232 registers a thread, 40 for the others), then bias,
-//               rounding and the store through a swizzled strip of 4 KB
+//               CTA 0's barrier; warp 0 the block's scales too (asynchronous copies: as loads of the adding warps, first-level cache or not,
+//               they cost a quarter of the kernel's time)
+//   warps 1, 2  CTA 0: issue the instructions (cta_group::2, 256 x 128 x 32) of one half each, commit to both CTAs' barriers
+//   warps 4-11  scale and add: 32 token rows x 128 columns each in registers, (so 232 registers a thread, 40 for the others), then bias,
+//               rounding and the store through two swizzled strips of 4 KB
 //
 // Half h is columns 64 h .. 64 h + 63 of each CTA's 128 weight rows: with cta_group::2 either CTA brings half of the columns.
-#include "tdq_fp8.cuh"
 #include "tdq_tc.cuh"
+#include "tdq_fp8.cuh"
 
 namespace tdq {
 namespace {
 
-constexpr int kPairMaxStages = 6;
+constexpr int kPairStages = 4;                           // five leave no room for the second strip and gain nothing
 constexpr uint32_t kPairOperand = 128 * 128;             // bytes of a stage's rows of either operand
 constexpr uint32_t kPairStage = 2 * kPairOperand;
-constexpr uint32_t kPairCtrl = 1024;
+constexpr uint32_t kPairCtrl = 1024;                     // the ring behind it is on the 1 KB grid that the swizzles need, as the block's shared memory is
 constexpr int kAddWarp0 = 4, kAddWarps = 8;
 constexpr int kPairThreads = (kAddWarp0 + kAddWarps) * 32;
 constexpr uint32_t kStrip = 32 * 128;                    // 32 rows of 128 bytes
-constexpr uint32_t kBiasBytes = 128 * 4;                 // a warp's columns
+constexpr uint32_t kBiasBytes = 128 * 4;                 // of a warp's 128 columns
+constexpr int kStrips = 2;                               // of a warp: 128 columns of 16 bits, so that no store is waited for in a tile
+// Scales of a block: 128 token rows', then two weight blocks'.  Eight blocks of them, without a barrier that hands them back: block n + 8's
+// are copied once the instructions of block n + 4 have completed, which were issued after all of n + 2's sums had been taken.
+constexpr int kScaleSlots = 8;
+constexpr uint32_t kScaleBytes = 128 * 4 + 16;
 constexpr uint32_t kPairIdesc = (1u << 4) | ((128u >> 3) << 17) | ((256u >> 4) << 24);
 constexpr int kRegsLoad = 40, kRegsAdd = 232;            // 128 * 40 + 256 * 232 <= 384 * 168
 
 struct PairCtrl {
-    uint64_t full[kPairMaxStages];                       // CTA 0: both CTAs' operands of the stage have landed
-    uint64_t empty[kPairMaxStages];
-    uint64_t tfull[4], tempty[4];                        // accumulator 2 (block & 1) + half (tempty: CTA 0 only)
+    uint64_t full[kPairStages];                       // CTA 0: both CTAs' operands of the stage have landed
+    uint64_t empty[kPairStages];
+    uint64_t scales[kScaleSlots];                        // a block's scales have landed in this CTA
+    uint64_t tfull[4], tempty[4];                        // accumulator 2 (a tile's block & 1) + half (tempty: CTA 0 only)
 };
 
 __device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, uint32_t bar) {
@@ -55,28 +61,67 @@ __device__ __forceinline__ void arrive_cluster_lane0(uint32_t bar_c, int lane) {
     asm volatile("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %1, 0;\n\t@p mbarrier.arrive.shared::cluster.b64 _, [%0];\n\t}"
                  ::"r"(bar_c), "r"(lane) : "memory");
 }
-__device__ __forceinline__ void scale_add32(uint64_t* acc, const uint32_t* v, uint64_t d) {
+__device__ __forceinline__ void bulk_wait_group_read1() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
+// 64 consecutive columns of this warp's 32 TMEM lanes, waited for: lane i receives row i.  The other adding warp of the scheduler works meanwhile.
+__device__ __forceinline__ void tmem_ld64_wait(uint32_t taddr, uint32_t* v) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
+                 "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
+                 "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, "
+                 "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\t"
+                 "tcgen05.wait::ld.sync.aligned;"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+                   "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]),
+                   "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
+                   "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31]),
+                   "=r"(v[32]), "=r"(v[33]), "=r"(v[34]), "=r"(v[35]), "=r"(v[36]), "=r"(v[37]), "=r"(v[38]), "=r"(v[39]),
+                   "=r"(v[40]), "=r"(v[41]), "=r"(v[42]), "=r"(v[43]), "=r"(v[44]), "=r"(v[45]), "=r"(v[46]), "=r"(v[47]),
+                   "=r"(v[48]), "=r"(v[49]), "=r"(v[50]), "=r"(v[51]), "=r"(v[52]), "=r"(v[53]), "=r"(v[54]), "=r"(v[55]),
+                   "=r"(v[56]), "=r"(v[57]), "=r"(v[58]), "=r"(v[59]), "=r"(v[60]), "=r"(v[61]), "=r"(v[62]), "=r"(v[63])
+                 : "r"(taddr)
+                 : "memory");
+}
+// acc += d v, two columns an instruction.  The empty statement makes the compiler have the sums before it goes on to the next load: moved behind
+// it, they need registers of their own for v.
+__device__ __forceinline__ void scale_add64(float2* acc, const uint32_t* v, float d) {
 #pragma unroll
-    for (int j = 0; j < 16; ++j) fma2(acc[j], pack2(v[2 * j], v[2 * j + 1]), d);
+    for (int j = 0; j < 32; ++j) acc[j] = __ffma2_rn(make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])), make_float2(d, d), acc[j]);
+#pragma unroll
+    for (int j = 0; j < 32; j += 8)
+        asm volatile("" ::"f"(acc[j].x), "f"(acc[j + 1].x), "f"(acc[j + 2].x), "f"(acc[j + 3].x), "f"(acc[j + 4].x), "f"(acc[j + 5].x), "f"(acc[j + 6].x),
+                     "f"(acc[j + 7].x));
+}
+__device__ __forceinline__ float4 lds_f4(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ void copy4_async(uint32_t dst, const float* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+// arrives on the barrier when this thread's copies so far have landed
+__device__ __forceinline__ void copies_arrive(uint32_t bar_s) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar_s) : "memory");
 }
 
-// Y16: y has 16-bit elements.
-template <bool Y16>
+// DT: y's tdq_dtype.
+template <int DT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 fp8_pair_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap wmap,
                 const __grid_constant__ CUtensorMap ymap) {
-    extern __shared__ __align__(128) uint8_t smem_raw[];
+    constexpr bool Y16 = DT != TDQ_F32;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
     Ctrl* c = reinterpret_cast<Ctrl*>(smem_raw);             // its abort flag and TMEM address; the barriers are g's
     PairCtrl* g = reinterpret_cast<PairCtrl*>(smem_raw + sizeof(Ctrl));
     static_assert(sizeof(Ctrl) + sizeof(PairCtrl) <= kPairCtrl, "control block outgrew its reservation");
     const uint32_t sm_s = smem_u32(smem_raw);
-    const uint32_t ring_s = (sm_s + kPairCtrl + 1023u) & ~1023u;   // the same offset in both CTAs
-    const uint32_t n_stages = (uint32_t)a.n_stages;
+    const uint32_t ring_s = sm_s + kPairCtrl;                // the same offset in both CTAs
     const int warp = uniform_warp(), lane = threadIdx.x & 31;
     const uint32_t rank = fp8_cluster_rank();
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kPairMaxStages; ++i) { mbar_init(&g->full[i], 2); mbar_init(&g->empty[i], 1); }
+        for (int i = 0; i < kPairStages; ++i) { mbar_init(&g->full[i], 2); mbar_init(&g->empty[i], 2); }
+        for (int i = 0; i < kScaleSlots; ++i) mbar_init(&g->scales[i], 32);
         for (int i = 0; i < 4; ++i) { mbar_init(&g->tfull[i], 1); mbar_init(&g->tempty[i], kAddWarps); }
         c->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -96,6 +141,9 @@ fp8_pair_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const
     const int n_tiles = a.tiles_m * a.tiles_n, n_clusters = (int)gridDim.x / 2, first = (int)blockIdx.x / 2;
     const int K = a.K;
 
+    const uint32_t strips0_s = ring_s + kPairStages * kPairStage, biases_s = strips0_s + kAddWarps * kStrips * kStrip;
+    const uint32_t scales_s = biases_s + kAddWarps * kBiasBytes;
+
     if (warp < kAddWarp0) {
         setmaxnreg_dec<kRegsLoad>();
         if (warp == 0 || warp == 3) {
@@ -103,113 +151,121 @@ fp8_pair_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const
             const bool is_x = warp == 0;
             const uint32_t dst0 = ring_s + (is_x ? 0u : kPairOperand);
             const uint32_t full0 = map_to_cta(smem_u32(&g->full[0]), 0), empty_s = smem_u32(&g->empty[0]);
-            uint32_t s = 0, ph = 1;
+            uint32_t s = 0, ph = 1, n = 0;
             for (int tile = first; tile < n_tiles && !c->abort_flag; tile += n_clusters) {
                 const int mt = tile / a.tiles_n, nt = tile - mt * a.tiles_n;
                 const int row = (is_x ? mt : nt) * 256 + (int)rank * 128;   // past the end: the map fills with zeros
+                // scales: rows lane, lane + 32, .. of xscale and, in lanes 0 and 1, the tile's two rows of wscale; the last row for those past the end
+                const float* xs[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) xs[i] = a.xscale + min((int64_t)row + lane + 32 * i, a.M - 1) * K;
+                const float* ws = a.wscale + min((int64_t)2 * nt + (lane & 1), (a.O - 1) >> 7) * K;
 #pragma unroll 1
-                for (int kb = 0; kb < K; ++kb) {
-                    wait_hot(empty_s + s * 8, ph, c, a.status, 5u);
+                for (int kb = 0; kb < K; ++kb, ++n) {
+                    fp8_wait(empty_s + s * 8, ph, c, a.status, 5u);
                     if (c->abort_flag) break;
                     if (elect_one()) {
                         if (rank == 0) mbar_expect_tx(&g->full[s], 2 * kPairOperand);   // this operand, both CTAs
                         tma_load_pair(dst0 + s * kPairStage, is_x ? &xmap : &wmap, kb * (int)kFp8Block, row, full0 + s * 8);
                     }
                     __syncwarp();
-                    if (++s == n_stages) { s = 0; ph ^= 1; }
+                    if (is_x) {
+                        const uint32_t at = scales_s + (n % kScaleSlots) * kScaleBytes + (uint32_t)lane * 4u;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) copy4_async(at + i * 128, xs[i] + kb);
+                        if (lane < 2) copy4_async(at + 512, ws + kb);
+                        copies_arrive(smem_u32(&g->scales[0]) + (n % kScaleSlots) * 8);
+                    }
+                    if (++s == kPairStages) { s = 0; ph ^= 1; }
                 }
             }
-        } else if (warp == 1 && rank == 0) {
-            // -------------------------------------------------------- MMA issue
+        } else if (rank == 0) {
+            // -------------------------------------------------------- MMA issue, half h of every block
+            const uint32_t h = (uint32_t)warp - 1u;
             const uint32_t full_s = smem_u32(&g->full[0]), empty_s = smem_u32(&g->empty[0]);
-            const uint32_t tfull_s = smem_u32(&g->tfull[0]), tempty_s = smem_u32(&g->tempty[0]);
-            const uint64_t xd0 = sw_desc(ring_s), wd0 = sw_desc(ring_s + kPairOperand);
-            uint32_t s = 0, ph = 0, n = 0;
-            for (int tile = first; tile < n_tiles && !c->abort_flag; tile += n_clusters)
-#pragma unroll 1
-                for (int kb = 0; kb < K; ++kb, ++n) {
-                    const uint32_t slot0 = (n & 1u) * 2, par = ((n >> 1) & 1u) ^ 1u;
-                    wait_hot(full_s + s * 8, ph, c, a.status, 4u);
-                    const uint64_t xd = xd0 + s * (kPairStage >> 4), wd = wd0 + s * (kPairStage >> 4);
+            const uint32_t tfull_s = smem_u32(&g->tfull[0]) + h * 8, tempty_s = smem_u32(&g->tempty[0]) + h * 8;
+            const uint32_t xd0 = (uint32_t)sw_desc(ring_s), wd0 = (uint32_t)sw_desc(ring_s + kPairOperand) + h * (64 * 128 >> 4);
+            const uint32_t d0 = tmem_base + h * 128;
+            uint32_t s = 0, ph = 0, par[2] = {1, 1};
+            bool landed = false;                                 // the stage's barrier, asked while the last block's instructions were issued
+            const auto block = [&](const int slot) {
+                if (!landed) fp8_wait(full_s + s * 8, ph, c, a.status, 4u);
+                fp8_wait(tempty_s + slot * 16, par[slot], c, a.status, 3u);
+                if (c->abort_flag) return false;
+                par[slot] ^= 1u;
+                const uint32_t now = s;
+                if (++s == kPairStages) { s = 0; ph ^= 1; }
+                landed = mbar_test_s(full_s + s * 8, ph);
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint64_t xd = (uint64_t)kSwDescHi << 32 | (xd0 + now * (kPairStage >> 4)), wd = (uint64_t)kSwDescHi << 32 | (wd0 + now * (kPairStage >> 4));
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        wait_hot(tempty_s + (slot0 + h) * 8, par, c, a.status, 3u);
-                        if (c->abort_flag) break;
-                        tc_fence_after();
-                        if (elect_one()) {
-#pragma unroll
-                            for (int k = 0; k < 4; ++k)
-                                mma_f8_pair(tmem_base + (slot0 + h) * 128, xd + 2 * k, wd + h * (64 * 128 >> 4) + 2 * k, k ? 1u : 0u);
-                            if (h == 1) commit_pair(empty_s + s * 8);
-                            commit_pair(tfull_s + (slot0 + h) * 8);
-                        }
-                        __syncwarp();
-                    }
-                    if (c->abort_flag) break;
-                    if (++s == n_stages) { s = 0; ph ^= 1; }
+                    for (int k = 0; k < 4; ++k) mma_f8_pair(d0 + slot * 256, xd + 2 * k, wd + 2 * k, k ? 1u : 0u);
+                    commit_pair(tfull_s + slot * 16);
+                    commit_pair(empty_s + now * 8);
                 }
+                __syncwarp();
+                return true;
+            };
+            bool on = true;
+            for (int tile = first; tile < n_tiles && on; tile += n_clusters) {
+#pragma unroll 1
+                for (int kb = 0; kb + 1 < K && on; kb += 2) on = block(0) && block(1);
+                if ((K & 1) && on) on = block(0);
+            }
         }
     } else {
         // ------------------------------------------------------------ scaled sums and epilogue
         setmaxnreg_inc<kRegsAdd>();
         const int aw = warp - kAddWarp0, quarter = warp & 3, h = aw >> 2;
-        const uint32_t after_s = ring_s + n_stages * kPairStage;
-        const uint32_t strip_s = after_s + (uint32_t)aw * kStrip, bias_s = after_s + kAddWarps * kStrip + (uint32_t)aw * kBiasBytes;
+        const uint32_t strips_s = strips0_s + (uint32_t)aw * (kStrips * kStrip), bias_s = biases_s + (uint32_t)aw * kBiasBytes;
+        const uint32_t x_s = scales_s + (uint32_t)(quarter * 32 + lane) * 4u, sfull_s = smem_u32(&g->scales[0]);
         const uint32_t tfull_s = smem_u32(&g->tfull[h]), tempty_c = map_to_cta(smem_u32(&g->tempty[h]), 0);
         const uint32_t tm0 = tmem_base + ((uint32_t)(quarter * 32) << 16) + h * 128;
-        uint32_t va[32], vb[32];
-#pragma unroll
-        for (int q = 0; q < 32; ++q) { va[q] = 0u; vb[q] = 0u; }
-        uint32_t n = 0;
+        uint32_t par = 0, n = 0;                                 // phase bits of the half's two accumulators; blocks so far
+        bool full = false, scaled = false;                       // the next block's barriers, asked ahead of their use
         for (int tile = first; tile < n_tiles && !c->abort_flag; tile += n_clusters) {
             const int mt = tile / a.tiles_n, nt = tile - mt * a.tiles_n;
             const int64_t m0 = (int64_t)mt * 256 + rank * 128 + quarter * 32;
             const int64_t n0 = (int64_t)nt * 256 + h * 64;       // columns n0 + 0..63 and n0 + 128 + 0..63
-            const int64_t row = m0 + lane < a.M ? m0 + lane : a.M - 1;
-            const float* xs = a.xscale + row * K;
-            const int last = (int)((a.O - 1) >> 7);
-            const float* ws0 = a.wscale + (int64_t)min(2 * nt, last) * K;
-            const float* ws1 = a.wscale + (int64_t)min(2 * nt + 1, last) * K;
-            uint64_t acc[64];
-#pragma unroll
-            for (int j = 0; j < 64; ++j) acc[j] = 0ull;
             __syncwarp();                                        // the last tile's biases have been read
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int64_t col = n0 + (i >> 1) * 128 + (i & 1) * 32 + lane;
-                sts32(bias_s + (uint32_t)(i * 32 + lane) * 4u, (a.bias && col < a.O) ? __float_as_uint(__ldg(a.bias + col)) : 0u);
+                sts32(bias_s + (uint32_t)(i * 32 + lane) * 4u, a.bias && col < a.O ? __float_as_uint(__ldg(a.bias + col)) : 0u);
             }
-            float fx = __ldg(xs), f0 = __ldg(ws0), f1 = __ldg(ws1);
-#pragma unroll 1
-            for (int kb = 0; kb < K; ++kb, ++n) {
-                const float d0f = fx * f0, d1f = fx * f1;
-                const int next = min(kb + 1, K - 1);
-                fx = __ldg(xs + next);
-                f0 = __ldg(ws0 + next);
-                f1 = __ldg(ws1 + next);
-                const uint64_t d0 = pack2(__float_as_uint(d0f), __float_as_uint(d0f)), d1 = pack2(__float_as_uint(d1f), __float_as_uint(d1f));
-                const uint32_t so = (n & 1u) * 2;
-                wait_hot(tfull_s + so * 8, (n >> 1) & 1u, c, a.status, 2u);
-                if (c->abort_flag) break;
+            float2 acc[64];
+#pragma unroll
+            for (int j = 0; j < 64; ++j) acc[j] = make_float2(0.f, 0.f);
+            const auto block = [&](const int slot, uint32_t then) {
+                const uint32_t at = n % kScaleSlots;
+                if (!full) fp8_wait_more(tfull_s + slot * 16, (par >> slot) & 1u, c, a.status, 2u);
+                if (!scaled) fp8_wait_more(sfull_s + at * 8, (n / kScaleSlots) & 1u, c, a.status, 6u);
+                par ^= 1u << slot;
+                ++n;
                 tc_fence_after();
-                const uint32_t tm = tm0 + so * 128;
-                tmem_ld32(tm, va);
-                tmem_ld_wait_on(va);
-                tmem_ld32(tm + 32, vb);
-                scale_add32(acc, va, d0);
-                tmem_ld_wait_on(vb);
-                tmem_ld32(tm + 64, va);
-                scale_add32(acc + 16, vb, d0);
-                tmem_ld_wait_on(va);
-                tmem_ld32(tm + 96, vb);
-                scale_add32(acc + 32, va, d1);
-                tmem_ld_wait_on(vb);
+                const float x = __uint_as_float(lds32(x_s + at * kScaleBytes));
+                const float w0 = __uint_as_float(lds32(scales_s + at * kScaleBytes + 512)), w1 = __uint_as_float(lds32(scales_s + at * kScaleBytes + 516));
+                uint32_t v[64];
+                tmem_ld64_wait(tm0 + slot * 256, v);
+                scale_add64(acc, v, x * w0);
+                tmem_ld64_wait(tm0 + slot * 256 + 64, v);
                 tc_fence_before();
                 __syncwarp();
-                arrive_cluster_lane0(tempty_c + so * 8, lane);
-                scale_add32(acc + 48, vb, d1);
+                arrive_cluster_lane0(tempty_c + slot * 16, lane);
+                full = mbar_test_s(tfull_s + then * 16, (par >> then) & 1u);
+                scaled = mbar_test_s(sfull_s + n % kScaleSlots * 8, (n / kScaleSlots) & 1u);
+                scale_add64(acc + 32, v, x * w1);
+            };
+#pragma unroll 1
+            for (int kb = 0; kb + 1 < K; kb += 2) {
+                block(0, 1u);
+                block(1, 0u);
+                if (c->abort_flag) break;
             }
+            if (K & 1) block(0, 0u);
             if (c->abort_flag) break;
+            __syncwarp();
             // 32 rows x 128 bytes at a time: 32 columns of binary32 or 64 of 16 bits
             constexpr int kStripCols = Y16 ? 64 : 32;
             __syncwarp();
@@ -217,7 +273,11 @@ fp8_pair_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const
             for (int piece = 0; piece < 128 / kStripCols; ++piece) {
                 const int c0 = piece * kStripCols;
                 const int64_t col0 = n0 + (c0 >> 6) * 128 + (c0 & 63);
-                if (lane == 0) bulk_wait_group_read0();          // the strip has been read
+                const uint32_t strip_s = strips_s + (uint32_t)(piece & 1) * kStrip;
+                if (lane == 0) {                                 // the strip has been read: the last tile's stores, then but the last one
+                    if (piece == 0) bulk_wait_group_read0();
+                    else if (piece > 1) bulk_wait_group_read1();
+                }
                 __syncwarp();
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {                    // 16 bytes each
@@ -225,20 +285,15 @@ fp8_pair_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const
                     float o[kPer];
 #pragma unroll
                     for (int q = 0; q < kPer; q += 4) {
-                        uint64_t b0, b1;
-                        float bl, bh;
-                        lds128(bias_s + (uint32_t)(c0 + j * kPer + q) * 4u, b0, b1);
-                        unpack2(acc[(c0 + j * kPer + q) / 2], o[q], o[q + 1]);
-                        unpack2(acc[(c0 + j * kPer + q) / 2 + 1], o[q + 2], o[q + 3]);
-                        unpack2(b0, bl, bh);
-                        o[q] += bl; o[q + 1] += bh;
-                        unpack2(b1, bl, bh);
-                        o[q + 2] += bl; o[q + 3] += bh;
+                        const float4 b = lds_f4(bias_s + (uint32_t)(c0 + j * kPer + q) * 4u);
+                        const float2 r0 = __fadd2_rn(acc[(c0 + j * kPer + q) / 2], make_float2(b.x, b.y));
+                        const float2 r1 = __fadd2_rn(acc[(c0 + j * kPer + q) / 2 + 1], make_float2(b.z, b.w));
+                        o[q] = r0.x; o[q + 1] = r0.y; o[q + 2] = r1.x; o[q + 3] = r1.y;
                     }
                     const uint32_t at = strip_s + (uint32_t)lane * 128u + (((uint32_t)j ^ ((uint32_t)lane & 7u)) << 4);
                     if constexpr (Y16)
-                        sts128(at, pack16(o[0], o[1], a.y_type == TDQ_F16), pack16(o[2], o[3], a.y_type == TDQ_F16),
-                               pack16(o[4], o[5], a.y_type == TDQ_F16), pack16(o[6], o[7], a.y_type == TDQ_F16));
+                        sts128(at, pack16(o[0], o[1], DT == TDQ_F16), pack16(o[2], o[3], DT == TDQ_F16),
+                               pack16(o[4], o[5], DT == TDQ_F16), pack16(o[6], o[7], DT == TDQ_F16));
                     else
                         sts128(at, __float_as_uint(o[0]), __float_as_uint(o[1]), __float_as_uint(o[2]), __float_as_uint(o[3]));
                 }
@@ -264,7 +319,6 @@ fp8_pair_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const
                 }
             }
         }
-        tmem_ld_wait();
         if (lane == 0) bulk_wait_group0();                       // no store may still be reading this CTA's shared memory at exit
     }
 
@@ -279,23 +333,21 @@ fp8_pair_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const
 }  // namespace
 
 tdq_status launch_fp8_pair(Fp8Args a, const CUtensorMap& xmap, const CUtensorMap& wmap, int n_sm, int dev, cudaStream_t stream) {
-    const bool y16 = a.y_type != TDQ_F32;
+    const bool y16 = a.y_type != TDQ_F32, f16 = a.y_type == TDQ_F16;
     CUtensorMap ymap;
     memset(&ymap, 0, sizeof ymap);
-    if (a.y_vec && !encode_y_map(&ymap, a.y, y16, a.M, a.O, a.y_stride, y16 ? 64 : 32, 32, a.y_type == TDQ_F16)) a.y_vec = 0;
+    if (a.y_vec && !encode_y_map(&ymap, a.y, y16, a.M, a.O, a.y_stride, y16 ? 64 : 32, 32, f16)) a.y_vec = 0;
     a.tiles_m = (int32_t)((a.M + 255) / 256);
     a.tiles_n = (int32_t)((a.O + 255) / 256);
-    constexpr uint32_t fixed = kPairCtrl + 1024 + kAddWarps * (kStrip + kBiasBytes);
-    a.n_stages = (kSmemLimit - (int)fixed) / (int)kPairStage;
-    if (a.n_stages > kPairMaxStages) a.n_stages = kPairMaxStages;
-    const uint32_t smem = fixed + (uint32_t)a.n_stages * kPairStage;
-    static std::atomic<uint64_t> smem_done[2];
-    void (*const kernels[2])(Fp8Args, CUtensorMap, CUtensorMap, CUtensorMap) = {fp8_pair_kernel<false>, fp8_pair_kernel<true>};
-    if (allow_smem(kernels[y16], kSmemLimit, smem_done[y16], dev) != cudaSuccess) return TDQ_ERR_CUDA;
+    constexpr uint32_t smem = kPairCtrl + kPairStages * kPairStage + kAddWarps * (kStrips * kStrip + kBiasBytes) + kScaleSlots * kScaleBytes;
+    static_assert(smem <= (uint32_t)kSmemLimit, "shared memory");
+    static std::atomic<uint64_t> smem_done[3];
+    void (*const kernels[3])(Fp8Args, CUtensorMap, CUtensorMap, CUtensorMap) = {fp8_pair_kernel<TDQ_F32>, fp8_pair_kernel<TDQ_BF16>, fp8_pair_kernel<TDQ_F16>};
+    if (allow_smem(kernels[a.y_type], (int)smem, smem_done[a.y_type], dev) != cudaSuccess) return TDQ_ERR_CUDA;
     const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n;
     if (tiles > INT32_MAX / 2) return TDQ_ERR_UNSUPPORTED;
     const unsigned clusters = (unsigned)(tiles < n_sm / 2 ? tiles : n_sm / 2);
-    if (launch_pdl(kernels[y16], dim3(2 * clusters), dim3(kPairThreads), smem, stream, a, xmap, wmap, ymap) != cudaSuccess) return TDQ_ERR_CUDA;
+    if (launch_pdl(kernels[a.y_type], dim3(2 * clusters), dim3(kPairThreads), smem, stream, a, xmap, wmap, ymap) != cudaSuccess) return TDQ_ERR_CUDA;
     g_launch_count.fetch_add(1, std::memory_order_relaxed);
     return TDQ_OK;
 }

@@ -4,6 +4,7 @@
 // fused and the power-of-two variants), tdq_linear_pair.cu, tdq_linear_defer.cu, tdq_linear_solo.cu, tdq_linear_strip.cu,
 // tdq_linear_g32.cu and tdq_linear_one.cu.
 #pragma once
+#define TDQ_TC_CUH_
 #include <cuda.h>
 #include <cuda_fp16.h>
 #include <cstring>
