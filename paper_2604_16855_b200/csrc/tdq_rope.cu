@@ -9,8 +9,11 @@
 //
 // Bound by HBM: every head is read and written once.  A thread owns the two 16-byte vectors of a head whose elements form pairs (halves:
 // one from either half; adjacent: neighbours), so that a head is a power of two of lanes, its sum of squares a few shuffles, and
-// no element passes through another thread: in place is safe.  A thread block takes a few tokens with all their heads: their cosines and sines
-// are computed once, into shared memory, while the heads' loads are in flight.
+// no element passes through another thread: in place is safe.  A thread block takes some tokens with all their heads; a warp keeps to a
+// group of heads and goes through the tokens with the next two's loads in flight.  The weights and the block's cosines and
+// sines, computed once, are in shared memory, laid out so that the lanes of a head read consecutive 16-byte pieces: with a thread's
+// eight pairs in one piece, four lanes met in every bank and shared memory was busy for 77 % of the time (88 us on 16384 tokens x 40 heads x 128
+// bf16).  A warp per token with cosines times weights in 32 registers had too few loads in flight (95 us).
 #include <cuda_fp16.h>
 
 #include "tdq_common.cuh"
@@ -18,7 +21,8 @@
 namespace tdq {
 namespace {
 
-constexpr int kMaxWarps = 16;
+constexpr int kRopeWarps = 8;
+constexpr size_t kTableMax = 32 * 1024;     // bytes of cosines and sines of a block (16 KB for eight tokens of 256 pairs)
 
 struct RopeArgs {
     tdq_rope_heads q, k;
@@ -30,7 +34,8 @@ struct RopeArgs {
     int32_t D, half, n_axes;   // half = R / 2
     int32_t norm, adjacent;
     float eps;
-    int32_t tokens, groups;    // per block: tokens; head groups (one warp each) per token
+    int32_t tokens, groups;    // of a block; of a token's heads, one for a warp at a time
+    int32_t warps_across;      // warps of a block that share a token's groups
     int32_t lanes_log2;        // lanes of a head
 };
 
@@ -92,90 +97,117 @@ __device__ __forceinline__ float2 turn_of(const RopeArgs& a, int64_t m, int i) {
     return make_float2(c, s);
 }
 
+// Blocks of 256 threads per SM, which bounds the registers: loads in flight are what counts.  16 bits, three against none asked for:
+// 16384 x 40 x 128 65.3 -> 62.1 us, 18432 x 24 x 64 28.6 -> 24.6 (four: 62.6, 25.9); binary32, four: 8192 x 32 x 80 42.0 -> 37.2 (three: 44.7).
+template <int DT> constexpr int rope_blocks = DT == TDQ_F32 ? 4 : 3;
 template <int DT, bool ADJ>
-__global__ void __launch_bounds__(kMaxWarps * 32) rope_kernel(const RopeArgs a) {
+__global__ void __launch_bounds__(kRopeWarps * 32, rope_blocks<DT>) rope_kernel(const RopeArgs a) {
     using T = typename Bits<DT>::T;
     constexpr int V = 16 / (int)sizeof(T);                 // elements of a vector, pairs of a thread
-    extern __shared__ float2 table[];                      // [tokens][half]
+    extern __shared__ float4 shared[];
     pdl_wait();
     pdl_trigger();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t m0 = (int64_t)blockIdx.x * a.tokens;
     const int n_tok = (int)min((int64_t)a.tokens, a.M - m0);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = blockDim.x >> 5;
-    const int L = 1 << a.lanes_log2, unit = lane & (L - 1), sub = lane >> a.lanes_log2, per_warp = 32 >> a.lanes_log2;
-    const bool has = unit * 2 * V < a.D;
-    const bool turns = unit * V < a.half;                  // a unit of the rotated channels (R is a multiple of 2 V)
-    // element offsets of the thread's two vectors in a head
-    const int e0 = ADJ || !turns ? 2 * unit * V : unit * V, e1 = ADJ || !turns ? e0 + V : a.half + unit * V;
-    bool have_table = false;                               // every warp has an item
-    for (int item = warp; item < a.tokens * a.groups; item += n_warps) {
-        const int tb = item / a.groups, head = (item - tb * a.groups) * per_warp + sub;
-        const bool on = has && tb < n_tok && head < a.H;
-        const bool is_q = head < a.Hq;
-        const tdq_rope_heads& s = is_q ? a.q : a.k;
-        const int64_t m = m0 + tb;
-        const int hh = is_q ? head : head - a.Hq;
-        uint4 v0 = make_uint4(0, 0, 0, 0), v1 = v0;
-        if (on) {
-            const T* p = reinterpret_cast<const T*>(s.x) + m * s.row_stride + hh * s.head_stride;
-            v0 = *reinterpret_cast<const uint4*>(p + e0);
-            v1 = *reinterpret_cast<const uint4*>(p + e1);
-        }
-        if (!have_table) {                                 // the first loads are in flight
+    const int L = 1 << a.lanes_log2, unit = lane & (L - 1), units = a.half / V, all_units = a.D / (2 * V);
+    float4* const weights = shared;                        // [queries, keys][V / 2][units of a head]: four weights
+    float4* const table = shared + (a.norm ? V * all_units : 0);   // [tokens][V / 2][turned units]: two pairs' cosine and sine
+    const int row = warp / a.warps_across, across = warp - row * a.warps_across;   // the warp's first token and head group
+    const int rows = (int)(blockDim.x >> 5) / a.warps_across;
+    const bool has = unit < all_units, turns = unit < units;   // a unit of the turned channels (R is a multiple of 2 V)
+    // element offsets of a unit's two vectors in a head
+    const auto first_of = [&](int u) { return ADJ || u >= units ? 2 * u * V : u * V; };
+    const auto second_of = [&](int u) { return ADJ || u >= units ? (2 * u + 1) * V : a.half + u * V; };
+    const int e0 = first_of(unit), e1 = second_of(unit);
+    bool have_table = false;                               // every warp goes through the loop at least once
+    for (int group = across; group < a.groups; group += a.warps_across) {
+        const int head = (group << (5 - a.lanes_log2)) + (lane >> a.lanes_log2);
+        const bool mine = has && head < a.H, is_q = head < a.Hq;
+        const int64_t in_step = rows * (is_q ? a.q.row_stride : a.k.row_stride), out_step = rows * (is_q ? a.q.out_row_stride : a.k.out_row_stride);
+        const T* src = is_q ? reinterpret_cast<const T*>(a.q.x) + head * a.q.head_stride + (m0 + row) * a.q.row_stride
+                            : reinterpret_cast<const T*>(a.k.x) + (head - a.Hq) * a.k.head_stride + (m0 + row) * a.k.row_stride;
+        T* dst = is_q ? reinterpret_cast<T*>(a.q.out) + head * a.q.out_head_stride + (m0 + row) * a.q.out_row_stride
+                      : reinterpret_cast<T*>(a.k.out) + (head - a.Hq) * a.k.out_head_stride + (m0 + row) * a.k.out_row_stride;
+        uint4 ahead[2][2];                                 // the loads of two tokens
+        const auto load = [&](uint4* v, int t) {
+            v[0] = v[1] = make_uint4(0, 0, 0, 0);
+            if (mine && t < n_tok) {
+                v[0] = *reinterpret_cast<const uint4*>(src + e0);
+                v[1] = *reinterpret_cast<const uint4*>(src + e1);
+            }
+            src += in_step;
+        };
+        load(ahead[0], row);
+        load(ahead[1], row + rows);
+        if (!have_table) {                                 // meanwhile
+            if (a.norm)
+                for (int i = threadIdx.x; i < V * all_units; i += blockDim.x) {
+                    const int k = i / all_units, u = i - k * all_units, c = k % (V / 2);
+                    const float* w = k >= V / 2 ? a.k.weight : a.q.weight;
+                    const int e = c < V / 4 ? first_of(u) + 4 * c : second_of(u) + 4 * (c - V / 4);
+                    weights[i] = w ? __ldg(reinterpret_cast<const float4*>(w + e)) : make_float4(1.f, 1.f, 1.f, 1.f);
+                }
             for (int i = threadIdx.x; i < n_tok * a.half; i += blockDim.x) {
-                const int t = i / a.half;
-                table[i] = turn_of(a, m0 + t, i - t * a.half);
+                const int t = i / a.half, pair = i - t * a.half, u = pair / V, j = pair - u * V;
+                reinterpret_cast<float2*>(table)[((t * (V / 2) + (j >> 1)) * units + u) * 2 + (j & 1)] = turn_of(a, m0 + t, pair);
             }
             __syncthreads();
             have_table = true;
         }
-        float x[V], y[V];
-        unpack<DT>(v0, x);
-        unpack<DT>(v1, y);
-        if (a.norm) {
-            float ss = 0.f;
+        const float4* const wt = weights + (is_q ? 0 : V / 2 * all_units) + unit;
+        const auto head_of_token = [&](uint4* v, int t) {
+            float x[V], y[V];
+            unpack<DT>(v[0], x);
+            unpack<DT>(v[1], y);
+            load(v, t + 2 * rows);
+            if (a.norm) {
+                float ss = 0.f, st = 0.f;
 #pragma unroll
-            for (int j = 0; j < V; ++j) ss = fmaf(x[j], x[j], fmaf(y[j], y[j], ss));
-            for (int d = 1; d < L; d <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
-            const float r = rsqrtf(ss / (float)a.D + a.eps);
-            if (on && s.weight) {
-#pragma unroll
-                for (int j = 0; j < V; j += 4) {
-                    const float4 w0 = __ldg(reinterpret_cast<const float4*>(s.weight + e0 + j)), w1 = __ldg(reinterpret_cast<const float4*>(s.weight + e1 + j));
-                    x[j] *= r * w0.x; x[j + 1] *= r * w0.y; x[j + 2] *= r * w0.z; x[j + 3] *= r * w0.w;
-                    y[j] *= r * w1.x; y[j + 1] *= r * w1.y; y[j + 2] *= r * w1.z; y[j + 3] *= r * w1.w;
+                for (int j = 0; j < V; ++j) {
+                    ss = fmaf(x[j], x[j], ss);
+                    st = fmaf(y[j], y[j], st);
                 }
-            } else {
+                ss += st;
+                for (int d = 1; d < L; d <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
+                const float r = rsqrtf(ss / (float)a.D + a.eps);
+                if (mine) {
 #pragma unroll
-                for (int j = 0; j < V; ++j) { x[j] *= r; y[j] *= r; }
-            }
-        }
-        if (on) {
-            if (turns) {
-                const float2* cs = table + tb * a.half + unit * V;
-                if constexpr (ADJ) {
-#pragma unroll
-                    for (int j = 0; j < V; j += 2) {
-                        const float2 p = cs[j / 2], q = cs[V / 2 + j / 2];
-                        const float xa = x[j], xb = x[j + 1], ya = y[j], yb = y[j + 1];
-                        x[j] = xa * p.x - xb * p.y;
-                        x[j + 1] = xb * p.x + xa * p.y;
-                        y[j] = ya * q.x - yb * q.y;
-                        y[j + 1] = yb * q.x + ya * q.y;
-                    }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        const float2 p = cs[j];
-                        const float xa = x[j], yb = y[j];
-                        x[j] = xa * p.x - yb * p.y;
-                        y[j] = yb * p.x + xa * p.y;
+                    for (int c = 0; c < V / 4; ++c) {
+                        const float4 p = wt[c * all_units], q = wt[(c + V / 4) * all_units];
+                        x[4 * c] *= r * p.x; x[4 * c + 1] *= r * p.y; x[4 * c + 2] *= r * p.z; x[4 * c + 3] *= r * p.w;
+                        y[4 * c] *= r * q.x; y[4 * c + 1] *= r * q.y; y[4 * c + 2] *= r * q.z; y[4 * c + 3] *= r * q.w;
                     }
                 }
             }
-            T* p = reinterpret_cast<T*>(s.out) + m * s.out_row_stride + hh * s.out_head_stride;
-            *reinterpret_cast<uint4*>(p + e0) = pack<DT>(x);
-            *reinterpret_cast<uint4*>(p + e1) = pack<DT>(y);
+            if (mine) {
+                if (turns) {
+                    // pair j: halves x[j], y[j]; adjacent the neighbours of x, then of y
+                    const float4* cs = table + t * (V / 2) * units + unit;
+#pragma unroll
+                    for (int i = 0; i < V / 2; ++i) {
+                        const float4 two = cs[i * units];
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const int j = 2 * i + k;
+                            const float c = k ? two.z : two.x, n = k ? two.w : two.y;
+                            float& p = ADJ ? (j < V / 2 ? x[(2 * j) % V] : y[(2 * j) % V]) : x[j];
+                            float& q = ADJ ? (j < V / 2 ? x[(2 * j + 1) % V] : y[(2 * j + 1) % V]) : y[j];
+                            const float p0 = p, q0 = q;
+                            p = p0 * c - q0 * n;
+                            q = q0 * c + p0 * n;
+                        }
+                    }
+                }
+                *reinterpret_cast<uint4*>(dst + e0) = pack<DT>(x);
+                *reinterpret_cast<uint4*>(dst + e1) = pack<DT>(y);
+            }
+            dst += out_step;
+        };
+        for (int t = row; t < n_tok; t += 2 * rows) {
+            head_of_token(ahead[0], t);
+            if (t + rows >= n_tok) break;
+            head_of_token(ahead[1], t + rows);
         }
     }
 }
@@ -226,20 +258,28 @@ tdq_status launch(RopeArgs a, cudaStream_t st) {
         return reinterpret_cast<uintptr_t>(s.x) % 16 == 0 && reinterpret_cast<uintptr_t>(s.out) % 16 == 0 && reinterpret_cast<uintptr_t>(s.weight) % 16 == 0 &&
                s.row_stride % V == 0 && s.head_stride % V == 0 && s.out_row_stride % V == 0 && s.out_head_stride % V == 0;
     };
+    const int n_sm = current_device_sm_count();
+    if (n_sm <= 0) return TDQ_ERR_CUDA;
     cudaError_t e;
     // a head of at most 32 lanes, whole vectors on either side of the rotated channels' middle and end
     if (a.D % (2 * V) == 0 && a.half % V == 0 && a.D <= 64 * V && fits(a.q) && fits(a.k)) {
         a.lanes_log2 = 0;
         while ((2 * V << a.lanes_log2) < a.D) ++a.lanes_log2;
-        const int per_warp = 32 >> a.lanes_log2;
-        a.groups = (a.H + per_warp - 1) / per_warp;
-        // about eight warps a block, each with one item; small heads come several tokens at a time
-        a.tokens = a.groups >= 8 ? 1 : 8 / a.groups;
-        const int items = a.tokens * a.groups, warps = items < kMaxWarps ? items : kMaxWarps;
-        const size_t smem = (size_t)a.tokens * a.half * sizeof(float2);   // at most 8 x 256 pairs, 16 KB
+        const int per_warp = 32 >> a.lanes_log2, groups = (a.H + per_warp - 1) / per_warp;
+        // about eight warps: all of a token's head groups side by side where there are no more, several tokens where there are few
+        a.groups = groups;
+        a.warps_across = groups < kRopeWarps ? groups : (groups + (groups + kRopeWarps - 1) / kRopeWarps - 1) / ((groups + kRopeWarps - 1) / kRopeWarps);
+        const int rows = kRopeWarps / a.warps_across;
+        // Tokens a warp goes through: eight, fewer where that leaves fewer than four blocks an SM (as many as make whole rounds of the blocks
+        // that the SMs hold: 2048 tokens 11.5 -> 13.7 us, 16384 62.1 -> 64.0; twice as many: 65.1).
+        int64_t deep = a.M / ((int64_t)n_sm * 4 * rows);
+        deep = deep > 8 ? 8 : deep < 1 ? 1 : deep;
+        a.tokens = rows * (int)deep;
+        while ((size_t)a.tokens * a.half * sizeof(float2) > kTableMax && a.tokens > rows) a.tokens -= rows;
+        const size_t smem = (size_t)a.tokens * a.half * sizeof(float2) + (a.norm ? 2 * a.D * sizeof(float) : 0);
         const int64_t blocks = (a.M + a.tokens - 1) / a.tokens;
         if (blocks > INT32_MAX) return TDQ_ERR_UNSUPPORTED;
-        e = launch_pdl(a.adjacent ? rope_kernel<DT, true> : rope_kernel<DT, false>, dim3((unsigned)blocks), dim3(warps * 32), smem, st, a);
+        e = launch_pdl(a.adjacent ? rope_kernel<DT, true> : rope_kernel<DT, false>, dim3((unsigned)blocks), dim3(rows * a.warps_across * 32), smem, st, a);
     } else {
         const int64_t blocks = (a.M * a.H + 7) / 8;
         if (blocks > INT32_MAX) return TDQ_ERR_UNSUPPORTED;
