@@ -8,8 +8,8 @@
 // has.  128 output channels are the instruction's 128 rows and NT tokens (16 .. 128) its columns; the contraction is cut in up to eight
 // parts, one CTA of a cluster each, whose sums meet in distributed shared memory and are added there in rank order: no
 // atomics, no workspace, the same bits every time.  Warp 0 loads (tensor maps, 16 KB of weights and the tokens' 128 bytes a stage), warp 1
-// issues, the others scale and add: a thread has one output channel and up to 32 tokens, whose factors xs * ws are laid out
-// in shared memory eight blocks at a time, before they are needed.
+// issues, warp 3 lays out the tokens' factors xs * ws of a block in shared memory, the others scale and add: a thread has one output channel and up
+// to 32 tokens.
 #include "tdq_tc.cuh"
 #include "tdq_fp8.cuh"
 
@@ -39,7 +39,8 @@ constexpr int kSplitMax = 8;                 // CTAs of a cluster
 constexpr int kSplitSlots = 4;               // accumulators in TMEM
 constexpr uint32_t kSplitCtrl = 1024;
 constexpr uint32_t kWBytes = 128 * 128;      // a stage's weights
-constexpr int kChunkF = 8;                   // blocks whose factors are laid out at a time
+constexpr int kFactorChunk = 8;              // blocks whose factors are handed over at a time; two chunks' places
+constexpr int kFactorSlots = 2 * kFactorChunk;
 constexpr int kSplitWarp0 = 4;               // first adding warp
 
 template <int NT> struct SplitShape {
@@ -47,20 +48,43 @@ template <int NT> struct SplitShape {
     static constexpr int kWarps = 4 * (NT / kCols);
     static constexpr int kThreads = (kSplitWarp0 + kWarps) * 32;
     static constexpr uint32_t kStage = kWBytes + NT * 128;
-    static constexpr uint32_t kTable = kChunkF * kCols * 4;  // a warp's factors
     static constexpr uint32_t kIdesc = (1u << 4) | ((uint32_t)(NT >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
-    static constexpr uint32_t kFixed = kSplitCtrl + 1024 + kWarps * kTable;
+    static constexpr uint32_t kFixed = kSplitCtrl + 1024 + kFactorSlots * NT * 4;
 };
 
 struct SplitCtrl {
     uint64_t full[kSplitMaxStages], empty[kSplitMaxStages];
     uint64_t tfull[kSplitSlots], tempty[kSplitSlots];
+    uint64_t factors[kFactorSlots];              // a block's factors are there
+    uint64_t taken[2];                           // a chunk's factors have been read
 };
 static_assert(sizeof(Ctrl) + sizeof(SplitCtrl) <= kSplitCtrl, "control block outgrew its reservation");
 
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, uint64_t* bar) {
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                  ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(smem_u32(bar)) : "memory");
+}
+// N consecutive columns of this warp's 32 TMEM lanes, waited for: lane i receives row i
+template <int N>
+__device__ __forceinline__ void tmem_ld_wait(uint32_t taddr, uint32_t* v) {
+    static_assert(N == 16 || N == 32, "columns");
+    if constexpr (N == 16)
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {"
+                     "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\ttcgen05.wait::ld.sync.aligned;"
+                     : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+                       "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+                     : "r"(taddr)
+                     : "memory");
+    else
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {"
+                     "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+                     "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\ttcgen05.wait::ld.sync.aligned;"
+                     : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+                       "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]),
+                       "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]),
+                       "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+                     : "r"(taddr)
+                     : "memory");
 }
 __device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
     float4 v;
@@ -84,8 +108,12 @@ fp8_split_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, cons
     if (threadIdx.x == 0) {
         for (int i = 0; i < kSplitMaxStages; ++i) { mbar_init(&g->full[i], 1); mbar_init(&g->empty[i], 1); }
         for (int i = 0; i < kSplitSlots; ++i) { mbar_init(&g->tfull[i], 1); mbar_init(&g->tempty[i], Sh::kWarps); }
+        for (int i = 0; i < kFactorSlots; ++i) mbar_init(&g->factors[i], 1);
+        for (int i = 0; i < 2; ++i) mbar_init(&g->taken[i], Sh::kWarps);
         c->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&wmap)) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&xmap)) : "memory");
     }
     if (warp == 2) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&c->tmem_base)), "n"(kSplitSlots * NT) : "memory");
@@ -101,6 +129,7 @@ fp8_split_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, cons
     const uint32_t split = (uint32_t)a.split, rank = split > 1 ? fp8_cluster_rank() : 0u;
     const uint32_t tile = blockIdx.x / split;                // token tiles of an output tile follow each other: its weights stay in L2
     const int ot = (int)(tile / (uint32_t)a.tiles_m), tt = (int)(tile - (uint32_t)ot * (uint32_t)a.tiles_m);
+    const uint32_t factors_s = ring_s + n_stages * Sh::kStage;
     const int kb0 = (int)((int64_t)a.K * rank / split), n_kb = (int)((int64_t)a.K * (rank + 1) / split) - kb0;
 
     if (warp == 0) {
@@ -137,66 +166,76 @@ fp8_split_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, cons
             __syncwarp();
             if (++s == n_stages) { s = 0; ph ^= 1; }
         }
+    } else if (warp == 3) {
+        // ------------------------------------------------------------ factors
+        constexpr int kTok = (NT + 31) / 32;                 // tokens per lane
+        const float* ws = a.wscale + (int64_t)ot * a.K + kb0;
+        const float* xs[kTok];
+#pragma unroll
+        for (int i = 0; i < kTok; ++i) xs[i] = a.xscale + min((int64_t)tt * NT + lane + 32 * i, a.M - 1) * a.K + kb0;   // past the end: never stored
+        float f[kFactorChunk][kTok];
+        const auto load = [&](int c0) {
+#pragma unroll
+            for (int q = 0; q < kFactorChunk; ++q) {
+                const int kb = min(c0 + q, n_kb - 1);
+                const float w = __ldg(ws + kb);
+#pragma unroll
+                for (int i = 0; i < kTok; ++i) f[q][i] = __ldg(xs[i] + kb) * w;
+            }
+        };
+        load(0);
+        for (int c0 = 0; c0 < n_kb && !c->abort_flag; c0 += kFactorChunk) {
+            const int half = (c0 / kFactorChunk) & 1;
+            if (c0 >= kFactorSlots) fp8_wait(smem_u32(&g->taken[half]), (uint32_t)(c0 / kFactorSlots + 1) & 1u, c, a.status, 6u);
+#pragma unroll
+            for (int q = 0; q < kFactorChunk; ++q) {
+                const uint32_t place = (uint32_t)(half * kFactorChunk + q), at = factors_s + (place * NT + lane) * 4u;
+                if (c0 + q < n_kb) {
+#pragma unroll
+                    for (int j = 0; j < kTok; ++j)
+                        if (NT >= 32 || lane < NT) sts32(at + j * 128, __float_as_uint(f[q][j]));
+                    __syncwarp();
+                    mbar_arrive_lane0_s(smem_u32(&g->factors[place]), lane);
+                }
+            }
+            if (c0 + kFactorChunk < n_kb) load(c0 + kFactorChunk);
+        }
     } else if (warp >= kSplitWarp0) {
         // ------------------------------------------------------------ scaled sums
         const int pw = warp - kSplitWarp0, quarter = warp & 3, cg = pw >> 2;
-        const uint32_t table_s = ring_s + n_stages * Sh::kStage + (uint32_t)pw * Sh::kTable;
-        const int64_t tok = (int64_t)tt * NT + cg * CW + lane;
-        const bool mine = lane < CW && tok < a.M;
-        const float* xs = a.xscale + (mine ? tok * a.K + kb0 : 0);
-        const float* ws = a.wscale + (int64_t)ot * a.K + kb0;
-        float f[kChunkF];
+        float2 acc[CW / 2];
 #pragma unroll
-        for (int q = 0; q < kChunkF; ++q) f[q] = mine && q < n_kb ? __ldg(xs + q) * __ldg(ws + q) : 0.f;
-        uint64_t acc[CW / 2];
-#pragma unroll
-        for (int j = 0; j < CW / 2; ++j) acc[j] = 0ull;
-        uint32_t v[32];
-#pragma unroll
-        for (int q = 0; q < 32; ++q) v[q] = 0u;
-        for (int c0 = 0; c0 < n_kb && !c->abort_flag; c0 += kChunkF) {
-            __syncwarp();
-            if (lane < CW) {
-#pragma unroll
-                for (int q = 0; q < kChunkF; ++q) sts32(table_s + (uint32_t)(q * CW + lane) * 4u, __float_as_uint(f[q]));
-            }
-            __syncwarp();
-#pragma unroll
-            for (int q = 0; q < kChunkF; ++q) {
-                const int kb = c0 + kChunkF + q;
-                f[q] = mine && kb < n_kb ? __ldg(xs + kb) * __ldg(ws + kb) : 0.f;
-            }
-            const int n = min(kChunkF, n_kb - c0);
+        for (int j = 0; j < CW / 2; ++j) acc[j] = make_float2(0.f, 0.f);
 #pragma unroll 1
-            for (int q = 0; q < n; ++q) {
-                const uint32_t i = (uint32_t)(c0 + q), slot = i % kSplitSlots;
-                fp8_wait(smem_u32(&g->tfull[slot]), (i / kSplitSlots) & 1u, c, a.status, 2u);
-                if (c->abort_flag) break;
-                tc_fence_after();
-                const uint32_t tm = tmem_base + ((uint32_t)(quarter * 32) << 16) + slot * NT + cg * CW;
-                if constexpr (CW == 32) tmem_ld32(tm, v);
-                else tmem_ld16(tm, v);
-                tmem_ld_wait_on(v);
-                tc_fence_before();
-                __syncwarp();
-                mbar_arrive_lane0_s(smem_u32(&g->tempty[slot]), lane);
+        for (int i = 0; i < n_kb; ++i) {
+            const uint32_t slot = (uint32_t)i % kSplitSlots, place = (uint32_t)i % kFactorSlots;
+            fp8_wait(smem_u32(&g->factors[place]), ((uint32_t)i / kFactorSlots) & 1u, c, a.status, 7u);
+            fp8_wait(smem_u32(&g->tfull[slot]), ((uint32_t)i / kSplitSlots) & 1u, c, a.status, 2u);
+            if (c->abort_flag) break;
+            tc_fence_after();
+            uint32_t v[CW];
+            tmem_ld_wait<CW>(tmem_base + ((uint32_t)(quarter * 32) << 16) + slot * NT + cg * CW, v);
+            tc_fence_before();
+            __syncwarp();
+            mbar_arrive_lane0_s(smem_u32(&g->tempty[slot]), lane);
+            const uint32_t f_s = factors_s + (place * NT + cg * CW) * 4u;
 #pragma unroll
-                for (int j = 0; j < CW / 4; ++j) {
-                    uint64_t f0, f1;
-                    lds128(table_s + (uint32_t)(q * CW + 4 * j) * 4u, f0, f1);
-                    fma2(acc[2 * j], pack2(v[4 * j], v[4 * j + 1]), f0);
-                    fma2(acc[2 * j + 1], pack2(v[4 * j + 2], v[4 * j + 3]), f1);
-                }
+            for (int j = 0; j < CW / 4; ++j) {
+                const float4 f = lds_f4(f_s + 16u * j);
+                acc[2 * j] = __ffma2_rn(make_float2(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1])), make_float2(f.x, f.y), acc[2 * j]);
+                acc[2 * j + 1] = __ffma2_rn(make_float2(__uint_as_float(v[4 * j + 2]), __uint_as_float(v[4 * j + 3])), make_float2(f.z, f.w), acc[2 * j + 1]);
+            }
+            if (i % kFactorChunk == kFactorChunk - 1) {
+                __syncwarp();
+                mbar_arrive_lane0_s(smem_u32(&g->taken[(i / kFactorChunk) & 1]), lane);
             }
         }
         // the last instruction has read the ring; the sums take its place, token by token
 #pragma unroll
         for (int j = 0; j < CW / 2; ++j) {
-            float lo, hi;
-            unpack2(acc[j], lo, hi);
             const uint32_t at = ring_s + ((uint32_t)(cg * CW + 2 * j) * 128u + (uint32_t)(quarter * 32 + lane)) * 4u;
-            sts32(at, __float_as_uint(lo));
-            sts32(at + 512u, __float_as_uint(hi));
+            sts32(at, __float_as_uint(acc[j].x));
+            sts32(at + 512u, __float_as_uint(acc[j].y));
         }
     }
 

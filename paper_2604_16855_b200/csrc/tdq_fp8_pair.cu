@@ -91,11 +91,6 @@ __device__ __forceinline__ void scale_add64(float2* acc, const uint32_t* v, floa
         asm volatile("" ::"f"(acc[j].x), "f"(acc[j + 1].x), "f"(acc[j + 2].x), "f"(acc[j + 3].x), "f"(acc[j + 4].x), "f"(acc[j + 5].x), "f"(acc[j + 6].x),
                      "f"(acc[j + 7].x));
 }
-__device__ __forceinline__ float4 lds_f4(uint32_t addr) {
-    float4 v;
-    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-    return v;
-}
 __device__ __forceinline__ void copy4_async(uint32_t dst, const float* src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
