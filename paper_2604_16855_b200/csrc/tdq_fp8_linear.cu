@@ -6,8 +6,11 @@
 //
 // fp8_split_kernel.  Few tokens: the time is that of reading the weights once, so all SMs have to read, however few rows the output
 // has.  128 output channels are the instruction's 128 rows and NT tokens (16 .. 128) its columns; the contraction is cut in up to eight
-// parts, one CTA of a cluster each, whose sums meet in distributed shared memory and are added there in rank order: no
-// atomics, no workspace, the same bits every time.  Warp 0 loads (tensor maps, 16 KB of weights and the tokens' 128 bytes a stage), warp 1
+// parts, one CTA of a cluster each, whose sums meet in distributed shared memory and are added in rank order: no atomics, no
+// workspace, the same bits every time.  Up to 32 tokens the parts send their sums (st.async, counted by a barrier of the channel's owner): read between
+// two cluster barriers that order memory they took 3100 of 9500 clocks on 1 x 4096 -> 4096, as much as the loads (6.2 -> 5.4 us).
+// More sums than that are read by their owners all the same (128 tokens: 10.1 us, sent 11.3), since the room that they need where they are sent
+// is two ring stages, and an owner of channels stores narrower pieces than an owner of tokens.  Warps 0 and 2 load (tensor maps, 16 KB of weights and the tokens' 128 bytes a stage), warp 1
 // issues, warp 3 lays out the tokens' factors xs * ws of a block in shared memory, the others scale and add: a thread has one output channel and up
 // to 32 tokens.
 #include "tdq_tc.cuh"
@@ -49,7 +52,9 @@ template <int NT> struct SplitShape {
     static constexpr int kThreads = (kSplitWarp0 + kWarps) * 32;
     static constexpr uint32_t kStage = kWBytes + NT * 128;
     static constexpr uint32_t kIdesc = (1u << 4) | ((uint32_t)(NT >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
-    static constexpr uint32_t kFixed = kSplitCtrl + 1024 + kFactorSlots * NT * 4;
+    static constexpr uint32_t kSumStride = (NT + 4) * 4;     // bytes of a channel's sums, one part
+    static constexpr bool kSend = NT <= 32;                  // sums are sent, not read
+    static constexpr uint32_t kFixed = kSplitCtrl + 1024 + kFactorSlots * NT * 4 + (kSend ? (128 + kSplitMax) * kSumStride : 0);
 };
 
 struct SplitCtrl {
@@ -57,6 +62,7 @@ struct SplitCtrl {
     uint64_t tfull[kSplitSlots], tempty[kSplitSlots];
     uint64_t factors[kFactorSlots];              // a block's factors are there
     uint64_t taken[2];                           // a chunk's factors have been read
+    uint64_t sums;                               // all parts' sums of this CTA's channels have arrived
 };
 static_assert(sizeof(Ctrl) + sizeof(SplitCtrl) <= kSplitCtrl, "control block outgrew its reservation");
 
@@ -91,6 +97,14 @@ __device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
     asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
     return v;
 }
+// The arrival that orders nothing: one that does waits for the thread's stores, about 2000 clocks behind those of y.
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// sixteen bytes to another CTA's shared memory, counted by a barrier there
+__device__ __forceinline__ void send16(uint32_t addr_c, float2 a, float2 b, uint32_t bar_c) {
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
+                 ::"r"(addr_c), "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "r"(bar_c) : "memory");
+}
 
 template <int NT>
 __global__ void __launch_bounds__(SplitShape<NT>::kThreads, NT == 128 ? 1 : 2)
@@ -106,10 +120,11 @@ fp8_split_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, cons
     const int warp = uniform_warp(), lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kSplitMaxStages; ++i) { mbar_init(&g->full[i], 1); mbar_init(&g->empty[i], 1); }
+        for (int i = 0; i < kSplitMaxStages; ++i) { mbar_init(&g->full[i], 2); mbar_init(&g->empty[i], 1); }
         for (int i = 0; i < kSplitSlots; ++i) { mbar_init(&g->tfull[i], 1); mbar_init(&g->tempty[i], Sh::kWarps); }
         for (int i = 0; i < kFactorSlots; ++i) mbar_init(&g->factors[i], 1);
         for (int i = 0; i < 2; ++i) mbar_init(&g->taken[i], Sh::kWarps);
+        mbar_init(&g->sums, 1);
         c->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&wmap)) : "memory");
@@ -119,33 +134,40 @@ fp8_split_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, cons
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&c->tmem_base)), "n"(kSplitSlots * NT) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    const uint32_t split = (uint32_t)a.split, rank = split > 1 ? fp8_cluster_rank() : 0u;
     tc_fence_before();
     __syncthreads();
+    if (split > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");   // this CTA's barriers are initialised
     tc_fence_after();
     pdl_wait();
     pdl_trigger();
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0u;
     const uint32_t tmem_base = c->tmem_base;
-    const uint32_t split = (uint32_t)a.split, rank = split > 1 ? fp8_cluster_rank() : 0u;
     const uint32_t tile = blockIdx.x / split;                // token tiles of an output tile follow each other: its weights stay in L2
     const int ot = (int)(tile / (uint32_t)a.tiles_m), tt = (int)(tile - (uint32_t)ot * (uint32_t)a.tiles_m);
-    const uint32_t factors_s = ring_s + n_stages * Sh::kStage;
+    const uint32_t factors_s = ring_s + n_stages * Sh::kStage, sums_s = factors_s + kFactorSlots * NT * 4;
+    const int n_tok = (int)min((int64_t)NT, a.M - (int64_t)tt * NT);
+    // channels [mine, mine + n_mine) of the tile are finished here
+    const uint32_t per = (128u + split - 1u) / split, mine = rank * per, n_mine = min(per, 128u - mine);
+    if (Sh::kSend && split > 1 && threadIdx.x == 0) mbar_expect_tx(&g->sums, n_mine * split * (((uint32_t)n_tok + 3u) & ~3u) * 4u);
     const int kb0 = (int)((int64_t)a.K * rank / split), n_kb = (int)((int64_t)a.K * (rank + 1) / split) - kb0;
 
-    if (warp == 0) {
-        // ------------------------------------------------------------ loads
-        uint32_t s = 0, ph = 1;
+    if (warp == 0 || warp == 2) {
+        // ------------------------------------------------------------ loads: weights by warp 0, tokens by warp 2
+        const bool is_w = warp == 0;
+        const uint32_t bytes = is_w ? kWBytes : NT * 128, dst = ring_s + (is_w ? 0u : kWBytes);
+        const int row = is_w ? ot * 128 : tt * NT;
+        uint32_t s = 0, ph = 0;
+#pragma unroll 1
         for (int i = 0; i < n_kb; ++i) {
-            fp8_wait(smem_u32(&g->empty[s]), ph, c, a.status, 5u);
+            if (i >= (int)n_stages) fp8_wait(smem_u32(&g->empty[s]), ph, c, a.status, 5u);
             if (c->abort_flag) break;
             if (elect_one()) {
-                const uint32_t dst = ring_s + s * Sh::kStage;
-                mbar_expect_tx(&g->full[s], Sh::kStage);
-                tma_load_2d(dst, &wmap, (kb0 + i) * (int)kFp8Block, ot * 128, &g->full[s]);
-                tma_load_2d(dst + kWBytes, &xmap, (kb0 + i) * (int)kFp8Block, tt * NT, &g->full[s]);
+                mbar_expect_tx(&g->full[s], bytes);
+                tma_load_2d(dst + s * Sh::kStage, is_w ? &wmap : &xmap, (kb0 + i) * (int)kFp8Block, row, &g->full[s]);
             }
             __syncwarp();
-            if (++s == n_stages) { s = 0; ph ^= 1; }
+            if (++s == n_stages) { s = 0; ph ^= (uint32_t)(i >= (int)n_stages); }
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------ MMA issue
@@ -230,55 +252,95 @@ fp8_split_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, cons
                 mbar_arrive_lane0_s(smem_u32(&g->taken[(i / kFactorChunk) & 1]), lane);
             }
         }
-        // the last instruction has read the ring; the sums take its place, token by token
+        if (split > 1) cluster_wait();                       // all CTAs' barriers are initialised
+        if constexpr (Sh::kSend) {
+            const uint32_t ch = (uint32_t)(quarter * 32 + lane), owner = ch / per;
+            const uint32_t to = sums_s + (rank * per + ch - owner * per) * Sh::kSumStride + cg * CW * 4u;
+            const uint32_t to_c = map_to_cta(to, split > 1 ? owner : 0u), bar_c = map_to_cta(smem_u32(&g->sums), split > 1 ? owner : 0u);
 #pragma unroll
-        for (int j = 0; j < CW / 2; ++j) {
-            const uint32_t at = ring_s + ((uint32_t)(cg * CW + 2 * j) * 128u + (uint32_t)(quarter * 32 + lane)) * 4u;
-            sts32(at, __float_as_uint(acc[j].x));
-            sts32(at + 512u, __float_as_uint(acc[j].y));
-        }
-    }
-
-    tc_fence_before();
-    __syncthreads();
-    if (c->abort_flag) __nanosleep(1000000);                 // a wait gave up: give copies and tensor core a moment
-    if (split > 1) fp8_cluster_sync();
-    const int n_tok = (int)min((int64_t)NT, a.M - (int64_t)tt * NT);
-    const int64_t o0 = (int64_t)ot * 128;
-    for (uint32_t u = rank * Sh::kThreads + threadIdx.x; u < (uint32_t)n_tok * 32u; u += split * Sh::kThreads) {
-        const int64_t o = o0 + (u & 31u) * 4;
-        if (o >= a.O) continue;
-        float r[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-        for (uint32_t p = 0; p < split; ++p) {
-            const float4 q = ld_cluster4(map_to_cta(ring_s + u * 16u, p));
-            r[0] += q.x; r[1] += q.y; r[2] += q.z; r[3] += q.w;
-        }
-        const int left = (int)min((int64_t)4, a.O - o);
-        if (a.bias) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (j < left) r[j] += __ldg(a.bias + o + j);
-        }
-        const int64_t at = ((int64_t)tt * NT + (u >> 5)) * a.y_stride + o;
-        if (a.y_type == TDQ_F32) {
-            float* y = reinterpret_cast<float*>(a.y) + at;
-            if (a.y_vec && left == 4) *reinterpret_cast<float4*>(y) = make_float4(r[0], r[1], r[2], r[3]);
-            else
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (j < left) y[j] = r[j];
+            for (int j = 0; j < CW / 4; ++j) {
+                if (cg * CW + 4 * j >= n_tok) break;
+                if (split > 1) send16(to_c + 16u * j, acc[2 * j], acc[2 * j + 1], bar_c);
+                else sts128(to + 16u * j, __float_as_uint(acc[2 * j].x), __float_as_uint(acc[2 * j].y), __float_as_uint(acc[2 * j + 1].x), __float_as_uint(acc[2 * j + 1].y));
+            }
         } else {
-            uint16_t* y = reinterpret_cast<uint16_t*>(a.y) + at;
-            const uint32_t w0 = pack16(r[0], r[1], a.y_type == TDQ_F16), w1 = pack16(r[2], r[3], a.y_type == TDQ_F16);
-            if (a.y_vec && left == 4) *reinterpret_cast<uint2*>(y) = make_uint2(w0, w1);
-            else
+            // the last instruction has read the ring; the sums take its place, token by token
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (j < left) y[j] = (uint16_t)((j & 2 ? w1 : w0) >> (16 * (j & 1)));
+            for (int j = 0; j < CW / 2; ++j) {
+                const uint32_t at = ring_s + ((uint32_t)(cg * CW + 2 * j) * 128u + (uint32_t)(quarter * 32 + lane)) * 4u;
+                sts32(at, __float_as_uint(acc[j].x));
+                sts32(at + 512u, __float_as_uint(acc[j].y));
+            }
         }
     }
-    if (split > 1) fp8_cluster_sync();                       // no CTA leaves while another reads its sums
+    if (split > 1 && warp < kSplitWarp0) cluster_wait();
+    tc_fence_before();
+    if constexpr (Sh::kSend) {
+        if (split > 1) cluster_arrive_relaxed();                 // nothing more is sent
+        __syncthreads();
+        if (split > 1) fp8_wait(smem_u32(&g->sums), 0u, c, a.status, 8u);
+        // four tokens of a channel a thread: lanes store neighbouring channels
+        const int64_t o0 = (int64_t)ot * 128 + mine;
+        for (uint32_t u = threadIdx.x; u < n_mine * (((uint32_t)n_tok + 3u) / 4u); u += Sh::kThreads) {
+            const uint32_t quad = u / n_mine, ch = u - quad * n_mine;
+            const int64_t o = o0 + ch;
+            if (o >= a.O) continue;
+            const float b = a.bias ? __ldg(a.bias + o) : 0.f;
+            float r[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+            for (uint32_t p = 0; p < split; ++p) {
+                const float4 q = lds_f4(sums_s + (p * per + ch) * Sh::kSumStride + quad * 16u);
+                r[0] += q.x; r[1] += q.y; r[2] += q.z; r[3] += q.w;
+            }
+            const int64_t at = ((int64_t)tt * NT + quad * 4) * a.y_stride + o;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if ((int)(quad * 4) + j >= n_tok) break;
+                if (a.y_type == TDQ_F32) reinterpret_cast<float*>(a.y)[at + j * a.y_stride] = r[j] + b;
+                else reinterpret_cast<uint16_t*>(a.y)[at + j * a.y_stride] = (uint16_t)pack16(r[j] + b, 0.f, a.y_type == TDQ_F16);
+            }
+        }
+    } else {
+        __syncthreads();
+        if (split > 1) fp8_cluster_sync();                       // all CTAs' sums are there
+        const int64_t o0 = (int64_t)ot * 128;
+        for (uint32_t u = rank * Sh::kThreads + threadIdx.x; u < (uint32_t)n_tok * 32u; u += split * Sh::kThreads) {
+            const int64_t o = o0 + (u & 31u) * 4;
+            if (o >= a.O) continue;
+            float r[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+            for (uint32_t p = 0; p < split; ++p) {
+                const float4 q = ld_cluster4(map_to_cta(ring_s + u * 16u, p));
+                r[0] += q.x; r[1] += q.y; r[2] += q.z; r[3] += q.w;
+            }
+            const int left = (int)min((int64_t)4, a.O - o);
+            if (a.bias) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (j < left) r[j] += __ldg(a.bias + o + j);
+            }
+            const int64_t at = ((int64_t)tt * NT + (u >> 5)) * a.y_stride + o;
+            if (a.y_type == TDQ_F32) {
+                float* y = reinterpret_cast<float*>(a.y) + at;
+                if (a.y_vec && left == 4) *reinterpret_cast<float4*>(y) = make_float4(r[0], r[1], r[2], r[3]);
+                else
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (j < left) y[j] = r[j];
+            } else {
+                uint16_t* y = reinterpret_cast<uint16_t*>(a.y) + at;
+                const uint32_t w0 = pack16(r[0], r[1], a.y_type == TDQ_F16), w1 = pack16(r[2], r[3], a.y_type == TDQ_F16);
+                if (a.y_vec && left == 4) *reinterpret_cast<uint2*>(y) = make_uint2(w0, w1);
+                else
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (j < left) y[j] = (uint16_t)((j & 2 ? w1 : w0) >> (16 * (j & 1)));
+            }
+        }
+        if (split > 1) cluster_arrive_relaxed();                 // nothing more is read
+    }
+    if (c->abort_flag) __nanosleep(1000000);                 // a wait gave up: give copies and tensor core a moment
+    if (split > 1) cluster_wait();                           // no CTA leaves while another sends to it or reads from it
     if (warp == 2)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "n"(kSplitSlots * NT) : "memory");
 }
