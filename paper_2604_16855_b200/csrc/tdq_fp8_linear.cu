@@ -345,27 +345,40 @@ fp8_split_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, cons
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "n"(kSplitSlots * NT) : "memory");
 }
 
-// The kernel divides the blocks in `split` nearly equal parts; a part costs its blocks and, when there is more than one, about
-// two blocks' time for meeting.
-int choose_split(int64_t tiles, int K, int n_sm) {
-    int best = 1;
-    int64_t best_cost = INT64_MAX;
-    for (int s = 1; s <= kSplitMax && s <= K; ++s) {
-        const int64_t waves = (tiles * s + n_sm - 1) / n_sm;
-        const int64_t cost = waves * ((K + s - 1) / s + (s > 1 ? 2 : 0));
-        if (cost < best_cost) { best_cost = cost; best = s; }
+// Which kernel, and in how many parts: the least of these estimates in units of 10 ns, fitted to 75 layers (1 to 2304 tokens, 384 to 4096 ->
+// 960 to 8192 channels, from a graph; the choice is within 1 % of the best one measured in the mean, 15 % at worst).
+//   NT tokens, s parts:  start x rounds + block x (blocks of a part) x (CTAs per SM) + 45 for meeting where sums are read (s > 1, NT >= 64);
+//                        a round is two CTAs per SM, one of NT = 128
+//   pairs of CTAs:       385 + 37 K rounds + 160 (rounds - 1);  a round is a tile of 256 x 256 for every pair of SMs
+// Against 128 tokens a tile throughout: 576 x 384 -> 960 6.9 -> 4.7 us, 64 x 768 -> 2304 5.2 -> 4.3, 256 x 1024 -> 1024 6.9 -> 5.4.
+struct Way { int nt, split; };                             // nt == 256: pairs
+Way choose_way(int64_t M, int64_t O, int K, int n_sm) {
+    const int64_t tiles_n = fp8_blocks(O), pair_tiles = ((M + 255) / 256) * ((O + 255) / 256);
+    if (pair_tiles >= n_sm) return {256, 1};
+    Way best = {256, 1};
+    const int64_t pairs = n_sm / 2 > 0 ? n_sm / 2 : 1, pair_rounds = (pair_tiles + pairs - 1) / pairs;
+    int64_t least = M > 64 ? 385 + 37 * K * pair_rounds + 160 * (pair_rounds - 1) : INT64_MAX;
+    static const struct { int nt, start, block; } kinds[4] = {{16, 320, 21}, {32, 360, 32}, {64, 350, 37}, {128, 470, 44}};
+    for (const auto& k : kinds) {
+        if (k.nt > 16 && k.nt / 2 >= M) break;             // more than half of the tile would be empty
+        const int64_t tiles = tiles_n * ((M + k.nt - 1) / k.nt);
+        for (int s = 1; s <= kSplitMax && s <= K; ++s) {
+            const int64_t ctas = tiles * s, per_sm = (ctas + n_sm - 1) / n_sm, rounds = k.nt == 128 ? per_sm : (per_sm + 1) / 2;
+            const int64_t cost = k.start * rounds + (int64_t)k.block * ((K + s - 1) / s) * per_sm + (s > 1 && k.nt >= 64 ? 45 : 0);
+            if (cost < least) { least = cost; best = {k.nt, s}; }
+        }
     }
     return best;
 }
 
 template <int NT>
-tdq_status launch_split(Fp8Args a, const uint8_t* xcodes, const CUtensorMap& wmap, int n_sm, int dev, cudaStream_t stream) {
+tdq_status launch_split(Fp8Args a, int split, const uint8_t* xcodes, const CUtensorMap& wmap, int n_sm, int dev, cudaStream_t stream) {
     using Sh = SplitShape<NT>;
     CUtensorMap xmap;
     if (!fp8_operand_map(&xmap, xcodes, a.M, (int64_t)a.K * kFp8Block, NT)) return TDQ_ERR_CUDA;
     const int64_t tiles_m = (a.M + NT - 1) / NT, tiles_n = fp8_blocks(a.O), tiles = tiles_m * tiles_n;
     if (tiles > (int64_t)INT32_MAX / kSplitMax) return TDQ_ERR_UNSUPPORTED;
-    a.split = choose_split(tiles, a.K, n_sm);
+    a.split = split;
     a.tiles_m = (int32_t)tiles_m;
     a.tiles_n = (int32_t)tiles_n;
     // One CTA per SM with a deep ring while there is an SM for each, else two that share an SM.  Two CTAs of clusters that wait for each
@@ -436,13 +449,12 @@ extern "C" tdq_status tdq_fp8_linear(const uint8_t* xcodes, const float* xscale,
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
     CUtensorMap wmap;
     if (!fp8_operand_map(&wmap, wcodes, O, I_pad, 128)) return TDQ_ERR_CUDA;
-    if (M > 128 && ((M + 255) / 256) * ((O + 255) / 256) >= n_sm / 4) {
-        CUtensorMap xmap;
-        if (!fp8_operand_map(&xmap, xcodes, M, I_pad, 128)) return TDQ_ERR_CUDA;
-        return launch_fp8_pair(a, xmap, wmap, n_sm, dev, st);
-    }
-    if (M <= 16) return launch_split<16>(a, xcodes, wmap, n_sm, dev, st);
-    if (M <= 32) return launch_split<32>(a, xcodes, wmap, n_sm, dev, st);
-    if (M <= 64) return launch_split<64>(a, xcodes, wmap, n_sm, dev, st);
-    return launch_split<128>(a, xcodes, wmap, n_sm, dev, st);
+    const Way way = choose_way(M, O, a.K, n_sm);
+    if (way.nt == 16) return launch_split<16>(a, way.split, xcodes, wmap, n_sm, dev, st);
+    if (way.nt == 32) return launch_split<32>(a, way.split, xcodes, wmap, n_sm, dev, st);
+    if (way.nt == 64) return launch_split<64>(a, way.split, xcodes, wmap, n_sm, dev, st);
+    if (way.nt == 128) return launch_split<128>(a, way.split, xcodes, wmap, n_sm, dev, st);
+    CUtensorMap xmap;
+    if (!fp8_operand_map(&xmap, xcodes, M, I_pad, 128)) return TDQ_ERR_CUDA;
+    return launch_fp8_pair(a, xmap, wmap, n_sm, dev, st);
 }
