@@ -198,14 +198,25 @@ def test_long_contractions_and_many_tiles(tdq, M, I, O):
     _run(tdq, M, I, O, "bf16", False)
 
 
+# The layer's tiles are 16, 32, 64 or 128 tokens wide, with the contraction in one part or several, or 256 x 256: shapes that take each of them.
+WIDTHS = [(9, 200, 300), (31, 1030, 200), (77, 640, 5165), (20, 4096, 4095), (400, 768, 2303), (64, 4096, 4001), (48, 2048, 8190), (100, 4096, 4097),
+          (127, 2048, 8191), (2742, 33 * 128, 100), (1030, 300, 1300)]
+
+
+@pytest.mark.parametrize("M,I,O", WIDTHS)
+@pytest.mark.parametrize("dtype,pitch", [("fp32", 1), ("bf16", 0), ("bf16", 3), ("fp16", 8)])
+def test_every_width_of_tile(tdq, M, I, O, dtype, pitch):
+    _run(tdq, M, I, O, dtype, pitch != 1, pitch)
+
+
 @pytest.mark.parametrize("M,O", [(257, 256 * 37 + 1), (256 * 5 + 1, 256 * 9 - 1), (256 * 38 - 127, 100), (20000, 257)])
 def test_ragged_large_tiles(tdq, M, O):
     _run(tdq, M, 256, O, "fp32", True)
 
 
-@pytest.mark.parametrize("M,O", [(3, 300), (100, 300), (2600, 1000)])
-def test_nan_codes_and_scales_reach_their_outputs_only(tdq, M, O):
-    xc, xs, wc, ws, b, K = _operands(M, 300, O, 6)
+@pytest.mark.parametrize("M,I,O", [(3, 300, 300), (100, 300, 300), (2600, 300, 1000)] + [w for w in WIDTHS if w[1] > 256 and w[2] > 258])
+def test_nan_codes_and_scales_reach_their_outputs_only(tdq, M, I, O):
+    xc, xs, wc, ws, b, K = _operands(M, I, O, 6)
     xc.view(torch.uint8)[1, 200] = 0x7F
     wc.view(torch.uint8)[257, 5] = 0xFF
     ws[1, 2] = float("inf")
