@@ -35,6 +35,9 @@ tdq_status launch_fp8_pair(Fp8Args a, const CUtensorMap& xmap, const CUtensorMap
 #ifdef __CUDACC__
 namespace {
 
+__device__ __forceinline__ void copy4_async(uint32_t dst, const void* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
 // K-major operand rows of 128 bytes with the 128-byte swizzle: bands of eight rows follow each other every 1024 bytes; 32 more
 // channels are 32 bytes further on (the hardware applies the swizzle to the address that results).
 constexpr uint32_t kSwDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);

@@ -91,9 +91,6 @@ __device__ __forceinline__ void scale_add64(float2* acc, const uint32_t* v, floa
         asm volatile("" ::"f"(acc[j].x), "f"(acc[j + 1].x), "f"(acc[j + 2].x), "f"(acc[j + 3].x), "f"(acc[j + 4].x), "f"(acc[j + 5].x), "f"(acc[j + 6].x),
                      "f"(acc[j + 7].x));
 }
-__device__ __forceinline__ void copy4_async(uint32_t dst, const float* src) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
-}
 // arrives on the barrier when this thread's copies so far have landed
 __device__ __forceinline__ void copies_arrive(uint32_t bar_s) {
     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar_s) : "memory");

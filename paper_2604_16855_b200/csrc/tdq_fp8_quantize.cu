@@ -9,15 +9,15 @@
 // numbers, with NaN above infinity above everything finite, so the maximum carries them along.
 //
 // Bound by HBM: 2 (4) bytes in and 1 out an element, the input read once.  A block of a token is eight threads of sixteen
-// channels each (16-byte loads, a 16-byte store, three shuffles for the maximum); rows off the 16-byte grid are read by a warp per
-// block, four channels a thread.  A weight block stays in the registers of 256 threads between its maximum and its codes.
+// channels each (16-byte loads, a 16-byte store, three shuffles for the maximum); rows off the 16-byte grid pass through
+// shared memory word by word.  A weight block stays in the registers of 512 threads between its maximum and its codes.
 #include "tdq_fp8.cuh"
 
 namespace tdq {
 namespace {
 
 constexpr int kThreadsA = 256;
-constexpr int kThreadsW = 256;
+constexpr int kThreadsW = 512;
 
 template <int DT> struct Elem { using T = uint16_t; };   // DT: tdq_dtype
 template <> struct Elem<TDQ_F32> { using T = float; };
@@ -95,6 +95,41 @@ __device__ __forceinline__ uint4 load_part(const typename Elem<DT>::T* p, int64_
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// the first n elements of a 16-byte vector, the rest zero
+template <int DT>
+__device__ __forceinline__ uint4 keep_first(const uint4& v, int n) {
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (DT == TDQ_F32) w[i] = i < n ? w[i] : 0u;
+        else w[i] = 2 * i >= n ? 0u : 2 * i + 1 >= n ? w[i] & 0xffffu : w[i];
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// Sixteen channels a thread, eight neighbouring threads a block: scale and codes.  All lanes of the warp take part, `on` or not.
+template <int DT>
+__device__ __forceinline__ void quantize16(const uint4* v, bool on, uint4* codes, float* scale, bool first) {
+    constexpr int kVecs = (int)sizeof(typename Elem<DT>::T);
+    uint32_t mx = 0;
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+        mx = max_abs<DT>(mx, v[i].x);
+        mx = max_abs<DT>(mx, v[i].y);
+        mx = max_abs<DT>(mx, v[i].z);
+        mx = max_abs<DT>(mx, v[i].w);
+    }
+#pragma unroll
+    for (int d = 1; d < 8; d <<= 1) mx = max_abs<DT>(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+    if (!on) return;
+    float s, r;
+    block_scale(max_bits<DT>(mx), s, r);
+    uint32_t out[4];
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) codes_of<DT>(v[i], r, out + i * (4 / kVecs));
+    *codes = make_uint4(out[0], out[1], out[2], out[3]);
+    if (first) *scale = s;
+}
+
 // Rows on the 16-byte grid: a thread holds sixteen consecutive channels, eight threads a block of 128.
 template <int DT>
 __global__ void __launch_bounds__(kThreadsA) act_fp8_kernel(const typename Elem<DT>::T* __restrict__ x, uint32_t n_blocks, uint32_t K,
@@ -118,68 +153,69 @@ __global__ void __launch_bounds__(kThreadsA) act_fp8_kernel(const typename Elem<
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) v[i] = load_part<DT>(src + i * kPer, on ? C - c0 - i * kPer : 0);
     }
-    uint32_t mx = 0;
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
-        mx = max_abs<DT>(mx, v[i].x);
-        mx = max_abs<DT>(mx, v[i].y);
-        mx = max_abs<DT>(mx, v[i].z);
-        mx = max_abs<DT>(mx, v[i].w);
-    }
-#pragma unroll
-    for (int d = 1; d < 8; d <<= 1) mx = max_abs<DT>(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-    if (!on) return;
-    float s, r;
-    block_scale(max_bits<DT>(mx), s, r);
-    uint32_t out[4];
-#pragma unroll
-    for (int i = 0; i < kVecs; ++i) codes_of<DT>(v[i], r, out + i * (4 / kVecs));
-    codes[t] = make_uint4(out[0], out[1], out[2], out[3]);   // rows of C_pad codes follow each other without a gap
-    if ((threadIdx.x & 7) == 0) scale[b] = s;
+    quantize16<DT>(v, on, codes + t, scale + b, (threadIdx.x & 7) == 0);   // rows of C_pad codes follow each other without a gap
 }
 
-// Rows anywhere: a warp takes kRagged blocks, their loads in flight together, a thread four consecutive channels of each.
-constexpr int kRagged = 4;
+// Rows anywhere: a warp passes the aligned words of up to four consecutive blocks of a row through shared memory, coalesced, and reads them
+// back as the kernel above holds them, sixteen channels a thread, shifted by an element where the row of 16-bit elements starts in the middle
+// of a word.  A word that holds an element of the row is read whole; what lies beside the row in it is not used.  Bound by instructions: a
+// warp per block, whose quotients every lane then computes, took 112 a block (4097 x 1000 fp16 5.0 us, 18464 x 768 bf16 14.3), four blocks of any rows 80
+// (4.7 and 11.8); this one 3.5 and 11.5.
 template <int DT>
-__global__ void __launch_bounds__(kThreadsA) act_fp8_ragged_kernel(const typename Elem<DT>::T* __restrict__ x, uint32_t n_blocks, uint32_t K,
-                                                                   int64_t C, int64_t stride, uint32_t* __restrict__ codes,
+__global__ void __launch_bounds__(kThreadsA) act_fp8_ragged_kernel(const typename Elem<DT>::T* __restrict__ x, uint32_t n_chunks, uint32_t chunks, uint32_t K,
+                                                                   int32_t C, int64_t stride, uint4* __restrict__ codes,
                                                                    float* __restrict__ scale) {
     using T = typename Elem<DT>::T;
+    constexpr int kChunk = 4 * (int)kFp8Block, kWords = kChunk * (int)sizeof(T) / 4;
+    constexpr int kEach = kWords / 32, kPitch = kEach + 4;   // words of a thread, four apart from the next one's: no bank is met twice
+    __shared__ __align__(16) uint32_t words[kThreadsA / 32][32 * kPitch + 4];   // a word more where the row is shifted
     pdl_wait();
     pdl_trigger();
-    const uint32_t b0 = (blockIdx.x * (kThreadsA / 32) + (threadIdx.x >> 5)) * kRagged;
-    const int lane = threadIdx.x & 31;
-    T v[kRagged][4];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t item = blockIdx.x * (kThreadsA / 32) + warp;
+    if (item >= n_chunks) return;
+    const uint32_t m = item / chunks, c = item - m * chunks;
+    const int n = min(kChunk, C - (int)c * kChunk);        // channels
+    const uintptr_t src = reinterpret_cast<uintptr_t>(x + (int64_t)m * stride + (int64_t)c * kChunk);
+    const int off = (int)(src >> 1) & 1;
+    const uint32_t* from = reinterpret_cast<const uint32_t*>(src & ~(uintptr_t)3) + lane;
+    uint32_t w[kEach + 1];
+    const int n_words = sizeof(T) == 4 ? n : (n + off + 1) / 2;
+    if (n_words >= kWords) {
 #pragma unroll
-    for (int i = 0; i < kRagged; ++i) {
-        const uint32_t b = b0 + i < n_blocks ? b0 + i : n_blocks - 1;
-        const uint32_t m = b / K, k = b - m * K;
-        const int64_t c0 = (int64_t)k * kFp8Block + lane * 4;
-        const T* src = x + (int64_t)m * stride + c0;
+        for (int j = 0; j < kEach; ++j) w[j] = __ldg(from + 32 * j);
+    } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[i][j] = c0 + j < C ? __ldg(src + j) : T(0);
+        for (int j = 0; j < kEach; ++j) w[j] = lane + 32 * j < n_words ? __ldg(from + 32 * j) : 0u;
     }
+    w[kEach] = n_words > kWords && lane == 0 ? __ldg(from + kWords) : 0u;
 #pragma unroll
-    for (int i = 0; i < kRagged; ++i) {
-        if (b0 + i >= n_blocks) return;
-        float f[4];
-        uint32_t mx = 0;
+    for (int j = 0; j < kEach; ++j) words[warp][lane + lane / kEach * 4 + 32 / kEach * kPitch * j] = w[j];
+    if (lane == 0) words[warp][32 * kPitch] = w[kEach];
+    __syncwarp();
+    constexpr int kVecs = (int)sizeof(T);
+    const uint4* mine = reinterpret_cast<const uint4*>(&words[warp][lane * kPitch]);
+    uint4 v[kVecs];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            f[j] = widen<DT>(v[i][j]);
-            mx = max(mx, __float_as_uint(f[j]) & 0x7fffffffu);
-        }
-        mx = __reduce_max_sync(0xffffffffu, mx);
-        float s, r;
-        block_scale(mx, s, r);
-        codes[(int64_t)(b0 + i) * 32 + lane] = cvt4(f[0], f[1], f[2], f[3], r);
-        if (lane == 0) scale[b0 + i] = s;
+    for (int i = 0; i < kVecs; ++i) v[i] = mine[i];
+    if (sizeof(T) == 2 && off) {
+        const uint32_t next = words[warp][(lane + 1) * kPitch];
+        v[0] = make_uint4(__funnelshift_r(v[0].x, v[0].y, 16), __funnelshift_r(v[0].y, v[0].z, 16), __funnelshift_r(v[0].z, v[0].w, 16), __funnelshift_r(v[0].w, v[1].x, 16));
+        v[1] = make_uint4(__funnelshift_r(v[1].x, v[1].y, 16), __funnelshift_r(v[1].y, v[1].z, 16), __funnelshift_r(v[1].z, v[1].w, 16), __funnelshift_r(v[1].w, next, 16));
     }
+    const int valid = n - lane * 16;                       // of the thread's sixteen channels
+    if (valid < 16) {
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) v[i] = keep_first<DT>(v[i], valid - i * (16 / kVecs));
+    }
+    const uint32_t b = m * K + c * 4;
+    quantize16<DT>(v, c * 4 + (lane >> 3) < K, codes + (int64_t)b * 8 + lane, scale + b + (lane >> 3), (lane & 7) == 0);
 }
 
-// One block of 128 x 128 weights in registers; VEC: rows on the 16-byte grid.
+// One block of 128 x 128 weights in registers; VEC: rows on the 16-byte grid, and three thread blocks per SM (4096 x 4096 fp32 16.0 us, bf16 10.0; 256
+// threads with twice the registers, two per SM: 17.7 and 11.0).
 template <int DT, bool VEC>
-__global__ void __launch_bounds__(kThreadsW) weight_fp8_kernel(const typename Elem<DT>::T* __restrict__ w, int64_t O, int64_t I, int64_t I_pad,
+__global__ void __launch_bounds__(kThreadsW, VEC ? 3 : 1) weight_fp8_kernel(const typename Elem<DT>::T* __restrict__ w, int64_t O, int64_t I, int64_t I_pad,
                                                                uint8_t* __restrict__ codes, float* __restrict__ scale) {
     using T = typename Elem<DT>::T;
     constexpr int kPer = 16 / (int)sizeof(T);              // elements of a vector
@@ -235,9 +271,9 @@ cudaError_t launch_act(const void* x, uint32_t n_blocks, uint32_t K, int64_t C, 
     if (reinterpret_cast<uintptr_t>(x) % 16 == 0 && (stride * (int64_t)sizeof(T)) % 16 == 0)
         return launch_pdl(act_fp8_kernel<DT>, dim3((n_blocks + kThreadsA / 8 - 1) / (kThreadsA / 8)), dim3(kThreadsA), 0, st, p, n_blocks, K, C, stride,
                           reinterpret_cast<uint4*>(codes), scale);
-    constexpr uint32_t per = kThreadsA / 32 * kRagged;
-    return launch_pdl(act_fp8_ragged_kernel<DT>, dim3((n_blocks + per - 1) / per), dim3(kThreadsA), 0, st, p, n_blocks, K, C, stride,
-                      reinterpret_cast<uint32_t*>(codes), scale);
+    const uint32_t chunks = (K + 3) / 4, n_chunks = n_blocks / K * chunks;
+    return launch_pdl(act_fp8_ragged_kernel<DT>, dim3((n_chunks + kThreadsA / 32 - 1) / (kThreadsA / 32)), dim3(kThreadsA), 0, st, p, n_chunks, chunks, K, (int32_t)C, stride,
+                      reinterpret_cast<uint4*>(codes), scale);
 }
 template <int DT>
 cudaError_t launch_weight(const void* w, int64_t O, int64_t I, uint8_t* codes, float* scale, cudaStream_t st) {
