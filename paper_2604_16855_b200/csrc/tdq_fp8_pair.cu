@@ -226,6 +226,8 @@ fp8_pair_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const
                 const int64_t col = n0 + (i >> 1) * 128 + (i & 1) * 32 + lane;
                 sts32(bias_s + (uint32_t)(i * 32 + lane) * 4u, a.bias && col < a.O ? __float_as_uint(__ldg(a.bias + col)) : 0u);
             }
+            full = mbar_test_s(tfull_s, par & 1u);               // the tensor core has run ahead during the last tile's epilogue
+            scaled = mbar_test_s(sfull_s + n % kScaleSlots * 8, (n / kScaleSlots) & 1u);
             float2 acc[64];
 #pragma unroll
             for (int j = 0; j < 64; ++j) acc[j] = make_float2(0.f, 0.f);
@@ -271,15 +273,19 @@ fp8_pair_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const
                     else if (piece > 1) bulk_wait_group_read1();
                 }
                 __syncwarp();
+                // biases first, all of them: behind a store to the strip every load of them waited out its latency
+                float4 b[kStripCols / 4];
+#pragma unroll
+                for (int j = 0; j < kStripCols / 4; ++j) b[j] = lds_f4(bias_s + (uint32_t)(c0 + 4 * j) * 4u);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {                    // 16 bytes each
                     constexpr int kPer = Y16 ? 8 : 4;
                     float o[kPer];
 #pragma unroll
                     for (int q = 0; q < kPer; q += 4) {
-                        const float4 b = lds_f4(bias_s + (uint32_t)(c0 + j * kPer + q) * 4u);
-                        const float2 r0 = __fadd2_rn(acc[(c0 + j * kPer + q) / 2], make_float2(b.x, b.y));
-                        const float2 r1 = __fadd2_rn(acc[(c0 + j * kPer + q) / 2 + 1], make_float2(b.z, b.w));
+                        const float4 t = b[(j * kPer + q) / 4];
+                        const float2 r0 = __fadd2_rn(acc[(c0 + j * kPer + q) / 2], make_float2(t.x, t.y));
+                        const float2 r1 = __fadd2_rn(acc[(c0 + j * kPer + q) / 2 + 1], make_float2(t.z, t.w));
                         o[q] = r0.x; o[q + 1] = r0.y; o[q + 2] = r1.x; o[q + 3] = r1.y;
                     }
                     const uint32_t at = strip_s + (uint32_t)lane * 128u + (((uint32_t)j ^ ((uint32_t)lane & 7u)) << 4);
