@@ -26,6 +26,7 @@ constexpr size_t kTableMax = 32 * 1024;     // bytes of cosines and sines of a b
 
 struct RopeArgs {
     tdq_rope_heads q, k;
+    const void* any;           // readable and 16-byte aligned
     const int64_t* pos;
     const double* freq;
     const int32_t* axis;
@@ -33,7 +34,7 @@ struct RopeArgs {
     int32_t Hq, H;             // query heads, all heads
     int32_t D, half, n_axes;   // half = R / 2
     int32_t norm, adjacent;
-    float eps;
+    float eps, inv_dim;        // inv_dim = 1 / D
     int32_t tokens, groups;    // of a block; of a token's heads, one for a warp at a time
     int32_t warps_across;      // warps of a block that share a token's groups
     int32_t lanes_log2;        // lanes of a head
@@ -88,6 +89,15 @@ __device__ __forceinline__ uint4 pack(const float* f) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// sixteen bytes to shared memory, asynchronously; zeros if not `there`
+__device__ __forceinline__ void copy16_async(uint32_t dst, const void* src, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ uint4 lds_u4(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
 // cosine and sine of pair i of token m; an axis outside the positions counts as their last
 __device__ __forceinline__ float2 turn_of(const RopeArgs& a, int64_t m, int i) {
     const uint32_t ax = min((uint32_t)__ldg(a.axis + i), (uint32_t)a.n_axes - 1u);
@@ -97,13 +107,17 @@ __device__ __forceinline__ float2 turn_of(const RopeArgs& a, int64_t m, int i) {
     return make_float2(c, s);
 }
 
-// Blocks of 256 threads per SM, which bounds the registers: loads in flight are what counts.  16 bits, three against none asked for:
-// 16384 x 40 x 128 65.3 -> 62.1 us, 18432 x 24 x 64 28.6 -> 24.6 (four: 62.6, 25.9); binary32, four: 8192 x 32 x 80 42.0 -> 37.2 (three: 44.7).
+// Blocks of 256 threads per SM, which bounds the registers.  16 bits, three: 18432 x 24 x 64 fp16 24.8 us, two 29.8, four 25.9; binary32, four: 8192 x 32 x
+// 80 39, three 47.
+template <int DT> constexpr int rope_ahead = 2;
+template <int DT> constexpr int rope_ring = DT == TDQ_F32 ? 0 : rope_ahead<DT> * 32;   // bytes of shared memory a thread
 template <int DT> constexpr int rope_blocks = DT == TDQ_F32 ? 4 : 3;
 template <int DT, bool ADJ>
 __global__ void __launch_bounds__(kRopeWarps * 32, rope_blocks<DT>) rope_kernel(const RopeArgs a) {
     using T = typename Bits<DT>::T;
     constexpr int V = 16 / (int)sizeof(T);                 // elements of a vector, pairs of a thread
+    constexpr bool kAsync = DT != TDQ_F32;
+    constexpr int kAhead = rope_ahead<DT>;                 // tokens whose loads are in flight
     extern __shared__ float4 shared[];
     pdl_wait();
     pdl_trigger();
@@ -111,8 +125,9 @@ __global__ void __launch_bounds__(kRopeWarps * 32, rope_blocks<DT>) rope_kernel(
     const int64_t m0 = (int64_t)blockIdx.x * a.tokens;
     const int n_tok = (int)min((int64_t)a.tokens, a.M - m0);
     const int L = 1 << a.lanes_log2, unit = lane & (L - 1), units = a.half / V, all_units = a.D / (2 * V);
-    float4* const weights = shared;                        // [queries, keys][V / 2][units of a head]: four weights
-    float4* const table = shared + (a.norm ? V * all_units : 0);   // [tokens][V / 2][turned units]: two pairs' cosine and sine
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(shared) + 16u * threadIdx.x;   // [tokens ahead][2][threads] vectors
+    float4* const weights = shared + (kAsync ? kAhead * 2 * blockDim.x : 0);   // [queries, keys][V / 2][units of a head]: four weights
+    float4* const table = weights + (a.norm ? V * all_units : 0);   // [tokens][V / 2][turned units]: two pairs' cosines, then their sines
     const int row = warp / a.warps_across, across = warp - row * a.warps_across;   // the warp's first token and head group
     const int rows = (int)(blockDim.x >> 5) / a.warps_across;
     const bool has = unit < all_units, turns = unit < units;   // a unit of the turned channels (R is a multiple of 2 V)
@@ -129,17 +144,30 @@ __global__ void __launch_bounds__(kRopeWarps * 32, rope_blocks<DT>) rope_kernel(
                             : reinterpret_cast<const T*>(a.k.x) + (head - a.Hq) * a.k.head_stride + (m0 + row) * a.k.row_stride;
         T* dst = is_q ? reinterpret_cast<T*>(a.q.out) + head * a.q.out_head_stride + (m0 + row) * a.q.out_row_stride
                       : reinterpret_cast<T*>(a.k.out) + (head - a.Hq) * a.k.out_head_stride + (m0 + row) * a.k.out_row_stride;
-        uint4 ahead[2][2];                                 // the loads of two tokens
-        const auto load = [&](uint4* v, int t) {
-            v[0] = v[1] = make_uint4(0, 0, 0, 0);
-            if (mine && t < n_tok) {
-                v[0] = *reinterpret_cast<const uint4*>(src + e0);
-                v[1] = *reinterpret_cast<const uint4*>(src + e1);
+        // The thread's two vectors of the next tokens, zeros where it has none: 16 bits on their way to its own pieces of shared memory (16384 x
+        // 40 x 128 bf16 62.1 -> 56.3 us; four tokens ahead 55.5, but 18432 x 24 x 64 fp16 24.7 instead of 22.6), binary32 in registers (8192 x 32 x 80: 39,
+        // through shared memory 45).
+        uint32_t next = 0;
+        uint4 held[kAhead][2];
+        const auto load = [&](uint4* to_regs, int t) {
+            const bool there = mine && t < n_tok;
+            if constexpr (kAsync) {
+                const uint32_t to = ring + (next % kAhead) * 32u * blockDim.x;
+                copy16_async(to, there ? src + e0 : reinterpret_cast<const T*>(a.any), there);
+                copy16_async(to + 16u * blockDim.x, there ? src + e1 : reinterpret_cast<const T*>(a.any), there);
+                asm volatile("cp.async.commit_group;" ::: "memory");
+                ++next;
+            } else {
+                to_regs[0] = to_regs[1] = make_uint4(0, 0, 0, 0);
+                if (there) {
+                    to_regs[0] = *reinterpret_cast<const uint4*>(src + e0);
+                    to_regs[1] = *reinterpret_cast<const uint4*>(src + e1);
+                }
             }
             src += in_step;
         };
-        load(ahead[0], row);
-        load(ahead[1], row + rows);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) load(held[i], row + i * rows);
         if (!have_table) {                                 // meanwhile
             if (a.norm)
                 for (int i = threadIdx.x; i < V * all_units; i += blockDim.x) {
@@ -150,65 +178,79 @@ __global__ void __launch_bounds__(kRopeWarps * 32, rope_blocks<DT>) rope_kernel(
                 }
             for (int i = threadIdx.x; i < n_tok * a.half; i += blockDim.x) {
                 const int t = i / a.half, pair = i - t * a.half, u = pair / V, j = pair - u * V;
-                reinterpret_cast<float2*>(table)[((t * (V / 2) + (j >> 1)) * units + u) * 2 + (j & 1)] = turn_of(a, m0 + t, pair);
+                const float2 cs = turn_of(a, m0 + t, pair);
+                float* const to = reinterpret_cast<float*>(table + (t * (V / 2) + (j >> 1)) * units + u) + (j & 1);
+                to[0] = cs.x;
+                to[2] = cs.y;
             }
             __syncthreads();
             have_table = true;
         }
         const float4* const wt = weights + (is_q ? 0 : V / 2 * all_units) + unit;
-        const auto head_of_token = [&](uint4* v, int t) {
-            float x[V], y[V];
-            unpack<DT>(v[0], x);
-            unpack<DT>(v[1], y);
-            load(v, t + 2 * rows);
-            if (a.norm) {
-                float ss = 0.f, st = 0.f;
+        for (int t = row; t < n_tok; t += rows) {
+            uint4 v0 = held[0][0], v1 = held[0][1];
+            if constexpr (kAsync) {
+                asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
+                const uint32_t from = ring + (next % kAhead) * 32u * blockDim.x;   // the oldest
+                v0 = lds_u4(from);
+                v1 = lds_u4(from + 16u * blockDim.x);
+            } else {
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    ss = fmaf(x[j], x[j], ss);
-                    st = fmaf(y[j], y[j], st);
+                for (int i = 0; i + 1 < kAhead; ++i) {
+                    held[i][0] = held[i + 1][0];
+                    held[i][1] = held[i + 1][1];
                 }
-                ss += st;
+            }
+            // two elements an instruction: the kernel issues close to what the schedulers take (250 of them a warp and token, 309 with single elements, 18432 x 24 x 64 fp16)
+            float2 x[V / 2], y[V / 2];
+            unpack<DT>(v0, reinterpret_cast<float*>(x));
+            unpack<DT>(v1, reinterpret_cast<float*>(y));
+            load(held[kAhead - 1], t + kAhead * rows);
+            if (a.norm) {
+                float2 sx = make_float2(0.f, 0.f), sy = sx;
+#pragma unroll
+                for (int j = 0; j < V / 2; ++j) {
+                    sx = __ffma2_rn(x[j], x[j], sx);
+                    sy = __ffma2_rn(y[j], y[j], sy);
+                }
+                float ss = (sx.x + sx.y) + (sy.x + sy.y);
                 for (int d = 1; d < L; d <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
-                const float r = rsqrtf(ss / (float)a.D + a.eps);
+                const float r = rsqrtf(fmaf(ss, a.inv_dim, a.eps));
                 if (mine) {
+                    const float2 rr = make_float2(r, r);
 #pragma unroll
                     for (int c = 0; c < V / 4; ++c) {
                         const float4 p = wt[c * all_units], q = wt[(c + V / 4) * all_units];
-                        x[4 * c] *= r * p.x; x[4 * c + 1] *= r * p.y; x[4 * c + 2] *= r * p.z; x[4 * c + 3] *= r * p.w;
-                        y[4 * c] *= r * q.x; y[4 * c + 1] *= r * q.y; y[4 * c + 2] *= r * q.z; y[4 * c + 3] *= r * q.w;
+                        x[2 * c] = __fmul2_rn(x[2 * c], __fmul2_rn(rr, make_float2(p.x, p.y)));
+                        x[2 * c + 1] = __fmul2_rn(x[2 * c + 1], __fmul2_rn(rr, make_float2(p.z, p.w)));
+                        y[2 * c] = __fmul2_rn(y[2 * c], __fmul2_rn(rr, make_float2(q.x, q.y)));
+                        y[2 * c + 1] = __fmul2_rn(y[2 * c + 1], __fmul2_rn(rr, make_float2(q.z, q.w)));
                     }
                 }
             }
             if (mine) {
                 if (turns) {
-                    // pair j: halves x[j], y[j]; adjacent the neighbours of x, then of y
                     const float4* cs = table + t * (V / 2) * units + unit;
 #pragma unroll
                     for (int i = 0; i < V / 2; ++i) {
                         const float4 two = cs[i * units];
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            const int j = 2 * i + k;
-                            const float c = k ? two.z : two.x, n = k ? two.w : two.y;
-                            float& p = ADJ ? (j < V / 2 ? x[(2 * j) % V] : y[(2 * j) % V]) : x[j];
-                            float& q = ADJ ? (j < V / 2 ? x[(2 * j + 1) % V] : y[(2 * j + 1) % V]) : y[j];
-                            const float p0 = p, q0 = q;
-                            p = p0 * c - q0 * n;
-                            q = q0 * c + p0 * n;
+                        if constexpr (ADJ) {               // pairs 2 i and 2 i + 1: neighbours in x, then in y
+                            float2 &p = i < V / 4 ? x[2 * i] : y[2 * i - V / 2], &q = i < V / 4 ? x[2 * i + 1] : y[2 * i + 1 - V / 2];
+                            p = make_float2(p.x * two.x - p.y * two.z, p.y * two.x + p.x * two.z);
+                            q = make_float2(q.x * two.y - q.y * two.w, q.y * two.y + q.x * two.w);
+                        } else {                           // x[i] and y[i]
+                            const float2 c = make_float2(two.x, two.y), n = make_float2(two.z, two.w), x0 = x[i], y0 = y[i];
+                            x[i] = __ffma2_rn(__fmul2_rn(y0, make_float2(-1.f, -1.f)), n, __fmul2_rn(x0, c));
+                            y[i] = __ffma2_rn(x0, n, __fmul2_rn(y0, c));
                         }
                     }
                 }
-                *reinterpret_cast<uint4*>(dst + e0) = pack<DT>(x);
-                *reinterpret_cast<uint4*>(dst + e1) = pack<DT>(y);
+                *reinterpret_cast<uint4*>(dst + e0) = pack<DT>(reinterpret_cast<const float*>(x));
+                *reinterpret_cast<uint4*>(dst + e1) = pack<DT>(reinterpret_cast<const float*>(y));
             }
             dst += out_step;
-        };
-        for (int t = row; t < n_tok; t += 2 * rows) {
-            head_of_token(ahead[0], t);
-            if (t + rows >= n_tok) break;
-            head_of_token(ahead[1], t + rows);
         }
+        if constexpr (kAsync) asm volatile("cp.async.wait_group 0;" ::: "memory");
     }
 }
 
@@ -236,7 +278,7 @@ __global__ void __launch_bounds__(256) rope_any_kernel(const RopeArgs a) {
             ss = fmaf(f, f, ss);
         }
         for (int d = 1; d < 32; d <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
-        r = rsqrtf(ss / (float)a.D + a.eps);
+        r = rsqrtf(fmaf(ss, a.inv_dim, a.eps));
     }
     const float* w = a.norm ? s.weight : nullptr;
     for (int i = lane; i < a.half; i += 32) {
@@ -258,7 +300,8 @@ tdq_status launch(RopeArgs a, cudaStream_t st) {
         return reinterpret_cast<uintptr_t>(s.x) % 16 == 0 && reinterpret_cast<uintptr_t>(s.out) % 16 == 0 && reinterpret_cast<uintptr_t>(s.weight) % 16 == 0 &&
                s.row_stride % V == 0 && s.head_stride % V == 0 && s.out_row_stride % V == 0 && s.out_head_stride % V == 0;
     };
-    const int n_sm = current_device_sm_count();
+    int dev = 0;
+    const int n_sm = current_device_sm_count(&dev);
     if (n_sm <= 0) return TDQ_ERR_CUDA;
     cudaError_t e;
     // a head of at most 32 lanes, whole vectors on either side of the rotated channels' middle and end
@@ -270,16 +313,20 @@ tdq_status launch(RopeArgs a, cudaStream_t st) {
         a.groups = groups;
         a.warps_across = groups < kRopeWarps ? groups : (groups + (groups + kRopeWarps - 1) / kRopeWarps - 1) / ((groups + kRopeWarps - 1) / kRopeWarps);
         const int rows = kRopeWarps / a.warps_across;
-        // Tokens a warp goes through: eight, fewer where that leaves fewer than four blocks an SM (as many as make whole rounds of the blocks
-        // that the SMs hold: 2048 tokens 11.5 -> 13.7 us, 16384 62.1 -> 64.0; twice as many: 65.1).
+        // Tokens a warp goes through: eight, fewer where that leaves fewer than four blocks an SM (sixteen: 16384 x 40 x 128 65 instead of 57 us).
         int64_t deep = a.M / ((int64_t)n_sm * 4 * rows);
         deep = deep > 8 ? 8 : deep < 1 ? 1 : deep;
         a.tokens = rows * (int)deep;
         while ((size_t)a.tokens * a.half * sizeof(float2) > kTableMax && a.tokens > rows) a.tokens -= rows;
-        const size_t smem = (size_t)a.tokens * a.half * sizeof(float2) + (a.norm ? 2 * a.D * sizeof(float) : 0);
+        const size_t smem = (size_t)a.tokens * a.half * sizeof(float2) + (a.norm ? 2 * a.D * sizeof(float) : 0) + (size_t)rope_ring<DT> * rows * a.warps_across * 32;
+        a.any = a.q.heads ? a.q.x : a.k.x;
         const int64_t blocks = (a.M + a.tokens - 1) / a.tokens;
         if (blocks > INT32_MAX) return TDQ_ERR_UNSUPPORTED;
-        e = launch_pdl(a.adjacent ? rope_kernel<DT, true> : rope_kernel<DT, false>, dim3((unsigned)blocks), dim3(rows * a.warps_across * 32), smem, st, a);
+        void (*const kernel)(RopeArgs) = a.adjacent ? rope_kernel<DT, true> : rope_kernel<DT, false>;
+        static std::atomic<uint64_t> smem_done[2];
+        if (allow_smem(kernel, (int)(kTableMax + rope_ring<DT> * 32 * kRopeWarps + 2 * 64 * V * sizeof(float)), smem_done[a.adjacent], dev) != cudaSuccess)
+            return TDQ_ERR_CUDA;
+        e = launch_pdl(kernel, dim3((unsigned)blocks), dim3(rows * a.warps_across * 32), smem, st, a);
     } else {
         const int64_t blocks = (a.M * a.H + 7) / 8;
         if (blocks > INT32_MAX) return TDQ_ERR_UNSUPPORTED;
@@ -348,6 +395,7 @@ extern "C" tdq_status tdq_qk_norm_rope(const tdq_rope_heads* q, const tdq_rope_h
     a.norm = (p->flags & TDQ_ROPE_NORM) != 0;
     a.adjacent = (p->flags & TDQ_ROPE_ADJACENT) != 0;
     a.eps = p->eps;
+    a.inv_dim = 1.f / (float)p->head_dim;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
     return dtype == TDQ_F32 ? launch<TDQ_F32>(a, st) : dtype == TDQ_BF16 ? launch<TDQ_BF16>(a, st) : launch<TDQ_F16>(a, st);
 }
