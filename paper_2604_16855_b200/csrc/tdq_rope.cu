@@ -135,8 +135,9 @@ __global__ void __launch_bounds__(kRopeWarps * 32, rope_blocks<DT>) rope_kernel(
     const auto first_of = [&](int u) { return ADJ || u >= units ? 2 * u * V : u * V; };
     const auto second_of = [&](int u) { return ADJ || u >= units ? (2 * u + 1) * V : a.half + u * V; };
     const int e0 = first_of(unit), e1 = second_of(unit);
-    bool have_table = false;                               // every warp goes through the loop at least once
-    for (int group = across; group < a.groups; group += a.warps_across) {
+    bool have_table = false;                               // all warps make the same passes
+    for (int first = blockIdx.y * a.warps_across; first < a.groups; first += gridDim.y * a.warps_across) {
+        const int group = first + across;                  // behind the last one: no heads
         const int head = (group << (5 - a.lanes_log2)) + (lane >> a.lanes_log2);
         const bool mine = has && head < a.H, is_q = head < a.Hq;
         const int64_t in_step = rows * (is_q ? a.q.row_stride : a.k.row_stride), out_step = rows * (is_q ? a.q.out_row_stride : a.k.out_row_stride);
@@ -322,11 +323,13 @@ tdq_status launch(RopeArgs a, cudaStream_t st) {
         a.any = a.q.heads ? a.q.x : a.k.x;
         const int64_t blocks = (a.M + a.tokens - 1) / a.tokens;
         if (blocks > INT32_MAX) return TDQ_ERR_UNSUPPORTED;
+        // few tokens: a token's groups on several thread blocks
+        const int passes = (groups + a.warps_across - 1) / a.warps_across, across = blocks * passes <= n_sm ? passes : 1;
         void (*const kernel)(RopeArgs) = a.adjacent ? rope_kernel<DT, true> : rope_kernel<DT, false>;
         static std::atomic<uint64_t> smem_done[2];
         if (allow_smem(kernel, (int)(kTableMax + rope_ring<DT> * 32 * kRopeWarps + 2 * 64 * V * sizeof(float)), smem_done[a.adjacent], dev) != cudaSuccess)
             return TDQ_ERR_CUDA;
-        e = launch_pdl(kernel, dim3((unsigned)blocks), dim3(rows * a.warps_across * 32), smem, st, a);
+        e = launch_pdl(kernel, dim3((unsigned)blocks, (unsigned)across), dim3(rows * a.warps_across * 32), smem, st, a);
     } else {
         const int64_t blocks = (a.M * a.H + 7) / 8;
         if (blocks > INT32_MAX) return TDQ_ERR_UNSUPPORTED;
