@@ -298,7 +298,8 @@ tdq_status tdq_quantize_weight_fp8(const void* w, tdq_dtype w_dtype, int64_t O, 
  * The linear layer on E4M3 codes, on the tensor cores' 8-bit floating point instructions:
  *   y[m,o] = bias[o] + sum_k xscale[m,k] wscale[o/128,k] sum_{i in block k} x[m,i] w[o,i]
  *   The sum over a block is the tensor core's, in binary32; across blocks acc = fma(sum, fl(xscale wscale), acc) in binary32, in
- *   order of k, or in up to eight parts of consecutive blocks that are added in order (few tokens).  The same call gives the same bits.
+ *   order of k, or in up to eight parts of consecutive blocks that are added in order (few tokens).  The same call gives the same bits; with
+ *   another M or O the parts may be others.
  *   xcodes [M, I_pad], xscale [M, I_pad/128], wcodes [O, I_pad], wscale [ceil(O/128), I_pad/128], bias NULL or [O] float32.
  *   I_pad a multiple of 128.  Codes are any E4M3 bytes; a NaN code or scale makes the outputs it reaches NaN.
  *   y      [M, O], y_dtype (float32, bf16 or fp16, rounded to nearest even from the float32 result), rows y_row_stride elements
@@ -318,7 +319,8 @@ size_t tdq_fp8_linear_workspace_bytes(int64_t M, int64_t I_pad, int64_t O);
  *   with TDQ_ROPE_NORM   n_i = x_i w_i / sqrt(mean_j x_j^2 + eps)   (w == 1 where weight is NULL), else n = x;
  *   pair i < R/2 is channels (i, i + R/2), with TDQ_ROPE_ADJACENT (2i, 2i+1):   t = positions[m, axis[i]] freq[i],
  *   (n_a, n_b) -> (n_a cos t - n_b sin t, n_b cos t + n_a sin t);   channels from R on are n.
- *   Angles are binary64 up to the fraction of a turn; everything else is binary32, rounded once when stored.
+ *   Angles are binary64 up to the fraction of a turn; everything else is binary32, rounded once when stored (squares whose sum passes
+ *   binary32's range make a head zero).
  *   q, k       either may be NULL or have no heads.  Element (m, h, i) of x is x[m row_stride + h head_stride + i], of out
  *              likewise; heads and rows of out must not overlap each other.  out == x (with the same strides) works in place;
  *              otherwise out overlaps neither x, and the two outs do not overlap.  weight NULL or [D] float32.  A qkv matrix of the
@@ -327,7 +329,8 @@ size_t tdq_fp8_linear_workspace_bytes(int64_t M, int64_t I_pad, int64_t O);
  *   positions  [M, n_axes] int64;  freq [R/2] float64, radians per position;  axis [R/2] int32, the column of positions that
  *              turns the pair (a number outside 0 .. n_axes-1 counts as the last column).  Unused when R == 0.
  *   Pointers and strides on the 16-byte grid with D a multiple of 16 (float32: 8), R/2 of 8 (4) and D <= 512 (256) take the
- *   vector kernel, anything else a slower general one.  M == 0 is a no-op.
+ *   vector kernel, anything else a slower general one.  M == 0 is a no-op.  TDQ_ERR_UNSUPPORTED for head_dim or heads above 65536
+ *   and M above 2^31 - 1.
  */
 #define TDQ_ROPE_NORM 1u
 #define TDQ_ROPE_ADJACENT 2u

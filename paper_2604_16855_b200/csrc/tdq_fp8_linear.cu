@@ -10,9 +10,13 @@
 // workspace, the same bits every time.  Up to 32 tokens the parts send their sums (st.async, counted by a barrier of the channel's owner): read between
 // two cluster barriers that order memory they took 3100 of 9500 clocks on 1 x 4096 -> 4096, as much as the loads (6.2 -> 5.4 us).
 // More sums than that are read by their owners all the same (128 tokens: 10.1 us, sent 11.3), since the room that they need where they are sent
-// is two ring stages, and an owner of channels stores narrower pieces than an owner of tokens.  Warps 0 and 2 load (tensor maps, 16 KB of weights and the tokens' 128 bytes a stage), warp 1
-// issues, warp 3 lays out the tokens' factors xs * ws of a block in shared memory, the others scale and add: a thread has one output channel and up
-// to 32 tokens.
+// is two ring stages, and an owner of channels stores narrower pieces than an owner of tokens.
+// Warps 0 and 2 load (tensor maps, 16 KB of weights and the tokens' 128 bytes a stage), warp 1 issues, warp 3 lays out the tokens' factors
+// xs * ws of a block in shared memory, the others scale and add: a thread has one output channel and up to 32 tokens.
+// Measured, from a graph: 1 x 4096 -> 4096 bf16 5.1 us with the weights in L2, 6.9 from memory (floor 2.6), 1 x 8192 -> 8192 14.7 (10.3), 576 x 384 -> 960 4.7.
+// The tensor copies bring 38 bytes a clock to an SM, whatever their size (stages of two blocks: no gain); the rest is the chain from launch to
+// first tile (1500 clocks), through the last tile, and the meeting.  Not kept: the weights prefetched to L2 ahead of the wait for the kernel
+// before (a layer behind its quantizer 6.5 -> 7.0 us, 1 x 8192 -> 8192 14.7 -> 19.9).
 #include "tdq_tc.cuh"
 #include "tdq_fp8.cuh"
 
@@ -354,7 +358,7 @@ fp8_split_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, cons
 struct Way { int nt, split; };                             // nt == 256: pairs
 Way choose_way(int64_t M, int64_t O, int K, int n_sm) {
     const int64_t tiles_n = fp8_blocks(O), pair_tiles = ((M + 255) / 256) * ((O + 255) / 256);
-    if (pair_tiles >= n_sm) return {256, 1};
+    if (M > 64 && pair_tiles >= n_sm) return {256, 1};
     Way best = {256, 1};
     const int64_t pairs = n_sm / 2 > 0 ? n_sm / 2 : 1, pair_rounds = (pair_tiles + pairs - 1) / pairs;
     int64_t least = M > 64 ? 385 + 37 * K * pair_rounds + 160 * (pair_rounds - 1) : INT64_MAX;

@@ -373,7 +373,7 @@ extern "C" tdq_status tdq_qk_norm_rope(const tdq_rope_heads* q, const tdq_rope_h
     if (p->flags & ~(uint32_t)(TDQ_ROPE_NORM | TDQ_ROPE_ADJACENT)) return TDQ_ERR_INVALID_ARG;
     if ((p->flags & TDQ_ROPE_NORM) && !(p->eps >= 0.f)) return TDQ_ERR_INVALID_ARG;
     if (p->rotary_dim > 0 && p->n_axes <= 0) return TDQ_ERR_INVALID_ARG;
-    if (M > INT32_MAX) return TDQ_ERR_UNSUPPORTED;
+    if (M > INT32_MAX || p->head_dim > 65536) return TDQ_ERR_UNSUPPORTED;
     const uintptr_t esz = dtype == TDQ_F32 ? 4 : 2;
     RopeArgs a = {};
     for (int i = 0; i < 2; ++i) {

@@ -86,7 +86,7 @@ def test_rope(tdq):
         return f(ctypes.byref(q) if q else None, ctypes.byref(k) if k else None, dt, M, ctypes.byref(rp) if rp else None, pos, freq, axis, None)
     inv, ali, uns = tdq.ERR_INVALID_ARG, tdq.ERR_ALIGNMENT, tdq.ERR_UNSUPPORTED
     assert call() == inv and call(q=h(), p=None) == inv and call(q=h(), M=-1) == inv and call(q=h(), dt=3) == inv
-    assert call(q=h(), M=1 << 31) == uns
+    assert call(q=h(), M=1 << 31) == uns and call(q=h(heads=1, row_stride=1 << 17, out_row_stride=1 << 17), p=(1 << 17, 64, 1, 1, 1e-6)) == uns
     for p in [(0, 0, 1, 1, 1e-6), (64, 66, 1, 1, 1e-6), (64, -2, 1, 1, 1e-6), (64, 31, 1, 1, 1e-6), (64, 64, 0, 1, 1e-6), (64, 64, 1, 4, 1e-6),
               (64, 64, 1, 1, -1.0), (64, 64, 1, 1, float("nan"))]:
         assert call(q=h(), p=p) == inv, p

@@ -214,6 +214,11 @@ def test_ragged_large_tiles(tdq, M, O):
     _run(tdq, M, 256, O, "fp32", True)
 
 
+@pytest.mark.parametrize("M,I,O", [(1, 256, 40000), (33, 130, 37889), (64, 256, 65537), (65, 256, 37890)])
+def test_few_tokens_and_very_many_outputs(tdq, M, I, O):
+    _run(tdq, M, I, O, "bf16", True)
+
+
 @pytest.mark.parametrize("M,I,O", [(3, 300, 300), (100, 300, 300), (2600, 300, 1000)] + [w for w in WIDTHS if w[1] > 256 and w[2] > 258])
 def test_nan_codes_and_scales_reach_their_outputs_only(tdq, M, I, O):
     xc, xs, wc, ws, b, K = _operands(M, I, O, 6)
@@ -343,3 +348,33 @@ def test_qkv_layer_then_rotation_in_place(tdq, M, hq, hk, D):
     for now, was, w in ((q, before[:, :hq * D].view(M, hq, D), qw), (k, before[:, hq * D:(hq + hk) * D].view(M, hk, D), kw)):
         fu.check_rope(now, *fu.rope(was, w, pos, freq, axis.long(), 1e-6, False))
     assert torch.equal(qkv[:, (hq + hk) * D:], before[:, (hq + hk) * D:])       # the values are left as they were
+
+
+FIRST_IN_A_CAPTURE = """
+import torch
+from paper_2604_16855_b200 import tdq
+x = torch.randn((%(M)d, 300), device="cuda").bfloat16()
+w = torch.randn((%(O)d, 300), device="cuda")
+pos, table = torch.arange(%(M)d, device="cuda"), tdq.rope_table(64)
+torch.cuda.synchronize()
+side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+    wc, ws = tdq.quantize_weight_fp8(w)
+    y = tdq.fp8_linear(*tdq.quantize_act_fp8(x), wc, ws, out_dtype=torch.bfloat16)
+    q, _ = tdq.qk_norm_rope(y[:, :128].view(-1, 2, 64), None, pos, table)
+graph.replay()
+torch.cuda.synchronize()
+wc, ws = tdq.quantize_weight_fp8(w)
+z = tdq.fp8_linear(*tdq.quantize_act_fp8(x), wc, ws, out_dtype=torch.bfloat16)
+assert torch.equal(y, z) and torch.equal(q, tdq.qk_norm_rope(z[:, :128].view(-1, 2, 64), None, pos, table)[0])
+"""
+
+
+@pytest.mark.parametrize("M,O", [(3, 200), (2600, 1000)])
+def test_first_use_inside_a_capture(M, O):
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_IN_A_CAPTURE % dict(M=M, O=O)], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
