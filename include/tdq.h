@@ -277,7 +277,7 @@ tdq_status tdq_w4a4_linear_static(const uint8_t* xcodes, const float* xscale, co
  *   a = max(max |x|, 2^-64);  scale = a / 448;  r = 448 / a;  code = E4M3(x r)   (each operation in binary32, the codes
  *   nearest even, at most 448 in magnitude).  A block with a NaN or an infinity gets scale NaN and codes NaN.
  *   x       [B*N rows, C], float32, bf16 or fp16, rows row_stride_elems apart (>= C).  x and row pitch on the 16-byte grid
- *           are read with vector loads, anything else element by element; the results are the same.
+ *           are read with vector loads, anything else in words that hold an element of the row; the results are the same.
  *   codes   [B*N, C_pad] bytes, C_pad = 128 ceil(C/128), 16-byte aligned; the codes behind C are 0 (NaN in a NaN block).
  *   scale   [B*N, C_pad/128] float32.
  * B*N == 0 is a no-op.  TDQ_ERR_UNSUPPORTED for 2^36 elements or more.
@@ -319,11 +319,11 @@ size_t tdq_fp8_linear_workspace_bytes(int64_t M, int64_t I_pad, int64_t O);
  *   with TDQ_ROPE_NORM   n_i = x_i w_i / sqrt(mean_j x_j^2 + eps)   (w == 1 where weight is NULL), else n = x;
  *   pair i < R/2 is channels (i, i + R/2), with TDQ_ROPE_ADJACENT (2i, 2i+1):   t = positions[m, axis[i]] freq[i],
  *   (n_a, n_b) -> (n_a cos t - n_b sin t, n_b cos t + n_a sin t);   channels from R on are n.
- *   Angles are binary64 up to the fraction of a turn; everything else is binary32, rounded once when stored (squares whose sum passes
- *   binary32's range make a head zero).
+ *   Angles are binary64 up to the fraction of a turn; everything else is binary32, rounded once when stored.  The squares are not
+ *   scaled before they are added: a head whose sum passes binary32's range becomes zero.
  *   q, k       either may be NULL or have no heads.  Element (m, h, i) of x is x[m row_stride + h head_stride + i], of out
  *              likewise; heads and rows of out must not overlap each other.  out == x (with the same strides) works in place;
- *              otherwise out overlaps neither x, and the two outs do not overlap.  weight NULL or [D] float32.  A qkv matrix of the
+ *              otherwise out overlaps neither x, and the two outs do not overlap (one pointer for both is refused).  weight NULL or [D] float32.  A qkv matrix of the
  *              linear layer is x = its first query or key channel, row_stride its pitch, head_stride D.
  *   dtype      of x and out: float32, bf16 or fp16.
  *   positions  [M, n_axes] int64;  freq [R/2] float64, radians per position;  axis [R/2] int32, the column of positions that

@@ -384,6 +384,8 @@ extern "C" tdq_status tdq_qk_norm_rope(const tdq_rope_heads* q, const tdq_rope_h
         (i ? a.k : a.q) = *s;
     }
     if (M == 0 || a.q.heads + a.k.heads == 0) return TDQ_OK;
+    // one tensor passed for both sides and written: a head would be read after it was turned
+    if (a.q.heads && a.k.heads && (a.q.out == a.k.out || a.q.out == a.k.x || a.k.out == a.q.x)) return TDQ_ERR_INVALID_ARG;
     if (p->rotary_dim > 0 && (!positions || !freq || !axis)) return TDQ_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(positions) % 8 || reinterpret_cast<uintptr_t>(freq) % 8 || reinterpret_cast<uintptr_t>(axis) % 4) return TDQ_ERR_ALIGNMENT;
     a.pos = positions;

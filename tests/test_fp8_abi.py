@@ -98,6 +98,10 @@ def test_rope(tdq):
         assert call(q=h(**kw)) == inv and call(q=h(), k=h(**kw)) == inv, kw
     assert call(q=h(x=0x1001)) == ali and call(q=h(out=0x2001)) == ali and call(k=h(weight=0x3002)) == ali
     assert call(q=h(heads=70000, out_row_stride=70000 * 64)) == uns
+    # one tensor for both sides, written: refused unless one side has no heads
+    for q, k in [(h(), h()), (h(), h(x=0x5000)), (h(), h(x=0x2000, out=0x6000)), (h(x=0x6000), h(x=0x5000, out=0x6000)),
+                 (h(x=0x2000, out_row_stride=512), h(x=0x2000, out=0x6000))]:
+        assert call(q=q, k=k) == inv
     assert call(q=h(), M=0) == tdq.OK and call(q=h(heads=0), k=h(heads=0)) == tdq.OK
 
 

@@ -132,6 +132,23 @@ def test_refusals_of_the_binding(tdq):
     assert tdq.kernel_launch_count() == n0
 
 
+@pytest.mark.parametrize("D", [64, 72])
+def test_the_same_tensor_for_both_sides(tdq, D):
+    x, pos, table = _heads(9, 3, D, 4, torch.bfloat16), torch.arange(9, device="cuda"), tdq.rope_table(D)
+    w = torch.linspace(0.5, 1.5, D, device="cuda")
+    before = x.clone()
+    q, k = tdq.qk_norm_rope(x, x, pos, table, None, w)    # read twice, written to two new tensors
+    assert torch.equal(x, before)
+    assert torch.equal(q, tdq.qk_norm_rope(x, None, pos, table)[0]) and torch.equal(k, tdq.qk_norm_rope(x, None, pos, table, w)[0])
+    e, k = tdq.qk_norm_rope(x[:, :0], x, pos, table, None, w)   # queries without heads
+    assert e.shape == (9, 0, D) and torch.equal(k, tdq.qk_norm_rope(x, None, pos, table, w)[0])
+    for kw in [dict(q_out=x), dict(k_out=x), dict(q_out=x, k_out=x), dict(q_out=q, k_out=q)]:
+        with pytest.raises(tdq.TdqError) as error:
+            tdq.qk_norm_rope(x, x, pos, table, **kw)
+        assert error.value.code == tdq.ERR_INVALID_ARG
+    assert torch.equal(x, before)
+
+
 @pytest.mark.parametrize("D", [128, 72])
 def test_graph_replay_in_place(tdq, D):
     q, k = _heads(40, 4, D, 1, torch.bfloat16), _heads(40, 2, D, 2, torch.bfloat16)
