@@ -17,6 +17,8 @@
 // The tensor copies bring 38 bytes a clock to an SM, whatever their size (stages of two blocks: no gain); the rest is the chain from launch to
 // first tile (1500 clocks), through the last tile, and the meeting.  Not kept: the weights prefetched to L2 ahead of the wait for the kernel
 // before (a layer behind its quantizer 6.5 -> 7.0 us, 1 x 8192 -> 8192 14.7 -> 19.9).
+#include <algorithm>
+
 #include "tdq_tc.cuh"
 #include "tdq_fp8.cuh"
 
@@ -349,26 +351,32 @@ fp8_split_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, cons
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "n"(kSplitSlots * NT) : "memory");
 }
 
-// Which kernel, and in how many parts: the least of these estimates in units of 10 ns, fitted to 75 layers (1 to 2304 tokens, 384 to 4096 ->
-// 960 to 8192 channels, from a graph; the choice is within 1 % of the best one measured in the mean, 15 % at worst).
-//   NT tokens, s parts:  start x rounds + block x (blocks of a part) x (CTAs per SM) + 45 for meeting where sums are read (s > 1, NT >= 64);
-//                        a round is two CTAs per SM, one of NT = 128
+// Which kernel, and in how many parts: the least of these estimates in units of 10 ns, fitted to 156 layers (1 to 9000 tokens, 384 to 7040 ->
+// 48 to 8192 channels, every kernel and number of parts, from a graph; the choice costs 1.5 % more than the best one in the mean, 25 % at worst).
+//   NT tokens, s parts:  start x rounds + block x (blocks of a part) x (CTAs an SM runs) + meet x s (s > 1);  a round is as many clusters of s
+//                        CTAs as the GPU holds, two CTAs per SM, one of NT = 128
 //   pairs of CTAs:       385 + 37 K rounds + 160 (rounds - 1);  a round is a tile of 256 x 256 for every pair of SMs
-// Against 128 tokens a tile throughout: 576 x 384 -> 960 6.9 -> 4.7 us, 64 x 768 -> 2304 5.2 -> 4.3, 256 x 1024 -> 1024 6.9 -> 5.4.
+// A cluster lies in one group of SMs, so fewer of them fit than SMs / s: with rounds counted in CTAs 2259 x 5113 -> 45 waited for two of
+// eighteen clusters of eight (14.2 us; now 8.9).  Against 128 tokens a tile throughout: 576 x 384 -> 960 6.9 -> 4.7 us, 256 x 1024 -> 1024 6.9 -> 5.4.
 struct Way { int nt, split; };                             // nt == 256: pairs
 Way choose_way(int64_t M, int64_t O, int K, int n_sm) {
+    // Clusters of 1 .. 8 CTAs that a B200 of 148 SMs holds, one CTA and two per SM, as the runtime reports them.  Constants, not a question to the GPU
+    // at hand: which SMs form a group differs from one to the next, and the bits of a sum would with it.
+    static const int holds[2][kSplitMax] = {{148, 74, 45, 33, 26, 22, 15, 15}, {296, 148, 93, 71, 56, 45, 37, 33}};
+    static const struct { int nt, start, block, meet; } kinds[4] = {{16, 305, 22, 3}, {32, 350, 32, 2}, {64, 354, 35, 10}, {128, 480, 36, 0}};
     const int64_t tiles_n = fp8_blocks(O), pair_tiles = ((M + 255) / 256) * ((O + 255) / 256);
     if (M > 64 && pair_tiles >= n_sm) return {256, 1};
     Way best = {256, 1};
     const int64_t pairs = n_sm / 2 > 0 ? n_sm / 2 : 1, pair_rounds = (pair_tiles + pairs - 1) / pairs;
     int64_t least = M > 64 ? 385 + 37 * K * pair_rounds + 160 * (pair_rounds - 1) : INT64_MAX;
-    static const struct { int nt, start, block; } kinds[4] = {{16, 320, 21}, {32, 360, 32}, {64, 350, 37}, {128, 470, 44}};
     for (const auto& k : kinds) {
         if (k.nt > 16 && k.nt / 2 >= M) break;             // more than half of the tile would be empty
         const int64_t tiles = tiles_n * ((M + k.nt - 1) / k.nt);
         for (int s = 1; s <= kSplitMax && s <= K; ++s) {
-            const int64_t ctas = tiles * s, per_sm = (ctas + n_sm - 1) / n_sm, rounds = k.nt == 128 ? per_sm : (per_sm + 1) / 2;
-            const int64_t cost = k.start * rounds + (int64_t)k.block * ((K + s - 1) / s) * per_sm + (s > 1 && k.nt >= 64 ? 45 : 0);
+            const int two = k.nt != 128;
+            const int64_t at_once = std::max<int64_t>(1, (int64_t)holds[two][s - 1] * n_sm / 148), rounds = (tiles + at_once - 1) / at_once;
+            const int64_t per_sm = std::max<int64_t>((tiles * s + n_sm - 1) / n_sm, two ? 2 * rounds - 1 : rounds);
+            const int64_t cost = k.start * rounds + (int64_t)k.block * ((K + s - 1) / s) * per_sm + (s > 1 ? k.meet * s : 0);
             if (cost < least) { least = cost; best = {k.nt, s}; }
         }
     }

@@ -209,6 +209,18 @@ def test_every_width_of_tile(tdq, M, I, O, dtype, pitch):
     _run(tdq, M, I, O, dtype, pitch != 1, pitch)
 
 
+# for every width of tile, one to eight parts
+SPLITS = [(145, 64, 6359), (18, 1425, 6807), (1502, 690, 42), (853, 1989, 34), (924, 1747, 41), (723, 3711, 32), (622, 3208, 37),
+          (540, 4951, 41), (4838, 66, 37), (2596, 390, 37), (2437, 262, 36), (1926, 970, 36), (1242, 1236, 35), (1276, 2016, 34),
+          (1266, 1768, 44), (929, 2797, 32), (2959, 922, 160), (4970, 771, 40), (3335, 2330, 33), (3251, 1578, 39), (2427, 1995, 45),
+          (1897, 2622, 36), (1559, 4031, 43), (5664, 65, 137), (1, 67, 34), (1, 907, 33)]
+
+
+@pytest.mark.parametrize("n", range(len(SPLITS)))
+def test_every_number_of_parts(tdq, n):
+    _run(tdq, *SPLITS[n], ("fp32", "bf16", "fp16")[n % 3], n % 2 == 0, n % 4)
+
+
 @pytest.mark.parametrize("M,O", [(257, 256 * 37 + 1), (256 * 5 + 1, 256 * 9 - 1), (256 * 38 - 127, 100), (20000, 257)])
 def test_ragged_large_tiles(tdq, M, O):
     _run(tdq, M, 256, O, "fp32", True)
