@@ -3,9 +3,10 @@
 //   r = 1 / sqrt(mean_i x_i^2 + eps);  n_i = x_i (r w_i);   for pair i < R/2:  t = pos[m, axis_i] freq_i,
 //   (n_a, n_b) -> (n_a cos t - n_b sin t,  n_b cos t + n_a sin t);   channels from R on: n_i
 //
-// Angles.  t reaches 10^6 and more, where binary32 has lost the fraction of a turn: the product, the turns and their
-// fraction are binary64 (three operations per pair and token, shared by all heads), and only the fraction of a turn is rounded to
-// binary32 for sincospif.  Sum of squares, norm and rotation are binary32; one rounding at the store.
+// Angles.  t reaches 10^6 and more, where binary32 has lost the fraction of a turn.  A pair's turns per position are a fraction in units of 2^-64 (from
+// binary64, once a thread); its product with the position, modulo 2^64, is the fraction of a turn to position x 2^-65, exact for what matters
+// up to positions of 2^40, and is rounded to binary32 for sincospif.  In binary64 (product, turns, fraction for every token) 29386 x 2 x 256 bf16
+// took 32.6 us for 28.2.  Sum of squares, norm and rotation are binary32; one rounding at the store.
 //
 // Bound by HBM: every head is read and written once.  A thread owns the two 16-byte vectors of a head whose elements form pairs (halves:
 // one from either half; adjacent: neighbours), so that a head is a power of two of lanes, its sum of squares a few shuffles, and
@@ -16,12 +17,15 @@
 // bf16).  A warp per token with cosines times weights in 32 registers had too few loads in flight (95 us).
 #include <cuda_fp16.h>
 
+#include <algorithm>
+
 #include "tdq_common.cuh"
 
 namespace tdq {
 namespace {
 
 constexpr int kRopeWarps = 8;
+constexpr int kSmSharedBytes = 227 * 1024;
 constexpr size_t kTableMax = 32 * 1024;     // bytes of cosines and sines of a block (16 KB for eight tokens of 256 pairs)
 
 struct RopeArgs {
@@ -98,22 +102,32 @@ __device__ __forceinline__ uint4 lds_u4(uint32_t addr) {
     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
     return v;
 }
-// cosine and sine of pair i of token m; an axis outside the positions counts as their last
-__device__ __forceinline__ float2 turn_of(const RopeArgs& a, int64_t m, int i) {
-    const uint32_t ax = min((uint32_t)__ldg(a.axis + i), (uint32_t)a.n_axes - 1u);
-    const double turns = (double)__ldg(reinterpret_cast<const long long*>(a.pos) + m * a.n_axes + ax) * __ldg(a.freq + i) * 0.15915494309189533577;
+// The turns a pair makes per position: the fraction of freq / 2 pi in units of 2^-64 (whole turns of it stay whole turns at every position).
+struct Speed { int64_t step; float bad; };                 // bad: NaN where freq is not finite, else 0
+__device__ __forceinline__ Speed speed_of(double freq) {
+    const double turns = freq * 0.15915494309189533577;
+    const double f = turns - rint(turns);                  // [-1/2, 1/2]; +1/2 saturates below 2^63
+    return {__double2ll_rn(f * 18446744073709551616.0), (float)(f - f)};
+}
+// cosine and sine at a position; the product's 64 low bits are its fraction of a turn, of which 32 are rounded to binary32
+__device__ __forceinline__ float2 turn_at(const Speed& v, int64_t pos) {
+    const int32_t frac = (int32_t)(((uint64_t)pos * (uint64_t)v.step) >> 32);
     float s, c;
-    sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
+    sincospif(fmaf((float)frac, 4.6566128730773926e-10f, v.bad), &s, &c);   // 2^-31: half turns
     return make_float2(c, s);
 }
+__device__ __forceinline__ uint32_t axis_of(const RopeArgs& a, int i) {   // an axis outside the positions counts as their last
+    return min((uint32_t)__ldg(a.axis + i), (uint32_t)a.n_axes - 1u);
+}
 
-// Blocks of 256 threads per SM, which bounds the registers.  16 bits, three: 18432 x 24 x 64 fp16 24.8 us, two 29.8, four 25.9; binary32, four: 8192 x 32 x
-// 80 39, three 47.
+// Registers a thread, and with them warps an SM.  16 bits, 28 warps of 72: with 78 registers only 24 fit, and 2949 x 20 x 96 bf16 takes 10.6 us
+// for 7.8; 20 warps 18432 x 24 x 64 fp16 29.8 us for 24.8, 32 warps of 64 25.9.  binary32, 32 warps of 64: 8192 x 32 x 80 39, 24 warps 47.
 template <int DT> constexpr int rope_ahead = 2;
 template <int DT> constexpr int rope_ring = DT == TDQ_F32 ? 0 : rope_ahead<DT> * 32;   // bytes of shared memory a thread
-template <int DT> constexpr int rope_blocks = DT == TDQ_F32 ? 4 : 3;
+template <int DT> constexpr int rope_regs = DT == TDQ_F32 ? 64 : 72;
+template <int DT> constexpr int rope_warps_per_sm = DT == TDQ_F32 ? 32 : 28;
 template <int DT, bool ADJ>
-__global__ void __launch_bounds__(kRopeWarps * 32, rope_blocks<DT>) rope_kernel(const RopeArgs a) {
+__global__ void __maxnreg__(rope_regs<DT>) rope_kernel(const RopeArgs a) {
     using T = typename Bits<DT>::T;
     constexpr int V = 16 / (int)sizeof(T);                 // elements of a vector, pairs of a thread
     constexpr bool kAsync = DT != TDQ_F32;
@@ -177,12 +191,18 @@ __global__ void __launch_bounds__(kRopeWarps * 32, rope_blocks<DT>) rope_kernel(
                     const int e = c < V / 4 ? first_of(u) + 4 * c : second_of(u) + 4 * (c - V / 4);
                     weights[i] = w ? __ldg(reinterpret_cast<const float4*>(w + e)) : make_float4(1.f, 1.f, 1.f, 1.f);
                 }
-            for (int i = threadIdx.x; i < n_tok * a.half; i += blockDim.x) {
-                const int t = i / a.half, pair = i - t * a.half, u = pair / V, j = pair - u * V;
-                const float2 cs = turn_of(a, m0 + t, pair);
-                float* const to = reinterpret_cast<float*>(table + (t * (V / 2) + (j >> 1)) * units + u) + (j & 1);
-                to[0] = cs.x;
-                to[2] = cs.y;
+            // a pair of every so many tokens for a thread
+            const int wide = min(a.half, (int)blockDim.x), skip = wide ? (int)blockDim.x / wide : 1;
+            for (int pair = wide ? (int)threadIdx.x % wide : a.half, t0 = wide ? (int)threadIdx.x / wide : 0; pair < a.half && t0 < skip; pair += wide) {
+                const Speed v = speed_of(__ldg(a.freq + pair));
+                const long long* pos = reinterpret_cast<const long long*>(a.pos) + (m0 + t0) * a.n_axes + axis_of(a, pair);
+                const int u = pair / V, j = pair - u * V;
+                float* to = reinterpret_cast<float*>(table + (t0 * (V / 2) + (j >> 1)) * units + u) + (j & 1);
+                for (int t = t0; t < n_tok; t += skip, pos += skip * a.n_axes, to += skip * (V / 2) * units * 4) {
+                    const float2 cs = turn_at(v, __ldg(pos));
+                    to[0] = cs.x;
+                    to[2] = cs.y;
+                }
             }
             __syncthreads();
             have_table = true;
@@ -285,7 +305,7 @@ __global__ void __launch_bounds__(256) rope_any_kernel(const RopeArgs a) {
     for (int i = lane; i < a.half; i += 32) {
         const int ia = a.adjacent ? 2 * i : i, ib = a.adjacent ? 2 * i + 1 : a.half + i;
         const float na = to_f<DT>(x[ia]) * (w ? r * __ldg(w + ia) : r), nb = to_f<DT>(x[ib]) * (w ? r * __ldg(w + ib) : r);
-        const float2 t = turn_of(a, m, i);
+        const float2 t = turn_at(speed_of(__ldg(a.freq + i)), __ldg(reinterpret_cast<const long long*>(a.pos) + m * a.n_axes + axis_of(a, i)));
         out[ia] = from_f<DT>(na * t.x - nb * t.y);
         out[ib] = from_f<DT>(nb * t.x + na * t.y);
     }
@@ -314,17 +334,29 @@ tdq_status launch(RopeArgs a, cudaStream_t st) {
         a.groups = groups;
         a.warps_across = groups < kRopeWarps ? groups : (groups + (groups + kRopeWarps - 1) / kRopeWarps - 1) / ((groups + kRopeWarps - 1) / kRopeWarps);
         const int rows = kRopeWarps / a.warps_across;
-        // Tokens a warp goes through: eight, fewer where that leaves fewer than four blocks an SM (sixteen: 16384 x 40 x 128 65 instead of 57 us).
-        int64_t deep = a.M / ((int64_t)n_sm * 4 * rows);
-        deep = deep > 8 ? 8 : deep < 1 ? 1 : deep;
-        a.tokens = rows * (int)deep;
-        while ((size_t)a.tokens * a.half * sizeof(float2) > kTableMax && a.tokens > rows) a.tokens -= rows;
-        const size_t smem = (size_t)a.tokens * a.half * sizeof(float2) + (a.norm ? 2 * a.D * sizeof(float) : 0) + (size_t)rope_ring<DT> * rows * a.warps_across * 32;
+        const int warps = rows * a.warps_across, passes = (groups + a.warps_across - 1) / a.warps_across;
+        const size_t per_block = (a.norm ? 2 * a.D * sizeof(float) : 0) + (size_t)rope_ring<DT> * warps * 32, per_token = (size_t)a.half * sizeof(float2);
+        const int table_deep = per_token ? (int)(kTableMax / (per_token * rows)) : 8;
+        // Tokens a warp goes through (`deep`, eight at most: sixteen 16384 x 40 x 128 65 us for 57), and a token's groups of heads in one thread block after
+        // another or in as many blocks: the least of rounds of resident blocks x (tokens x groups of a warp + 1), and blocks of an SM x warps / 16.
+        // Against as many tokens as leave four blocks an SM, whatever fits at once: 2619 x 72 x 128 bf16 23.7 -> 18.8 us, 3272 x 6 x 128 6.0 -> 4.6, 314 x
+        // 20 x 256 fp32 6.5 -> 4.7; 227 x 60 x 128, the worst of 23 sizes, 4.7 -> 4.9.
+        uint64_t least = UINT64_MAX;
+        int across = 1;
+        for (int deep = 1; deep <= 8 && (deep == 1 || (deep <= table_deep && rows * (deep - 1) < a.M)); ++deep) {
+            const uint32_t blocks = ((uint32_t)a.M + rows * deep - 1) / (rows * deep);
+            const uint32_t fit = std::min<uint32_t>(rope_warps_per_sm<DT> / warps, (uint32_t)((size_t)kSmSharedBytes / (per_block + per_token * rows * deep + 1024)));
+            for (int y = 1; y <= passes; y += passes > 1 ? passes - 1 : 1) {
+                const uint64_t n = (uint64_t)blocks * y;
+                if (n > INT32_MAX) break;
+                const uint32_t held = fit * n_sm, rounds = ((uint32_t)n + held - 1) / held, an_sm = ((uint32_t)n + n_sm - 1) / n_sm;
+                const uint64_t cost = 16ull * rounds * (1 + deep * (passes / y)) + (uint64_t)an_sm * warps;
+                if (cost < least) { least = cost; a.tokens = rows * deep; across = y; }
+            }
+        }
+        const size_t smem = per_block + per_token * a.tokens;
         a.any = a.q.heads ? a.q.x : a.k.x;
         const int64_t blocks = (a.M + a.tokens - 1) / a.tokens;
-        if (blocks > INT32_MAX) return TDQ_ERR_UNSUPPORTED;
-        // few tokens: a token's groups on several thread blocks
-        const int passes = (groups + a.warps_across - 1) / a.warps_across, across = blocks * passes <= n_sm ? passes : 1;
         void (*const kernel)(RopeArgs) = a.adjacent ? rope_kernel<DT, true> : rope_kernel<DT, false>;
         static std::atomic<uint64_t> smem_done[2];
         if (allow_smem(kernel, (int)(kTableMax + rope_ring<DT> * 32 * kRopeWarps + 2 * 64 * V * sizeof(float)), smem_done[a.adjacent], dev) != cudaSuccess)

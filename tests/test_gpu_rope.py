@@ -64,6 +64,26 @@ def test_far_positions(tdq, far, D):
 
 
 @pytest.mark.parametrize("D", [64, 72])
+def test_whole_turns_and_frequencies_that_are_no_numbers(tdq, D):
+    x = _heads(6, 3, D, 8, torch.float32)
+    pos = torch.tensor([0, 1, -1, 1 << 31, (1 << 52) + 3, -(1 << 62)], device="cuda")
+    freq, axis = tdq.rope_table(D)
+    out, _ = tdq.qk_norm_rope(x, None, pos, (torch.zeros_like(freq), axis), eps=None)
+    assert torch.equal(out, x)                            # no turn at any position
+    freq[3], freq[5], freq[7] = float("nan"), float("inf"), -float("inf")
+    out, _ = tdq.qk_norm_rope(x, None, pos, (freq, axis), eps=None)
+    bad = torch.zeros(D, dtype=torch.bool, device="cuda")
+    bad[[3, 5, 7]] = bad[[D // 2 + 3, D // 2 + 5, D // 2 + 7]] = True
+    assert out[:, :, bad].isnan().all() and torch.isfinite(out[:, :, ~bad]).all()
+
+
+@pytest.mark.parametrize("M,hq,hk,D,dtype", [(6000, 32, 8, 128, "bf16"), (702, 60, 12, 64, "bf16"), (314, 16, 4, 256, "fp32"), (2219, 48, 12, 96, "fp32"),
+                                             (29386, 1, 1, 256, "bf16"), (300, 300, 1, 128, "fp16"), (40000, 1, 0, 16, "fp32"), (149, 9, 9, 512, "bf16")])
+def test_blocks_of_tokens_and_groups(tdq, M, hq, hk, D, dtype):
+    _case(tdq, M, hq, hk, D, D // 2, 2, dtype, far=1 << 20)
+
+
+@pytest.mark.parametrize("D", [64, 72])
 def test_without_norm_and_without_weights(tdq, D):
     _case(tdq, 20, 4, 2, D, D, 1, "fp16", eps=None)
     _case(tdq, 20, 4, 2, D, D, 1, "fp16", weights=False)
