@@ -156,50 +156,54 @@ __global__ void __launch_bounds__(kThreadsA) act_fp8_kernel(const typename Elem<
     quantize16<DT>(v, on, codes + t, scale + b, (threadIdx.x & 7) == 0);   // rows of C_pad codes follow each other without a gap
 }
 
-// Rows anywhere: a warp passes the aligned words of up to four consecutive blocks of a row through shared memory, coalesced, and reads them
-// back as the kernel above holds them, sixteen channels a thread, shifted by an element where the row of 16-bit elements starts in the middle
-// of a word.  A word that holds an element of the row is read whole; what lies beside the row in it is not used.  Bound by instructions: a
+// Rows anywhere: eight lanes per block of a row, KB consecutive blocks of it at a time, pass their aligned words through shared memory, coalesced, and read
+// them back as the kernel above holds them, sixteen channels a thread, shifted by an element where the row of 16-bit elements starts in the
+// middle of a word.  A word that holds an element of the row is read whole; what lies beside the row in it is not used.  Bound by instructions: a
 // warp per block, whose quotients every lane then computes, took 112 a block (4097 x 1000 fp16 5.0 us, 18464 x 768 bf16 14.3), four blocks of any rows 80
 // (4.7 and 11.8); this one 3.5 and 11.5.
-template <int DT>
+template <int DT, int KB>
 __global__ void __launch_bounds__(kThreadsA) act_fp8_ragged_kernel(const typename Elem<DT>::T* __restrict__ x, uint32_t n_chunks, uint32_t chunks, uint32_t K,
                                                                    int32_t C, int64_t stride, uint4* __restrict__ codes,
                                                                    float* __restrict__ scale) {
     using T = typename Elem<DT>::T;
-    constexpr int kChunk = 4 * (int)kFp8Block, kWords = kChunk * (int)sizeof(T) / 4;
-    constexpr int kEach = kWords / 32, kPitch = kEach + 4;   // words of a thread, four apart from the next one's: no bank is met twice
-    __shared__ __align__(16) uint32_t words[kThreadsA / 32][32 * kPitch + 4];   // a word more where the row is shifted
+    constexpr int kChunk = KB * (int)kFp8Block, kWords = kChunk * (int)sizeof(T) / 4, kLanes = 8 * KB;
+    constexpr int kEach = kWords / kLanes, kPitch = kEach + 4;   // words of a thread, four apart from the next one's: no bank is met twice
+    constexpr int kRoom = kLanes * kPitch + 4;             // a word more where the row is shifted
+    __shared__ __align__(16) uint32_t words[kThreadsA / kLanes][kRoom];
     pdl_wait();
     pdl_trigger();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const uint32_t item = blockIdx.x * (kThreadsA / 32) + warp;
-    if (item >= n_chunks) return;
-    const uint32_t m = item / chunks, c = item - m * chunks;
-    const int n = min(kChunk, C - (int)c * kChunk);        // channels
+    const int lane = (int)threadIdx.x % kLanes, group = (int)threadIdx.x / kLanes;
+    const uint32_t item = blockIdx.x * (kThreadsA / kLanes) + group;
+    const bool on = item < n_chunks;
+    const uint32_t m = on ? item / chunks : 0u, c = on ? item - m * chunks : 0u;
+    const int n = on ? min(kChunk, C - (int)c * kChunk) : 0;   // channels
     const uintptr_t src = reinterpret_cast<uintptr_t>(x + (int64_t)m * stride + (int64_t)c * kChunk);
     const int off = (int)(src >> 1) & 1;
     const uint32_t* from = reinterpret_cast<const uint32_t*>(src & ~(uintptr_t)3) + lane;
     uint32_t w[kEach + 1];
-    const int n_words = sizeof(T) == 4 ? n : (n + off + 1) / 2;
+    const int n_words = sizeof(T) == 4 ? n : n ? (n + off + 1) / 2 : 0;
     if (n_words >= kWords) {
 #pragma unroll
-        for (int j = 0; j < kEach; ++j) w[j] = __ldg(from + 32 * j);
+        for (int j = 0; j < kEach; ++j) w[j] = __ldg(from + kLanes * j);
     } else {
 #pragma unroll
-        for (int j = 0; j < kEach; ++j) w[j] = lane + 32 * j < n_words ? __ldg(from + 32 * j) : 0u;
+        for (int j = 0; j < kEach; ++j) w[j] = lane + kLanes * j < n_words ? __ldg(from + kLanes * j) : 0u;
     }
     w[kEach] = n_words > kWords && lane == 0 ? __ldg(from + kWords) : 0u;
 #pragma unroll
-    for (int j = 0; j < kEach; ++j) words[warp][lane + lane / kEach * 4 + 32 / kEach * kPitch * j] = w[j];
-    if (lane == 0) words[warp][32 * kPitch] = w[kEach];
+    for (int j = 0; j < kEach; ++j) {
+        const int i = lane + kLanes * j, owner = kEach <= kLanes ? lane / kEach + kLanes / kEach * j : i / kEach;
+        words[group][i + 4 * owner] = w[j];
+    }
+    if (lane == 0) words[group][kLanes * kPitch] = w[kEach];
     __syncwarp();
     constexpr int kVecs = (int)sizeof(T);
-    const uint4* mine = reinterpret_cast<const uint4*>(&words[warp][lane * kPitch]);
+    const uint4* mine = reinterpret_cast<const uint4*>(&words[group][lane * kPitch]);
     uint4 v[kVecs];
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) v[i] = mine[i];
     if (sizeof(T) == 2 && off) {
-        const uint32_t next = words[warp][(lane + 1) * kPitch];
+        const uint32_t next = words[group][(lane + 1) * kPitch];
         v[0] = make_uint4(__funnelshift_r(v[0].x, v[0].y, 16), __funnelshift_r(v[0].y, v[0].z, 16), __funnelshift_r(v[0].z, v[0].w, 16), __funnelshift_r(v[0].w, v[1].x, 16));
         v[1] = make_uint4(__funnelshift_r(v[1].x, v[1].y, 16), __funnelshift_r(v[1].y, v[1].z, 16), __funnelshift_r(v[1].z, v[1].w, 16), __funnelshift_r(v[1].w, next, 16));
     }
@@ -208,8 +212,8 @@ __global__ void __launch_bounds__(kThreadsA) act_fp8_ragged_kernel(const typenam
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) v[i] = keep_first<DT>(v[i], valid - i * (16 / kVecs));
     }
-    const uint32_t b = m * K + c * 4;
-    quantize16<DT>(v, c * 4 + (lane >> 3) < K, codes + (int64_t)b * 8 + lane, scale + b + (lane >> 3), (lane & 7) == 0);
+    const uint32_t b = m * K + c * KB;
+    quantize16<DT>(v, on && c * KB + (lane >> 3) < K, codes + (int64_t)b * 8 + lane, scale + b + (lane >> 3), (lane & 7) == 0);
 }
 
 // One block of 128 x 128 weights in registers; VEC: rows on the 16-byte grid, and three thread blocks per SM (4096 x 4096 fp32 16.0 us, bf16 10.0; 256
@@ -271,9 +275,15 @@ cudaError_t launch_act(const void* x, uint32_t n_blocks, uint32_t K, int64_t C, 
     if (reinterpret_cast<uintptr_t>(x) % 16 == 0 && (stride * (int64_t)sizeof(T)) % 16 == 0)
         return launch_pdl(act_fp8_kernel<DT>, dim3((n_blocks + kThreadsA / 8 - 1) / (kThreadsA / 8)), dim3(kThreadsA), 0, st, p, n_blocks, K, C, stride,
                           reinterpret_cast<uint4*>(codes), scale);
-    const uint32_t chunks = (K + 3) / 4, n_chunks = n_blocks / K * chunks;
-    return launch_pdl(act_fp8_ragged_kernel<DT>, dim3((n_chunks + kThreadsA / 32 - 1) / (kThreadsA / 32)), dim3(kThreadsA), 0, st, p, n_chunks, chunks, K, (int32_t)C, stride,
-                      reinterpret_cast<uint4*>(codes), scale);
+    // One block of a row at a time for rows of one block, two where four would leave half a warp idle at a row's end, else four (us on 25037 rows of bf16
+    // with one, two and four: 70 channels 3.8, 4.9, 8.7; 147 5.2, 5.1, 8.8; 767 14.7, 13.9, 15.6; 1023 17.9, 17.6, 16.5).
+    const auto ragged = [&](auto kernel, uint32_t kb) {
+        const uint32_t chunks = (K + kb - 1) / kb, n_chunks = n_blocks / K * chunks, per = kThreadsA / (8 * kb);
+        return launch_pdl(kernel, dim3((n_chunks + per - 1) / per), dim3(kThreadsA), 0, st, p, n_chunks, chunks, K, (int32_t)C, stride, reinterpret_cast<uint4*>(codes), scale);
+    };
+    if (K == 1) return ragged(act_fp8_ragged_kernel<DT, 1>, 1);
+    if ((K & 3) == 1 || (K & 3) == 2) return ragged(act_fp8_ragged_kernel<DT, 2>, 2);
+    return ragged(act_fp8_ragged_kernel<DT, 4>, 4);
 }
 template <int DT>
 cudaError_t launch_weight(const void* w, int64_t O, int64_t I, uint8_t* codes, float* scale, cudaStream_t st) {

@@ -43,6 +43,22 @@ def test_activations(tdq, dtype, M, C, pitch, offset):
     _same(codes, scale, x, 1)
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("C", [1, 70, 127, 128, 129, 147, 255, 257, 300, 383, 511, 513, 639, 767, 895, 1023, 1025, 1151, 1279, 2175])
+@pytest.mark.parametrize("M", [1, 5, 130])
+def test_rows_off_the_grid(tdq, dtype, C, M):
+    x = _tokens(M, C, M + C, fu.DT[dtype])
+    pitch = 1 + C % 2                                     # odd rows, in turn on either half of a word
+    buf = torch.full((1 + M * (C + pitch),), float("nan"), dtype=x.dtype, device="cuda")
+    v = buf[1:].view(M, C + pitch)[:, :C]
+    v.copy_(x)
+    K = fu.blocks(C)
+    codes, scale = torch.full((M + 2, K * 128), 77, dtype=torch.uint8, device="cuda"), torch.full((M + 2, K), 77.0, device="cuda")
+    c, s = tdq.quantize_act_fp8(v, codes=codes[:M], scale=scale[:M])
+    _same(c.view(torch.float8_e4m3fn), s, x, 1)
+    assert (codes[M:] == 77).all() and (scale[M:] == 77).all()
+
+
 def _edge_rows(C=256):
     """Rows at the edges of the formula: zeros, below the floor, denormals, the largest numbers, ties, one spike, signed zeros."""
     g = torch.Generator().manual_seed(5)
