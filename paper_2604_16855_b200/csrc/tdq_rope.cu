@@ -198,7 +198,7 @@ __global__ void __maxnreg__(rope_regs<DT>) rope_kernel(const RopeArgs a) {
                 const long long* pos = reinterpret_cast<const long long*>(a.pos) + (m0 + t0) * a.n_axes + axis_of(a, pair);
                 const int u = pair / V, j = pair - u * V;
                 float* to = reinterpret_cast<float*>(table + (t0 * (V / 2) + (j >> 1)) * units + u) + (j & 1);
-                for (int t = t0; t < n_tok; t += skip, pos += skip * a.n_axes, to += skip * (V / 2) * units * 4) {
+                for (int t = t0; t < n_tok; t += skip, pos += (int64_t)skip * a.n_axes, to += skip * (V / 2) * units * 4) {
                     const float2 cs = turn_at(v, __ldg(pos));
                     to[0] = cs.x;
                     to[2] = cs.y;
