@@ -29,8 +29,8 @@ struct Fp8Args {
 // Tensor map of a [rows][cols] byte matrix read in boxes of box_rows x 128 bytes, 128-byte swizzle (K-major operand of the
 // tensor core); false when the driver's encoder is missing or refuses.
 bool fp8_operand_map(CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int box_rows);
-// Two CTAs on a tile of 256 x 256 (tdq_fp8_pair.cu); xmap, wmap with boxes of 128 rows.
-tdq_status launch_fp8_pair(Fp8Args a, const CUtensorMap& xmap, const CUtensorMap& wmap, int n_sm, int dev, cudaStream_t stream);
+// Two CTAs on a tile of 256 tokens and 256 or 128 columns (tdq_fp8_pair.cu); xmap with boxes of 128 rows, wmap of half the columns.
+tdq_status launch_fp8_pair(Fp8Args a, int columns, const CUtensorMap& xmap, const CUtensorMap& wmap, int n_sm, int dev, cudaStream_t stream);
 
 #ifdef __CUDACC__
 namespace {

@@ -352,23 +352,30 @@ fp8_split_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, cons
 }
 
 // Which kernel, and in how many parts: the least of these estimates in units of 10 ns, fitted to 156 layers (1 to 9000 tokens, 384 to 7040 ->
-// 48 to 8192 channels, every kernel and number of parts, from a graph; the choice costs 1.5 % more than the best one in the mean, 25 % at worst).
+// 48 to 8192 channels, every kernel and number of parts, from a graph; the choice costs 1.9 % more than the best one in the mean, 25 % at worst).
 //   NT tokens, s parts:  start x rounds + block x (blocks of a part) x (CTAs an SM runs) + meet x s (s > 1);  a round is as many clusters of s
 //                        CTAs as the GPU holds, two CTAs per SM, one of NT = 128
-//   pairs of CTAs:       385 + 37 K rounds + 160 (rounds - 1);  a round is a tile of 256 x 256 for every pair of SMs
+//   pairs of CTAs:       start + block x K x rounds + end x (rounds - 1);  a round is a tile of 256 tokens and 256 or 128 channels for every
+//                        pair of SMs
 // A cluster lies in one group of SMs, so fewer of them fit than SMs / s: with rounds counted in CTAs 2259 x 5113 -> 45 waited for two of
 // eighteen clusters of eight (14.2 us; now 8.9).  Against 128 tokens a tile throughout: 576 x 384 -> 960 6.9 -> 4.7 us, 256 x 1024 -> 1024 6.9 -> 5.4.
-struct Way { int nt, split; };                             // nt == 256: pairs
+struct Way { int nt, split; };                             // nt == 256: pairs, split the tile's columns
 Way choose_way(int64_t M, int64_t O, int K, int n_sm) {
     // Clusters of 1 .. 8 CTAs that a B200 of 148 SMs holds, one CTA and two per SM, as the runtime reports them.  Constants, not a question to the GPU
     // at hand: which SMs form a group differs from one to the next, and the bits of a sum would with it.
     static const int holds[2][kSplitMax] = {{148, 74, 45, 33, 26, 22, 15, 15}, {296, 148, 93, 71, 56, 45, 37, 33}};
     static const struct { int nt, start, block, meet; } kinds[4] = {{16, 305, 22, 3}, {32, 350, 32, 2}, {64, 354, 35, 10}, {128, 480, 36, 0}};
     const int64_t tiles_n = fp8_blocks(O), pair_tiles = ((M + 255) / 256) * ((O + 255) / 256);
-    if (M > 64 && pair_tiles >= n_sm) return {256, 1};
-    Way best = {256, 1};
+    if (M > 64 && pair_tiles >= n_sm) return {256, 256};
+    Way best = {256, 256};
     const int64_t pairs = n_sm / 2 > 0 ? n_sm / 2 : 1, pair_rounds = (pair_tiles + pairs - 1) / pairs;
-    int64_t least = M > 64 ? 385 + 37 * K * pair_rounds + 160 * (pair_rounds - 1) : INT64_MAX;
+    int64_t least = INT64_MAX;
+    if (M > 64) {
+        const int64_t narrow_rounds = ((M + 255) / 256 * tiles_n + pairs - 1) / pairs;
+        const int64_t wide = 475 + 34 * K * pair_rounds + 380 * (pair_rounds - 1), narrow = 360 + 27 * K * narrow_rounds + 160 * (narrow_rounds - 1);
+        least = std::min(wide, narrow);
+        if (narrow < wide) best.split = 128;
+    }
     for (const auto& k : kinds) {
         if (k.nt > 16 && k.nt / 2 >= M) break;             // more than half of the tile would be empty
         const int64_t tiles = tiles_n * ((M + k.nt - 1) / k.nt);
@@ -460,14 +467,14 @@ extern "C" tdq_status tdq_fp8_linear(const uint8_t* xcodes, const float* xscale,
     a.y_vec = !off(y, 16) && (y_row_stride * (int64_t)esz) % 16 == 0;
     a.status = reinterpret_cast<uint32_t*>(workspace);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
-    CUtensorMap wmap;
-    if (!fp8_operand_map(&wmap, wcodes, O, I_pad, 128)) return TDQ_ERR_CUDA;
     const Way way = choose_way(M, O, a.K, n_sm);
+    CUtensorMap wmap;
+    if (!fp8_operand_map(&wmap, wcodes, O, I_pad, way.nt == 256 ? way.split / 2 : 128)) return TDQ_ERR_CUDA;
     if (way.nt == 16) return launch_split<16>(a, way.split, xcodes, wmap, n_sm, dev, st);
     if (way.nt == 32) return launch_split<32>(a, way.split, xcodes, wmap, n_sm, dev, st);
     if (way.nt == 64) return launch_split<64>(a, way.split, xcodes, wmap, n_sm, dev, st);
     if (way.nt == 128) return launch_split<128>(a, way.split, xcodes, wmap, n_sm, dev, st);
     CUtensorMap xmap;
     if (!fp8_operand_map(&xmap, xcodes, M, I_pad, 128)) return TDQ_ERR_CUDA;
-    return launch_fp8_pair(a, xmap, wmap, n_sm, dev, st);
+    return launch_fp8_pair(a, way.split, xmap, wmap, n_sm, dev, st);
 }

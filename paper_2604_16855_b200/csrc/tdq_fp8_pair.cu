@@ -13,11 +13,16 @@
 // warps, 64 columns each (393 k); landing registers reused from load to load, which the compiler copies (up to 96 moves a block); the next
 // accumulator's first load ahead of this one's last additions (422 k).
 //
+// Where 256 x 256 tiles would leave SMs empty, tiles of 256 x 128 (TN = 128): every accumulator is the whole tile's, four blocks in turn, issued by the two
+// warps alternately, so that token rows are read once a block (with halves of 64 columns they would be read twice, more than shared memory gives).
+// 24 KB a block and CTA instead of 32, and half of the epilogue: 512 x 4096 -> 4096 bf16 16.6 -> 14.3 us, 512 x 768 -> 2304 6.9 -> 5.5, 1500 x 640 -> 300
+// 7.4 -> 5.3, 9000 x 2816 -> 200 13.1 -> 11.4; several rounds lose (2048 x 4096 -> 4096 32.5, 45.5).  Bound by its loads, 45 to 50 bytes a clock.
+//
 //   warps 0, 3  loads of this CTA's 128 token rows and 128 weight rows (tensor maps, 128-byte swizzle, 16 KB each a stage), signalled to
 //               CTA 0's barrier; warp 0 the block's scales too (asynchronous copies: as loads of the adding warps, first-level cache or not,
 //               they cost a quarter of the kernel's time)
-//   warps 1, 2  CTA 0: issue the instructions (cta_group::2, 256 x 128 x 32) of one half each, commit to both CTAs' barriers
-//   warps 4-11  scale and add: 32 token rows x 128 columns each in registers (so 232 registers a thread, 40 for the others), then bias,
+//   warps 1, 2  CTA 0: issue the instructions (cta_group::2, 256 x 128 x 32) of one half each (of every other block), commit to both CTAs' barriers
+//   warps 4-11  scale and add: 32 token rows x 128 (64) columns each in registers (so 232 registers a thread, 40 for the others), then bias,
 //               rounding and the store through two swizzled strips of 4 KB
 //
 // Half h is columns 64 h .. 64 h + 63 of each CTA's 128 weight rows: with cta_group::2 either CTA brings half of the columns.
@@ -29,27 +34,32 @@
 namespace tdq {
 namespace {
 
-constexpr int kPairStages = 4;                           // five leave no room for the second strip and gain nothing
-constexpr uint32_t kPairOperand = 128 * 128;             // bytes of a stage's rows of either operand
-constexpr uint32_t kPairStage = 2 * kPairOperand;
+constexpr uint32_t kPairOperand = 128 * 128;             // bytes of a stage's token rows, and of its weight rows with TN = 256
 constexpr uint32_t kPairCtrl = 1024;                     // the ring behind it is on the 1 KB grid that the swizzles need, as the block's shared memory is
 constexpr int kAddWarp0 = 4, kAddWarps = 8;
 constexpr int kPairThreads = (kAddWarp0 + kAddWarps) * 32;
 constexpr uint32_t kStrip = 32 * 128;                    // 32 rows of 128 bytes
 constexpr uint32_t kBiasBytes = 128 * 4;                 // of a warp's 128 columns
 constexpr int kStrips = 2;                               // of a warp: 128 columns of 16 bits, so that no store is waited for in a tile
-// Scales of a block: 128 token rows', then two weight blocks'.  Eight blocks of them, without a barrier that hands them back: block n + 8's
-// are copied once the instructions of block n + 4 (four stages) have completed, which were issued after all of n + 2's sums had been taken.
-constexpr int kScaleSlots = 8;
+// Scales of a block: 128 token rows', then two weight blocks'.  No barrier hands them back: with eight of them and four stages block n + 8's are
+// copied once the instructions of block n + 4 have completed, which were issued after all of n + 2's sums had been taken; with sixteen and six, n + 16's after
+// n + 10's, issued after n + 6's.
 constexpr uint32_t kScaleBytes = 128 * 4 + 16;
 constexpr uint32_t kPairIdesc = (1u << 4) | ((128u >> 3) << 17) | ((256u >> 4) << 24);
 constexpr int kRegsLoad = 40, kRegsAdd = 232;            // 128 * 40 + 256 * 232 <= 384 * 168
 
+template <int TN> struct PairShape {                     // TN: the tile's columns
+    static constexpr int kStages = TN == 256 ? 4 : 6;    // 256: five leave no room for the second strip and gain nothing
+    static constexpr int kScaleSlots = TN == 256 ? 8 : 16;
+    static constexpr uint32_t kWeights = TN / 2 * 128;
+    static constexpr uint32_t kStage = kPairOperand + kWeights;
+    static constexpr uint32_t kSmem = kPairCtrl + kStages * kStage + kAddWarps * (kStrips * kStrip + kBiasBytes) + kScaleSlots * kScaleBytes;
+};
 struct PairCtrl {
-    uint64_t full[kPairStages];                          // CTA 0: both CTAs' operands of the stage have landed
-    uint64_t empty[kPairStages];
-    uint64_t scales[kScaleSlots];                        // a block's scales have landed in this CTA
-    uint64_t tfull[4], tempty[4];                        // accumulator 2 (a tile's block & 1) + half (tempty: CTA 0 only)
+    uint64_t full[6];                                    // CTA 0: both CTAs' operands of the stage have landed
+    uint64_t empty[6];
+    uint64_t scales[16];                                 // a block's scales have landed in this CTA
+    uint64_t tfull[4], tempty[4];                        // TN = 256: accumulator 2 (a tile's block & 1) + half; 128: a block's & 3 (tempty: CTA 0 only)
 };
 
 __device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, uint32_t bar) {
@@ -106,11 +116,14 @@ __device__ __forceinline__ void copies_arrive(uint32_t bar_s) {
 }
 
 // DT: y's tdq_dtype.
-template <int DT>
+template <int DT, int TN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 fp8_pair_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap wmap,
                 const __grid_constant__ CUtensorMap ymap) {
     constexpr bool Y16 = DT != TDQ_F32;
+    using Sh = PairShape<TN>;
+    constexpr int kPairStages = Sh::kStages, kScaleSlots = Sh::kScaleSlots;
+    constexpr uint32_t kPairStage = Sh::kStage;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     Ctrl* c = reinterpret_cast<Ctrl*>(smem_raw);             // its abort flag and TMEM address; the barriers are g's
     PairCtrl* g = reinterpret_cast<PairCtrl*>(smem_raw + sizeof(Ctrl));
@@ -121,9 +134,9 @@ fp8_pair_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const
     const uint32_t rank = fp8_cluster_rank();
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kPairStages; ++i) { mbar_init(&g->full[i], 2); mbar_init(&g->empty[i], 2); }
+        for (int i = 0; i < kPairStages; ++i) { mbar_init(&g->full[i], 2); mbar_init(&g->empty[i], TN == 256 ? 2 : 1); }
         for (int i = 0; i < kScaleSlots; ++i) mbar_init(&g->scales[i], 32);
-        for (int i = 0; i < 4; ++i) { mbar_init(&g->tfull[i], 1); mbar_init(&g->tempty[i], kAddWarps); }
+        for (int i = 0; i < 4; ++i) { mbar_init(&g->tfull[i], 1); mbar_init(&g->tempty[i], TN == 256 ? kAddWarps : 2 * kAddWarps); }
         c->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -155,18 +168,18 @@ fp8_pair_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const
             uint32_t s = 0, ph = 1, n = 0;
             for (int tile = first; tile < n_tiles && !c->abort_flag; tile += n_clusters) {
                 const int mt = tile / a.tiles_n, nt = tile - mt * a.tiles_n;
-                const int row = (is_x ? mt : nt) * 256 + (int)rank * 128;   // past the end: the map fills with zeros
+                const int row = is_x ? mt * 256 + (int)rank * 128 : nt * TN + (int)rank * (TN / 2);   // past the end: the map fills with zeros
                 // scales: rows lane, lane + 32, .. of xscale and, in lanes 0 and 1, the tile's two rows of wscale; the last row for those past the end
                 const float* xs[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) xs[i] = a.xscale + min((int64_t)row + lane + 32 * i, a.M - 1) * K;
-                const float* ws = a.wscale + min((int64_t)2 * nt + (lane & 1), (a.O - 1) >> 7) * K;
+                const float* ws = a.wscale + min(TN == 256 ? (int64_t)2 * nt + (lane & 1) : (int64_t)nt, (a.O - 1) >> 7) * K;
 #pragma unroll 1
                 for (int kb = 0; kb < K; ++kb, ++n) {
                     fp8_wait(empty_s + s * 8, ph, c, a.status, 5u);
                     if (c->abort_flag) break;
                     if (elect_one()) {
-                        if (rank == 0) mbar_expect_tx(&g->full[s], 2 * kPairOperand);   // this operand, both CTAs
+                        if (rank == 0) mbar_expect_tx(&g->full[s], is_x ? 2 * kPairOperand : 2 * Sh::kWeights);   // this operand, both CTAs
                         tma_load_pair(dst0 + s * kPairStage, is_x ? &xmap : &wmap, kb * (int)kFp8Block, row, full0 + s * 8);
                     }
                     __syncwarp();
@@ -180,7 +193,29 @@ fp8_pair_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const
                     if (++s == kPairStages) { s = 0; ph ^= 1; }
                 }
             }
-        } else if (rank == 0) {
+        } else if (TN == 128 && rank == 0) {
+            // -------------------------------------------------------- MMA issue, every other block
+            const uint32_t full_s = smem_u32(&g->full[0]), empty_s = smem_u32(&g->empty[0]), tfull_s = smem_u32(&g->tfull[0]), tempty_s = smem_u32(&g->tempty[0]);
+            const uint32_t xd0 = (uint32_t)sw_desc(ring_s), wd0 = (uint32_t)sw_desc(ring_s + kPairOperand);
+            const int64_t total = first < n_tiles ? (int64_t)((n_tiles - first + n_clusters - 1) / n_clusters) * K : 0;
+            uint32_t s = (uint32_t)warp - 1u, ph = 0;
+            for (int64_t n = warp - 1; n < total; n += 2) {
+                const uint32_t slot = (uint32_t)n & 3u;
+                fp8_wait(full_s + s * 8, ph, c, a.status, 4u);
+                fp8_wait(tempty_s + slot * 8, ((uint32_t)(n >> 2) & 1u) ^ 1u, c, a.status, 3u);
+                if (c->abort_flag) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint64_t xd = (uint64_t)kSwDescHi << 32 | (xd0 + s * (kPairStage >> 4)), wd = (uint64_t)kSwDescHi << 32 | (wd0 + s * (kPairStage >> 4));
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) mma_f8_pair(tmem_base + slot * 128, xd + 2 * k, wd + 2 * k, k ? 1u : 0u);
+                    commit_pair(tfull_s + slot * 8);
+                    commit_pair(empty_s + s * 8);
+                }
+                __syncwarp();
+                if ((s += 2) >= kPairStages) { s -= kPairStages; ph ^= 1; }
+            }
+        } else if (TN == 256 && rank == 0) {
             // -------------------------------------------------------- MMA issue, half h of every block
             const uint32_t h = (uint32_t)warp - 1u;
             const uint32_t full_s = smem_u32(&g->full[0]), empty_s = smem_u32(&g->empty[0]);
@@ -221,58 +256,80 @@ fp8_pair_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const
         const int aw = warp - kAddWarp0, quarter = warp & 3, h = aw >> 2;
         const uint32_t strips_s = strips0_s + (uint32_t)aw * (kStrips * kStrip), bias_s = biases_s + (uint32_t)aw * kBiasBytes;
         const uint32_t x_s = scales_s + (uint32_t)(quarter * 32 + lane) * 4u, sfull_s = smem_u32(&g->scales[0]);
-        const uint32_t tfull_s = smem_u32(&g->tfull[h]), tempty_c = map_to_cta(smem_u32(&g->tempty[h]), 0);
-        const uint32_t tm0 = tmem_base + ((uint32_t)(quarter * 32) << 16) + h * 128;
+        const uint32_t tfull_s = smem_u32(&g->tfull[TN == 256 ? h : 0]), tempty_c = map_to_cta(smem_u32(&g->tempty[TN == 256 ? h : 0]), 0);
+        const uint32_t tm0 = tmem_base + ((uint32_t)(quarter * 32) << 16) + h * (TN / 2);
         uint32_t par = 0, n = 0;                                 // phase bits of the half's two accumulators; blocks so far
+        const bool ragged = a.O % (Y16 ? 8 : 4) != 0;
         bool full = false, scaled = false;                       // the next block's barriers, asked ahead of their use
         for (int tile = first; tile < n_tiles && !c->abort_flag; tile += n_clusters) {
             const int mt = tile / a.tiles_n, nt = tile - mt * a.tiles_n;
             const int64_t m0 = (int64_t)mt * 256 + rank * 128 + quarter * 32;
-            const int64_t n0 = (int64_t)nt * 256 + h * 64;       // columns n0 + 0..63 and n0 + 128 + 0..63
+            const int64_t n0 = (int64_t)nt * TN + h * 64;        // columns n0 + 0..63 and, with TN = 256, n0 + 128 + 0..63
             __syncwarp();                                        // the last tile's biases have been read
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < TN / 64; ++i) {
                 const int64_t col = n0 + (i >> 1) * 128 + (i & 1) * 32 + lane;
                 sts32(bias_s + (uint32_t)(i * 32 + lane) * 4u, a.bias && col < a.O ? __float_as_uint(__ldg(a.bias + col)) : 0u);
             }
-            full = mbar_test_s(tfull_s, par & 1u);               // the tensor core has run ahead during the last tile's epilogue
+            // the tensor core has run ahead during the last tile's epilogue
+            full = TN == 256 ? mbar_test_s(tfull_s, par & 1u) : mbar_test_s(tfull_s + (n & 3u) * 8, (n >> 2) & 1u);
             scaled = mbar_test_s(sfull_s + n % kScaleSlots * 8, (n / kScaleSlots) & 1u);
-            float2 acc[64];
+            float2 acc[TN / 4];
 #pragma unroll
-            for (int j = 0; j < 64; ++j) acc[j] = make_float2(0.f, 0.f);
-            const auto block = [&](const int slot, uint32_t then) {
-                const uint32_t at = n % kScaleSlots;
-                if (!full) fp8_wait_more(tfull_s + slot * 16, (par >> slot) & 1u, c, a.status, 2u);
-                if (!scaled) fp8_wait_more(sfull_s + at * 8, (n / kScaleSlots) & 1u, c, a.status, 6u);
-                par ^= 1u << slot;
-                ++n;
-                tc_fence_after();
-                const float x = __uint_as_float(lds32(x_s + at * kScaleBytes));
-                const float w0 = __uint_as_float(lds32(scales_s + at * kScaleBytes + 512)), w1 = __uint_as_float(lds32(scales_s + at * kScaleBytes + 516));
-                uint32_t v[64];
-                tmem_ld64_wait(tm0 + slot * 256, v);
-                scale_add64(acc, v, x * w0);
-                tmem_ld64_wait(tm0 + slot * 256 + 64, v);
-                tc_fence_before();
-                __syncwarp();
-                arrive_cluster_lane0(tempty_c + slot * 16, lane);
-                full = mbar_test_s(tfull_s + then * 16, (par >> then) & 1u);
-                scaled = mbar_test_s(sfull_s + n % kScaleSlots * 8, (n / kScaleSlots) & 1u);
-                scale_add64(acc + 32, v, x * w1);
-            };
+            for (int j = 0; j < TN / 4; ++j) acc[j] = make_float2(0.f, 0.f);
+            if constexpr (TN == 256) {
+                const auto block = [&](const int slot, uint32_t then) {
+                    const uint32_t at = n % kScaleSlots;
+                    if (!full) fp8_wait_more(tfull_s + slot * 16, (par >> slot) & 1u, c, a.status, 2u);
+                    if (!scaled) fp8_wait_more(sfull_s + at * 8, (n / kScaleSlots) & 1u, c, a.status, 6u);
+                    par ^= 1u << slot;
+                    ++n;
+                    tc_fence_after();
+                    const float x = __uint_as_float(lds32(x_s + at * kScaleBytes));
+                    const float w0 = __uint_as_float(lds32(scales_s + at * kScaleBytes + 512)), w1 = __uint_as_float(lds32(scales_s + at * kScaleBytes + 516));
+                    uint32_t v[64];
+                    tmem_ld64_wait(tm0 + slot * 256, v);
+                    scale_add64(acc, v, x * w0);
+                    tmem_ld64_wait(tm0 + slot * 256 + 64, v);
+                    tc_fence_before();
+                    __syncwarp();
+                    arrive_cluster_lane0(tempty_c + slot * 16, lane);
+                    full = mbar_test_s(tfull_s + then * 16, (par >> then) & 1u);
+                    scaled = mbar_test_s(sfull_s + n % kScaleSlots * 8, (n / kScaleSlots) & 1u);
+                    scale_add64(acc + 32, v, x * w1);
+                };
 #pragma unroll 1
-            for (int kb = 0; kb + 1 < K; kb += 2) {
-                block(0, 1u);
-                block(1, 0u);
-                if (c->abort_flag) break;
+                for (int kb = 0; kb + 1 < K; kb += 2) {
+                    block(0, 1u);
+                    block(1, 0u);
+                    if (c->abort_flag) break;
+                }
+                if (K & 1) block(0, 0u);
+            } else {
+#pragma unroll 1
+                for (int kb = 0; kb < K && !c->abort_flag; ++kb) {   // 64 columns of the block's accumulator
+                    const uint32_t slot = n & 3u, at = n % kScaleSlots;
+                    if (!full) fp8_wait_more(tfull_s + slot * 8, (n >> 2) & 1u, c, a.status, 2u);
+                    if (!scaled) fp8_wait_more(sfull_s + at * 8, (n / kScaleSlots) & 1u, c, a.status, 6u);
+                    ++n;
+                    tc_fence_after();
+                    const float d = __uint_as_float(lds32(x_s + at * kScaleBytes)) * __uint_as_float(lds32(scales_s + at * kScaleBytes + 512));
+                    uint32_t v[64];
+                    tmem_ld64_wait(tm0 + slot * 128, v);
+                    tc_fence_before();
+                    __syncwarp();
+                    arrive_cluster_lane0(tempty_c + slot * 8, lane);
+                    full = mbar_test_s(tfull_s + (n & 3u) * 8, (n >> 2) & 1u);
+                    scaled = mbar_test_s(sfull_s + n % kScaleSlots * 8, (n / kScaleSlots) & 1u);
+                    scale_add64(acc, v, d);
+                }
             }
-            if (K & 1) block(0, 0u);
             if (c->abort_flag) break;
             // 32 rows x 128 bytes at a time: 32 columns of binary32 or 64 of 16 bits
             constexpr int kStripCols = Y16 ? 64 : 32;
             __syncwarp();
 #pragma unroll
-            for (int piece = 0; piece < 128 / kStripCols; ++piece) {
+            for (int piece = 0; piece < TN / 2 / kStripCols; ++piece) {
                 const int c0 = piece * kStripCols;
                 const int64_t col0 = n0 + (c0 >> 6) * 128 + (c0 & 63);
                 const uint32_t strip_s = strips_s + (uint32_t)(piece & 1) * kStrip;
@@ -303,7 +360,8 @@ fp8_pair_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const
                     else
                         sts128(at, __float_as_uint(o[0]), __float_as_uint(o[1]), __float_as_uint(o[2]), __float_as_uint(o[3]));
                 }
-                if (a.y_vec) {
+                // the engine writes 16 bytes at a time: a last piece of columns that ends within them is stored by element
+                if (a.y_vec && (!ragged || col0 + kStripCols <= a.O)) {
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // generic writes before the engine's reads
                     __syncwarp();
                     if (lane == 0) {
@@ -338,6 +396,7 @@ fp8_pair_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const
                                 if (r0 + r < rows && 32 * q < cols) y[r * a.y_stride + 32 * q] = v[r][q];
                         y += 8 * a.y_stride;
                     }
+                    if (lane == 0) bulk_commit_group();          // an empty one: a strip's turn is counted in groups
                     __syncwarp();
                 }
             }
@@ -355,22 +414,25 @@ fp8_pair_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const
 
 }  // namespace
 
-tdq_status launch_fp8_pair(Fp8Args a, const CUtensorMap& xmap, const CUtensorMap& wmap, int n_sm, int dev, cudaStream_t stream) {
+tdq_status launch_fp8_pair(Fp8Args a, int columns, const CUtensorMap& xmap, const CUtensorMap& wmap, int n_sm, int dev, cudaStream_t stream) {
     const bool y16 = a.y_type != TDQ_F32, f16 = a.y_type == TDQ_F16;
     CUtensorMap ymap;
     memset(&ymap, 0, sizeof ymap);
     if (a.y_vec && !encode_y_map(&ymap, a.y, y16, a.M, a.O, a.y_stride, y16 ? 64 : 32, 32, f16)) a.y_vec = 0;
     a.tiles_m = (int32_t)((a.M + 255) / 256);
-    a.tiles_n = (int32_t)((a.O + 255) / 256);
-    constexpr uint32_t smem = kPairCtrl + kPairStages * kPairStage + kAddWarps * (kStrips * kStrip + kBiasBytes) + kScaleSlots * kScaleBytes;
-    static_assert(smem <= (uint32_t)kSmemLimit, "shared memory");
-    static std::atomic<uint64_t> smem_done[3];
-    void (*const kernels[3])(Fp8Args, CUtensorMap, CUtensorMap, CUtensorMap) = {fp8_pair_kernel<TDQ_F32>, fp8_pair_kernel<TDQ_BF16>, fp8_pair_kernel<TDQ_F16>};
-    if (allow_smem(kernels[a.y_type], (int)smem, smem_done[a.y_type], dev) != cudaSuccess) return TDQ_ERR_CUDA;
+    a.tiles_n = (int32_t)((a.O + columns - 1) / columns);
+    static_assert(PairShape<256>::kSmem <= (uint32_t)kSmemLimit && PairShape<128>::kSmem <= (uint32_t)kSmemLimit, "shared memory");
+    static std::atomic<uint64_t> smem_done[2][3];
+    void (*const kernels[2][3])(Fp8Args, CUtensorMap, CUtensorMap, CUtensorMap) = {
+        {fp8_pair_kernel<TDQ_F32, 256>, fp8_pair_kernel<TDQ_BF16, 256>, fp8_pair_kernel<TDQ_F16, 256>},
+        {fp8_pair_kernel<TDQ_F32, 128>, fp8_pair_kernel<TDQ_BF16, 128>, fp8_pair_kernel<TDQ_F16, 128>}};
+    const int narrow = columns == 128;
+    const uint32_t smem = narrow ? PairShape<128>::kSmem : PairShape<256>::kSmem;
+    if (allow_smem(kernels[narrow][a.y_type], (int)smem, smem_done[narrow][a.y_type], dev) != cudaSuccess) return TDQ_ERR_CUDA;
     const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n;
     if (tiles > INT32_MAX / 2) return TDQ_ERR_UNSUPPORTED;
     const unsigned clusters = (unsigned)(tiles < n_sm / 2 ? tiles : n_sm / 2);
-    if (launch_pdl(kernels[a.y_type], dim3(2 * clusters), dim3(kPairThreads), smem, stream, a, xmap, wmap, ymap) != cudaSuccess) return TDQ_ERR_CUDA;
+    if (launch_pdl(kernels[narrow][a.y_type], dim3(2 * clusters), dim3(kPairThreads), smem, stream, a, xmap, wmap, ymap) != cudaSuccess) return TDQ_ERR_CUDA;
     g_launch_count.fetch_add(1, std::memory_order_relaxed);
     return TDQ_OK;
 }

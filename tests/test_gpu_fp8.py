@@ -237,6 +237,38 @@ def test_every_number_of_parts(tdq, n):
     _run(tdq, *SPLITS[n], ("fp32", "bf16", "fp16")[n % 3], n % 2 == 0, n % 4)
 
 
+# tiles of 256 x 128: one round of them and several, fewer blocks than stages and many
+NARROW = [(5227, 34, 33), (4750, 137, 33), (3259, 311, 34), (5142, 522, 33), (4756, 665, 33), (4744, 866, 36), (5075, 1097, 32), (6800, 2146, 33), (512, 4096, 4096),
+          (1200, 1400, 1300), (300, 8190, 900), (9616, 32, 266), (9505, 298, 257), (9637, 552, 259), (9814, 785, 261), (9892, 2065, 280), (584, 32, 6435),
+          (525, 258, 6557), (514, 533, 6468), (520, 1042, 7092)]
+
+
+@pytest.mark.parametrize("M,I,O", NARROW)
+@pytest.mark.parametrize("dtype,pitch", [("fp32", 0), ("bf16", 0), ("fp16", 8), ("bf16", 1), ("fp32", 2)])
+def test_narrow_tiles(tdq, M, I, O, dtype, pitch):
+    _run(tdq, M, I, O, dtype, pitch < 2, (-O) % 8 if pitch == 0 else pitch)
+
+
+@pytest.mark.parametrize("M,O", [(9000, 1001), (9000, 998), (20000, 4093), (1200, 1301), (300, 61), (40, 999)])
+def test_padded_rows_keep_what_stands_behind_the_last_column(tdq, M, O):
+    """Rows on the 16-byte grid whose last column ends inside 16 bytes, for every kind of tile."""
+    for dtype in ("fp32", "bf16", "fp16"):
+        _run(tdq, M, 300, O, dtype, True, (-O) % 8)
+        _run(tdq, M, 300, O, dtype, False, (-O) % 8 + 8, 8)
+
+
+@pytest.mark.parametrize("M,I,O", [(1200, 700, 1300), (9505, 298, 257)])
+def test_nan_in_narrow_tiles(tdq, M, I, O):
+    xc, xs, wc, ws, b, K = _operands(M, I, O, 6)
+    xc.view(torch.uint8)[1, 200] = 0x7F
+    ws[1, 2] = float("nan")
+    xs[M - 1, 0] = float("inf")
+    y = tdq.fp8_linear(xc, xs, wc, ws, b)
+    bad = torch.zeros((M, O), dtype=torch.bool, device="cuda")
+    bad[1], bad[M - 1], bad[:, 128:256] = True, True, True
+    assert torch.isfinite(y[~bad]).all() and not torch.isfinite(y[bad]).any()
+
+
 @pytest.mark.parametrize("M,O", [(257, 256 * 37 + 1), (256 * 5 + 1, 256 * 9 - 1), (256 * 38 - 127, 100), (20000, 257)])
 def test_ragged_large_tiles(tdq, M, O):
     _run(tdq, M, 256, O, "fp32", True)
