@@ -2,7 +2,7 @@
 //
 // The sum of a block of 128 channels is four tensor-core instructions (kind::f8f6f4, binary32 accumulator in TMEM); its two scales
 // change from block to block, so each block's sums are taken out of TMEM and added, scaled, to binary32 registers.
-// Two kernels: tiles of 256 x 256 by pairs of CTAs (tdq_fp8_pair.cu) for layers with enough of them, and here the one for few tokens.
+// Two kernels: tiles of 256 x 256 or 256 x 128 by pairs of CTAs (tdq_fp8_pair.cu) for layers with enough of them, and here the one for few tokens.
 //
 // fp8_split_kernel.  Few tokens: the time is that of reading the weights once, so all SMs have to read, however few rows the output
 // has.  128 output channels are the instruction's 128 rows and NT tokens (16 .. 128) its columns; the contraction is cut in up to eight
@@ -13,7 +13,7 @@
 // is two ring stages, and an owner of channels stores narrower pieces than an owner of tokens.
 // Warps 0 and 2 load (tensor maps, 16 KB of weights and the tokens' 128 bytes a stage), warp 1 issues, warp 3 lays out the tokens' factors
 // xs * ws of a block in shared memory, the others scale and add: a thread has one output channel and up to 32 tokens.
-// Measured, from a graph: 1 x 4096 -> 4096 bf16 5.1 us with the weights in L2, 6.9 from memory (floor 2.6), 1 x 8192 -> 8192 14.7 (10.3), 576 x 384 -> 960 4.7.
+// Measured, from a graph: 1 x 4096 -> 4096 bf16 5.1 us with the weights in L2, 6.9 from memory (floor 2.6), 1 x 8192 -> 8192 14.7 (10.3), 576 x 384 -> 960 4.5.
 // The tensor copies bring 38 bytes a clock to an SM, whatever their size (stages of two blocks: no gain); the rest is the chain from launch to
 // first tile (1500 clocks), through the last tile, and the meeting.  Not kept: the weights prefetched to L2 ahead of the wait for the kernel
 // before (a layer behind its quantizer 6.5 -> 7.0 us, 1 x 8192 -> 8192 14.7 -> 19.9).

@@ -1,4 +1,4 @@
-// tdq_fp8_linear for layers with many tiles: two CTAs of a cluster on a tile of 256 tokens x 256 output channels.
+// tdq_fp8_linear for layers with many tiles: two CTAs of a cluster on a tile of 256 tokens x 256 (or 128) output channels.
 //
 // What bounds it.  A block of 128 channels is 512 clocks of tensor time per 256 x 256 tile; the 32 KB of operands that it uses in each
 // CTA are written to shared memory meanwhile (64 bytes of the 128 a clock).  The sums of a block have scales of their own, so
