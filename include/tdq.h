@@ -330,7 +330,8 @@ size_t tdq_fp8_linear_workspace_bytes(int64_t M, int64_t I_pad, int64_t O);
  *   positions  [M, n_axes] int64;  freq [R/2] float64, radians per position;  axis [R/2] int32, the column of positions that
  *              turns the pair (a number outside 0 .. n_axes-1 counts as the last column).  Unused when R == 0.
  *   Pointers and strides on the 16-byte grid with D a multiple of 16 (float32: 8), R/2 of 8 (4) and D <= 512 (256) take the
- *   vector kernel, anything else a slower general one.  M == 0 is a no-op.  TDQ_ERR_UNSUPPORTED for head_dim or heads above 65536
+ *   vector kernel, 16-bit heads on the 8-byte grid with D a multiple of 8, R/2 of 4 and D <= 256 its form for half vectors, anything else a
+ *   slower general one; weights for the first two on the 16-byte grid.  M == 0 is a no-op.  TDQ_ERR_UNSUPPORTED for head_dim or heads above 65536
  *   and M above 2^31 - 1.
  */
 #define TDQ_ROPE_NORM 1u

@@ -58,11 +58,13 @@ __device__ __forceinline__ typename Bits<DT>::T from_f(float v) {
     else if constexpr (DT == TDQ_BF16) return __bfloat16_as_ushort(__float2bfloat16_rn(v));
     else return __half_as_ushort(__float2half_rn(v));
 }
-template <int DT>
-__device__ __forceinline__ void unpack(const uint4& v, float* f) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+template <int VB> struct Bytes { using T = uint4; };      // a vector of VB bytes
+template <> struct Bytes<8> { using T = uint2; };
+template <int DT, int VB>
+__device__ __forceinline__ void unpack(const typename Bytes<VB>::T& v, float* f) {
+    const uint32_t* w = &v.x;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < VB / 4; ++i) {
         if constexpr (DT == TDQ_F32) {
             f[i] = __uint_as_float(w[i]);
         } else if constexpr (DT == TDQ_BF16) {
@@ -75,11 +77,12 @@ __device__ __forceinline__ void unpack(const uint4& v, float* f) {
         }
     }
 }
-template <int DT>
-__device__ __forceinline__ uint4 pack(const float* f) {
-    uint32_t w[4];
+template <int DT, int VB>
+__device__ __forceinline__ typename Bytes<VB>::T pack(const float* f) {
+    typename Bytes<VB>::T v;
+    uint32_t* w = &v.x;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < VB / 4; ++i) {
         if constexpr (DT == TDQ_F32) {
             w[i] = __float_as_uint(f[i]);
         } else if constexpr (DT == TDQ_BF16) {
@@ -90,16 +93,20 @@ __device__ __forceinline__ uint4 pack(const float* f) {
             w[i] = *reinterpret_cast<const uint32_t*>(&h);
         }
     }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+    return v;
 }
 
-// sixteen bytes to shared memory, asynchronously; zeros if not `there`
-__device__ __forceinline__ void copy16_async(uint32_t dst, const void* src, bool there) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+// a vector to shared memory, asynchronously; zeros if not `there`
+template <int VB>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool there) {
+    if constexpr (VB == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(there ? 8 : 0) : "memory");
 }
-__device__ __forceinline__ uint4 lds_u4(uint32_t addr) {
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+template <int VB>
+__device__ __forceinline__ typename Bytes<VB>::T lds_vec(uint32_t addr) {
+    typename Bytes<VB>::T v;
+    if constexpr (VB == 16) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    else asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
     return v;
 }
 // The turns a pair makes per position: the fraction of freq / 2 pi in units of 2^-64 (whole turns of it stay whole turns at every position).
@@ -123,13 +130,14 @@ __device__ __forceinline__ uint32_t axis_of(const RopeArgs& a, int i) {   // an 
 // Registers a thread, and with them warps an SM.  16 bits, 28 warps of 72: with 78 registers only 24 fit, and 2949 x 20 x 96 bf16 takes 10.6 us
 // for 7.8; 20 warps 18432 x 24 x 64 fp16 29.8 us for 24.8, 32 warps of 64 25.9.  binary32, 32 warps of 64: 8192 x 32 x 80 39, 24 warps 47.
 template <int DT> constexpr int rope_ahead = 2;
-template <int DT> constexpr int rope_ring = DT == TDQ_F32 ? 0 : rope_ahead<DT> * 32;   // bytes of shared memory a thread
+template <int DT, int VB> constexpr int rope_ring = DT == TDQ_F32 ? 0 : rope_ahead<DT> * 2 * VB;   // bytes of shared memory a thread
 template <int DT> constexpr int rope_regs = DT == TDQ_F32 ? 64 : 72;
 template <int DT> constexpr int rope_warps_per_sm = DT == TDQ_F32 ? 32 : 28;
-template <int DT, bool ADJ>
+template <int DT, bool ADJ, int VB>
 __global__ void __maxnreg__(rope_regs<DT>) rope_kernel(const RopeArgs a) {
     using T = typename Bits<DT>::T;
-    constexpr int V = 16 / (int)sizeof(T);                 // elements of a vector, pairs of a thread
+    using Vec = typename Bytes<VB>::T;
+    constexpr int V = VB / (int)sizeof(T);                 // elements of a vector, pairs of a thread
     constexpr bool kAsync = DT != TDQ_F32;
     constexpr int kAhead = rope_ahead<DT>;                 // tokens whose loads are in flight
     extern __shared__ float4 shared[];
@@ -139,8 +147,8 @@ __global__ void __maxnreg__(rope_regs<DT>) rope_kernel(const RopeArgs a) {
     const int64_t m0 = (int64_t)blockIdx.x * a.tokens;
     const int n_tok = (int)min((int64_t)a.tokens, a.M - m0);
     const int L = 1 << a.lanes_log2, unit = lane & (L - 1), units = a.half / V, all_units = a.D / (2 * V);
-    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(shared) + 16u * threadIdx.x;   // [tokens ahead][2][threads] vectors
-    float4* const weights = shared + (kAsync ? kAhead * 2 * blockDim.x : 0);   // [queries, keys][V / 2][units of a head]: four weights
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(shared) + VB * threadIdx.x;   // [tokens ahead][2][threads] vectors
+    float4* const weights = shared + (kAsync ? kAhead * 2 * blockDim.x * VB / 16 : 0);   // [queries, keys][V / 2][units of a head]: four weights
     float4* const table = weights + (a.norm ? V * all_units : 0);   // [tokens][V / 2][turned units]: two pairs' cosines, then their sines
     const int row = warp / a.warps_across, across = warp - row * a.warps_across;   // the warp's first token and head group
     const int rows = (int)(blockDim.x >> 5) / a.warps_across;
@@ -163,20 +171,20 @@ __global__ void __maxnreg__(rope_regs<DT>) rope_kernel(const RopeArgs a) {
         // 40 x 128 bf16 62.1 -> 56.3 us; four tokens ahead 55.5, but 18432 x 24 x 64 fp16 24.7 instead of 22.6), binary32 in registers (8192 x 32 x 80: 39,
         // through shared memory 45).
         uint32_t next = 0;
-        uint4 held[kAhead][2];
-        const auto load = [&](uint4* to_regs, int t) {
+        Vec held[kAhead][2];
+        const auto load = [&](Vec* to_regs, int t) {
             const bool there = mine && t < n_tok;
             if constexpr (kAsync) {
-                const uint32_t to = ring + (next % kAhead) * 32u * blockDim.x;
-                copy16_async(to, there ? src + e0 : reinterpret_cast<const T*>(a.any), there);
-                copy16_async(to + 16u * blockDim.x, there ? src + e1 : reinterpret_cast<const T*>(a.any), there);
+                const uint32_t to = ring + (next % kAhead) * 2u * VB * blockDim.x;
+                copy_async<VB>(to, there ? src + e0 : reinterpret_cast<const T*>(a.any), there);
+                copy_async<VB>(to + VB * blockDim.x, there ? src + e1 : reinterpret_cast<const T*>(a.any), there);
                 asm volatile("cp.async.commit_group;" ::: "memory");
                 ++next;
             } else {
-                to_regs[0] = to_regs[1] = make_uint4(0, 0, 0, 0);
+                to_regs[0] = to_regs[1] = Vec{};
                 if (there) {
-                    to_regs[0] = *reinterpret_cast<const uint4*>(src + e0);
-                    to_regs[1] = *reinterpret_cast<const uint4*>(src + e1);
+                    to_regs[0] = *reinterpret_cast<const Vec*>(src + e0);
+                    to_regs[1] = *reinterpret_cast<const Vec*>(src + e1);
                 }
             }
             src += in_step;
@@ -209,12 +217,12 @@ __global__ void __maxnreg__(rope_regs<DT>) rope_kernel(const RopeArgs a) {
         }
         const float4* const wt = weights + (is_q ? 0 : V / 2 * all_units) + unit;
         for (int t = row; t < n_tok; t += rows) {
-            uint4 v0 = held[0][0], v1 = held[0][1];
+            Vec v0 = held[0][0], v1 = held[0][1];
             if constexpr (kAsync) {
                 asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
-                const uint32_t from = ring + (next % kAhead) * 32u * blockDim.x;   // the oldest
-                v0 = lds_u4(from);
-                v1 = lds_u4(from + 16u * blockDim.x);
+                const uint32_t from = ring + (next % kAhead) * 2u * VB * blockDim.x;   // the oldest
+                v0 = lds_vec<VB>(from);
+                v1 = lds_vec<VB>(from + VB * blockDim.x);
             } else {
 #pragma unroll
                 for (int i = 0; i + 1 < kAhead; ++i) {
@@ -224,8 +232,8 @@ __global__ void __maxnreg__(rope_regs<DT>) rope_kernel(const RopeArgs a) {
             }
             // two elements an instruction: the kernel issues close to what the schedulers take (250 of them a warp and token, 309 with single elements, 18432 x 24 x 64 fp16)
             float2 x[V / 2], y[V / 2];
-            unpack<DT>(v0, reinterpret_cast<float*>(x));
-            unpack<DT>(v1, reinterpret_cast<float*>(y));
+            unpack<DT, VB>(v0, reinterpret_cast<float*>(x));
+            unpack<DT, VB>(v1, reinterpret_cast<float*>(y));
             load(held[kAhead - 1], t + kAhead * rows);
             if (a.norm) {
                 float2 sx = make_float2(0.f, 0.f), sy = sx;
@@ -266,8 +274,8 @@ __global__ void __maxnreg__(rope_regs<DT>) rope_kernel(const RopeArgs a) {
                         }
                     }
                 }
-                *reinterpret_cast<uint4*>(dst + e0) = pack<DT>(reinterpret_cast<const float*>(x));
-                *reinterpret_cast<uint4*>(dst + e1) = pack<DT>(reinterpret_cast<const float*>(y));
+                *reinterpret_cast<Vec*>(dst + e0) = pack<DT, VB>(reinterpret_cast<const float*>(x));
+                *reinterpret_cast<Vec*>(dst + e1) = pack<DT, VB>(reinterpret_cast<const float*>(y));
             }
             dst += out_step;
         }
@@ -312,56 +320,69 @@ __global__ void __launch_bounds__(256) rope_any_kernel(const RopeArgs a) {
     for (int i = 2 * a.half + lane; i < a.D; i += 32) out[i] = from_f<DT>(to_f<DT>(x[i]) * (w ? r * __ldg(w + i) : r));
 }
 
+// vectors of VB bytes everywhere, a head of at most 32 lanes, whole vectors on either side of the rotated channels' middle and end
+template <int DT, int VB>
+bool rope_fits(const RopeArgs& a) {
+    constexpr int V = VB / (int)sizeof(typename Bits<DT>::T);
+    const auto side = [&](const tdq_rope_heads& s) {
+        return s.heads == 0 || (reinterpret_cast<uintptr_t>(s.x) % VB == 0 && reinterpret_cast<uintptr_t>(s.out) % VB == 0 && reinterpret_cast<uintptr_t>(s.weight) % 16 == 0 &&
+                                s.row_stride % V == 0 && s.head_stride % V == 0 && s.out_row_stride % V == 0 && s.out_head_stride % V == 0);
+    };
+    return a.D % (2 * V) == 0 && a.half % V == 0 && a.D <= 64 * V && side(a.q) && side(a.k);
+}
+
+template <int DT, int VB>
+cudaError_t launch_vec(RopeArgs a, int n_sm, int dev, cudaStream_t st) {
+    constexpr int V = VB / (int)sizeof(typename Bits<DT>::T);
+    a.lanes_log2 = 0;
+    while ((2 * V << a.lanes_log2) < a.D) ++a.lanes_log2;
+    const int per_warp = 32 >> a.lanes_log2, groups = (a.H + per_warp - 1) / per_warp;
+    // about eight warps: all of a token's head groups side by side where there are no more, several tokens where there are few
+    a.groups = groups;
+    a.warps_across = groups < kRopeWarps ? groups : (groups + (groups + kRopeWarps - 1) / kRopeWarps - 1) / ((groups + kRopeWarps - 1) / kRopeWarps);
+    const int rows = kRopeWarps / a.warps_across;
+    const int warps = rows * a.warps_across, passes = (groups + a.warps_across - 1) / a.warps_across;
+    const size_t per_block = (a.norm ? 2 * a.D * sizeof(float) : 0) + (size_t)rope_ring<DT, VB> * warps * 32, per_token = (size_t)a.half * sizeof(float2);
+    const int table_deep = per_token ? (int)(kTableMax / (per_token * rows)) : 8;
+    // Tokens a warp goes through (`deep`, eight at most: sixteen 16384 x 40 x 128 65 us for 57), and a token's groups of heads in one thread block after
+    // another or in as many blocks: the least of rounds of resident blocks x (tokens x groups of a warp + 1), and blocks of an SM x warps / 16.
+    // Against as many tokens as leave four blocks an SM, whatever fits at once: 2619 x 72 x 128 bf16 23.7 -> 18.8 us, 3272 x 6 x 128 6.0 -> 4.6, 314 x
+    // 20 x 256 fp32 6.5 -> 4.7; 227 x 60 x 128, the worst of 23 sizes, 4.7 -> 4.9.
+    uint64_t least = UINT64_MAX;
+    int across = 1;
+    for (int deep = 1; deep <= 8 && (deep == 1 || (deep <= table_deep && rows * (deep - 1) < a.M)); ++deep) {
+        const uint32_t blocks = ((uint32_t)a.M + rows * deep - 1) / (rows * deep);
+        const uint32_t fit = std::min<uint32_t>(rope_warps_per_sm<DT> / warps, (uint32_t)((size_t)kSmSharedBytes / (per_block + per_token * rows * deep + 1024)));
+        for (int y = 1; y <= passes; y += passes > 1 ? passes - 1 : 1) {
+            const uint64_t n = (uint64_t)blocks * y;
+            if (n > INT32_MAX) break;
+            const uint32_t held = fit * n_sm, rounds = ((uint32_t)n + held - 1) / held, an_sm = ((uint32_t)n + n_sm - 1) / n_sm;
+            const uint64_t cost = 16ull * rounds * (1 + deep * (passes / y)) + (uint64_t)an_sm * warps;
+            if (cost < least) { least = cost; a.tokens = rows * deep; across = y; }
+        }
+    }
+    const size_t smem = per_block + per_token * a.tokens;
+    a.any = a.q.heads ? a.q.x : a.k.x;
+    const int64_t blocks = (a.M + a.tokens - 1) / a.tokens;
+    void (*const kernel)(RopeArgs) = a.adjacent ? rope_kernel<DT, true, VB> : rope_kernel<DT, false, VB>;
+    static std::atomic<uint64_t> smem_done[2];
+    const cudaError_t e = allow_smem(kernel, (int)(kTableMax + rope_ring<DT, VB> * 32 * kRopeWarps + 2 * 64 * V * sizeof(float)), smem_done[a.adjacent], dev);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(kernel, dim3((unsigned)blocks, (unsigned)across), dim3(rows * a.warps_across * 32), smem, st, a);
+}
+
 template <int DT>
 tdq_status launch(RopeArgs a, cudaStream_t st) {
-    using T = typename Bits<DT>::T;
-    constexpr int V = 16 / (int)sizeof(T);
-    const auto fits = [&](const tdq_rope_heads& s) {       // 16-byte vectors everywhere
-        if (s.heads == 0) return true;
-        return reinterpret_cast<uintptr_t>(s.x) % 16 == 0 && reinterpret_cast<uintptr_t>(s.out) % 16 == 0 && reinterpret_cast<uintptr_t>(s.weight) % 16 == 0 &&
-               s.row_stride % V == 0 && s.head_stride % V == 0 && s.out_row_stride % V == 0 && s.out_head_stride % V == 0;
-    };
     int dev = 0;
     const int n_sm = current_device_sm_count(&dev);
     if (n_sm <= 0) return TDQ_ERR_CUDA;
-    cudaError_t e;
-    // a head of at most 32 lanes, whole vectors on either side of the rotated channels' middle and end
-    if (a.D % (2 * V) == 0 && a.half % V == 0 && a.D <= 64 * V && fits(a.q) && fits(a.k)) {
-        a.lanes_log2 = 0;
-        while ((2 * V << a.lanes_log2) < a.D) ++a.lanes_log2;
-        const int per_warp = 32 >> a.lanes_log2, groups = (a.H + per_warp - 1) / per_warp;
-        // about eight warps: all of a token's head groups side by side where there are no more, several tokens where there are few
-        a.groups = groups;
-        a.warps_across = groups < kRopeWarps ? groups : (groups + (groups + kRopeWarps - 1) / kRopeWarps - 1) / ((groups + kRopeWarps - 1) / kRopeWarps);
-        const int rows = kRopeWarps / a.warps_across;
-        const int warps = rows * a.warps_across, passes = (groups + a.warps_across - 1) / a.warps_across;
-        const size_t per_block = (a.norm ? 2 * a.D * sizeof(float) : 0) + (size_t)rope_ring<DT> * warps * 32, per_token = (size_t)a.half * sizeof(float2);
-        const int table_deep = per_token ? (int)(kTableMax / (per_token * rows)) : 8;
-        // Tokens a warp goes through (`deep`, eight at most: sixteen 16384 x 40 x 128 65 us for 57), and a token's groups of heads in one thread block after
-        // another or in as many blocks: the least of rounds of resident blocks x (tokens x groups of a warp + 1), and blocks of an SM x warps / 16.
-        // Against as many tokens as leave four blocks an SM, whatever fits at once: 2619 x 72 x 128 bf16 23.7 -> 18.8 us, 3272 x 6 x 128 6.0 -> 4.6, 314 x
-        // 20 x 256 fp32 6.5 -> 4.7; 227 x 60 x 128, the worst of 23 sizes, 4.7 -> 4.9.
-        uint64_t least = UINT64_MAX;
-        int across = 1;
-        for (int deep = 1; deep <= 8 && (deep == 1 || (deep <= table_deep && rows * (deep - 1) < a.M)); ++deep) {
-            const uint32_t blocks = ((uint32_t)a.M + rows * deep - 1) / (rows * deep);
-            const uint32_t fit = std::min<uint32_t>(rope_warps_per_sm<DT> / warps, (uint32_t)((size_t)kSmSharedBytes / (per_block + per_token * rows * deep + 1024)));
-            for (int y = 1; y <= passes; y += passes > 1 ? passes - 1 : 1) {
-                const uint64_t n = (uint64_t)blocks * y;
-                if (n > INT32_MAX) break;
-                const uint32_t held = fit * n_sm, rounds = ((uint32_t)n + held - 1) / held, an_sm = ((uint32_t)n + n_sm - 1) / n_sm;
-                const uint64_t cost = 16ull * rounds * (1 + deep * (passes / y)) + (uint64_t)an_sm * warps;
-                if (cost < least) { least = cost; a.tokens = rows * deep; across = y; }
-            }
-        }
-        const size_t smem = per_block + per_token * a.tokens;
-        a.any = a.q.heads ? a.q.x : a.k.x;
-        const int64_t blocks = (a.M + a.tokens - 1) / a.tokens;
-        void (*const kernel)(RopeArgs) = a.adjacent ? rope_kernel<DT, true> : rope_kernel<DT, false>;
-        static std::atomic<uint64_t> smem_done[2];
-        if (allow_smem(kernel, (int)(kTableMax + rope_ring<DT> * 32 * kRopeWarps + 2 * 64 * V * sizeof(float)), smem_done[a.adjacent], dev) != cudaSuccess)
-            return TDQ_ERR_CUDA;
-        e = launch_pdl(kernel, dim3((unsigned)blocks, (unsigned)across), dim3(rows * a.warps_across * 32), smem, st, a);
+    cudaError_t e = cudaErrorInvalidValue;
+    // Heads of 72 or 80 channels whose halves are no whole vectors of 16 bytes, and rows on the 8-byte grid: vectors of 8 bytes (18432 x 32 x 72 bf16
+    // 265 us with the general kernel, 61 so).
+    if (rope_fits<DT, 16>(a)) {
+        e = launch_vec<DT, 16>(a, n_sm, dev, st);
+    } else if (DT != TDQ_F32 && rope_fits<DT, 8>(a)) {
+        if constexpr (DT != TDQ_F32) e = launch_vec<DT, 8>(a, n_sm, dev, st);
     } else {
         const int64_t blocks = (a.M * a.H + 7) / 8;
         if (blocks > INT32_MAX) return TDQ_ERR_UNSUPPORTED;

@@ -63,6 +63,21 @@ def test_far_positions(tdq, far, D):
     _case(tdq, 50, 2, 2, D, D, 2, "fp32", far=far)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("adjacent", [False, True])
+@pytest.mark.parametrize("D,R", [(8, 8), (8, 0), (24, 16), (40, 8), (72, 72), (80, 40), (88, 80), (104, 104), (200, 40), (248, 248), (256, 8)])
+def test_vectors_of_eight_bytes(tdq, D, R, adjacent, dtype):
+    def views(x):                                         # rows and heads on the 8-byte grid only
+        M, H, D = x.shape
+        v = torch.full((4 + M * (H * (D + 4) + 4),), float("nan"), dtype=x.dtype, device="cuda")[4:]
+        v = v.as_strided((M, H, D), (H * (D + 4) + 4, D + 4, 1))
+        v.copy_(x)
+        return v
+    for M, hq, hk in ((1, 1, 1), (37, 9, 2), (700, 3, 3)):
+        _case(tdq, M, hq, hk, D, R, 2, dtype, adjacent=adjacent)
+        _case(tdq, M, hq, hk, D, R, 1, dtype, adjacent=adjacent, views=views, weights=False)
+
+
 @pytest.mark.parametrize("D", [64, 72])
 def test_whole_turns_and_frequencies_that_are_no_numbers(tdq, D):
     x = _heads(6, 3, D, 8, torch.float32)
