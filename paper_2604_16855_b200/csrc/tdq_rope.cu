@@ -8,7 +8,7 @@
 // up to positions of 2^40, and is rounded to binary32 for sincospif.  In binary64 (product, turns, fraction for every token) 29386 x 2 x 256 bf16
 // took 32.6 us for 28.2.  Sum of squares, norm and rotation are binary32; one rounding at the store.
 //
-// Bound by HBM: every head is read and written once.  A thread owns the two 16-byte vectors of a head whose elements form pairs (halves:
+// Bound by HBM: every head is read and written once.  A thread owns the two vectors (16 bytes, or 8) of a head whose elements form pairs (halves:
 // one from either half; adjacent: neighbours), so that a head is a power of two of lanes, its sum of squares a few shuffles, and
 // no element passes through another thread: in place is safe.  A thread block takes some tokens with all their heads; a warp keeps to a
 // group of heads and goes through the tokens with the next two's loads in flight.  The weights and the block's cosines and
