@@ -319,8 +319,9 @@ size_t tdq_fp8_linear_workspace_bytes(int64_t M, int64_t I_pad, int64_t O);
  *   with TDQ_ROPE_NORM   n_i = x_i w_i / sqrt(mean_j x_j^2 + eps)   (w == 1 where weight is NULL), else n = x;
  *   pair i < R/2 is channels (i, i + R/2), with TDQ_ROPE_ADJACENT (2i, 2i+1):   t = positions[m, axis[i]] freq[i],
  *   (n_a, n_b) -> (n_a cos t - n_b sin t, n_b cos t + n_a sin t);   channels from R on are n.
- *   freq / 2 pi is rounded to binary64, its fraction of a turn to a multiple of 2^-64; the product with the position is exact up to whole
- *   turns, so that positions of 2^40 still turn by the right angle.  Everything else is binary32, rounded once when stored.  The squares are not
+ *   The fraction of a turn in freq / 2 pi is rounded to a multiple of 2^-64 and its product with the position is exact up to whole turns: the
+ *   angle is off by position x 2^-65 of a turn, so that positions of 2^40 still turn by the right one to binary32's precision (frequencies up to
+ *   2^44).  Everything else is binary32, rounded once when stored.  The squares are not
  *   scaled before they are added: a head whose sum passes binary32's range becomes zero.
  *   q, k       either may be NULL or have no heads.  Element (m, h, i) of x is x[m row_stride + h head_stride + i], of out
  *              likewise; heads and rows of out must not overlap each other.  out == x (with the same strides) works in place;

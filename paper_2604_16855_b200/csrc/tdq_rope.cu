@@ -3,10 +3,11 @@
 //   r = 1 / sqrt(mean_i x_i^2 + eps);  n_i = x_i (r w_i);   for pair i < R/2:  t = pos[m, axis_i] freq_i,
 //   (n_a, n_b) -> (n_a cos t - n_b sin t,  n_b cos t + n_a sin t);   channels from R on: n_i
 //
-// Angles.  t reaches 10^6 and more, where binary32 has lost the fraction of a turn.  A pair's turns per position are a fraction in units of 2^-64 (from
-// binary64, once a thread); its product with the position, modulo 2^64, is the fraction of a turn to position x 2^-65, exact for what matters
-// up to positions of 2^40, and is rounded to binary32 for sincospif.  In binary64 (product, turns, fraction for every token) 29386 x 2 x 256 bf16
-// took 32.6 us for 28.2.  Sum of squares, norm and rotation are binary32; one rounding at the store.
+// Angles.  t reaches 10^6 and more, where binary32 has lost the fraction of a turn.  A pair's turns per position are a fraction in units of 2^-64, right to
+// half a unit (once a thread); its product with the position, modulo 2^64, is the fraction of a turn to position x 2^-65, no worse than the rounding to
+// binary32 for sincospif up to positions of 2^40.  freq / 2 pi in binary64 alone is off by 2^-53 of itself, which the position multiplies: 9e-5 radians at 2^40,
+// binary32's own step from 2^28 on.  In binary64 (product, turns, fraction for every token) 29386 x 2 x 256 bf16 took 32.6 us for 28.2.  Sum of
+// squares, norm and rotation are binary32; one rounding at the store.
 //
 // Bound by HBM: every head is read and written once.  A thread owns the two vectors (16 bytes, or 8) of a head whose elements form pairs (halves:
 // one from either half; adjacent: neighbours), so that a head is a power of two of lanes, its sum of squares a few shuffles, and
@@ -109,12 +110,17 @@ __device__ __forceinline__ typename Bytes<VB>::T lds_vec(uint32_t addr) {
     else asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
     return v;
 }
-// The turns a pair makes per position: the fraction of freq / 2 pi in units of 2^-64 (whole turns of it stay whole turns at every position).
+// The turns a pair makes per position: the fraction of freq / 2 pi to the nearest 2^-64 (whole turns of it stay whole turns at every position).
+// 1 / 2 pi is taken as the sum of two binary64 numbers, right to 2^-109, and the first product with its rounding error, so nothing above that is lost
+// for frequencies up to 2^44.
 struct Speed { int64_t step; float bad; };                 // bad: NaN where freq is not finite, else 0
 __device__ __forceinline__ Speed speed_of(double freq) {
-    const double turns = freq * 0.15915494309189533577;
-    const double f = turns - rint(turns);                  // [-1/2, 1/2]; +1/2 saturates below 2^63
-    return {__double2ll_rn(f * 18446744073709551616.0), (float)(f - f)};
+    constexpr double kInv2Pi = 0x1.45f306dc9c883p-3, kInv2PiLow = -0x1.6b01ec5417056p-57, kUnits = 0x1p64;
+    const double turns = __dmul_rn(freq, kInv2Pi), low = fma(freq, kInv2PiLow, fma(freq, kInv2Pi, -turns));
+    const double f = turns - rint(turns), g = low - rint(low);   // [-1/2, 1/2]
+    const double units = rint(f * kUnits), rest = f * kUnits - units;   // the products and the difference are exact
+    const uint64_t high = units < 0x1p63 ? (uint64_t)__double2ll_rn(units) : 1ull << 63;
+    return {(int64_t)(high + (uint64_t)__double2ll_rn(fma(g, kUnits, rest))), (float)(f - f)};
 }
 // cosine and sine at a position; the product's 64 low bits are its fraction of a turn, of which 32 are rounded to binary32
 __device__ __forceinline__ float2 turn_at(const Speed& v, int64_t pos) {

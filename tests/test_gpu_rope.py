@@ -1,4 +1,6 @@
 """Norm and rotation of queries and keys against the 64-bit form."""
+import math
+
 import pytest
 import torch
 
@@ -202,3 +204,47 @@ def test_graph_replay_in_place(tdq, D):
     torch.cuda.synchronize()
     want = tdq.qk_norm_rope(q, k, pos, table)
     assert torch.equal(qo, want[0]) and torch.equal(ko, want[1])
+
+
+def _turns_per_radian():
+    """1 / 2 pi as an integer over 2^400: Machin's formula, pi = 16 arctan(1/5) - 4 arctan(1/239), in integers."""
+    bits = 460
+
+    def arctan(n):
+        term, total, k = (1 << bits) // n, 0, 0
+        while term:
+            total += (-1) ** k * (term // (2 * k + 1))
+            term //= n * n
+            k += 1
+        return total
+    pi = 16 * arctan(5) - 4 * arctan(239)
+    return (1 << (400 + bits)) // (2 * pi)
+
+
+@pytest.mark.parametrize("adjacent", [False, True])
+@pytest.mark.parametrize("D", [64, 70])
+def test_angles_up_to_positions_of_2_to_the_40(tdq, D, adjacent):
+    """Both kernels against angles reduced in integers, where a binary64 product of position and frequency has lost 2^-13 of a turn.
+
+    The pair's fraction of a turn is off by 2^-64 a position at most and by 2^-32 where it is cut, its binary32 form by 2^-25; then two
+    units of the cosine (2^-23) and two products and a sum (3 2^-24), relative to the pair's magnitudes."""
+    from fractions import Fraction
+    turns, half = _turns_per_radian(), D // 2
+    freq, axis = tdq.rope_table(2 * half, base=5e5, device="cpu")
+    odd = [1.0, math.pi, -math.pi, 2 * math.pi, 3 * math.pi, 7.5, -0.7, 1000.25, 1e6 + 0.1, 2.0 ** -30, 1e-12, 0.0]
+    freq[5:5 + len(odd)] = torch.tensor(odd, dtype=torch.float64)
+    far = [1 << 40, -(1 << 40), (1 << 40) - 1, (1 << 39) + 12345, (1 << 34) + 77, -(1 << 31) - 5, 1 << 28, 12345, -7, 0]
+    x = _heads(len(far), 2, D, 6, torch.float32)
+    out, _ = tdq.qk_norm_rope(x, None, torch.tensor(far, device="cuda"), (freq.cuda(), axis.cuda()), eps=None, adjacent=adjacent)
+    angle = torch.empty((len(far), half), dtype=torch.float64)
+    for i, p in enumerate(far):
+        for j, f in enumerate(freq.tolist()):
+            t = Fraction(f) * p * turns / (1 << 400)
+            angle[i, j] = 2 * math.pi * float(t - round(t))
+    c, s = torch.cos(angle).cuda()[:, None], torch.sin(angle).cuda()[:, None]
+    a, b = (slice(0, D, 2), slice(1, D, 2)) if adjacent else (slice(0, half), slice(half, D))
+    xa, xb = x[..., a].double(), x[..., b].double()
+    off = 2.0 ** -64 * torch.tensor(far, device="cuda").abs().double()[:, None, None] + 2.0 ** -32 + 2.0 ** -25
+    tol = (xa.abs() + xb.abs()) * (2 * math.pi * off + 2.0 ** -23 + 3 * 2.0 ** -24)
+    for got, want in ((out[..., a], xa * c - xb * s), (out[..., b], xb * c + xa * s)):
+        assert ((got.double() - want).abs() <= tol).all(), float(((got.double() - want).abs() / tol).max())
