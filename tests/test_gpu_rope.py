@@ -248,3 +248,29 @@ def test_angles_up_to_positions_of_2_to_the_40(tdq, D, adjacent):
     tol = (xa.abs() + xb.abs()) * (2 * math.pi * off + 2.0 ** -23 + 3 * 2.0 ** -24)
     for got, want in ((out[..., a], xa * c - xb * s), (out[..., b], xb * c + xa * s)):
         assert ((got.double() - want).abs() <= tol).all(), float(((got.double() - want).abs() / tol).max())
+
+
+@pytest.mark.parametrize("M,hq,hk,D", [(1, 8, 2, 64), (577, 5, 5, 64), (300, 6, 2, 72)])
+def test_four_bit_qkv_layer_then_rotation_in_place(tdq, M, hq, hk, D):
+    """The 4-bit layer's bf16 output, its query and key channels turned where they are, each stage against its own reference."""
+    import oracle
+    from parity_utils import compare_y
+    C, O = 320, (hq + 2 * hk) * D
+    g = torch.Generator().manual_seed(M)
+    x, w = torch.randn((M, C), generator=g), 0.05 * torch.randn((O, C), generator=g)
+    codes, scale = tdq.quantize_act(x.cuda())
+    wcodes, wscale = tdq.quantize_weight(w.cuda())
+    qkv = tdq.w4a4_linear(codes, scale, wcodes, wscale, out_dtype=torch.bfloat16)
+    xa, wq = oracle.quantize_act(x.numpy()), oracle.quantize_weight(w.numpy())
+    # half a step of bf16, of a number that is off by the sum's bound itself
+    compare_y(qkv.float().cpu().numpy(), oracle.w4a4_linear(xa["codes"], xa["scale"], wq["codes"], wq["scale"]), C // 32, out_eps=1.01 * 2.0 ** -8)
+    before = qkv.clone()
+    q, k = qkv[:, :hq * D].view(M, hq, D), qkv[:, hq * D:(hq + hk) * D].view(M, hk, D)
+    at = torch.arange(M, device="cuda")
+    pos = torch.stack([at // 24, at % 24], 1).contiguous()
+    freq, axis = tdq.rope_table(D, [D // 4, D // 4], restart=True)
+    qw, kw = 1 + 0.1 * torch.randn((D,), generator=g).cuda(), 1 + 0.1 * torch.randn((D,), generator=g).cuda()
+    tdq.qk_norm_rope(q, k, pos, (freq, axis), qw, kw, q_out=q, k_out=k)
+    for now, was, weight in ((q, before[:, :hq * D].view(M, hq, D), qw), (k, before[:, hq * D:(hq + hk) * D].view(M, hk, D), kw)):
+        fu.check_rope(now, *fu.rope(was, weight, pos, freq, axis.long(), 1e-6, False))
+    assert torch.equal(qkv[:, (hq + hk) * D:], before[:, (hq + hk) * D:])       # the values stay
