@@ -383,6 +383,7 @@ tdq_status tdq_quantize_status(void* cuda_stream, uint32_t* detail /* HOST */);
  *               tdq_workspace_status().
  *   which == 1: the quantizer's routine; the code (14) goes to the per-device word that
  *               tdq_quantize_status() reads; workspace is ignored.
+ *   which == 3: the 8-bit layer's routine; the code (13) goes where which == 0 puts its own.  (2 stands for nothing.)
  * The call is asynchronous on cuda_stream like every other one.
  */
 tdq_status tdq_selftest_wait_timeout(int32_t which, int64_t limit_cycles, void* workspace, void* cuda_stream);

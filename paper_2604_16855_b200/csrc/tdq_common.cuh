@@ -49,6 +49,8 @@ bool act_fast_path_ok(const void* x, tdq_dtype dt, int64_t C, int64_t stride, co
 // One warp waits, with the bounded-wait routine of the kernels and the given cycle limit, on a barrier nobody arrives on
 // (tdq_selftest_wait_timeout; tdq_quantize_act.cu).
 tdq_status act_wait_selftest(long long limit_cycles, cudaStream_t stream);
+// The same with the 8-bit layer's routine; the code goes to *status (tdq_fp8_linear.cu).
+tdq_status fp8_wait_selftest(long long limit_cycles, uint32_t* status, cudaStream_t stream);
 
 // Bookkeeping kept per device (a process may drive several): the SM count of the current device, looked up once
 // for each, and which devices a kernel's opt-in to large dynamic shared memory has been made on (the attribute

@@ -431,7 +431,25 @@ tdq_status launch_split(Fp8Args a, int split, const uint8_t* xcodes, const CUten
     return TDQ_OK;
 }
 
+// One warp: a fresh barrier with one expected arrival that never comes, waited on with the two kernels' own routine and a short limit.  Nothing is
+// in flight when the warp leaves.
+__global__ void __launch_bounds__(32) fp8_wait_selftest_kernel(uint32_t* status, uint32_t limit) {
+    __shared__ Ctrl c;
+    if (threadIdx.x == 0) {
+        mbar_init(&c.full[0], 1);
+        c.abort_flag = 0;
+    }
+    __syncwarp();
+    fp8_wait_more(smem_u32(&c.full[0]), 0u, &c, status, 13u, limit);
+}
+
 }  // namespace
+
+tdq_status fp8_wait_selftest(long long limit_cycles, uint32_t* status, cudaStream_t stream) {
+    fp8_wait_selftest_kernel<<<1, 32, 0, stream>>>(status, (uint32_t)limit_cycles);
+    return cuda_status(cudaGetLastError());
+}
+
 }  // namespace tdq
 
 using namespace tdq;

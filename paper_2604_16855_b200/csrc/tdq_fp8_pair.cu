@@ -282,6 +282,7 @@ fp8_pair_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const
                     const uint32_t at = n % kScaleSlots;
                     if (!full) fp8_wait_more(tfull_s + slot * 16, (par >> slot) & 1u, c, a.status, 2u);
                     if (!scaled) fp8_wait_more(sfull_s + at * 8, (n / kScaleSlots) & 1u, c, a.status, 6u);
+                    __syncwarp();
                     par ^= 1u << slot;
                     ++n;
                     tc_fence_after();
@@ -311,6 +312,7 @@ fp8_pair_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const
                     const uint32_t slot = n & 3u, at = n % kScaleSlots;
                     if (!full) fp8_wait_more(tfull_s + slot * 8, (n >> 2) & 1u, c, a.status, 2u);
                     if (!scaled) fp8_wait_more(sfull_s + at * 8, (n / kScaleSlots) & 1u, c, a.status, 6u);
+                    __syncwarp();
                     ++n;
                     tc_fence_after();
                     const float d = __uint_as_float(lds32(x_s + at * kScaleBytes)) * __uint_as_float(lds32(scales_s + at * kScaleBytes + 512));

@@ -1445,15 +1445,20 @@ __global__ void __launch_bounds__(32) linear_wait_selftest_kernel(uint32_t* stat
 }  // namespace tdq
 
 extern "C" tdq_status tdq_selftest_wait_timeout(int32_t which, int64_t limit_cycles, void* workspace, void* cuda_stream) {
-    if (which != 0 && which != 1) return TDQ_ERR_INVALID_ARG;
+    if (which != 0 && which != 1 && which != 3) return TDQ_ERR_INVALID_ARG;
     if (limit_cycles < 1000 || limit_cycles > 2000000000LL) return TDQ_ERR_INVALID_ARG;   // at most about a second
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
     if (which == 1) return act_wait_selftest(limit_cycles, stream);
     if (!workspace) return TDQ_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(workspace) % 16) return TDQ_ERR_ALIGNMENT;
     if (cudaMemsetAsync(workspace, 0, 16, stream) != cudaSuccess) return TDQ_ERR_CUDA;
-    linear_wait_selftest_kernel<<<1, 32, 0, stream>>>(reinterpret_cast<uint32_t*>(workspace), limit_cycles);
-    if (cudaGetLastError() != cudaSuccess) return TDQ_ERR_CUDA;
+    if (which == 3) {
+        const tdq_status st = fp8_wait_selftest(limit_cycles, reinterpret_cast<uint32_t*>(workspace), stream);
+        if (st != TDQ_OK) return st;
+    } else {
+        linear_wait_selftest_kernel<<<1, 32, 0, stream>>>(reinterpret_cast<uint32_t*>(workspace), limit_cycles);
+        if (cudaGetLastError() != cudaSuccess) return TDQ_ERR_CUDA;
+    }
     g_launch_count.fetch_add(1, std::memory_order_relaxed);
     return TDQ_OK;
 }

@@ -131,3 +131,9 @@ def test_rope_table(tdq):
     assert np.allclose(freq.numpy(), 100.0 ** (-np.tile(np.arange(16), 2) / 16.0), rtol=1e-14)
     freq, axis = tdq.rope_table(0, device="cpu")
     assert freq.numel() == 0 and axis.numel() == 0
+
+
+def test_wait_selftest_of_the_layer(tdq):
+    f = tdq.lib().tdq_selftest_wait_timeout
+    assert f(3, 100000, None, None) == f(3, 10, FAKE, None) == f(3, 1 << 40, FAKE, None) == tdq.ERR_INVALID_ARG
+    assert f(3, 100000, OFF4, None) == tdq.ERR_ALIGNMENT

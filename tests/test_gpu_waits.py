@@ -52,3 +52,18 @@ def test_quantizer_wait_that_runs_out_is_reported_once_and_the_device_stays_usab
     ref = oracle.quantize_act(x)
     np.testing.assert_array_equal(codes.cpu().numpy(), ref["codes"])
     np.testing.assert_array_equal(scale.cpu().numpy(), ref["scale"])
+
+
+@pytest.mark.parametrize("M,O", [(5, 200), (300, 1300), (2600, 4000)])
+def test_eight_bit_layers_wait_that_runs_out_is_reported_and_the_workspace_stays_usable(M, O):
+    from paper_2604_16855_b200 import tdq
+    g = torch.Generator().manual_seed(M)
+    xc, xs = tdq.quantize_act_fp8(torch.randn((M, 640), generator=g).cuda())
+    wc, ws = tdq.quantize_weight_fp8(torch.randn((O, 640), generator=g).cuda())
+    wsp = tdq.fp8_linear_workspace("cuda")
+    before = tdq.fp8_linear(xc, xs, wc, ws, workspace=wsp)
+    assert tdq.workspace_status(wsp) == (tdq.OK, 0)
+    tdq.selftest_wait_timeout(3, 300000, wsp)
+    assert tdq.workspace_status(wsp) == (tdq.ERR_DEVICE_TIMEOUT, 13)
+    after = tdq.fp8_linear(xc, xs, wc, ws, workspace=wsp)
+    assert tdq.workspace_status(wsp) == (tdq.OK, 0) and torch.equal(before, after)
