@@ -312,6 +312,11 @@ tdq_status tdq_fp8_linear(const uint8_t* xcodes, const float* xscale, const uint
                           const float* bias, int64_t M, int64_t I_pad, int64_t O, void* y, tdq_dtype y_dtype,
                           int64_t y_row_stride, void* workspace, size_t workspace_bytes, void* cuda_stream);
 size_t tdq_fp8_linear_workspace_bytes(int64_t M, int64_t I_pad, int64_t O);
+/*
+ * How that call computes a layer on a GPU of sm_count SMs: the tokens and output channels of a tile (HOST; 16, 32, 64 or 128 x 128, or 256 x 128
+ * or 256) and in how many parts of consecutive blocks the contraction is summed (HOST; 1 to 8).  All 0 for a layer without tokens or outputs.  Asks no GPU.
+ */
+tdq_status tdq_fp8_linear_tiles(int64_t M, int64_t I_pad, int64_t O, int32_t sm_count, int32_t* tokens, int32_t* channels, int32_t* parts);
 
 /*
  * What follows a qkv layer (the paper has no counterpart): the norm of every query and key head and the rotation by the token's positions,

@@ -29,7 +29,8 @@ EXPORTS = ["tdq_default_act_params", "tdq_quantize_act", "tdq_quantize_weight", 
            "tdq_quant_linear_fused", "tdq_quant_linear_host", "tdq_quantize_act_nchw", "tdq_quantize_act_fixed", "tdq_w4a4_linear_pow2", "tdq_linear_workspace_bytes",
            "tdq_workspace_status", "tdq_status_string", "tdq_kernel_launch_count", "tdq_w4a4_linear_static",
            "tdq_quantize_status", "tdq_selftest_wait_timeout", "tdq_fold_output_affine", "tdq_measure_mma_clocks",
-           "tdq_quantize_act_fp8", "tdq_quantize_weight_fp8", "tdq_fp8_linear", "tdq_fp8_linear_workspace_bytes", "tdq_qk_norm_rope"]
+           "tdq_quantize_act_fp8", "tdq_quantize_weight_fp8", "tdq_fp8_linear", "tdq_fp8_linear_workspace_bytes",
+           "tdq_fp8_linear_tiles", "tdq_qk_norm_rope"]
 
 
 class ActParams(ctypes.Structure):
@@ -93,6 +94,8 @@ _lib.tdq_fp8_linear.argtypes = [_vp, _vp, _vp, _vp, _vp, _i64, _i64, _i64, _vp, 
 _lib.tdq_fp8_linear.restype = ctypes.c_int
 _lib.tdq_fp8_linear_workspace_bytes.argtypes = [_i64, _i64, _i64]
 _lib.tdq_fp8_linear_workspace_bytes.restype = _sz
+_lib.tdq_fp8_linear_tiles.argtypes = [_i64, _i64, _i64, _i32] + [ctypes.POINTER(_i32)] * 3
+_lib.tdq_fp8_linear_tiles.restype = ctypes.c_int
 _lib.tdq_qk_norm_rope.argtypes = [ctypes.POINTER(RopeHeads), ctypes.POINTER(RopeHeads), ctypes.c_int, _i64, ctypes.POINTER(RopeParams),
                                   _vp, _vp, _vp, _vp]
 _lib.tdq_qk_norm_rope.restype = ctypes.c_int
@@ -237,6 +240,15 @@ def fp8_linear(xcodes, xscale, wcodes, wscale, bias=None, *, out_dtype=torch.flo
     """tdq_fp8_linear on codes and scales of quantize_act_fp8 and quantize_weight_fp8 (codes float8_e4m3fn, or uint8 with the same
     bytes).  Returns y [M, O]."""
     return _host.fp8_linear(xcodes, xscale, wcodes, wscale, bias, out_dtype, y, workspace)
+
+
+def fp8_linear_tiles(M: int, I_pad: int, O: int, sm_count: int | None = None):
+    """tdq_fp8_linear_tiles: (tokens, output channels) of a tile and the parts of the contraction.  sm_count: of the current device if None."""
+    if sm_count is None:
+        sm_count = torch.cuda.get_device_properties(torch.cuda.current_device()).multi_processor_count
+    out = [_i32(0) for _ in range(3)]
+    _check(_lib.tdq_fp8_linear_tiles(M, I_pad, O, sm_count, *[ctypes.byref(v) for v in out]), "tdq_fp8_linear_tiles")
+    return tuple(v.value for v in out)
 
 
 def rope_table(rotary_dim: int, sections=None, base: float = 10000.0, *, restart: bool = False, device="cuda"):

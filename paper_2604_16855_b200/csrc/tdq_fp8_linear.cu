@@ -43,6 +43,7 @@ bool fp8_operand_map(CUtensorMap* map, const void* p, int64_t rows, int64_t cols
 
 namespace {
 
+constexpr int64_t kFp8MaxExtent = INT32_MAX - 256;   // coordinates of the copies are 32-bit
 constexpr int kSplitMaxStages = 12;
 constexpr int kSplitMax = 8;                 // CTAs of a cluster
 constexpr int kSplitSlots = 4;               // accumulators in TMEM
@@ -456,6 +457,18 @@ using namespace tdq;
 
 extern "C" size_t tdq_fp8_linear_workspace_bytes(int64_t, int64_t, int64_t) { return kWorkspaceHeader; }
 
+extern "C" tdq_status tdq_fp8_linear_tiles(int64_t M, int64_t I_pad, int64_t O, int32_t sm_count, int32_t* tokens, int32_t* channels, int32_t* parts) {
+    if (M < 0 || O < 0 || I_pad <= 0 || I_pad % kFp8Block || sm_count <= 0 || !tokens || !channels || !parts) return TDQ_ERR_INVALID_ARG;
+    if (M > kFp8MaxExtent || O > kFp8MaxExtent || I_pad > kFp8MaxExtent) return TDQ_ERR_UNSUPPORTED;
+    *tokens = *channels = *parts = 0;
+    if (M == 0 || O == 0) return TDQ_OK;
+    const Way way = choose_way(M, O, (int)(I_pad / kFp8Block), sm_count);
+    *tokens = way.nt;
+    *channels = way.nt == 256 ? way.split : 128;
+    *parts = way.nt == 256 ? 1 : way.split;
+    return TDQ_OK;
+}
+
 extern "C" tdq_status tdq_fp8_linear(const uint8_t* xcodes, const float* xscale, const uint8_t* wcodes, const float* wscale, const float* bias,
                                      int64_t M, int64_t I_pad, int64_t O, void* y, tdq_dtype y_dtype, int64_t y_row_stride, void* workspace,
                                      size_t workspace_bytes, void* cuda_stream) {
@@ -467,8 +480,7 @@ extern "C" tdq_status tdq_fp8_linear(const uint8_t* xcodes, const float* xscale,
     const uintptr_t esz = y_dtype == TDQ_F32 ? 4 : 2;
     const auto off = [](const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; };
     if (off(xcodes, 16) || off(wcodes, 16) || off(workspace, 16) || off(xscale, 4) || off(wscale, 4) || off(bias, 4) || off(y, esz)) return TDQ_ERR_ALIGNMENT;
-    // coordinates of the copies are 32-bit
-    if (M > INT32_MAX - 256 || O > INT32_MAX - 256 || I_pad > INT32_MAX - 256) return TDQ_ERR_UNSUPPORTED;
+    if (M > kFp8MaxExtent || O > kFp8MaxExtent || I_pad > kFp8MaxExtent) return TDQ_ERR_UNSUPPORTED;
     int dev = 0;
     const int n_sm = current_device_sm_count(&dev);
     if (n_sm <= 0) return TDQ_ERR_CUDA;

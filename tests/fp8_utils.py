@@ -7,6 +7,50 @@ DT = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}
 HALF_STEP = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
 
 
+# Layers (M, I, O) for each way that the layer is computed in on 148 SMs: (tile's tokens, tile's output channels, parts of the contraction).  Ragged in every
+# direction; a block a part or less than two, a few that do not divide, more than the ring and the factors' places hold; for pairs of CTAs 1, 2, 5, 6, 9 and 33
+# blocks in one round of tiles, two and three.  128 tokens in one part is never chosen.
+WAYS = {
+    (16, 128, 1): [(9, 2175, 17908), (23, 639, 8035), (12, 91, 937)],
+    (16, 128, 2): [(12, 4223, 8598), (35, 796, 2214), (8, 219, 347)],
+    (16, 128, 3): [(5, 6875, 4906), (9, 897, 4919), (2, 284, 74)],
+    (16, 128, 4): [(46, 8575, 1289), (14, 6016, 4106), (23, 385, 203)],
+    (16, 128, 5): [(51, 13953, 775), (206, 2139, 164), (22, 540, 55)],
+    (16, 128, 6): [(356, 15132, 119), (44, 8988, 1020), (23, 731, 315)],
+    (16, 128, 7): [(54, 17152, 529), (150, 4124, 101), (7, 796, 654)],
+    (16, 128, 8): [(21, 17023, 67), (30, 8193, 75), (53, 987, 203)],
+    (32, 128, 1): [(23, 2431, 12559), (22, 511, 19916), (26, 1, 35559)],
+    (32, 128, 2): [(17, 4224, 8310), (27, 2907, 7201)],
+    (32, 128, 3): [(19, 6273, 4828), (27, 895, 10621), (17, 284, 10220)],
+    (32, 128, 4): [(19, 8348, 4418), (19, 4097, 4606)],
+    (32, 128, 5): [(28, 10396, 3159), (846, 2176, 51)],
+    (32, 128, 6): [(29, 13825, 2782), (346, 4380, 156)],
+    (32, 128, 7): [(157, 15489, 460), (27, 2560, 2625)],
+    (32, 128, 8): [(53, 16987, 1142), (506, 8575, 34)],
+    (64, 128, 1): [(39, 2305, 15582), (46, 896, 15234), (34, 128, 39489)],
+    (64, 128, 2): [(58, 4353, 7643), (147, 1883, 2577)],
+    (64, 128, 3): [(46, 6529, 5010), (860, 1663, 257), (2593, 384, 118)],
+    (64, 128, 4): [(54, 10241, 3740), (58, 4864, 4730)],
+    (64, 128, 5): [(35, 11995, 3220), (1844, 2139, 68), (600, 513, 525)],
+    (64, 128, 6): [(51, 12801, 2730), (744, 5532, 135)],
+    (64, 128, 7): [(151, 17792, 855), (44, 5248, 2255)],
+    (64, 128, 8): [(828, 17792, 74), (250, 4992, 410)],
+    (128, 128, 2): [(441, 8923, 1766), (1592, 2561, 460)],
+    (128, 128, 3): [(132, 13403, 2108), (4945, 1564, 119)],
+    (128, 128, 4): [(155, 16768, 1939), (3409, 3291, 87)],
+    (128, 128, 5): [(634, 15873, 612), (242, 2432, 1204)],
+    (128, 128, 6): [(492, 13439, 446), (1268, 3841, 165)],
+    (128, 128, 7): [(88, 3100, 1902)],
+    (128, 128, 8): [(231, 16603, 726), (68, 10369, 1429)],
+    (256, 128, 1): [(1354, 127, 898), (3658, 1, 1085), (2534, 1, 2235), (2594, 156, 140), (3313, 255, 1383), (1478, 156, 4055),
+                    (2543, 4124, 630), (3139, 4187, 1329), (6349, 540, 41), (1750, 513, 2580), (5641, 540, 1095), (4626, 668, 155),
+                    (865, 768, 4694), (6160, 668, 983), (1176, 1151, 919), (3659, 1052, 1025), (749, 1025, 8099)],
+    (256, 256, 1): [(1688, 91, 2164), (3952, 128, 1779), (1612, 91, 7339), (1069, 156, 3217), (1296, 219, 5228), (606, 156, 13082),
+                    (1285, 4187, 2865), (4404, 4224, 1510), (615, 513, 5015), (2082, 639, 3932), (704, 603, 16014), (1718, 731, 1850),
+                    (3595, 731, 2178), (1647, 641, 5829), (4043, 1025, 674), (5783, 1025, 1369), (866, 1151, 13519)],
+}
+
+
 def blocks(n):
     return (n + BLOCK - 1) // BLOCK
 

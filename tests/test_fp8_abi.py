@@ -137,3 +137,30 @@ def test_wait_selftest_of_the_layer(tdq):
     f = tdq.lib().tdq_selftest_wait_timeout
     assert f(3, 100000, None, None) == f(3, 10, FAKE, None) == f(3, 1 << 40, FAKE, None) == tdq.ERR_INVALID_ARG
     assert f(3, 100000, OFF4, None) == tdq.ERR_ALIGNMENT
+
+
+def test_the_ways_a_layer_is_computed(tdq):
+    """Every way that the estimate can choose has shapes that the GPU tests run it with."""
+    for way, shapes in fu.WAYS.items():
+        for M, I, O in shapes:
+            assert tdq.fp8_linear_tiles(M, fu.blocks(I) * 128, O, 148) == way, (M, I, O)
+    rng = np.random.default_rng(0)
+    seen = {tdq.fp8_linear_tiles(*[int(v) for v in (m, 128 * k, o)], 148)
+            for m, k, o in zip(np.exp(rng.uniform(0, 12, 40000)), np.exp(rng.uniform(0, 5, 40000)).astype(int), np.exp(rng.uniform(0, 11.5, 40000)))}
+    assert seen <= set(fu.WAYS), seen - set(fu.WAYS)
+    assert {(16, 128, s) for s in range(1, 9)} <= set(fu.WAYS) and {(n, 128, s) for n in (32, 64, 128) for s in range(2, 9)} <= set(fu.WAYS)
+    assert tdq.fp8_linear_tiles(0, 128, 5, 148) == tdq.fp8_linear_tiles(5, 128, 0, 148) == (0, 0, 0)
+    f, out = tdq.lib().tdq_fp8_linear_tiles, [ctypes.byref(ctypes.c_int32(0)) for _ in range(3)]
+    inv, uns = tdq.ERR_INVALID_ARG, tdq.ERR_UNSUPPORTED
+    _each(f, [4, 256, 8, 148] + out, [(0, -1, inv), (1, 0, inv), (1, 100, inv), (2, -1, inv), (3, 0, inv), (4, None, inv), (5, None, inv), (6, None, inv),
+                                      (0, 1 << 31, uns), (1, 1 << 31, uns), (2, 1 << 31, uns), (0, 4, tdq.OK)])
+
+
+@pytest.mark.parametrize("sm_count", [1, 7, 66, 132, 148, 160])
+def test_a_way_exists_on_any_number_of_sms(tdq, sm_count):
+    rng = np.random.default_rng(sm_count)
+    for _ in range(3000):
+        M, K, O = (int(np.exp(rng.uniform(0, top))) for top in (13, 5, 12))
+        tokens, channels, parts = tdq.fp8_linear_tiles(M, 128 * K, O, sm_count)
+        assert (tokens, channels) in {(16, 128), (32, 128), (64, 128), (128, 128), (256, 128), (256, 256)}
+        assert 1 <= parts <= min(8, K) and (tokens < 256 or parts == 1)

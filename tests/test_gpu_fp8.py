@@ -438,3 +438,56 @@ def test_first_use_inside_a_capture(M, O):
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", FIRST_IN_A_CAPTURE % dict(M=M, O=O)], cwd=root, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("way,n", [(way, n) for way, shapes in fu.WAYS.items() for n in range(len(shapes))])
+def test_every_way_of_the_layer(tdq, way, n):
+    """Each kind of tile with each number of parts, and the shapes are computed that way (tdq_fp8_linear_tiles; the lists above were drawn for earlier choices)."""
+    M, I, O = fu.WAYS[way][n]
+    assert torch.cuda.get_device_properties(0).multi_processor_count != 148 or tdq.fp8_linear_tiles(M, fu.blocks(I) * 128, O) == way
+    _run(tdq, M, I, O, "fp32", n % 2 == 0, n % 3)
+    _run(tdq, M, I, O, "bf16", n % 2 == 1, (-O) % 8)
+    _run(tdq, M, I, O, "fp16", True, (-O) % 8 + 8, 8 * (n % 2))
+
+
+TILES = """
+import sys, json
+import torch
+from torch.profiler import ProfilerActivity, profile
+from paper_2604_16855_b200 import tdq
+shapes = %s
+calls = []
+for M, I, O in shapes:
+    K = (I + 127) // 128
+    calls.append((torch.zeros((M, K * 128), dtype=torch.uint8, device="cuda"), torch.ones((M, K), device="cuda"), torch.zeros((O, K * 128), dtype=torch.uint8, device="cuda"),
+                  torch.ones(((O + 127) // 128, K), device="cuda")))
+torch.cuda.synchronize()
+with profile(activities=[ProfilerActivity.CUDA]) as p:
+    for c in calls:
+        tdq.fp8_linear(*c)
+    torch.cuda.synchronize()
+p.export_chrome_trace(sys.argv[1])
+"""
+
+
+def test_the_query_says_what_runs(tdq, tmp_path):
+    """Kernel and grid of one layer for each way, from the profiler's record."""
+    import json
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    shapes = [v[0] for v in fu.WAYS.values()]
+    r = subprocess.run([sys.executable, "-c", TILES % shapes, str(tmp_path / "trace")], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
+    events = [e for e in json.load(open(tmp_path / "trace"))["traceEvents"] if e.get("cat") == "kernel" and "fp8_" in e["name"]]
+    events.sort(key=lambda e: e["ts"])
+    assert len(events) == len(shapes)
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    for (M, I, O), e in zip(shapes, events):
+        tokens, channels, parts = tdq.fp8_linear_tiles(M, fu.blocks(I) * 128, O)
+        tiles = -(-M // tokens) * -(-O // channels)
+        if tokens == 256:
+            assert "fp8_pair_kernel<0, %d>" % channels in e["name"] and e["args"]["grid"][0] == 2 * min(tiles, sms // 2), e
+        else:
+            assert "fp8_split_kernel<%d>" % tokens in e["name"] and e["args"]["grid"][0] == tiles * parts, e
