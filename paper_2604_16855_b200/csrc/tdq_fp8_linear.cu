@@ -353,11 +353,14 @@ fp8_split_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, cons
 }
 
 // Which kernel, and in how many parts: the least of these estimates in units of 10 ns, fitted to 156 layers (1 to 9000 tokens, 384 to 7040 ->
-// 48 to 8192 channels, every kernel and number of parts, from a graph; the choice costs 1.9 % more than the best one in the mean, 25 % at worst).
+// 48 to 8192 channels, every kernel and number of parts, from a graph; over those the choice costs 1.9 % more than the best one in the mean, 25 % at worst).
 //   NT tokens, s parts:  start x rounds + block x (blocks of a part) x (CTAs an SM runs) + meet x s (s > 1);  a round is as many clusters of s
 //                        CTAs as the GPU holds, two CTAs per SM, one of NT = 128
 //   pairs of CTAs:       start + block x K x rounds + end x (rounds - 1);  a round is a tile of 256 tokens and 256 or 128 channels for every
 //                        pair of SMs
+// Above 64 tokens, from as many 256 x 256 tiles as SMs on (two rounds) those are taken without an estimate, which charges a further round of them too
+// much.  Measured with 256 x 128 instead: 148 tiles of 6 and 32 blocks 11.9 -> 13.2 and 36.5 -> 46 us, 152 of 16 and 32 25.4 -> 25.8 and 43.5 -> 45.5, 240
+// to 640 of 6 5 to 12 % slower; faster only just above two rounds of a short contraction (2000 x 768 -> 4712 13.8 -> 13.3, 2048 x 768 -> 5120 fp32 21.3 -> 19.4).
 // A cluster lies in one group of SMs, so fewer of them fit than SMs / s: with rounds counted in CTAs 2259 x 5113 -> 45 waited for two of
 // eighteen clusters of eight (14.2 us; now 8.9).  Against 128 tokens a tile throughout: 576 x 384 -> 960 6.9 -> 4.7 us, 256 x 1024 -> 1024 6.9 -> 5.4.
 struct Way { int nt, split; };                             // nt == 256: pairs, split the tile's columns

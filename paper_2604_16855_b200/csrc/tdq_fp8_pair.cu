@@ -41,9 +41,10 @@ constexpr int kPairThreads = (kAddWarp0 + kAddWarps) * 32;
 constexpr uint32_t kStrip = 32 * 128;                    // 32 rows of 128 bytes
 constexpr uint32_t kBiasBytes = 128 * 4;                 // of a warp's 128 columns
 constexpr int kStrips = 2;                               // of a warp: 128 columns of 16 bits, so that no store is waited for in a tile
-// Scales of a block: 128 token rows', then two weight blocks'.  No barrier hands them back: with eight of them and four stages block n + 8's are
-// copied once the instructions of block n + 4 have completed, which were issued after all of n + 2's sums had been taken; with sixteen and six, n + 16's after
-// n + 10's, issued after n + 6's.
+// Scales of a block: 128 token rows', then two weight blocks'.  No barrier hands their places back.  Block n's are copied once its stage is free: the
+// instructions of block n - stages have completed, and those were issued after the sums that their accumulator held before had been taken, at most
+// kReuse blocks further back (256: two, or one or three where a tile of an odd number of blocks ends in between; 128: four).  Sums are taken in order, so
+// the scales of all blocks up to n - stages - kReuse have been read: as many places as stages + kReuse are enough.
 constexpr uint32_t kScaleBytes = 128 * 4 + 16;
 constexpr uint32_t kPairIdesc = (1u << 4) | ((128u >> 3) << 17) | ((256u >> 4) << 24);
 constexpr int kRegsLoad = 40, kRegsAdd = 232;            // 128 * 40 + 256 * 232 <= 384 * 168
@@ -51,6 +52,8 @@ constexpr int kRegsLoad = 40, kRegsAdd = 232;            // 128 * 40 + 256 * 232
 template <int TN> struct PairShape {                     // TN: the tile's columns
     static constexpr int kStages = TN == 256 ? 4 : 6;    // 256: five leave no room for the second strip and gain nothing
     static constexpr int kScaleSlots = TN == 256 ? 8 : 16;
+    static constexpr int kReuse = TN == 256 ? 3 : 4;
+    static_assert(kScaleSlots >= kStages + kReuse, "a block's scales would be overwritten before they are read");
     static constexpr uint32_t kWeights = TN / 2 * 128;
     static constexpr uint32_t kStage = kPairOperand + kWeights;
     static constexpr uint32_t kSmem = kPairCtrl + kStages * kStage + kAddWarps * (kStrips * kStrip + kBiasBytes) + kScaleSlots * kScaleBytes;
