@@ -262,7 +262,7 @@ def rope_table(rotary_dim: int, sections=None, base: float = 10000.0, *, restart
     if rotary_dim < 0 or rotary_dim % 2 or sum(sections) != half or min(sections, default=0) < 0 or not base > 0:
         raise ValueError("rotary_dim must be even, base positive, and sections non-negative with sum rotary_dim / 2")
     axis = torch.tensor([i for i, n in enumerate(sections) for _ in range(n)], dtype=torch.int32)
-    exponent = torch.cat([torch.arange(n, dtype=torch.float64) / max(n, 1) for n in (sections if restart else [half])])
+    exponent = torch.tensor([j / n for n in (sections if restart else [half]) for j in range(n)], dtype=torch.float64)
     return (float(base) ** -exponent).to(device), axis.to(device)
 
 

@@ -164,3 +164,10 @@ def test_a_way_exists_on_any_number_of_sms(tdq, sm_count):
         tokens, channels, parts = tdq.fp8_linear_tiles(M, 128 * K, O, sm_count)
         assert (tokens, channels) in {(16, 128), (32, 128), (64, 128), (128, 128), (256, 128), (256, 256)}
         assert 1 <= parts <= min(8, K) and (tokens < 256 or parts == 1)
+
+
+def test_rope_table_without_pairs(tdq):
+    for sections in (None, [], [0], [0, 0]):
+        for restart in (False, True):
+            freq, axis = tdq.rope_table(0, sections, restart=restart, device="cpu")
+            assert freq.dtype == torch.float64 and axis.dtype == torch.int32 and freq.shape == axis.shape == (0,)
