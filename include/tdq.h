@@ -326,7 +326,7 @@ tdq_status tdq_fp8_linear_tiles(int64_t M, int64_t I_pad, int64_t O, int32_t sm_
  *   (n_a, n_b) -> (n_a cos t - n_b sin t, n_b cos t + n_a sin t);   channels from R on are n.
  *   The fraction of a turn in freq / 2 pi is rounded to a multiple of 2^-64 and its product with the position is exact up to whole turns: the
  *   angle is off by position x 2^-65 of a turn, so that positions of 2^40 still turn by the right one to binary32's precision (frequencies up to
- *   2^44).  Everything else is binary32, rounded once when stored.  The squares are not
+ *   2^40).  Everything else is binary32, rounded once when stored.  The squares are not
  *   scaled before they are added: a head whose sum passes binary32's range becomes zero.
  *   q, k       either may be NULL or have no heads.  Element (m, h, i) of x is x[m row_stride + h head_stride + i], of out
  *              likewise; heads and rows of out must not overlap each other.  out == x (with the same strides) works in place;
@@ -338,7 +338,7 @@ tdq_status tdq_fp8_linear_tiles(int64_t M, int64_t I_pad, int64_t O, int32_t sm_
  *   Pointers and strides on the 16-byte grid with D a multiple of 16 (float32: 8), R/2 of 8 (4) and D <= 512 (256) take the
  *   vector kernel, 16-bit heads on the 8-byte grid with D a multiple of 8, R/2 of 4 and D <= 256 its form for half vectors, anything else a
  *   slower general one; weights for the first two on the 16-byte grid.  M == 0 is a no-op.  TDQ_ERR_UNSUPPORTED for head_dim or heads above 65536
- *   and M above 2^31 - 1.
+ *   and M above 2^31 - 1, and in the general kernel for M x heads of both sides above 2^34 - 8.
  */
 #define TDQ_ROPE_NORM 1u
 #define TDQ_ROPE_ADJACENT 2u

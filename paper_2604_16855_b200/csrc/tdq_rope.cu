@@ -112,15 +112,17 @@ __device__ __forceinline__ typename Bytes<VB>::T lds_vec(uint32_t addr) {
 }
 // The turns a pair makes per position: the fraction of freq / 2 pi to the nearest 2^-64 (whole turns of it stay whole turns at every position).
 // 1 / 2 pi is taken as the sum of two binary64 numbers, right to 2^-109, and the first product with its rounding error, so nothing above that is lost
-// for frequencies up to 2^44.
+// for frequencies up to 2^40.  Added to 1.5 x 2^20, a number's multiple of 2^-32 stands in the low half of the sum's bits (modulo a turn), and what
+// that leaves is counted in units of 2^-64 the same way: with conversions to integers the general kernel takes 283 us for 277 (18432 x 32 x 72
+// bf16; 266 with the binary64 quotient alone).
 struct Speed { int64_t step; float bad; };                 // bad: NaN where freq is not finite, else 0
 __device__ __forceinline__ Speed speed_of(double freq) {
-    constexpr double kInv2Pi = 0x1.45f306dc9c883p-3, kInv2PiLow = -0x1.6b01ec5417056p-57, kUnits = 0x1p64;
-    const double turns = __dmul_rn(freq, kInv2Pi), low = fma(freq, kInv2PiLow, fma(freq, kInv2Pi, -turns));
-    const double f = turns - rint(turns), g = low - rint(low);   // [-1/2, 1/2]
-    const double units = rint(f * kUnits), rest = f * kUnits - units;   // the products and the difference are exact
-    const uint64_t high = units < 0x1p63 ? (uint64_t)__double2ll_rn(units) : 1ull << 63;
-    return {(int64_t)(high + (uint64_t)__double2ll_rn(fma(g, kUnits, rest))), (float)(f - f)};
+    constexpr double kInv2Pi = 0x1.45f306dc9c883p-3, kInv2PiLow = -0x1.6b01ec5417056p-57, kHigh = 0x1.8p20, kLow = 0x1.8p-12;
+    const double turns = __dmul_rn(freq, kInv2Pi), g = fma(freq, kInv2PiLow, fma(freq, kInv2Pi, -turns));
+    const double f = turns - rint(turns);                  // the fraction is f + g
+    const double high = f + g + kHigh, low = f - (high - kHigh) + g + kLow;
+    const uint64_t step = ((uint64_t)__double_as_longlong(high) << 32) + (uint64_t)(__double_as_longlong(low) - __double_as_longlong(kLow));
+    return {(int64_t)step, (float)(f - f)};
 }
 // cosine and sine at a position; the product's 64 low bits are its fraction of a turn, of which 32 are rounded to binary32
 __device__ __forceinline__ float2 turn_at(const Speed& v, int64_t pos) {
@@ -384,7 +386,7 @@ tdq_status launch(RopeArgs a, cudaStream_t st) {
     if (n_sm <= 0) return TDQ_ERR_CUDA;
     cudaError_t e = cudaErrorInvalidValue;
     // Heads of 72 or 80 channels whose halves are no whole vectors of 16 bytes, and rows on the 8-byte grid: vectors of 8 bytes (18432 x 32 x 72 bf16
-    // 265 us with the general kernel, 61 so).
+    // 277 us with the general kernel, 61 so).
     if (rope_fits<DT, 16>(a)) {
         e = launch_vec<DT, 16>(a, n_sm, dev, st);
     } else if (DT != TDQ_F32 && rope_fits<DT, 8>(a)) {
