@@ -352,8 +352,9 @@ fp8_split_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, cons
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "n"(kSplitSlots * NT) : "memory");
 }
 
-// Which kernel, and in how many parts: the least of these estimates in units of 10 ns, fitted to 156 layers (1 to 9000 tokens, 384 to 7040 ->
-// 48 to 8192 channels, every kernel and number of parts, from a graph; over those the choice costs 1.9 % more than the best one in the mean, 25 % at worst).
+// Which kernel, and in how many parts: the least of these estimates in units of 10 ns, fitted to layers of 1 to 9000 tokens, 384 to 7040
+// -> 48 to 8192 channels with every kernel and number of parts, from a graph.  On 70 others the choice costs 1.7 % more than the best one in the mean, 23 % at
+// worst (591 x 6317 -> 54 bf16 7.95 us for 6.47).
 //   NT tokens, s parts:  start x rounds + block x (blocks of a part) x (CTAs an SM runs) + meet x s (s > 1);  a round is as many clusters of s
 //                        CTAs as the GPU holds, two CTAs per SM, one of NT = 128
 //   pairs of CTAs:       start + block x K x rounds + end x (rounds - 1);  a round is a tile of 256 tokens and 256 or 128 channels for every

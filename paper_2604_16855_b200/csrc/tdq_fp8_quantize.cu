@@ -10,7 +10,8 @@
 //
 // Bound by HBM: 2 (4) bytes in and 1 out an element, the input read once.  A block of a token is eight threads of sixteen
 // channels each (16-byte loads, a 16-byte store, three shuffles for the maximum); rows off the 16-byte grid pass through
-// shared memory word by word.  A weight block stays in the registers of 512 threads between its maximum and its codes.
+// shared memory word by word.  A weight block stays in the registers of 512 threads between its maximum and its codes (of fp32 vectors, 32 words a thread
+// beside 40 registers, some go to local memory and back: 76 bytes a thread, which the first-level cache holds).
 #include "tdq_fp8.cuh"
 
 namespace tdq {
