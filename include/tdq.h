@@ -280,7 +280,7 @@ tdq_status tdq_w4a4_linear_static(const uint8_t* xcodes, const float* xscale, co
  *           are read with vector loads, anything else in words that hold an element of the row; the results are the same.
  *   codes   [B*N, C_pad] bytes, C_pad = 128 ceil(C/128), 16-byte aligned; the codes behind C are 0 (NaN in a NaN block).
  *   scale   [B*N, C_pad/128] float32.
- * B*N == 0 is a no-op.  TDQ_ERR_UNSUPPORTED for 2^36 elements or more.
+ * B*N == 0 is a no-op.  TDQ_ERR_UNSUPPORTED for more than 2^36 - 2^17 codes.
  */
 tdq_status tdq_quantize_act_fp8(const void* x, tdq_dtype x_dtype, int64_t B, int64_t N, int64_t C,
                                 int64_t row_stride_elems, uint8_t* codes, float* scale, void* cuda_stream);
@@ -290,6 +290,7 @@ tdq_status tdq_quantize_act_fp8(const void* x, tdq_dtype x_dtype, int64_t B, int
  *   w       [O, I] row-major, contiguous, float32, bf16 or fp16.
  *   wcodes  [O, I_pad] bytes, I_pad = 128 ceil(I/128), 16-byte aligned, codes behind I as above.
  *   wscale  [ceil(O/128), I_pad/128] float32.
+ * O == 0 is a no-op.  TDQ_ERR_UNSUPPORTED for O above 65535 x 128 and I above 2^31 - 1.
  */
 tdq_status tdq_quantize_weight_fp8(const void* w, tdq_dtype w_dtype, int64_t O, int64_t I, uint8_t* wcodes,
                                    float* wscale, void* cuda_stream);
@@ -306,7 +307,8 @@ tdq_status tdq_quantize_weight_fp8(const void* w, tdq_dtype w_dtype, int64_t O, 
  *          apart (>= O).  Rows on the 16-byte grid are stored by the copy engine, others element by element.
  *   workspace  at least tdq_fp8_linear_workspace_bytes(), 16-byte aligned: the status word that tdq_workspace_status() reads.  The call
  *              clears it; one workspace must not be shared by calls that overlap in time.
- * Alignment: xcodes, wcodes 16 bytes.
+ * Alignment: xcodes, wcodes 16 bytes.  M == 0 or O == 0 is a no-op that leaves the workspace as it is.  TDQ_ERR_UNSUPPORTED for M, I_pad or O above
+ * 2^31 - 257, and for more tiles than a grid holds.
  */
 tdq_status tdq_fp8_linear(const uint8_t* xcodes, const float* xscale, const uint8_t* wcodes, const float* wscale,
                           const float* bias, int64_t M, int64_t I_pad, int64_t O, void* y, tdq_dtype y_dtype,
