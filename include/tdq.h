@@ -286,6 +286,14 @@ tdq_status tdq_quantize_act_fp8(const void* x, tdq_dtype x_dtype, int64_t B, int
                                 int64_t row_stride_elems, uint8_t* codes, float* scale, void* cuda_stream);
 
 /*
+ * The same quantizer with scales that are powers of two, for activations kept for the backward pass: scale = the smallest 2^s (s integer) with
+ * a <= 448 2^s, r = 1 / scale.  code x scale is then exact in bf16, as tdq_fp8_weight_grad takes it.  Everything else as above; tdq_fp8_linear takes
+ * these codes and scales like any others.
+ */
+tdq_status tdq_quantize_act_fp8_pow2(const void* x, tdq_dtype x_dtype, int64_t B, int64_t N, int64_t C, int64_t row_stride_elems, uint8_t* codes,
+                                     float* scale, void* cuda_stream);
+
+/*
  * Quantizer of weights: the same formula over blocks of 128 output channels x 128 input channels.
  *   w       [O, I] row-major, contiguous, float32, bf16 or fp16.
  *   wcodes  [O, I_pad] bytes, I_pad = 128 ceil(I/128), 16-byte aligned, codes behind I as above.
@@ -358,6 +366,36 @@ typedef struct {
 tdq_status tdq_qk_norm_rope(const tdq_rope_heads* q /* HOST */, const tdq_rope_heads* k /* HOST */, tdq_dtype dtype,
                             int64_t M, const tdq_rope_params* p /* HOST */, const int64_t* positions,
                             const double* freq, const int32_t* axis, void* cuda_stream);
+
+/*
+ * Layer norm (the paper has no counterpart), in the input's type or straight to the codes of the 8-bit layer.  For row m of C channels:
+ *   mean = 1/C sum x;   rstd = 1 / sqrt(1/C sum (x - mean)^2 + eps);   y = (x - mean) rstd w + b     (binary32; w == 1, b == 0 where NULL)
+ *   x       [M, C] float32, bf16 or fp16 (dtype), rows x_row_stride elements apart (>= C).
+ *   y       [M, C] of dtype, rows y_row_stride apart, rounded once; it may be x itself with x's stride.  Or NULL, and then
+ *   codes   [M, C_pad] E4M3, 16-byte aligned, and scale [M, C_pad/128]: what tdq_quantize_act_fp8 gives for the binary32 y (with TDQ_NORM_POW2
+ *           tdq_quantize_act_fp8_pow2).  NULL where y is given.
+ *   mean, rstd   NULL or [M] float32, for the backward pass.   weight, bias   NULL or [C] float32.
+ * C up to 16384.  Rows and weights on the 16-byte grid with C a multiple of 8 (float32: 4) are read and written in place, others pass through
+ * shared memory; the results are the same.  M == 0 is a no-op.
+ */
+#define TDQ_NORM_POW2 1u
+tdq_status tdq_layer_norm(const void* x, tdq_dtype dtype, int64_t M, int64_t C, int64_t x_row_stride, const float* weight, const float* bias, float eps,
+                          uint32_t flags, void* y, int64_t y_row_stride, uint8_t* codes, float* scale, float* mean, float* rstd, void* cuda_stream);
+
+/*
+ * Its gradients, with g = dy w and h = (x - mean) rstd:
+ *   dx = rstd (g - 1/C sum_c g - h 1/C sum_c g h) + add;    dweight = sum_m dy h;    dbias = sum_m dy     (binary32, dx rounded once)
+ *   dy, x, dx, add   [M, C] of dtype, each with a row stride of its own; add (the gradient that reaches x past the norm) may be NULL.  dx may be dy, x or add
+ *                    itself with the same stride, and else overlaps none of them.
+ *   mean, rstd       [M] float32, as tdq_layer_norm gives them.   weight NULL or [C] float32.
+ *   dweight, dbias   NULL or [C] float32, overwritten (zeros where M == 0).
+ *   workspace        at least tdq_layer_norm_backward_workspace_bytes(), 16-byte aligned, of the current device's size; not shared by calls that overlap in time.
+ * The same call gives the same bits.  C up to 16384.
+ */
+tdq_status tdq_layer_norm_backward(const void* dy, int64_t dy_row_stride, const void* x, int64_t x_row_stride, tdq_dtype dtype, int64_t M, int64_t C,
+                                   const float* mean, const float* rstd, const float* weight, const void* add, int64_t add_row_stride, void* dx,
+                                   int64_t dx_row_stride, float* dweight, float* dbias, void* workspace, size_t workspace_bytes, void* cuda_stream);
+size_t tdq_layer_norm_backward_workspace_bytes(int64_t M, int64_t C);
 
 /* Bytes of workspace tdq_w4a4_linear / tdq_quant_linear_fused need for this problem. */
 size_t tdq_linear_workspace_bytes(int64_t M, int64_t I_pad, int64_t O, int32_t group_size);

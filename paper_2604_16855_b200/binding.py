@@ -30,7 +30,8 @@ EXPORTS = ["tdq_default_act_params", "tdq_quantize_act", "tdq_quantize_weight", 
            "tdq_workspace_status", "tdq_status_string", "tdq_kernel_launch_count", "tdq_w4a4_linear_static",
            "tdq_quantize_status", "tdq_selftest_wait_timeout", "tdq_fold_output_affine", "tdq_measure_mma_clocks",
            "tdq_quantize_act_fp8", "tdq_quantize_weight_fp8", "tdq_fp8_linear", "tdq_fp8_linear_workspace_bytes",
-           "tdq_fp8_linear_tiles", "tdq_qk_norm_rope"]
+           "tdq_fp8_linear_tiles", "tdq_qk_norm_rope", "tdq_quantize_act_fp8_pow2", "tdq_layer_norm", "tdq_layer_norm_backward",
+           "tdq_layer_norm_backward_workspace_bytes"]
 
 
 class ActParams(ctypes.Structure):
@@ -88,6 +89,8 @@ _lib.tdq_measure_mma_clocks.argtypes = [_i32, _i32, _vp, _sz, ctypes.POINTER(cty
 _lib.tdq_measure_mma_clocks.restype = ctypes.c_int
 _lib.tdq_quantize_act_fp8.argtypes = [_vp, ctypes.c_int, _i64, _i64, _i64, _i64, _vp, _vp, _vp]
 _lib.tdq_quantize_act_fp8.restype = ctypes.c_int
+_lib.tdq_quantize_act_fp8_pow2.argtypes = _lib.tdq_quantize_act_fp8.argtypes
+_lib.tdq_quantize_act_fp8_pow2.restype = ctypes.c_int
 _lib.tdq_quantize_weight_fp8.argtypes = [_vp, ctypes.c_int, _i64, _i64, _vp, _vp, _vp]
 _lib.tdq_quantize_weight_fp8.restype = ctypes.c_int
 _lib.tdq_fp8_linear.argtypes = [_vp, _vp, _vp, _vp, _vp, _i64, _i64, _i64, _vp, ctypes.c_int, _i64, _vp, _sz, _vp]
@@ -99,6 +102,12 @@ _lib.tdq_fp8_linear_tiles.restype = ctypes.c_int
 _lib.tdq_qk_norm_rope.argtypes = [ctypes.POINTER(RopeHeads), ctypes.POINTER(RopeHeads), ctypes.c_int, _i64, ctypes.POINTER(RopeParams),
                                   _vp, _vp, _vp, _vp]
 _lib.tdq_qk_norm_rope.restype = ctypes.c_int
+_lib.tdq_layer_norm.argtypes = [_vp, ctypes.c_int, _i64, _i64, _i64, _vp, _vp, ctypes.c_float, ctypes.c_uint32, _vp, _i64, _vp, _vp, _vp, _vp, _vp]
+_lib.tdq_layer_norm.restype = ctypes.c_int
+_lib.tdq_layer_norm_backward.argtypes = [_vp, _i64, _vp, _i64, ctypes.c_int, _i64, _i64, _vp, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _sz, _vp]
+_lib.tdq_layer_norm_backward.restype = ctypes.c_int
+_lib.tdq_layer_norm_backward_workspace_bytes.argtypes = [_i64, _i64]
+_lib.tdq_layer_norm_backward_workspace_bytes.restype = _sz
 _lib.tdq_status_string.argtypes = [ctypes.c_int]
 _lib.tdq_status_string.restype = ctypes.c_char_p
 _lib.tdq_kernel_launch_count.argtypes = []
@@ -217,11 +226,12 @@ def quant_linear_host(x_host: torch.Tensor, wcodes, wscale, bias=None, params: A
     return _host.quant_linear_host(x_host, wcodes, wscale, bias, params, out_dtype, y_host)
 
 
-def quantize_act_fp8(x: torch.Tensor, *, codes=None, scale=None):
+def quantize_act_fp8(x: torch.Tensor, *, pow2=False, codes=None, scale=None):
     """tdq_quantize_act_fp8 on x [..., C] (last dim contiguous, rows equally spaced; float32, bfloat16 or float16).
 
+    pow2=True: tdq_quantize_act_fp8_pow2, scales that are powers of two, for activations kept for the backward pass.
     Returns (codes float8_e4m3fn [M, C_pad], scale float32 [M, C_pad/128]), C_pad = C rounded up to 128."""
-    return _host.quantize_act_fp8(x, codes, scale)
+    return _host.quantize_act_fp8(x, codes, scale, pow2)
 
 
 def quantize_weight_fp8(w: torch.Tensor, *, wcodes=None, wscale=None):
@@ -274,6 +284,27 @@ def qk_norm_rope(q, k, positions, table, q_weight=None, k_weight=None, *, eps=1e
     q_out, k_out: pass q and k themselves to work in place; new tensors if None.  Returns (q_out, k_out)."""
     freq, axis = table
     return _host.qk_norm_rope(q, k, positions, freq, axis, q_weight, k_weight, eps, adjacent, q_out, k_out)
+
+
+def layer_norm(x, weight=None, bias=None, *, eps=1e-5, y=None, mean=None, rstd=None):
+    """tdq_layer_norm on x [..., C] (last dim contiguous, rows equally spaced).  Returns (y like x, mean float32 [M], rstd float32 [M]).
+
+    y=x works in place."""
+    return _host.layer_norm(x, weight, bias, eps, y, mean, rstd)
+
+
+def layer_norm_fp8(x, weight=None, bias=None, *, eps=1e-5, pow2=False, codes=None, scale=None, mean=None, rstd=None):
+    """tdq_layer_norm straight to the codes and scales that fp8_linear takes (pow2: and fp8_weight_grad keeps).
+
+    Returns (codes float8_e4m3fn [M, C_pad], scale float32 [M, C_pad/128], mean, rstd)."""
+    return _host.layer_norm_fp8(x, weight, bias, eps, pow2, codes, scale, mean, rstd)
+
+
+def layer_norm_backward(dy, x, mean, rstd, weight=None, *, add=None, dx=None, dweight=None, dbias=None, workspace=None):
+    """tdq_layer_norm_backward: dy, x and add [..., C] of one type, mean and rstd as layer_norm gave them.
+
+    add: the gradient that reaches x past the norm, added to dx.  Returns (dx like x, dweight float32 [C], dbias float32 [C])."""
+    return _host.layer_norm_backward(dy, x, mean, rstd, weight, add, dx, dweight, dbias, workspace)
 
 
 def workspace_status(workspace: torch.Tensor):

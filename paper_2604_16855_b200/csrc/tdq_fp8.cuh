@@ -1,4 +1,5 @@
-// Shared by the kernels of the block-scaled 8-bit floating point layer (tdq_fp8_quantize.cu, tdq_fp8_linear.cu, tdq_fp8_pair.cu).
+// Shared by the kernels of the block-scaled 8-bit floating point layer (tdq_fp8_quantize.cu, tdq_fp8_linear.cu, tdq_fp8_pair.cu)
+// and by what stands around it (tdq_norm.cu, tdq_fp8_grad.cu).
 #pragma once
 #include <cuda.h>
 #include <cuda_fp16.h>
@@ -35,6 +36,72 @@ tdq_status launch_fp8_pair(Fp8Args a, int columns, const CUtensorMap& xmap, cons
 #ifdef __CUDACC__
 namespace {
 
+template <int DT> struct Elem { using T = uint16_t; };   // DT: tdq_dtype
+template <> struct Elem<TDQ_F32> { using T = float; };
+
+template <int DT>
+__device__ __forceinline__ float widen(typename Elem<DT>::T v) {
+    if constexpr (DT == TDQ_F32) return v;
+    else if constexpr (DT == TDQ_BF16) return __uint_as_float((uint32_t)v << 16);
+    else return __half2float(__ushort_as_half(v));
+}
+// bit pattern of the larger magnitude of two words' elements, and of a word's own (as binary32)
+template <int DT>
+__device__ __forceinline__ uint32_t max_abs(uint32_t m, uint32_t w) {
+    if constexpr (DT == TDQ_F32) return max(m, w & 0x7fffffffu);
+    else return __vmaxu2(m, w & 0x7fff7fffu);
+}
+template <int DT>
+__device__ __forceinline__ uint32_t max_bits(uint32_t m) {
+    if constexpr (DT == TDQ_F32) return m;
+    else return __float_as_uint(widen<DT>((uint16_t)max(m & 0xffffu, m >> 16)));
+}
+// Scale and reciprocal of a block whose largest magnitude has this pattern.  POW2: the smallest power of two 2^s with a <= 448 2^s; with a = m 2^e,
+// 1 <= m < 2, and 448 = 1.75 2^8 that is s = e - 8, one more where m > 1.75: the carry of 0x1fffff added to the pattern.
+template <bool POW2>
+__device__ __forceinline__ void block_scale(uint32_t bits, float& scale, float& r) {
+    const float a = fmaxf(__uint_as_float(bits), kFp8Smallest);
+    if constexpr (POW2) {
+        const uint32_t e = (__float_as_uint(a) + 0x1fffffu) >> 23;
+        scale = __uint_as_float((e - 8u) << 23);
+        r = __uint_as_float((262u - e) << 23);
+    } else {
+        scale = __fdiv_rn(a, kFp8Max);
+        r = __fdiv_rn(kFp8Max, a);
+    }
+    if (bits >= 0x7f800000u) scale = r = __uint_as_float(0x7fffffffu);
+}
+// two elements' codes, the first in the low byte
+__device__ __forceinline__ uint32_t cvt2(float lo, float hi) {
+    uint16_t v;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(v) : "f"(hi), "f"(lo));
+    return v;
+}
+__device__ __forceinline__ uint32_t cvt4(float a, float b, float c, float d, float r) {
+    return cvt2(__fmul_rn(a, r), __fmul_rn(b, r)) | cvt2(__fmul_rn(c, r), __fmul_rn(d, r)) << 16;
+}
+template <int DT>
+__device__ __forceinline__ void widen2(uint32_t w, float& lo, float& hi) {
+    if constexpr (DT == TDQ_BF16) {
+        lo = __uint_as_float(w << 16);
+        hi = __uint_as_float(w & 0xffff0000u);
+    } else {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+        lo = f.x;
+        hi = f.y;
+    }
+}
+// the first n elements of a 16-byte vector, the rest zero
+template <int DT>
+__device__ __forceinline__ uint4 keep_first(const uint4& v, int n) {
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (DT == TDQ_F32) w[i] = i < n ? w[i] : 0u;
+        else w[i] = 2 * i >= n ? 0u : 2 * i + 1 >= n ? w[i] & 0xffffu : w[i];
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
 __device__ __forceinline__ void copy4_async(uint32_t dst, const void* src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }

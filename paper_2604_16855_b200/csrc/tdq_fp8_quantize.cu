@@ -3,6 +3,9 @@
 //
 //   a = max(max |x|, 2^-64);   scale = fl(a / 448);   r = fl(448 / a);   code = E4M3(fl(x r)), nearest, ties to even
 //
+// With POW2 (activations kept for the backward pass) scale is the smallest power of two that keeps a / scale <= 448, and r its reciprocal: every
+// value code x scale is then a bf16 number, so that it goes to the tensor core without a second rounding.
+//
 // Both quotients are IEEE divisions, one of each per block; an element costs one product, so that codes are those of the
 // formula bit for bit.  |x r| <= 448 (1 + 2^-23) rounds to 448 at most.  The floor 2^-64 keeps scale and r normal numbers.
 // A block with a NaN or an infinity gets scale NaN and codes NaN (0x7F): patterns of magnitudes compare as unsigned
@@ -20,53 +23,6 @@ namespace {
 constexpr int kThreadsA = 256;
 constexpr int kThreadsW = 512;
 
-template <int DT> struct Elem { using T = uint16_t; };   // DT: tdq_dtype
-template <> struct Elem<TDQ_F32> { using T = float; };
-
-template <int DT>
-__device__ __forceinline__ float widen(typename Elem<DT>::T v) {
-    if constexpr (DT == TDQ_F32) return v;
-    else if constexpr (DT == TDQ_BF16) return __uint_as_float((uint32_t)v << 16);
-    else return __half2float(__ushort_as_half(v));
-}
-// bit pattern of the larger magnitude of two words' elements, and of a word's own (as binary32)
-template <int DT>
-__device__ __forceinline__ uint32_t max_abs(uint32_t m, uint32_t w) {
-    if constexpr (DT == TDQ_F32) return max(m, w & 0x7fffffffu);
-    else return __vmaxu2(m, w & 0x7fff7fffu);
-}
-template <int DT>
-__device__ __forceinline__ uint32_t max_bits(uint32_t m) {
-    if constexpr (DT == TDQ_F32) return m;
-    else return __float_as_uint(widen<DT>((uint16_t)max(m & 0xffffu, m >> 16)));
-}
-// scale and reciprocal of a block whose largest magnitude has this pattern
-__device__ __forceinline__ void block_scale(uint32_t bits, float& scale, float& r) {
-    const float a = fmaxf(__uint_as_float(bits), kFp8Smallest);
-    scale = __fdiv_rn(a, kFp8Max);
-    r = __fdiv_rn(kFp8Max, a);
-    if (bits >= 0x7f800000u) scale = r = __uint_as_float(0x7fffffffu);
-}
-// two elements' codes, the first in the low byte
-__device__ __forceinline__ uint32_t cvt2(float lo, float hi) {
-    uint16_t v;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(v) : "f"(hi), "f"(lo));
-    return v;
-}
-__device__ __forceinline__ uint32_t cvt4(float a, float b, float c, float d, float r) {
-    return cvt2(__fmul_rn(a, r), __fmul_rn(b, r)) | cvt2(__fmul_rn(c, r), __fmul_rn(d, r)) << 16;
-}
-template <int DT>
-__device__ __forceinline__ void widen2(uint32_t w, float& lo, float& hi) {
-    if constexpr (DT == TDQ_BF16) {
-        lo = __uint_as_float(w << 16);
-        hi = __uint_as_float(w & 0xffff0000u);
-    } else {
-        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
-        lo = f.x;
-        hi = f.y;
-    }
-}
 // the codes of a 16-byte vector: one word (four binary32) or two (eight 16-bit elements)
 template <int DT>
 __device__ __forceinline__ void codes_of(const uint4& v, float r, uint32_t* out) {
@@ -96,19 +52,8 @@ __device__ __forceinline__ uint4 load_part(const typename Elem<DT>::T* p, int64_
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// the first n elements of a 16-byte vector, the rest zero
-template <int DT>
-__device__ __forceinline__ uint4 keep_first(const uint4& v, int n) {
-    uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if constexpr (DT == TDQ_F32) w[i] = i < n ? w[i] : 0u;
-        else w[i] = 2 * i >= n ? 0u : 2 * i + 1 >= n ? w[i] & 0xffffu : w[i];
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
 // Sixteen channels a thread, eight neighbouring threads a block: scale and codes.  All lanes of the warp take part, `on` or not.
-template <int DT>
+template <int DT, bool POW2>
 __device__ __forceinline__ void quantize16(const uint4* v, bool on, uint4* codes, float* scale, bool first) {
     constexpr int kVecs = (int)sizeof(typename Elem<DT>::T);
     uint32_t mx = 0;
@@ -123,7 +68,7 @@ __device__ __forceinline__ void quantize16(const uint4* v, bool on, uint4* codes
     for (int d = 1; d < 8; d <<= 1) mx = max_abs<DT>(mx, __shfl_xor_sync(0xffffffffu, mx, d));
     if (!on) return;
     float s, r;
-    block_scale(max_bits<DT>(mx), s, r);
+    block_scale<POW2>(max_bits<DT>(mx), s, r);
     uint32_t out[4];
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) codes_of<DT>(v[i], r, out + i * (4 / kVecs));
@@ -132,7 +77,7 @@ __device__ __forceinline__ void quantize16(const uint4* v, bool on, uint4* codes
 }
 
 // Rows on the 16-byte grid: a thread holds sixteen consecutive channels, eight threads a block of 128.
-template <int DT>
+template <int DT, bool POW2>
 __global__ void __launch_bounds__(kThreadsA) act_fp8_kernel(const typename Elem<DT>::T* __restrict__ x, uint32_t n_blocks, uint32_t K,
                                                             int64_t C, int64_t stride, uint4* __restrict__ codes, float* __restrict__ scale) {
     using T = typename Elem<DT>::T;
@@ -154,7 +99,7 @@ __global__ void __launch_bounds__(kThreadsA) act_fp8_kernel(const typename Elem<
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) v[i] = load_part<DT>(src + i * kPer, on ? C - c0 - i * kPer : 0);
     }
-    quantize16<DT>(v, on, codes + t, scale + b, (threadIdx.x & 7) == 0);   // rows of C_pad codes follow each other without a gap
+    quantize16<DT, POW2>(v, on, codes + t, scale + b, (threadIdx.x & 7) == 0);   // rows of C_pad codes follow each other without a gap
 }
 
 // Rows anywhere: eight lanes per block of a row, KB consecutive blocks of it at a time, pass their aligned words through shared memory, coalesced, and read
@@ -162,7 +107,7 @@ __global__ void __launch_bounds__(kThreadsA) act_fp8_kernel(const typename Elem<
 // middle of a word.  A word that holds an element of the row is read whole; what lies beside the row in it is not used.  Bound by instructions: a
 // warp per block, whose quotients every lane then computes, took 112 a block (4097 x 1000 fp16 5.0 us, 18464 x 768 bf16 14.3), four blocks of any rows 80
 // (4.7 and 11.8); this one 3.5 and 11.5.
-template <int DT, int KB>
+template <int DT, int KB, bool POW2>
 __global__ void __launch_bounds__(kThreadsA) act_fp8_ragged_kernel(const typename Elem<DT>::T* __restrict__ x, uint32_t n_chunks, uint32_t chunks, uint32_t K,
                                                                    int32_t C, int64_t stride, uint4* __restrict__ codes,
                                                                    float* __restrict__ scale) {
@@ -214,7 +159,7 @@ __global__ void __launch_bounds__(kThreadsA) act_fp8_ragged_kernel(const typenam
         for (int i = 0; i < kVecs; ++i) v[i] = keep_first<DT>(v[i], valid - i * (16 / kVecs));
     }
     const uint32_t b = m * K + c * KB;
-    quantize16<DT>(v, on && c * KB + (lane >> 3) < K, codes + (int64_t)b * 8 + lane, scale + b + (lane >> 3), (lane & 7) == 0);
+    quantize16<DT, POW2>(v, on && c * KB + (lane >> 3) < K, codes + (int64_t)b * 8 + lane, scale + b + (lane >> 3), (lane & 7) == 0);
 }
 
 // One block of 128 x 128 weights in registers; VEC: rows on the 16-byte grid, and three thread blocks per SM (4096 x 4096 fp32 16.0 us, bf16 10.0; 256
@@ -255,7 +200,7 @@ __global__ void __launch_bounds__(kThreadsW, VEC ? 3 : 1) weight_fp8_kernel(cons
 #pragma unroll
     for (int i = 0; i < kThreadsW / 32; ++i) mx = max(mx, warp_max[i]);
     float s, r;
-    block_scale(mx, s, r);
+    block_scale<false>(mx, s, r);
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
         const int64_t row = row0 + i * kRows;
@@ -269,12 +214,12 @@ __global__ void __launch_bounds__(kThreadsW, VEC ? 3 : 1) weight_fp8_kernel(cons
     if (threadIdx.x == 0) scale[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = s;
 }
 
-template <int DT>
+template <int DT, bool POW2>
 cudaError_t launch_act(const void* x, uint32_t n_blocks, uint32_t K, int64_t C, int64_t stride, uint8_t* codes, float* scale, cudaStream_t st) {
     using T = typename Elem<DT>::T;
     const T* p = reinterpret_cast<const T*>(x);
     if (reinterpret_cast<uintptr_t>(x) % 16 == 0 && (stride * (int64_t)sizeof(T)) % 16 == 0)
-        return launch_pdl(act_fp8_kernel<DT>, dim3((n_blocks + kThreadsA / 8 - 1) / (kThreadsA / 8)), dim3(kThreadsA), 0, st, p, n_blocks, K, C, stride,
+        return launch_pdl(act_fp8_kernel<DT, POW2>, dim3((n_blocks + kThreadsA / 8 - 1) / (kThreadsA / 8)), dim3(kThreadsA), 0, st, p, n_blocks, K, C, stride,
                           reinterpret_cast<uint4*>(codes), scale);
     // One block of a row at a time for rows of one block, two where four would leave half a warp idle at a row's end, else four (us on 25037 rows of bf16
     // with one, two and four: 70 channels 3.8, 4.9, 8.7; 147 5.2, 5.1, 8.8; 767 14.7, 13.9, 15.6; 1023 17.9, 17.6, 16.5).
@@ -282,9 +227,9 @@ cudaError_t launch_act(const void* x, uint32_t n_blocks, uint32_t K, int64_t C, 
         const uint32_t chunks = (K + kb - 1) / kb, n_chunks = n_blocks / K * chunks, per = kThreadsA / (8 * kb);
         return launch_pdl(kernel, dim3((n_chunks + per - 1) / per), dim3(kThreadsA), 0, st, p, n_chunks, chunks, K, (int32_t)C, stride, reinterpret_cast<uint4*>(codes), scale);
     };
-    if (K == 1) return ragged(act_fp8_ragged_kernel<DT, 1>, 1);
-    if ((K & 3) == 1 || (K & 3) == 2) return ragged(act_fp8_ragged_kernel<DT, 2>, 2);
-    return ragged(act_fp8_ragged_kernel<DT, 4>, 4);
+    if (K == 1) return ragged(act_fp8_ragged_kernel<DT, 1, POW2>, 1);
+    if ((K & 3) == 1 || (K & 3) == 2) return ragged(act_fp8_ragged_kernel<DT, 2, POW2>, 2);
+    return ragged(act_fp8_ragged_kernel<DT, 4, POW2>, 4);
 }
 template <int DT>
 cudaError_t launch_weight(const void* w, int64_t O, int64_t I, uint8_t* codes, float* scale, cudaStream_t st) {
@@ -303,8 +248,10 @@ bool known_dtype(tdq_dtype t) { return t == TDQ_F32 || t == TDQ_BF16 || t == TDQ
 
 using namespace tdq;
 
-extern "C" tdq_status tdq_quantize_act_fp8(const void* x, tdq_dtype x_dtype, int64_t B, int64_t N, int64_t C, int64_t row_stride_elems,
-                                           uint8_t* codes, float* scale, void* cuda_stream) {
+namespace {
+template <bool POW2>
+tdq_status quantize_act_fp8(const void* x, tdq_dtype x_dtype, int64_t B, int64_t N, int64_t C, int64_t row_stride_elems, uint8_t* codes, float* scale,
+                            void* cuda_stream) {
     if (!known_dtype(x_dtype) || B < 0 || N < 0 || C <= 0 || row_stride_elems < C) return TDQ_ERR_INVALID_ARG;
     if (C > INT32_MAX || (N > 0 && B > INT64_MAX / N)) return TDQ_ERR_INVALID_ARG;
     const int64_t M = B * N, K = fp8_blocks(C);
@@ -316,11 +263,21 @@ extern "C" tdq_status tdq_quantize_act_fp8(const void* x, tdq_dtype x_dtype, int
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
     const uint32_t n = (uint32_t)(M * K);
     cudaError_t e;
-    if (x_dtype == TDQ_F32) e = launch_act<TDQ_F32>(x, n, (uint32_t)K, C, row_stride_elems, codes, scale, st);
-    else if (x_dtype == TDQ_BF16) e = launch_act<TDQ_BF16>(x, n, (uint32_t)K, C, row_stride_elems, codes, scale, st);
-    else e = launch_act<TDQ_F16>(x, n, (uint32_t)K, C, row_stride_elems, codes, scale, st);
+    if (x_dtype == TDQ_F32) e = launch_act<TDQ_F32, POW2>(x, n, (uint32_t)K, C, row_stride_elems, codes, scale, st);
+    else if (x_dtype == TDQ_BF16) e = launch_act<TDQ_BF16, POW2>(x, n, (uint32_t)K, C, row_stride_elems, codes, scale, st);
+    else e = launch_act<TDQ_F16, POW2>(x, n, (uint32_t)K, C, row_stride_elems, codes, scale, st);
     if (e == cudaSuccess) g_launch_count.fetch_add(1, std::memory_order_relaxed);
     return cuda_status(e);
+}
+}  // namespace
+
+extern "C" tdq_status tdq_quantize_act_fp8(const void* x, tdq_dtype x_dtype, int64_t B, int64_t N, int64_t C, int64_t row_stride_elems,
+                                           uint8_t* codes, float* scale, void* cuda_stream) {
+    return quantize_act_fp8<false>(x, x_dtype, B, N, C, row_stride_elems, codes, scale, cuda_stream);
+}
+extern "C" tdq_status tdq_quantize_act_fp8_pow2(const void* x, tdq_dtype x_dtype, int64_t B, int64_t N, int64_t C, int64_t row_stride_elems,
+                                                uint8_t* codes, float* scale, void* cuda_stream) {
+    return quantize_act_fp8<true>(x, x_dtype, B, N, C, row_stride_elems, codes, scale, cuda_stream);
 }
 
 extern "C" tdq_status tdq_quantize_weight_fp8(const void* w, tdq_dtype w_dtype, int64_t O, int64_t I, uint8_t* wcodes, float* wscale,

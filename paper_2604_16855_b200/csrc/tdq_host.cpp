@@ -106,6 +106,17 @@ int64_t int_arg(PyObject* o) {
     return v;
 }
 
+bool truth(PyObject* o) {
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) throw python_error();
+    return v != 0;
+}
+double float_arg(PyObject* o) {
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw python_error();
+    return v;
+}
+
 template <typename T = void>
 T* ptr(const at::Tensor* t) { return t ? reinterpret_cast<T*>(t->data_ptr()) : nullptr; }
 template <typename T = void>
@@ -387,10 +398,11 @@ void check_tensor(const char* name, const at::Tensor& t, std::initializer_list<a
 constexpr int64_t kFp8Block = 128;
 int64_t fp8_blocks(int64_t n) { return (n + kFp8Block - 1) / kFp8Block; }
 
-// quantize_act_fp8(x, codes, scale)
+// quantize_act_fp8(x, codes, scale, pow2)
 PyObject* quantize_act_fp8(PyObject* const* a) {
     const at::Tensor& x = tensor(a[0]);
     const at::Tensor *oc = opt_tensor(a[1]), *os = opt_tensor(a[2]);
+    const bool pow2 = truth(a[3]);
     need_cuda({&x, oc, os});
     if (x.dim() < 1 || x.size(-1) < 1) throw Bad{PyExc_ValueError, "x must have channels"};
     const int64_t C = x.size(-1), K = fp8_blocks(C);
@@ -403,8 +415,9 @@ PyObject* quantize_act_fp8(PyObject* const* a) {
     const at::Tensor codes = oc ? *oc : new_like(x, {M, K * kFp8Block}, at::kFloat8_e4m3fn);
     const at::Tensor scale = os ? *os : new_like(x, {M, K}, at::kFloat);
     check(call(x, [&](void* st) {
-              return tdq_quantize_act_fp8(ptr(x2), dt, 1, M, C, M > 1 ? x2.stride(0) : C, ptr<uint8_t>(codes), ptr<float>(scale), st);
-          }), "tdq_quantize_act_fp8");
+              return (pow2 ? tdq_quantize_act_fp8_pow2 : tdq_quantize_act_fp8)(ptr(x2), dt, 1, M, C, M > 1 ? x2.stride(0) : C, ptr<uint8_t>(codes),
+                                                                               ptr<float>(scale), st);
+          }), pow2 ? "tdq_quantize_act_fp8_pow2" : "tdq_quantize_act_fp8");
     return tuple2(codes, scale);
 }
 
@@ -526,6 +539,138 @@ PyObject* qk_norm_rope(PyObject* const* a) {
     return t;
 }
 
+// The rows of a [..., C] tensor: M of them, `stride` elements apart, channels adjacent.
+struct Rows {
+    at::Tensor t;          // keeps a copy alive where the rows had to be brought together
+    int64_t M, C, stride;
+    void* p() const { return t.data_ptr(); }
+};
+Rows rows_of(const char* name, const at::Tensor& t, bool may_copy) {
+    if (t.dim() < 1 || t.size(-1) < 1) throw Bad{PyExc_ValueError, std::string(name) + " must have channels"};
+    const int64_t C = t.size(-1), M = t.numel() / C;
+    if (!may_copy && t.dim() != 2 && !t.is_contiguous()) throw Bad{PyExc_ValueError, std::string(name) + " must be a matrix or contiguous"};
+    const at::Tensor r = t.dim() == 2 ? t : t.reshape({M, C});
+    if (C > 1 && M > 0 && r.stride(1) != 1) throw Bad{PyExc_ValueError, std::string(name) + ": the channel axis must be contiguous"};
+    return {r, M, C, M > 1 ? r.stride(0) : C};
+}
+// a tensor whose rows go with those of x: as many, as long, of its type and device
+Rows rows_like(const char* name, const at::Tensor& t, const Rows& x, bool may_copy) {
+    if (t.device() != x.t.device()) throw Bad{PyExc_ValueError, std::string(name) + " is on " + t.device().str() + ", not on " + x.t.device().str()};
+    if (t.scalar_type() != x.t.scalar_type()) throw Bad{PyExc_TypeError, std::string(name) + " must be " + dtype_name(x.t.scalar_type()) + ", got " + dtype_name(t.scalar_type())};
+    const Rows r = rows_of(name, t, may_copy);
+    if (r.M != x.M || r.C != x.C)
+        throw Bad{PyExc_ValueError, std::string(name) + " must have " + std::to_string(x.M) + " rows of " + std::to_string(x.C) + " channels"};
+    return r;
+}
+at::Tensor vector_of(const char* name, const at::Tensor* given, int64_t n, const at::Tensor& on) {
+    if (given) check_tensor(name, *given, {at::kFloat}, {n}, on);
+    return given ? *given : new_like(on, {n}, at::kFloat);
+}
+PyObject* tuple_of(std::initializer_list<at::Tensor> ts) {
+    PyObject* t = PyTuple_New((Py_ssize_t)ts.size());
+    Py_ssize_t i = 0;
+    for (const at::Tensor& v : ts) {
+        if (!t) break;
+        PyObject* o = v.defined() ? THPVariable_Wrap(v) : Py_NewRef(Py_None);
+        if (!o) {
+            Py_DECREF(t);
+            return nullptr;
+        }
+        PyTuple_SET_ITEM(t, i++, o);
+    }
+    return t;
+}
+// The caller's workspace, or one from the caching allocator for the length of the call.
+struct Scratch {
+    at::DataPtr own;
+    void* p = nullptr;
+    size_t bytes = 0;
+    template <typename F>
+    Scratch(const at::Tensor* given, const at::Tensor& on, F&& size) {
+        if (given) {
+            check_tensor("workspace", *given, {at::kByte}, given->sizes(), on);
+            p = given->data_ptr();
+            bytes = (size_t)given->numel();
+            return;
+        }
+        c10::cuda::CUDAGuard guard(on.device());
+        bytes = size();
+        if (!bytes) return;
+        own = c10::cuda::CUDACachingAllocator::get()->allocate(bytes);
+        p = own.get();
+    }
+};
+
+// layer_norm(x, weight, bias, eps, y, mean, rstd)  ->  (y, mean, rstd)
+PyObject* layer_norm(PyObject* const* a) {
+    const at::Tensor& x0 = tensor(a[0]);
+    const at::Tensor *w = opt_tensor(a[1]), *b = opt_tensor(a[2]), *oy = opt_tensor(a[4]), *om = opt_tensor(a[5]), *orr = opt_tensor(a[6]);
+    need_cuda({&x0, w, b, oy, om, orr});
+    const double eps = float_arg(a[3]);
+    const Rows x = rows_of("x", x0, true);
+    const tdq_dtype dt = dtype_id(x0);
+    if (w) check_tensor("weight", *w, {at::kFloat}, {x.C}, x0);
+    if (b) check_tensor("bias", *b, {at::kFloat}, {x.C}, x0);
+    const at::Tensor out = oy ? *oy : new_like(x0, x0.sizes(), x0.scalar_type());
+    const Rows y = rows_like("y", out, x, false);
+    const at::Tensor mean = vector_of("mean", om, x.M, x0), rstd = vector_of("rstd", orr, x.M, x0);
+    if (x.M > 0)
+        check(call(x0, [&](void* st) {
+                  return tdq_layer_norm(x.p(), dt, x.M, x.C, x.stride, ptr<float>(w), ptr<float>(b), (float)eps, 0, y.p(), y.stride, nullptr, nullptr,
+                                        ptr<float>(mean), ptr<float>(rstd), st);
+              }), "tdq_layer_norm");
+    return tuple_of({out, mean, rstd});
+}
+
+// layer_norm_fp8(x, weight, bias, eps, pow2, codes, scale, mean, rstd)  ->  (codes, scale, mean, rstd)
+PyObject* layer_norm_fp8(PyObject* const* a) {
+    const at::Tensor& x0 = tensor(a[0]);
+    const at::Tensor *w = opt_tensor(a[1]), *b = opt_tensor(a[2]), *oc = opt_tensor(a[5]), *os = opt_tensor(a[6]), *om = opt_tensor(a[7]), *orr = opt_tensor(a[8]);
+    need_cuda({&x0, w, b, oc, os, om, orr});
+    const double eps = float_arg(a[3]);
+    const bool pow2 = truth(a[4]);
+    const Rows x = rows_of("x", x0, true);
+    const tdq_dtype dt = dtype_id(x0);
+    const int64_t K = fp8_blocks(x.C);
+    if (w) check_tensor("weight", *w, {at::kFloat}, {x.C}, x0);
+    if (b) check_tensor("bias", *b, {at::kFloat}, {x.C}, x0);
+    if (oc) check_tensor("codes", *oc, {at::kFloat8_e4m3fn, at::kByte}, {x.M, K * kFp8Block}, x0);
+    if (os) check_tensor("scale", *os, {at::kFloat}, {x.M, K}, x0);
+    const at::Tensor codes = oc ? *oc : new_like(x0, {x.M, K * kFp8Block}, at::kFloat8_e4m3fn);
+    const at::Tensor scale = os ? *os : new_like(x0, {x.M, K}, at::kFloat);
+    const at::Tensor mean = vector_of("mean", om, x.M, x0), rstd = vector_of("rstd", orr, x.M, x0);
+    if (x.M > 0)
+        check(call(x0, [&](void* st) {
+                  return tdq_layer_norm(x.p(), dt, x.M, x.C, x.stride, ptr<float>(w), ptr<float>(b), (float)eps, pow2 ? TDQ_NORM_POW2 : 0u, nullptr, 0,
+                                        ptr<uint8_t>(codes), ptr<float>(scale), ptr<float>(mean), ptr<float>(rstd), st);
+              }), "tdq_layer_norm");
+    return tuple_of({codes, scale, mean, rstd});
+}
+
+// layer_norm_backward(dy, x, mean, rstd, weight, add, dx, dweight, dbias, workspace)  ->  (dx, dweight, dbias)
+PyObject* layer_norm_backward(PyObject* const* a) {
+    const at::Tensor &dy0 = tensor(a[0]), &x0 = tensor(a[1]), &mean = tensor(a[2]), &rstd = tensor(a[3]);
+    const at::Tensor *w = opt_tensor(a[4]), *add0 = opt_tensor(a[5]), *odx = opt_tensor(a[6]), *odw = opt_tensor(a[7]), *odb = opt_tensor(a[8]), *ow = opt_tensor(a[9]);
+    need_cuda({&dy0, &x0, &mean, &rstd, w, add0, odx, odw, odb, ow});
+    const Rows x = rows_of("x", x0, true);
+    const tdq_dtype dt = dtype_id(x0);
+    const Rows dy = rows_like("dy", dy0, x, true);
+    Rows add = {};
+    if (add0) add = rows_like("add", *add0, x, true);
+    check_tensor("mean", mean, {at::kFloat}, {x.M}, x0);
+    check_tensor("rstd", rstd, {at::kFloat}, {x.M}, x0);
+    if (w) check_tensor("weight", *w, {at::kFloat}, {x.C}, x0);
+    const at::Tensor out = odx ? *odx : new_like(x0, x0.sizes(), x0.scalar_type());
+    const Rows dx = rows_like("dx", out, x, false);
+    const at::Tensor dw = vector_of("dweight", odw, x.C, x0), db = vector_of("dbias", odb, x.C, x0);
+    const Scratch ws(ow, x0, [&] { return tdq_layer_norm_backward_workspace_bytes(x.M, x.C); });
+    check(call(x0, [&](void* st) {
+              return tdq_layer_norm_backward(dy.p(), dy.stride, x.p(), x.stride, dt, x.M, x.C, ptr<float>(mean), ptr<float>(rstd), ptr<float>(w),
+                                             add0 ? add.p() : nullptr, add.stride, dx.p(), dx.stride, ptr<float>(dw), ptr<float>(db), ws.p, ws.bytes, st);
+          }), "tdq_layer_norm_backward");
+    return tuple_of({out, dw, db});
+}
+
 // Argument count, and C++ exceptions as Python ones.
 template <PyObject* (*F)(PyObject* const*), int N>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -553,7 +698,8 @@ PyObject* set_error_class(PyObject*, PyObject* cls) {
 PyMethodDef methods[] = {
     TDQ_ENTRY(quantize_act, 5), TDQ_ENTRY(quantize_act_fixed, 6), TDQ_ENTRY(quantize_act_nchw, 5), TDQ_ENTRY(quantize_weight, 4),
     TDQ_ENTRY(w4a4_linear, 11), TDQ_ENTRY(w4a4_linear_static, 8), TDQ_ENTRY(quant_linear_fused, 8), TDQ_ENTRY(quant_linear_host, 7),
-    TDQ_ENTRY(quantize_act_fp8, 3), TDQ_ENTRY(quantize_weight_fp8, 3), TDQ_ENTRY(fp8_linear, 8), TDQ_ENTRY(qk_norm_rope, 11),
+    TDQ_ENTRY(quantize_act_fp8, 4), TDQ_ENTRY(quantize_weight_fp8, 3), TDQ_ENTRY(fp8_linear, 8), TDQ_ENTRY(qk_norm_rope, 11),
+    TDQ_ENTRY(layer_norm, 7), TDQ_ENTRY(layer_norm_fp8, 9), TDQ_ENTRY(layer_norm_backward, 10),
     {"set_error_class", set_error_class, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 #undef TDQ_ENTRY
 
