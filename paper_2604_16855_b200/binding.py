@@ -31,7 +31,7 @@ EXPORTS = ["tdq_default_act_params", "tdq_quantize_act", "tdq_quantize_weight", 
            "tdq_quantize_status", "tdq_selftest_wait_timeout", "tdq_fold_output_affine", "tdq_measure_mma_clocks",
            "tdq_quantize_act_fp8", "tdq_quantize_weight_fp8", "tdq_fp8_linear", "tdq_fp8_linear_workspace_bytes",
            "tdq_fp8_linear_tiles", "tdq_qk_norm_rope", "tdq_quantize_act_fp8_pow2", "tdq_layer_norm", "tdq_layer_norm_backward",
-           "tdq_layer_norm_backward_workspace_bytes"]
+           "tdq_layer_norm_backward_workspace_bytes", "tdq_fp8_weight_grad", "tdq_fp8_weight_grad_workspace_bytes"]
 
 
 class ActParams(ctypes.Structure):
@@ -108,6 +108,10 @@ _lib.tdq_layer_norm_backward.argtypes = [_vp, _i64, _vp, _i64, ctypes.c_int, _i6
 _lib.tdq_layer_norm_backward.restype = ctypes.c_int
 _lib.tdq_layer_norm_backward_workspace_bytes.argtypes = [_i64, _i64]
 _lib.tdq_layer_norm_backward_workspace_bytes.restype = _sz
+_lib.tdq_fp8_weight_grad.argtypes = [_vp, ctypes.c_int, _i64, _vp, _vp, _i64, _i64, _i64, _vp, ctypes.c_int, _i64, _vp, _vp, _sz, _vp]
+_lib.tdq_fp8_weight_grad.restype = ctypes.c_int
+_lib.tdq_fp8_weight_grad_workspace_bytes.argtypes = [_vp, ctypes.c_int, _i64, _i64, _i64, _i64]
+_lib.tdq_fp8_weight_grad_workspace_bytes.restype = _sz
 _lib.tdq_status_string.argtypes = [ctypes.c_int]
 _lib.tdq_status_string.restype = ctypes.c_char_p
 _lib.tdq_kernel_launch_count.argtypes = []
@@ -305,6 +309,22 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, *, add=None, dx=None, dw
 
     add: the gradient that reaches x past the norm, added to dx.  Returns (dx like x, dweight float32 [C], dbias float32 [C])."""
     return _host.layer_norm_backward(dy, x, mean, rstd, weight, add, dx, dweight, dbias, workspace)
+
+
+def fp8_weight_grad_workspace(dy: torch.Tensor, cin: int) -> torch.Tensor:
+    """A workspace for fp8_weight_grad with gradients laid out as dy [..., O] is."""
+    rows = dy if dy.dim() == 2 else dy.reshape(-1, dy.shape[-1])
+    M, O = rows.shape
+    with torch.cuda.device(dy.device):
+        n = int(_lib.tdq_fp8_weight_grad_workspace_bytes(_ptr(rows), {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}[dy.dtype],
+                                                         rows.stride(0) if M > 1 else O, M, O, cin))
+    return torch.zeros((n,), dtype=torch.uint8, device=dy.device)
+
+
+def fp8_weight_grad(dy, xcodes, xscale, cin, *, out_dtype=torch.float32, bias=True, dw=None, db=None, workspace=None):
+    """tdq_fp8_weight_grad: gradients of a layer of cin input channels from dy [..., O] and its input's codes and scales (quantize_act_fp8 or
+    layer_norm_fp8 with pow2=True).  Returns (dw [O, cin], db float32 [O], or None with bias=False)."""
+    return _host.fp8_weight_grad(dy, xcodes, xscale, cin, out_dtype, bias, dw, db, workspace)
 
 
 def workspace_status(workspace: torch.Tensor):

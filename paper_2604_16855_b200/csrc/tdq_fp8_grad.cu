@@ -1,0 +1,644 @@
+// tdq_fp8_weight_grad: dw[o,i] = sum_m dy[m,o] x[m,i], db[o] = sum_m dy[m,o], with x = code x scale kept in 8 bits.
+//
+// The scale of x changes along the sum (a token's block of 128 channels has its own), so it cannot be taken out of the product: the codes are restored to
+// bf16 on their way to the tensor core, which with scales that are powers of two is exact.  The restored matrix is never in memory.
+//
+//   tile        256 outputs x 256 input channels by two CTAs (cta_group::2): each brings 128 outputs of dy (copied by the engine as they lie in memory,
+//               64 tokens x 64 outputs a box, an operand whose slow axis is the sum's) and one block of 128 channels, written in the same layout by the
+//               restoring warps.  64 tokens a stage: 16 KB of each.
+//   sum         binary32 accumulators in TMEM (two of 256 columns), taken to binary32 registers every kGroup stages: the tensor core drops what it adds below
+//               the accumulator's last place, which over a long sum leaves more than binary32's own rounding.
+//   work        all stages of all tiles in one row, cut in equal pieces, one for every pair of SMs; a tile that is cut goes to the workspace in parts, which a second
+//               kernel adds in order.  No atomics: the same call gives the same bits.
+//   dy          bf16 on the 16-byte grid is read in place; fp16 and float32 are cut into two and three bf16 addends (exact) and rows off the grid copied,
+//               into the workspace, and the sum goes over all addends.
+//
+//   warps 0, 1  copies of dy; the instructions (CTA 0)      warps 4-11  sums and output      warps 12-19  restore x, sum db
+#include <algorithm>
+
+#include "tdq_tc.cuh"
+#include "tdq_rows.cuh"
+
+namespace tdq {
+namespace {
+
+constexpr int kTok = 64;                                  // tokens a stage
+constexpr int kGradStages = 5;
+constexpr int kGroup = 8;                                 // stages whose products an accumulator adds
+constexpr uint32_t kGradOperand = kTok * 128 * 2;         // bytes: two halves of 64 columns, 128 bytes a token
+constexpr uint32_t kGradHalf = kTok * 128;
+constexpr uint32_t kGradStage = 2 * kGradOperand;
+constexpr uint32_t kGradCtrl = 1024;
+constexpr uint32_t kGradStrip = 32 * 128;
+constexpr int kSumWarp0 = 4, kSumWarps = 8, kFillWarp0 = 12, kFillWarps = 8;
+constexpr int kGradThreads = (kFillWarp0 + kFillWarps) * 32;
+constexpr uint32_t kGradDb = kFillWarps * 128 * 4;
+constexpr uint32_t kGradSmem = kGradCtrl + kGradStages * kGradStage + kSumWarps * kGradStrip + kGradDb;
+static_assert(kGradSmem <= (uint32_t)kSmemLimit, "shared memory");
+constexpr int kGradRegsLoad = 32, kGradRegsSum = 168, kGradRegsFill = 56;   // 128 * 32 + 256 * 168 + 256 * 56 <= 640 * 96
+// D binary32, both operands bf16 with the sum's axis slow, 256 columns x 256 rows
+constexpr uint32_t kGradIdesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((256u >> 3) << 17) | ((256u >> 4) << 24);
+constexpr uint32_t kGradDescLo = (kGradHalf >> 4) << 16;  // the next 64 columns; eight tokens further on are 1024 bytes (kSwDescHi)
+
+struct GradArgs {
+    const uint8_t* xcodes;     // [M][Kb * 128]
+    const float* xscale;       // [M][Kb]
+    const uint16_t* dy;        // bf16 [parts * rows_part][dy_stride]
+    void* dw;
+    float* db;                 // or null
+    float* dbpart;             // [slots][256]
+    float* part;               // [slots][256][256]
+    int64_t M, O, I, dy_stride, dw_stride, rows_part;
+    int32_t Kb, tiles_o, tiles_i, stages_part, parts;   // stages of an addend, addends
+    int32_t clusters;
+    int32_t dw_vec;            // rows of dw on the 16-byte grid
+    uint32_t* status;
+};
+struct GradCtrl {
+    uint64_t full[kGradStages], empty[kGradStages];
+    uint64_t tfull[2], tempty[2];
+    uint64_t met;                                            // the restoring warps meet, twice for each sum of db
+};
+static_assert(sizeof(Ctrl) + sizeof(GradCtrl) <= kGradCtrl, "control block outgrew its reservation");
+
+// stages [first, last) of the row of all tiles' stages that cluster w adds
+__host__ __device__ inline int64_t piece_begin(int64_t total, int32_t clusters, int32_t w) { return total / clusters * w + min((int64_t)w, total % clusters); }
+// the cluster that adds stage s
+__host__ __device__ inline int32_t piece_owner(int64_t total, int32_t clusters, int64_t s) {
+    const int64_t q = total / clusters, r = total % clusters, longer = r * (q + 1);
+    return (int32_t)(s < longer ? s / (q + 1) : r + (s - longer) / q);
+}
+
+__device__ __forceinline__ void grad_load(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void grad_mma(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(kGradIdesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void grad_commit(uint32_t bar_s) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(bar_s), "h"((uint16_t)3) : "memory");
+}
+// lane 0 of a converged warp arrives on a barrier of either CTA, given by its cluster address; what the warp wrote before is seen by who waits there
+__device__ __forceinline__ void grad_arrive(uint32_t bar_c, int lane) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %1, 0;\n\t@p mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n\t}"
+                 ::"r"(bar_c), "r"(lane) : "memory");
+}
+// four codes times their scale as four bf16, nearest even
+__device__ __forceinline__ void restore4(uint32_t codes, float scale, uint32_t& lo, uint32_t& hi) {
+    uint32_t h0, h1;
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(h0), "=r"(h1) : "r"(codes));
+    const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&h0)), f1 = __half22float2(*reinterpret_cast<const __half2*>(&h1));
+    lo = narrow2<TDQ_BF16>(f0.x * scale, f0.y * scale);
+    hi = narrow2<TDQ_BF16>(f1.x * scale, f1.y * scale);
+}
+
+// DT: dw's tdq_dtype
+template <int DT>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGradThreads, 1)
+fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, const __grid_constant__ CUtensorMap dwmap, const __grid_constant__ CUtensorMap partmap) {
+    constexpr bool W16 = DT != TDQ_F32;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    Ctrl* c = reinterpret_cast<Ctrl*>(smem_raw);             // its abort flag and TMEM address; the barriers are g's
+    GradCtrl* g = reinterpret_cast<GradCtrl*>(smem_raw + sizeof(Ctrl));
+    const uint32_t sm_s = smem_u32(smem_raw), ring_s = sm_s + kGradCtrl;
+    const uint32_t strips_s = ring_s + kGradStages * kGradStage;
+    float* db_room = reinterpret_cast<float*>(smem_raw + kGradCtrl + kGradStages * kGradStage + kSumWarps * kGradStrip);
+    const int warp = uniform_warp(), lane = threadIdx.x & 31;
+    const uint32_t rank = fp8_cluster_rank();
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kGradStages; ++i) { mbar_init(&g->full[i], 1 + 2 * kFillWarps); mbar_init(&g->empty[i], 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&g->tfull[i], 1); mbar_init(&g->tempty[i], 2 * kSumWarps); }
+        mbar_init(&g->met, kFillWarps);
+        c->abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&c->tmem_base)), "n"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    fp8_cluster_sync();                                      // both CTAs' barriers are initialised
+    tc_fence_after();
+    pdl_wait();
+    pdl_trigger();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0u;
+    const uint32_t tmem_base = c->tmem_base;
+    const int32_t w = (int32_t)blockIdx.x / 2;
+    const int64_t per_tile = (int64_t)a.stages_part * a.parts, total = per_tile * a.tiles_o * a.tiles_i;
+    const int64_t begin = piece_begin(total, a.clusters, w), end = piece_begin(total, a.clusters, w + 1);
+    int tile = (int)(begin / per_tile);
+    int64_t at = begin - tile * per_tile;                    // stage of the tile
+
+    if (warp < kSumWarp0) {
+        setmaxnreg_dec<kGradRegsLoad>();
+        if (warp == 0) {
+            // -------------------------------------------------------- copies of dy
+            const uint32_t full0 = map_to_cta(smem_u32(&g->full[0]), 0), empty_s = smem_u32(&g->empty[0]);
+            uint32_t s = 0, ph = 1;
+            int part = (int)(at / a.stages_part), tok = (int)(at - (int64_t)part * a.stages_part);
+#pragma unroll 1
+            for (int64_t n = begin; n < end; ++n) {
+                fp8_wait(empty_s + s * 8, ph, c, a.status, 5u);
+                if (c->abort_flag) break;
+                if (elect_one()) {
+                    if (rank == 0) mbar_expect_tx(&g->full[s], 2 * kGradOperand);
+                    const int32_t o = tile / a.tiles_i * 256 + (int)rank * 128;   // past the end: the map fills with zeros
+                    const int32_t row = (int32_t)(part * a.rows_part) + tok * kTok;
+                    grad_load(ring_s + s * kGradStage, &dymap, o, row, full0 + s * 8);
+                    grad_load(ring_s + s * kGradStage + kGradHalf, &dymap, o + 64, row, full0 + s * 8);
+                }
+                __syncwarp();
+                if (++s == kGradStages) { s = 0; ph ^= 1; }
+                if (++tok == a.stages_part) {
+                    tok = 0;
+                    if (++part == a.parts) { part = 0; ++tile; }
+                }
+            }
+        } else if (warp == 1 && rank == 0) {
+            // -------------------------------------------------------- instructions
+            const uint32_t full_s = smem_u32(&g->full[0]), empty_s = smem_u32(&g->empty[0]), tfull_s = smem_u32(&g->tfull[0]), tempty_s = smem_u32(&g->tempty[0]);
+            const uint32_t xd0 = kGradDescLo | ((ring_s & 0x3FFFFu) >> 4);
+            uint32_t s = 0, ph = 0, group = 0;
+            bool on = true;
+            for (int64_t n = begin; n < end && on;) {
+                const int64_t len = min(min((int64_t)kGroup, per_tile - at), end - n);
+                const uint32_t slot = group & 1u;
+                fp8_wait(tempty_s + slot * 8, ((group >> 1) & 1u) ^ 1u, c, a.status, 3u);
+#pragma unroll 1
+                for (int64_t j = 0; j < len; ++j) {
+                    fp8_wait(full_s + s * 8, ph, c, a.status, 4u);
+                    if (c->abort_flag) { on = false; break; }
+                    asm volatile("fence.acq_rel.cluster;" ::: "memory");   // the other CTA's restored operand too
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint32_t lo = xd0 + s * (kGradStage >> 4);
+                        const uint64_t ad = (uint64_t)kSwDescHi << 32 | lo, bd = (uint64_t)kSwDescHi << 32 | (lo + (kGradOperand >> 4));
+#pragma unroll
+                        for (int k = 0; k < kTok / 16; ++k) grad_mma(tmem_base + slot * 256, ad + k * (2048 >> 4), bd + k * (2048 >> 4), j || k ? 1u : 0u);
+                        grad_commit(empty_s + s * 8);
+                        if (j == len - 1) grad_commit(tfull_s + slot * 8);
+                    }
+                    __syncwarp();
+                    if (++s == kGradStages) { s = 0; ph ^= 1; }
+                }
+                ++group;
+                n += len;
+                at += len;
+                if (at == per_tile) at = 0;
+            }
+        }
+    } else if (warp < kFillWarp0) {
+        // ------------------------------------------------------------ sums and output
+        setmaxnreg_inc<kGradRegsSum>();
+        const int sw = warp - kSumWarp0, quarter = warp & 3, h = sw >> 2;
+        const uint32_t strip_s = strips_s + (uint32_t)sw * kGradStrip;
+        const uint32_t tfull_s = smem_u32(&g->tfull[0]), tempty_c = map_to_cta(smem_u32(&g->tempty[0]), 0);
+        const uint32_t tm0 = tmem_base + ((uint32_t)(quarter * 32) << 16) + h * 128;
+        uint32_t group = 0;
+        for (int64_t n = begin; n < end && !c->abort_flag;) {
+            const int64_t len = min(per_tile - at, end - n);
+            float2 acc[64];
+#pragma unroll
+            for (int j = 0; j < 64; ++j) acc[j] = make_float2(0.f, 0.f);
+#pragma unroll 1
+            for (int64_t done = 0; done < len; done += kGroup, ++group) {
+                const uint32_t slot = group & 1u;
+                fp8_wait(tfull_s + slot * 8, (group >> 1) & 1u, c, a.status, 2u);
+                if (c->abort_flag) break;
+                tc_fence_after();
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    uint32_t v[32];
+                    tmem_ld32(tm0 + slot * 256 + q * 32, v);
+                    tmem_ld_wait_on(v);
+                    if (q == 3) {
+                        tc_fence_before();
+                        __syncwarp();
+                        grad_arrive(tempty_c + slot * 8, lane);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        acc[q * 16 + j] = __fadd2_rn(acc[q * 16 + j], make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])));
+                }
+            }
+            if (c->abort_flag) break;
+            const int to = tile / a.tiles_i, ti = tile - to * a.tiles_i;
+            const bool whole = len == per_tile;
+            const int32_t slot = 2 * w + (n == begin ? 0 : 1);
+            const int64_t o0 = (int64_t)to * 256 + rank * 128 + quarter * 32, i0 = (int64_t)ti * 256 + h * 128;
+            if (!W16 || !whole) {
+                const CUtensorMap* map = whole ? &dwmap : &partmap;
+#pragma unroll
+                for (int piece = 0; piece < 4; ++piece) {
+                    if (lane == 0) bulk_wait_group_read0();          // the strip has been read
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float2 u = acc[piece * 16 + 2 * j], v = acc[piece * 16 + 2 * j + 1];
+                        sts128(strip_s + (uint32_t)lane * 128u + (((uint32_t)j ^ ((uint32_t)lane & 7u)) << 4), __float_as_uint(u.x), __float_as_uint(u.y),
+                               __float_as_uint(v.x), __float_as_uint(v.y));
+                    }
+                    const int64_t col = i0 + piece * 32;
+                    if (!whole || (a.dw_vec && (a.I % 4 == 0 || col + 32 <= a.I))) {
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) {
+                            if (!whole) tma_store_2d(map, strip_s, h * 128 + piece * 32, slot * 256 + (int)rank * 128 + quarter * 32);
+                            else if (o0 < a.O && col < a.I) tma_store_2d(map, strip_s, (int32_t)col, (int32_t)o0);
+                            bulk_commit_group();
+                        }
+                    } else {
+                        __syncwarp();
+                        float* dw = reinterpret_cast<float*>(a.dw) + o0 * a.dw_stride + col + lane;
+                        const int rows = (int)max((int64_t)0, min((int64_t)32, a.O - o0));
+                        if (col + lane < a.I)
+#pragma unroll 8
+                            for (int r = 0; r < rows; ++r)
+                                dw[r * a.dw_stride] = __uint_as_float(lds32(strip_s + (uint32_t)r * 128u + ((((uint32_t)lane >> 2) ^ ((uint32_t)r & 7u)) << 4) + ((uint32_t)lane & 3u) * 4u));
+                        __syncwarp();
+                    }
+                }
+            } else {
+                if constexpr (W16) {
+#pragma unroll
+                    for (int piece = 0; piece < 2; ++piece) {
+                        if (lane == 0) bulk_wait_group_read0();
+                        __syncwarp();
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const float2* u = acc + piece * 32 + 4 * j;
+                            sts128(strip_s + (uint32_t)lane * 128u + (((uint32_t)j ^ ((uint32_t)lane & 7u)) << 4), narrow2<DT>(u[0].x, u[0].y), narrow2<DT>(u[1].x, u[1].y),
+                                   narrow2<DT>(u[2].x, u[2].y), narrow2<DT>(u[3].x, u[3].y));
+                        }
+                        const int64_t col = i0 + piece * 64;
+                        if (a.dw_vec && (a.I % 8 == 0 || col + 64 <= a.I)) {
+                            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                            __syncwarp();
+                            if (lane == 0) {
+                                if (o0 < a.O && col < a.I) tma_store_2d(&dwmap, strip_s, (int32_t)col, (int32_t)o0);
+                                bulk_commit_group();
+                            }
+                        } else {
+                            __syncwarp();
+                            uint16_t* dw = reinterpret_cast<uint16_t*>(a.dw) + o0 * a.dw_stride + col + lane;
+                            const int rows = (int)max((int64_t)0, min((int64_t)32, a.O - o0));
+#pragma unroll
+                            for (int q = 0; q < 2; ++q) {
+                                const uint32_t b = (uint32_t)(lane + 32 * q) * 2u;
+                                if (col + lane + 32 * q < a.I)
+#pragma unroll 8
+                                    for (int r = 0; r < rows; ++r)
+                                        dw[r * a.dw_stride + 32 * q] = (uint16_t)lds16(strip_s + (uint32_t)r * 128u + (((b >> 4) ^ ((uint32_t)r & 7u)) << 4) + (b & 15u));
+                            }
+                            __syncwarp();
+                        }
+                    }
+                }
+            }
+            n += len;
+            at = 0;
+            ++tile;
+        }
+        if (lane == 0) bulk_wait_group0();                   // no store may still be reading this CTA's shared memory at exit
+    } else {
+        // ------------------------------------------------------------ restored operand, sums of dy
+        setmaxnreg_dec<kGradRegsFill>();
+        const int t = (int)threadIdx.x - kFillWarp0 * 32;    // 0 .. 255
+        const uint32_t full0 = map_to_cta(smem_u32(&g->full[0]), 0), empty_s = smem_u32(&g->empty[0]), met_s = smem_u32(&g->met);
+        // sixteen codes a thread and token: tokens t / 8 and t / 8 + 32, channels 16 (t & 7) ..; eight lanes write eight different 16-byte columns at a time
+        const int tk = t >> 3, ch = t & 7;
+        const uint32_t half = (uint32_t)ch >> 2;
+        uint32_t to[2][2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const uint32_t row = (uint32_t)(tk + 32 * q), col = 2u * ((uint32_t)ch & 3u) + ((uint32_t)j ^ half);
+                to[q][j] = ring_s + kGradOperand + half * kGradHalf + row * 128u + ((col ^ (row & 7u)) << 4);
+            }
+        const bool second = half != 0;                       // which of its two 16-byte columns a thread writes first
+        struct Item { uint4 code[2]; float scale[2]; };
+        int ltile = tile, ltok = (int)(at % a.stages_part), lpart = (int)(at / a.stages_part);   // the next stage to load
+        int64_t left = end - begin;
+        const auto load = [&](Item& v) {
+            const int to_ = ltile / a.tiles_i, block = 2 * (ltile - to_ * a.tiles_i) + (int)rank;
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const int64_t m = (int64_t)ltok * kTok + tk + 32 * q;
+                v.code[q] = make_uint4(0, 0, 0, 0);
+                v.scale[q] = 0.f;
+                if (left > 0 && m < a.M && block < a.Kb) {
+                    v.code[q] = __ldg(reinterpret_cast<const uint4*>(a.xcodes + (m * a.Kb + block) * 128) + ch);
+                    v.scale[q] = __ldg(a.xscale + m * a.Kb + block);
+                }
+            }
+            --left;
+            if (++ltok == a.stages_part) {
+                ltok = 0;
+                if (++lpart == a.parts) { lpart = 0; ++ltile; }
+            }
+        };
+        uint32_t s = 0, ph = 1;
+        // db: 8 outputs x 4 tokens a thread of the first tile of channels
+        float sum[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] = 0.f;
+        int64_t n = begin;
+        bool any = false;
+        const auto stage = [&](Item& v) {
+            fp8_wait(empty_s + s * 8, ph, c, a.status, 6u);
+            if (c->abort_flag) return false;
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                uint32_t r[8];
+                restore4(v.code[q].x, v.scale[q], r[0], r[1]);
+                restore4(v.code[q].y, v.scale[q], r[2], r[3]);
+                restore4(v.code[q].z, v.scale[q], r[4], r[5]);
+                restore4(v.code[q].w, v.scale[q], r[6], r[7]);
+                const uint32_t d = s * kGradStage;
+                sts128(to[q][0] + d, second ? r[4] : r[0], second ? r[5] : r[1], second ? r[6] : r[2], second ? r[7] : r[3]);
+                sts128(to[q][1] + d, second ? r[0] : r[4], second ? r[1] : r[5], second ? r[2] : r[6], second ? r[3] : r[7]);
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            grad_arrive(full0 + s * 8, lane);
+            if (++s == kGradStages) { s = 0; ph ^= 1; }
+            load(v);
+            // sums of dy, where this tile is the first of its outputs
+            const int to_ = tile / a.tiles_i;
+            if (a.db && tile == to_ * a.tiles_i) {
+                const int part = (int)(at / a.stages_part);
+                const int64_t col = (int64_t)to_ * 256 + rank * 128 + 8 * (t & 15), row = (at - (int64_t)part * a.stages_part) * kTok + (t >> 4);
+                const uint16_t* src = a.dy + (part * a.rows_part + row) * a.dy_stride + col;
+                any = true;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    if (col < a.O && row + 16 * q < a.M) {
+                        const uint4 u = __ldg(reinterpret_cast<const uint4*>(src + 16 * q * a.dy_stride));
+                        float f[8];
+                        widen_vec<TDQ_BF16>(u, f);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) sum[j] += f[j];
+                    }
+                }
+            }
+            ++n;
+            ++at;
+            if (any && (at == per_tile || n == end)) {       // this cluster's part of the column sums is complete
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 16);
+                if (lane < 16) {
+#pragma unroll
+                    for (int j = 0; j < 8; j += 4)
+                        *reinterpret_cast<float4*>(db_room + (warp - kFillWarp0) * 128 + 8 * lane + j) = make_float4(sum[j], sum[j + 1], sum[j + 2], sum[j + 3]);
+                }
+                __syncwarp();
+                mbar_arrive_lane0_s(met_s, lane);
+                fp8_wait(met_s, 0u, c, a.status, 7u);
+                const int64_t first = n - at;                // the tile's first stage
+                if (t < 128) {
+                    float v2 = 0.f;
+#pragma unroll
+                    for (int i = 0; i < kFillWarps; ++i) v2 += db_room[i * 128 + t];
+                    const int64_t o = (int64_t)to_ * 256 + rank * 128 + t;
+                    if (first >= begin && at == per_tile) {
+                        if (o < a.O) a.db[o] = v2;
+                    } else {
+                        a.dbpart[(int64_t)(2 * w + (first <= begin ? 0 : 1)) * 256 + rank * 128 + t] = v2;
+                    }
+                }
+                __syncwarp();
+                mbar_arrive_lane0_s(met_s, lane);
+                fp8_wait(met_s, 1u, c, a.status, 7u);
+                any = false;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum[j] = 0.f;
+            }
+            if (at == per_tile) { at = 0; ++tile; }
+            return true;
+        };
+        Item u, v;
+        load(u);
+        load(v);
+        while (n < end) {
+            if (!stage(u)) break;
+            if (n >= end || !stage(v)) break;
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (c->abort_flag) __nanosleep(1000000);                 // a wait gave up: give copies and tensor core a moment
+    fp8_cluster_sync();                                      // neither CTA leaves while the other may still signal it
+    if (warp == 2)
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "n"(512) : "memory");
+}
+
+// Adds the parts of the tiles that were cut, in order of the sum: a thread block for 32 rows of a tile.
+template <int DT>
+__global__ void __launch_bounds__(256) grad_parts_kernel(const GradArgs a) {
+    pdl_wait();
+    pdl_trigger();
+    const int tile = (int)blockIdx.x >> 3, band = (int)blockIdx.x & 7;
+    const int64_t per_tile = (int64_t)a.stages_part * a.parts, total = per_tile * a.tiles_o * a.tiles_i, first = tile * per_tile;
+    const int32_t w0 = piece_owner(total, a.clusters, first), w1 = piece_owner(total, a.clusters, first + per_tile - 1);
+    if (w0 == w1) return;                                    // stored by the one that added it
+    const int to = tile / a.tiles_i, ti = tile - to * a.tiles_i;
+    const auto slot = [&](int32_t w) { return (int64_t)2 * w + (piece_begin(total, a.clusters, w) < first ? 1 : 0); };
+    const int64_t i = (int64_t)ti * 256 + 4 * (threadIdx.x & 63);
+    const int left = (int)min((int64_t)4, a.I - i);
+#pragma unroll 2
+    for (int r = band * 32 + ((int)threadIdx.x >> 6); r < band * 32 + 32; r += 4) {
+        const int64_t o = (int64_t)to * 256 + r;
+        if (o >= a.O || left <= 0) break;
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+        for (int32_t w = w0; w <= w1; ++w) {
+            const float4 v = *reinterpret_cast<const float4*>(a.part + (slot(w) * 256 + r) * 256 + 4 * (threadIdx.x & 63));
+            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        }
+        const float f[4] = {s.x, s.y, s.z, s.w};
+        if constexpr (DT == TDQ_F32) {
+            float* dw = reinterpret_cast<float*>(a.dw) + o * a.dw_stride + i;
+            if (a.dw_vec && left == 4) *reinterpret_cast<float4*>(dw) = s;
+            else
+                for (int j = 0; j < left; ++j) dw[j] = f[j];
+        } else {
+            uint16_t* dw = reinterpret_cast<uint16_t*>(a.dw) + o * a.dw_stride + i;
+            const uint32_t lo = narrow2<DT>(f[0], f[1]), hi = narrow2<DT>(f[2], f[3]);
+            if (a.dw_vec && left == 4) *reinterpret_cast<uint2*>(dw) = make_uint2(lo, hi);
+            else
+                for (int j = 0; j < left; ++j) dw[j] = (uint16_t)((j & 2 ? hi : lo) >> (16 * (j & 1)));
+        }
+    }
+    if (a.db && ti == 0 && threadIdx.x < 32) {
+        const int r = band * 32 + (int)threadIdx.x;
+        const int64_t o = (int64_t)to * 256 + r;
+        float s = 0.f;
+        for (int32_t w = w0; w <= w1; ++w) s += a.dbpart[slot(w) * 256 + r];
+        if (o < a.O) a.db[o] = s;
+    }
+}
+
+// dy as `PARTS` bf16 addends, [PARTS][rows_part][stride], rows behind M zero: the leading eight bits of what is left, cut off, each time; exact.  A value
+// without a number goes to the first addend alone.
+template <int DT, int PARTS>
+__global__ void __launch_bounds__(256) grad_addends_kernel(const void* dy, int64_t M, int64_t O, int64_t stride, uint16_t* __restrict__ out, int64_t rows_part, int64_t out_stride) {
+    using E = typename Elem<DT>::T;
+    pdl_wait();
+    pdl_trigger();
+    const int64_t vecs = out_stride / 8, n = rows_part * vecs;
+    for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < n; u += (int64_t)gridDim.x * 256) {
+        const int64_t m = u / vecs, o = (u - m * vecs) * 8;
+        const E* src = reinterpret_cast<const E*>(dy) + m * stride + o;
+        float f[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = m < M && o + j < O ? widen<DT>(src[j]) : 0.f;
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+            uint32_t r[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t b[2];
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    float& v = f[2 * j + q];
+                    if (fabsf(v) < INFINITY) {
+                        const float lead = PARTS == 1 ? v : __uint_as_float(__float_as_uint(v) & 0xffff0000u);
+                        b[q] = __float_as_uint(lead) >> 16;
+                        v -= lead;
+                    } else {
+                        b[q] = narrow2<TDQ_BF16>(v, 0.f) & 0xffffu;
+                        v = 0.f;
+                    }
+                }
+                r[j] = b[0] | b[1] << 16;
+            }
+            *reinterpret_cast<uint4*>(out + (p * rows_part + m) * out_stride + o) = make_uint4(r[0], r[1], r[2], r[3]);
+        }
+    }
+}
+
+// dy [rows][cols] bf16 in boxes of 64 tokens x 64 outputs, 128-byte swizzle
+bool grad_operand_map(CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int64_t stride) {
+    return encode_y_map(map, const_cast<void*>(p), true, rows, cols, stride, 64, kTok, false);
+}
+
+struct GradPlan {
+    int parts;                 // addends of dy
+    bool copied;               // dy passes through the workspace
+    int64_t rows_part, dy_stride, stages_part, tiles_o, tiles_i, total;
+    int32_t clusters;
+    bool cut;                  // some tile is added by more than one cluster
+    size_t dy_bytes, part_bytes, db_bytes, bytes;
+};
+// How the work is cut, and the room that takes: the status word, parts of tiles and of db, dy's addends.
+GradPlan grad_plan(const void* dy, tdq_dtype dtype, int64_t dy_stride, int64_t M, int64_t O, int64_t I, int n_sm) {
+    GradPlan p = {};
+    p.parts = dtype == TDQ_BF16 ? 1 : dtype == TDQ_F16 ? 2 : 3;
+    p.copied = dtype != TDQ_BF16 || reinterpret_cast<uintptr_t>(dy) % 16 || (M > 1 && dy_stride % 8);
+    p.stages_part = (M + kTok - 1) / kTok;
+    p.rows_part = p.stages_part * kTok;
+    p.dy_stride = p.copied || M <= 1 ? (O + 7) / 8 * 8 : dy_stride;
+    p.tiles_o = (O + 255) / 256;
+    p.tiles_i = (I + 255) / 256;
+    const int64_t tiles = p.tiles_o * p.tiles_i, per_tile = p.stages_part * p.parts;
+    p.total = tiles * per_tile;
+    const int64_t pairs = std::max(1, n_sm / 2);
+    p.clusters = (int32_t)std::min<int64_t>(pairs, std::max<int64_t>(1, p.total));
+    p.cut = p.total % p.clusters != 0 || p.total / p.clusters % per_tile != 0;
+    p.dy_bytes = p.copied ? (size_t)(p.parts * p.rows_part * p.dy_stride) * 2 : 0;
+    p.part_bytes = p.cut ? (size_t)2 * p.clusters * 256 * 256 * 4 : 0;
+    p.db_bytes = p.cut ? (size_t)2 * p.clusters * 256 * 4 : 0;
+    p.bytes = kWorkspaceHeader + p.part_bytes + p.db_bytes + p.dy_bytes;
+    return p;
+}
+
+template <int DT>
+tdq_status launch_grad(const GradArgs& a, const GradPlan& p, const CUtensorMap& dymap, const CUtensorMap& dwmap, const CUtensorMap& partmap, int dev, cudaStream_t st) {
+    static std::atomic<uint64_t> smem_done{0};
+    if (allow_smem(fp8_grad_kernel<DT>, (int)kGradSmem, smem_done, dev) != cudaSuccess) return TDQ_ERR_CUDA;
+    if (launch_pdl(fp8_grad_kernel<DT>, dim3(2 * (unsigned)p.clusters), dim3(kGradThreads), kGradSmem, st, a, dymap, dwmap, partmap) != cudaSuccess) return TDQ_ERR_CUDA;
+    g_launch_count.fetch_add(1, std::memory_order_relaxed);
+    if (p.cut) {
+        if (launch_pdl(grad_parts_kernel<DT>, dim3((unsigned)(p.tiles_o * p.tiles_i * 8)), dim3(256), 0, st, a) != cudaSuccess) return TDQ_ERR_CUDA;
+        g_launch_count.fetch_add(1, std::memory_order_relaxed);
+    }
+    return TDQ_OK;
+}
+template <int DT, int PARTS>
+cudaError_t launch_addends(const void* dy, int64_t M, int64_t O, int64_t stride, uint16_t* out, const GradPlan& p, int n_sm, cudaStream_t st) {
+    const int64_t blocks = (p.rows_part * (p.dy_stride / 8) + 255) / 256;
+    return launch_pdl(grad_addends_kernel<DT, PARTS>, dim3((unsigned)std::min<int64_t>(blocks, 16 * n_sm)), dim3(256), 0, st, dy, M, O, stride, out, p.rows_part, p.dy_stride);
+}
+constexpr int64_t kGradMax = INT32_MAX - 512;               // coordinates of the copies are 32-bit
+
+}  // namespace
+}  // namespace tdq
+
+using namespace tdq;
+
+extern "C" size_t tdq_fp8_weight_grad_workspace_bytes(const void* dy, tdq_dtype dy_dtype, int64_t dy_row_stride, int64_t M, int64_t O, int64_t I) {
+    if (!known_dtype(dy_dtype) || M < 0 || O < 0 || I <= 0 || M > kGradMax / 3 || O > kGradMax || I > kGradMax) return 0;
+    if (M == 0 || O == 0) return kWorkspaceHeader;
+    const int n_sm = current_device_sm_count();
+    return grad_plan(dy, dy_dtype, dy_row_stride, M, O, I, n_sm > 0 ? n_sm : 148).bytes;
+}
+
+extern "C" tdq_status tdq_fp8_weight_grad(const void* dy, tdq_dtype dy_dtype, int64_t dy_row_stride, const uint8_t* xcodes, const float* xscale, int64_t M,
+                                          int64_t O, int64_t I, void* dw, tdq_dtype dw_dtype, int64_t dw_row_stride, float* db, void* workspace,
+                                          size_t workspace_bytes, void* cuda_stream) {
+    if (!known_dtype(dy_dtype) || !known_dtype(dw_dtype) || M < 0 || O < 0 || I <= 0 || dy_row_stride < O || dw_row_stride < I) return TDQ_ERR_INVALID_ARG;
+    if (O == 0) return TDQ_OK;
+    if (!dw || (M > 0 && (!dy || !xcodes || !xscale))) return TDQ_ERR_INVALID_ARG;
+    const uintptr_t ysz = dy_dtype == TDQ_F32 ? 4 : 2, wsz = dw_dtype == TDQ_F32 ? 4 : 2;
+    if (off_grid(dy, ysz) || off_grid(xcodes, 16) || off_grid(xscale, 4) || off_grid(dw, wsz) || off_grid(db, 4) || off_grid(workspace, 16)) return TDQ_ERR_ALIGNMENT;
+    if (M > kGradMax / 3 || O > kGradMax || I > kGradMax || dy_row_stride > INT64_MAX / 8 || dw_row_stride > INT64_MAX / 8) return TDQ_ERR_UNSUPPORTED;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+    if (M == 0) {
+        if (cudaMemset2DAsync(dw, (size_t)dw_row_stride * wsz, 0, (size_t)I * wsz, (size_t)O, st) != cudaSuccess) return TDQ_ERR_CUDA;
+        if (db && cudaMemsetAsync(db, 0, (size_t)O * 4, st) != cudaSuccess) return TDQ_ERR_CUDA;
+        return TDQ_OK;
+    }
+    int dev = 0;
+    const int n_sm = current_device_sm_count(&dev);
+    if (n_sm <= 0) return TDQ_ERR_CUDA;
+    const GradPlan p = grad_plan(dy, dy_dtype, dy_row_stride, M, O, I, n_sm);
+    if (p.tiles_o * p.tiles_i > INT32_MAX / 8 || p.parts * p.rows_part > kGradMax) return TDQ_ERR_UNSUPPORTED;
+    if (!workspace || workspace_bytes < p.bytes) return TDQ_ERR_WORKSPACE;
+    uint8_t* ws = reinterpret_cast<uint8_t*>(workspace);
+    GradArgs a = {};
+    a.xcodes = xcodes; a.xscale = xscale; a.dw = dw; a.db = db; a.M = M; a.O = O; a.I = I;
+    a.status = reinterpret_cast<uint32_t*>(ws);
+    a.part = reinterpret_cast<float*>(ws + kWorkspaceHeader);
+    a.dbpart = reinterpret_cast<float*>(ws + kWorkspaceHeader + p.part_bytes);
+    a.dy_stride = p.dy_stride; a.dw_stride = dw_row_stride; a.rows_part = p.rows_part;
+    a.Kb = (int32_t)fp8_blocks(I); a.tiles_o = (int32_t)p.tiles_o; a.tiles_i = (int32_t)p.tiles_i; a.stages_part = (int32_t)p.stages_part; a.parts = p.parts;
+    a.clusters = p.clusters;
+    a.dw_vec = on_grid(dw, dw_row_stride, O, (int64_t)wsz);
+    a.dy = reinterpret_cast<const uint16_t*>(dy);
+    if (p.copied) {
+        uint16_t* out = reinterpret_cast<uint16_t*>(ws + kWorkspaceHeader + p.part_bytes + p.db_bytes);
+        a.dy = out;
+        const cudaError_t e = dy_dtype == TDQ_BF16 ? launch_addends<TDQ_BF16, 1>(dy, M, O, dy_row_stride, out, p, n_sm, st)
+                            : dy_dtype == TDQ_F16  ? launch_addends<TDQ_F16, 2>(dy, M, O, dy_row_stride, out, p, n_sm, st)
+                                                   : launch_addends<TDQ_F32, 3>(dy, M, O, dy_row_stride, out, p, n_sm, st);
+        if (e != cudaSuccess) return TDQ_ERR_CUDA;
+        g_launch_count.fetch_add(1, std::memory_order_relaxed);
+    }
+    CUtensorMap dymap, dwmap, partmap;
+    memset(&dwmap, 0, sizeof dwmap);
+    memset(&partmap, 0, sizeof partmap);
+    if (!grad_operand_map(&dymap, a.dy, p.copied ? p.parts * p.rows_part : M, p.copied ? p.dy_stride : O, p.dy_stride)) return TDQ_ERR_CUDA;
+    const int64_t w_stride = O > 1 ? dw_row_stride : (I + 7) / 8 * 8;
+    if (a.dw_vec && !encode_y_map(&dwmap, dw, wsz == 2, O, I, w_stride, wsz == 2 ? 64 : 32, 32, dw_dtype == TDQ_F16)) a.dw_vec = 0;
+    if (p.cut && !encode_y_map(&partmap, a.part, false, (int64_t)2 * p.clusters * 256, 256, 256, 32, 32)) return TDQ_ERR_CUDA;
+    return dw_dtype == TDQ_F32 ? launch_grad<TDQ_F32>(a, p, dymap, dwmap, partmap, dev, st)
+         : dw_dtype == TDQ_BF16 ? launch_grad<TDQ_BF16>(a, p, dymap, dwmap, partmap, dev, st)
+                                : launch_grad<TDQ_F16>(a, p, dymap, dwmap, partmap, dev, st);
+}

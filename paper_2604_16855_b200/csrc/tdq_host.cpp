@@ -671,6 +671,34 @@ PyObject* layer_norm_backward(PyObject* const* a) {
     return tuple_of({out, dw, db});
 }
 
+// fp8_weight_grad(dy, xcodes, xscale, cin, out_dtype, bias, dw, db, workspace)  ->  (dw, db or None)
+PyObject* fp8_weight_grad(PyObject* const* a) {
+    const at::Tensor &dy0 = tensor(a[0]), &xc = tensor(a[1]), &xs = tensor(a[2]);
+    const at::Tensor *odw = opt_tensor(a[6]), *odb = opt_tensor(a[7]), *ow = opt_tensor(a[8]);
+    need_cuda({&dy0, &xc, &xs, odw, odb, ow});
+    const Rows dy = rows_of("dy", dy0, true);
+    const tdq_dtype dt = dtype_id(dy0);
+    const int64_t I = int_arg(a[3]), M = dy.M, O = dy.C;
+    if (I < 1) throw Bad{PyExc_ValueError, "cin must be positive"};
+    const int64_t K = fp8_blocks(I);
+    check_tensor("xcodes", xc, {at::kFloat8_e4m3fn, at::kByte}, {M, K * kFp8Block}, dy0);
+    check_tensor("xscale", xs, {at::kFloat}, {M, K}, dy0);
+    const at::Tensor dw = odw ? *odw : new_like(dy0, {O, I}, dtype_arg(a[4]));
+    if (dw.dim() != 2 || dw.size(0) != O || dw.size(1) != I || (I > 1 && dw.stride(1) != 1))
+        throw Bad{PyExc_ValueError, "dw must be of size [" + std::to_string(O) + ", " + std::to_string(I) + "], its columns adjacent in memory"};
+    if (dw.device() != dy0.device()) throw Bad{PyExc_ValueError, "dw is on " + dw.device().str() + ", not on " + dy0.device().str()};
+    const tdq_dtype wt = dtype_id(dw);
+    const bool bias = truth(a[5]);
+    if (!bias && odb) throw Bad{PyExc_ValueError, "db was given and bias is False"};
+    const at::Tensor db = bias ? vector_of("db", odb, O, dy0) : at::Tensor();
+    const Scratch ws(ow, dy0, [&] { return tdq_fp8_weight_grad_workspace_bytes(dy.p(), dt, dy.stride, M, O, I); });
+    check(call(dy0, [&](void* st) {
+              return tdq_fp8_weight_grad(dy.p(), dt, dy.stride, ptr<uint8_t>(xc), ptr<float>(xs), M, O, I, ptr(dw), wt, O > 1 ? dw.stride(0) : I,
+                                         bias ? ptr<float>(db) : nullptr, ws.p, ws.bytes, st);
+          }), "tdq_fp8_weight_grad");
+    return tuple_of({dw, db});
+}
+
 // Argument count, and C++ exceptions as Python ones.
 template <PyObject* (*F)(PyObject* const*), int N>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -700,6 +728,7 @@ PyMethodDef methods[] = {
     TDQ_ENTRY(w4a4_linear, 11), TDQ_ENTRY(w4a4_linear_static, 8), TDQ_ENTRY(quant_linear_fused, 8), TDQ_ENTRY(quant_linear_host, 7),
     TDQ_ENTRY(quantize_act_fp8, 4), TDQ_ENTRY(quantize_weight_fp8, 3), TDQ_ENTRY(fp8_linear, 8), TDQ_ENTRY(qk_norm_rope, 11),
     TDQ_ENTRY(layer_norm, 7), TDQ_ENTRY(layer_norm_fp8, 9), TDQ_ENTRY(layer_norm_backward, 10),
+    TDQ_ENTRY(fp8_weight_grad, 9),
     {"set_error_class", set_error_class, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 #undef TDQ_ENTRY
 

@@ -73,3 +73,21 @@ def test_binding_refuses_cpu_tensors(tdq):
     for f in (lambda: tdq.layer_norm(x), lambda: tdq.layer_norm_fp8(x), lambda: tdq.layer_norm_backward(x, x, v, v), lambda: tdq.quantize_act_fp8(x, pow2=True)):
         with pytest.raises(ValueError):
             f()
+
+
+def test_weight_grad(tdq):
+    inv, ali, uns = tdq.ERR_INVALID_ARG, tdq.ERR_ALIGNMENT, tdq.ERR_UNSUPPORTED
+    f, size = tdq.lib().tdq_fp8_weight_grad, tdq.lib().tdq_fp8_weight_grad_workspace_bytes
+    #       dy    dt st  xc    xs    M   O   I   dw    dt st   db    ws    bytes    stream
+    good = [FAKE, 1, 40, FAKE, FAKE, 64, 40, 90, FAKE, 0, 96, FAKE, FAKE, 1 << 40, None]
+    _each(f, good, [((i, v), c) for i, v, c in
+                    [(i, None, inv) for i in (0, 3, 4, 8)] + [(i, ODD, ali) for i in (0, 3, 4, 8, 11, 12)] +
+                    [(3, OFF4, ali), (12, OFF4, ali), (1, 3, inv), (9, -1, inv), (2, 39, inv), (10, 89, inv), (5, -1, inv), (6, -1, inv), (7, 0, inv),
+                     (5, 1 << 30, uns), (6, 0, tdq.OK)]])
+    _each(f, good, [((6, 1 << 31), (2, 1 << 31), uns), ((7, 1 << 31), (10, 1 << 31), uns)])
+    head = int(size(FAKE, 1, 40, 0, 40, 90))
+    assert head == 256 and size(FAKE, 3, 40, 64, 40, 90) == size(FAKE, 1, 40, -1, 40, 90) == size(FAKE, 1, 40, 64, 40, 0) == 0
+    # one stage, one tile: nothing is cut; fp16 and rows off the grid pass through the workspace
+    assert size(FAKE, 1, 40, 64, 40, 90) == 256 and size(FAKE, 1, 41, 64, 40, 90) == 256 + 64 * 40 * 2
+    two = 2 * 2 * 256 * (256 + 1) * 4                        # two stages, two clusters with two places each
+    assert size(FAKE, 1, 40, 65, 40, 90) == 256 + two and size(FAKE, 2, 40, 64, 40, 90) == 256 + two + 2 * 64 * 40 * 2
