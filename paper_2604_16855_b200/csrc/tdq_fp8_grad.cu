@@ -23,7 +23,7 @@ namespace tdq {
 namespace {
 
 constexpr int kTok = 64;                                  // tokens a stage
-constexpr int kGradStages = 5;
+constexpr int kGradStages = 6;
 constexpr int kGroup = 8;                                 // stages whose products an accumulator adds
 constexpr uint32_t kGradOperand = kTok * 128 * 2;         // bytes: two halves of 64 columns, 128 bytes a token
 constexpr uint32_t kGradHalf = kTok * 128;
@@ -32,10 +32,11 @@ constexpr uint32_t kGradCtrl = 1024;
 constexpr uint32_t kGradStrip = 32 * 128;
 constexpr int kSumWarp0 = 4, kSumWarps = 8, kFillWarp0 = 12, kFillWarps = 8;
 constexpr int kGradThreads = (kFillWarp0 + kFillWarps) * 32;
-constexpr uint32_t kGradDb = kFillWarps * 128 * 4;
+constexpr int kFillPairs = kFillWarps / 2;               // two warps fill a stage, every fourth one
+constexpr uint32_t kGradDb = kFillPairs * 128 * 4;
 constexpr uint32_t kGradSmem = kGradCtrl + kGradStages * kGradStage + kSumWarps * kGradStrip + kGradDb;
 static_assert(kGradSmem <= (uint32_t)kSmemLimit, "shared memory");
-constexpr int kGradRegsLoad = 32, kGradRegsSum = 168, kGradRegsFill = 56;   // 128 * 32 + 256 * 168 + 256 * 56 <= 640 * 96
+constexpr int kGradRegsLoad = 32, kGradRegsSum = 160, kGradRegsFill = 64;   // 128 * 32 + 256 * 160 + 256 * 64 <= 640 * 96
 // D binary32, both operands bf16 with the sum's axis slow, 256 columns x 256 rows
 constexpr uint32_t kGradIdesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((256u >> 3) << 17) | ((256u >> 4) << 24);
 constexpr uint32_t kGradDescLo = (kGradHalf >> 4) << 16;  // the next 64 columns; eight tokens further on are 1024 bytes (kSwDescHi)
@@ -55,22 +56,52 @@ struct GradArgs {
     uint32_t* status;
 };
 struct GradCtrl {
-    uint64_t full[kGradStages], empty[kGradStages];
+    uint64_t landed[kGradStages];                            // this CTA's dy
+    uint64_t full[kGradStages];                              // CTA 0: both CTAs' operands
+    uint64_t empty[kGradStages];
     uint64_t tfull[2], tempty[2];
     uint64_t met;                                            // the restoring warps meet, twice for each sum of db
 };
 static_assert(sizeof(Ctrl) + sizeof(GradCtrl) <= kGradCtrl, "control block outgrew its reservation");
 
-// stages [first, last) of the row of all tiles' stages that cluster w adds
-__host__ __device__ inline int64_t piece_begin(int64_t total, int32_t clusters, int32_t w) { return total / clusters * w + min((int64_t)w, total % clusters); }
+// the first of the row of all tiles' stages that cluster w adds
+__host__ __device__ inline int32_t piece_begin(int32_t total, int32_t clusters, int32_t w) { return total / clusters * w + min(w, total % clusters); }
 // the cluster that adds stage s
-__host__ __device__ inline int32_t piece_owner(int64_t total, int32_t clusters, int64_t s) {
-    const int64_t q = total / clusters, r = total % clusters, longer = r * (q + 1);
-    return (int32_t)(s < longer ? s / (q + 1) : r + (s - longer) / q);
+__host__ __device__ inline int32_t piece_owner(int32_t total, int32_t clusters, int32_t s) {
+    const int32_t q = total / clusters, r = total % clusters, longer = r * (q + 1);
+    return s < longer ? s / (q + 1) : r + (s - longer) / q;
 }
+// A cluster's stages, tile by tile, in the order in which it adds them: the tile at its end first, which begins with the first tokens, then the rest, which begins in the
+// middle of a tile.  So all clusters go through the tokens at about the same time, and what several tiles read is read from memory once (from the piece's
+// begin on instead: 16384 tokens, 1024 -> 4096 bf16 TODO us).
+struct Piece {
+    int32_t per_tile, begin, end, last;                      // last: where its last tile's stages begin, if it has more than one tile; else its end
+    __device__ Piece(int32_t per_tile_, int32_t total, int32_t clusters, int32_t w)
+        : per_tile(per_tile_), begin(piece_begin(total, clusters, w)), end(piece_begin(total, clusters, w + 1)) {
+        const int32_t t = (end - 1) / per_tile * per_tile;
+        last = t > begin ? t : end;
+    }
+    __device__ int32_t stages() const { return end - begin; }
+    // the k-th stage that is added
+    __device__ int32_t stage(int32_t k) const { return k < end - last ? last + k : begin + k - (end - last); }
+};
+// the stages of one tile: k .. k + len - 1 of the piece's order, from stage `at` of the tile on
+struct Stretch {
+    int32_t tile, at, len;
+    bool whole;
+    int32_t slot;                                            // of the cluster's two places for parts
+    __device__ Stretch(const Piece& p, int32_t k) {
+        const int32_t s = p.stage(k);
+        tile = s / p.per_tile;
+        at = s - tile * p.per_tile;
+        len = min(p.per_tile - at, (k < p.end - p.last ? p.end : p.last) - s);
+        whole = len == p.per_tile;
+        slot = s == p.begin ? 0 : 1;
+    }
+};
 
 __device__ __forceinline__ void grad_load(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, uint32_t bar) {
-    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                  ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void grad_mma(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t accumulate) {
@@ -81,10 +112,20 @@ __device__ __forceinline__ void grad_commit(uint32_t bar_s) {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                  ::"r"(bar_s), "h"((uint16_t)3) : "memory");
 }
-// lane 0 of a converged warp arrives on a barrier of either CTA, given by its cluster address; what the warp wrote before is seen by who waits there
+// Lane 0 of a converged warp arrives on a barrier of either CTA, given by its cluster address.  Not with release at cluster scope, which waits for all
+// that the thread has in flight (5000 clocks a stage instead of 700): what a restoring warp wrote is in its own CTA's shared memory, ordered by the proxy fence.
 __device__ __forceinline__ void grad_arrive(uint32_t bar_c, int lane) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %1, 0;\n\t@p mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n\t}"
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %1, 0;\n\t@p mbarrier.arrive.shared::cluster.b64 _, [%0];\n\t}"
                  ::"r"(bar_c), "r"(lane) : "memory");
+}
+// sixteen consecutive columns of this warp's 32 TMEM lanes, waited for: lane i receives row i
+__device__ __forceinline__ void tmem_ld16_wait(uint32_t taddr, uint32_t* v) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {"
+                 "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\ttcgen05.wait::ld.sync.aligned;"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+                   "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+                 : "r"(taddr)
+                 : "memory");
 }
 // four codes times their scale as four bf16, nearest even
 __device__ __forceinline__ void restore4(uint32_t codes, float scale, uint32_t& lo, uint32_t& hi) {
@@ -110,7 +151,7 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
     const uint32_t rank = fp8_cluster_rank();
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kGradStages; ++i) { mbar_init(&g->full[i], 1 + 2 * kFillWarps); mbar_init(&g->empty[i], 1); }
+        for (int i = 0; i < kGradStages; ++i) { mbar_init(&g->landed[i], 1); mbar_init(&g->full[i], 4); mbar_init(&g->empty[i], 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(&g->tfull[i], 1); mbar_init(&g->tempty[i], 2 * kSumWarps); }
         mbar_init(&g->met, kFillWarps);
         c->abort_flag = 0;
@@ -129,35 +170,35 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0u;
     const uint32_t tmem_base = c->tmem_base;
     const int32_t w = (int32_t)blockIdx.x / 2;
-    const int64_t per_tile = (int64_t)a.stages_part * a.parts, total = per_tile * a.tiles_o * a.tiles_i;
-    const int64_t begin = piece_begin(total, a.clusters, w), end = piece_begin(total, a.clusters, w + 1);
-    int tile = (int)(begin / per_tile);
-    int64_t at = begin - tile * per_tile;                    // stage of the tile
+    const int32_t per_tile = a.stages_part * a.parts;
+    const Piece piece(per_tile, per_tile * a.tiles_o * a.tiles_i, a.clusters, w);
+    const int32_t n_stages = piece.stages();
 
     if (warp < kSumWarp0) {
         setmaxnreg_dec<kGradRegsLoad>();
         if (warp == 0) {
             // -------------------------------------------------------- copies of dy
-            const uint32_t full0 = map_to_cta(smem_u32(&g->full[0]), 0), empty_s = smem_u32(&g->empty[0]);
+            const uint32_t landed_s = smem_u32(&g->landed[0]), empty_s = smem_u32(&g->empty[0]);
             uint32_t s = 0, ph = 1;
-            int part = (int)(at / a.stages_part), tok = (int)(at - (int64_t)part * a.stages_part);
+            for (int32_t k = 0; k < n_stages && !c->abort_flag;) {
+                const Stretch t(piece, k);
+                const int32_t o = t.tile / a.tiles_i * 256 + (int32_t)rank * 128;   // past the end: the map fills with zeros
+                int32_t part = t.at / a.stages_part, tok = t.at - part * a.stages_part;
 #pragma unroll 1
-            for (int64_t n = begin; n < end; ++n) {
-                fp8_wait(empty_s + s * 8, ph, c, a.status, 5u);
-                if (c->abort_flag) break;
-                if (elect_one()) {
-                    if (rank == 0) mbar_expect_tx(&g->full[s], 2 * kGradOperand);
-                    const int32_t o = tile / a.tiles_i * 256 + (int)rank * 128;   // past the end: the map fills with zeros
-                    const int32_t row = (int32_t)(part * a.rows_part) + tok * kTok;
-                    grad_load(ring_s + s * kGradStage, &dymap, o, row, full0 + s * 8);
-                    grad_load(ring_s + s * kGradStage + kGradHalf, &dymap, o + 64, row, full0 + s * 8);
+                for (int32_t i = 0; i < t.len; ++i) {
+                    fp8_wait(empty_s + s * 8, ph, c, a.status, 5u);
+                    if (c->abort_flag) break;
+                    if (elect_one()) {
+                        mbar_expect_tx(&g->landed[s], kGradOperand);
+                        const int32_t row = (int32_t)(part * a.rows_part) + tok * kTok;
+                        grad_load(ring_s + s * kGradStage, &dymap, o, row, landed_s + s * 8);
+                        grad_load(ring_s + s * kGradStage + kGradHalf, &dymap, o + 64, row, landed_s + s * 8);
+                    }
+                    __syncwarp();
+                    if (++s == kGradStages) { s = 0; ph ^= 1; }
+                    if (++tok == a.stages_part) { tok = 0; ++part; }
                 }
-                __syncwarp();
-                if (++s == kGradStages) { s = 0; ph ^= 1; }
-                if (++tok == a.stages_part) {
-                    tok = 0;
-                    if (++part == a.parts) { part = 0; ++tile; }
-                }
+                k += t.len;
             }
         } else if (warp == 1 && rank == 0) {
             // -------------------------------------------------------- instructions
@@ -165,31 +206,31 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
             const uint32_t xd0 = kGradDescLo | ((ring_s & 0x3FFFFu) >> 4);
             uint32_t s = 0, ph = 0, group = 0;
             bool on = true;
-            for (int64_t n = begin; n < end && on;) {
-                const int64_t len = min(min((int64_t)kGroup, per_tile - at), end - n);
-                const uint32_t slot = group & 1u;
-                fp8_wait(tempty_s + slot * 8, ((group >> 1) & 1u) ^ 1u, c, a.status, 3u);
+            for (int32_t k = 0; k < n_stages && on;) {
+                const Stretch t(piece, k);
+                for (int32_t i = 0; i < t.len && on; ++group) {
+                    const int32_t len = min(kGroup, t.len - i);
+                    const uint32_t slot = group & 1u;
+                    fp8_wait(tempty_s + slot * 8, ((group >> 1) & 1u) ^ 1u, c, a.status, 3u);
 #pragma unroll 1
-                for (int64_t j = 0; j < len; ++j) {
-                    fp8_wait(full_s + s * 8, ph, c, a.status, 4u);
-                    if (c->abort_flag) { on = false; break; }
-                    asm volatile("fence.acq_rel.cluster;" ::: "memory");   // the other CTA's restored operand too
-                    tc_fence_after();
-                    if (elect_one()) {
-                        const uint32_t lo = xd0 + s * (kGradStage >> 4);
-                        const uint64_t ad = (uint64_t)kSwDescHi << 32 | lo, bd = (uint64_t)kSwDescHi << 32 | (lo + (kGradOperand >> 4));
+                    for (int32_t j = 0; j < len; ++j) {
+                        fp8_wait(full_s + s * 8, ph, c, a.status, 4u);
+                        if (c->abort_flag) { on = false; break; }
+                        tc_fence_after();
+                        if (elect_one()) {
+                            const uint32_t lo = xd0 + s * (kGradStage >> 4);
+                            const uint64_t ad = (uint64_t)kSwDescHi << 32 | lo, bd = (uint64_t)kSwDescHi << 32 | (lo + (kGradOperand >> 4));
 #pragma unroll
-                        for (int k = 0; k < kTok / 16; ++k) grad_mma(tmem_base + slot * 256, ad + k * (2048 >> 4), bd + k * (2048 >> 4), j || k ? 1u : 0u);
-                        grad_commit(empty_s + s * 8);
-                        if (j == len - 1) grad_commit(tfull_s + slot * 8);
+                            for (int q = 0; q < kTok / 16; ++q) grad_mma(tmem_base + slot * 256, ad + q * (2048 >> 4), bd + q * (2048 >> 4), j || q ? 1u : 0u);
+                            grad_commit(empty_s + s * 8);
+                            if (j == len - 1) grad_commit(tfull_s + slot * 8);
+                        }
+                        __syncwarp();
+                        if (++s == kGradStages) { s = 0; ph ^= 1; }
                     }
-                    __syncwarp();
-                    if (++s == kGradStages) { s = 0; ph ^= 1; }
+                    i += len;
                 }
-                ++group;
-                n += len;
-                at += len;
-                if (at == per_tile) at = 0;
+                k += t.len;
             }
         }
     } else if (warp < kFillWarp0) {
@@ -200,36 +241,35 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
         const uint32_t tfull_s = smem_u32(&g->tfull[0]), tempty_c = map_to_cta(smem_u32(&g->tempty[0]), 0);
         const uint32_t tm0 = tmem_base + ((uint32_t)(quarter * 32) << 16) + h * 128;
         uint32_t group = 0;
-        for (int64_t n = begin; n < end && !c->abort_flag;) {
-            const int64_t len = min(per_tile - at, end - n);
+        for (int32_t k = 0; k < n_stages && !c->abort_flag;) {
+            const Stretch stretch(piece, k);
             float2 acc[64];
 #pragma unroll
             for (int j = 0; j < 64; ++j) acc[j] = make_float2(0.f, 0.f);
 #pragma unroll 1
-            for (int64_t done = 0; done < len; done += kGroup, ++group) {
+            for (int32_t done = 0; done < stretch.len; done += kGroup, ++group) {
                 const uint32_t slot = group & 1u;
                 fp8_wait(tfull_s + slot * 8, (group >> 1) & 1u, c, a.status, 2u);
                 if (c->abort_flag) break;
                 tc_fence_after();
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    uint32_t v[32];
-                    tmem_ld32(tm0 + slot * 256 + q * 32, v);
-                    tmem_ld_wait_on(v);
-                    if (q == 3) {
+                for (int q = 0; q < 8; ++q) {
+                    uint32_t v[16];
+                    tmem_ld16_wait(tm0 + slot * 256 + q * 16, v);
+                    if (q == 7) {
                         tc_fence_before();
                         __syncwarp();
                         grad_arrive(tempty_c + slot * 8, lane);
                     }
 #pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        acc[q * 16 + j] = __fadd2_rn(acc[q * 16 + j], make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])));
+                    for (int j = 0; j < 8; ++j)
+                        acc[q * 8 + j] = __fadd2_rn(acc[q * 8 + j], make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])));
                 }
             }
             if (c->abort_flag) break;
-            const int to = tile / a.tiles_i, ti = tile - to * a.tiles_i;
-            const bool whole = len == per_tile;
-            const int32_t slot = 2 * w + (n == begin ? 0 : 1);
+            const int to = stretch.tile / a.tiles_i, ti = stretch.tile - to * a.tiles_i;
+            const bool whole = stretch.whole;
+            const int32_t slot = 2 * w + stretch.slot;
             const int64_t o0 = (int64_t)to * 256 + rank * 128 + quarter * 32, i0 = (int64_t)ti * 256 + h * 128;
             if (!W16 || !whole) {
                 const CUtensorMap* map = whole ? &dwmap : &partmap;
@@ -300,134 +340,119 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
                     }
                 }
             }
-            n += len;
-            at = 0;
-            ++tile;
+            k += stretch.len;
         }
         if (lane == 0) bulk_wait_group0();                   // no store may still be reading this CTA's shared memory at exit
     } else {
         // ------------------------------------------------------------ restored operand, sums of dy
         setmaxnreg_dec<kGradRegsFill>();
-        const int t = (int)threadIdx.x - kFillWarp0 * 32;    // 0 .. 255
-        const uint32_t full0 = map_to_cta(smem_u32(&g->full[0]), 0), empty_s = smem_u32(&g->empty[0]), met_s = smem_u32(&g->met);
-        // sixteen codes a thread and token: tokens t / 8 and t / 8 + 32, channels 16 (t & 7) ..; eight lanes write eight different 16-byte columns at a time
-        const int tk = t >> 3, ch = t & 7;
-        const uint32_t half = (uint32_t)ch >> 2;
-        uint32_t to[2][2];
-#pragma unroll
-        for (int q = 0; q < 2; ++q)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const uint32_t row = (uint32_t)(tk + 32 * q), col = 2u * ((uint32_t)ch & 3u) + ((uint32_t)j ^ half);
-                to[q][j] = ring_s + kGradOperand + half * kGradHalf + row * 128u + ((col ^ (row & 7u)) << 4);
-            }
-        const bool second = half != 0;                       // which of its two 16-byte columns a thread writes first
-        struct Item { uint4 code[2]; float scale[2]; };
-        int ltile = tile, ltok = (int)(at % a.stages_part), lpart = (int)(at / a.stages_part);   // the next stage to load
-        int64_t left = end - begin;
-        const auto load = [&](Item& v) {
-            const int to_ = ltile / a.tiles_i, block = 2 * (ltile - to_ * a.tiles_i) + (int)rank;
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                const int64_t m = (int64_t)ltok * kTok + tk + 32 * q;
-                v.code[q] = make_uint4(0, 0, 0, 0);
-                v.scale[q] = 0.f;
-                if (left > 0 && m < a.M && block < a.Kb) {
-                    v.code[q] = __ldg(reinterpret_cast<const uint4*>(a.xcodes + (m * a.Kb + block) * 128) + ch);
-                    v.scale[q] = __ldg(a.xscale + m * a.Kb + block);
-                }
-            }
-            --left;
-            if (++ltok == a.stages_part) {
-                ltok = 0;
-                if (++lpart == a.parts) { lpart = 0; ++ltile; }
-            }
+        const int fw = warp - kFillWarp0, pair = fw >> 1, side = fw & 1;   // a warp restores 32 tokens and sums 64 outputs of every fourth stage
+        const uint32_t full0 = map_to_cta(smem_u32(&g->full[0]), 0), empty_s = smem_u32(&g->empty[0]), landed_s = smem_u32(&g->landed[0]);
+        const uint32_t met_s = smem_u32(&g->met);
+        // Sixteen codes a lane and token: tokens 4 q + lane / 8, channels 16 (lane & 7) ..; eight lanes write eight different 16-byte columns at a time, the second
+        // half of them its second column first
+        const uint32_t ch = (uint32_t)lane & 7u, half = ch >> 2, row0 = (uint32_t)(side * 32 + (lane >> 3));
+        const uint32_t to0 = ring_s + kGradOperand + half * kGradHalf + row0 * 128u;
+        const auto column = [&](int q, uint32_t j) { return ((2u * (ch & 3u) + (j ^ half)) ^ ((row0 + 4u * (uint32_t)q) & 7u)) << 4; };
+        uint4 code[8];
+        float scale;                                         // of token side * 32 + lane
+        const uint8_t* src = nullptr;                        // codes of the stage to load, this lane's; null: none
+        int32_t tokens = 0;                                  // of this warp's 32, so many exist
+        const auto aim = [&](int32_t k) {                    // at the k-th stage
+            tokens = 0;
+            scale = 0.f;
+            if (k >= n_stages) return;
+            const int32_t s = piece.stage(k), tile = s / per_tile, tok = (s - tile * per_tile) % a.stages_part;
+            const int32_t block = 2 * (tile % a.tiles_i) + (int32_t)rank;
+            const int64_t m = (int64_t)tok * kTok + side * 32;
+            if (block >= a.Kb || m >= a.M) return;
+            tokens = (int32_t)min((int64_t)32, a.M - m);
+            src = a.xcodes + ((m + (lane >> 3)) * a.Kb + block) * 128 + ch * 16;
+            if (lane < tokens) scale = __ldg(a.xscale + (m + lane) * a.Kb + block);
         };
-        uint32_t s = 0, ph = 1;
-        // db: 8 outputs x 4 tokens a thread of the first tile of channels
-        float sum[8];
+        const auto load = [&](int q) {
+            code[q] = make_uint4(0, 0, 0, 0);
+            if (4 * q + (lane >> 3) < tokens) code[q] = __ldg(reinterpret_cast<const uint4*>(src + (int64_t)(4 * q) * a.Kb * 128));
+        };
+        int32_t mine = pair;                                 // this warp's stage, in the piece's order
+        uint32_t s = (uint32_t)pair, ph = 0;                 // its place in the ring
+        aim(mine);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum[j] = 0.f;
-        int64_t n = begin;
-        bool any = false;
-        const auto stage = [&](Item& v) {
-            fp8_wait(empty_s + s * 8, ph, c, a.status, 6u);
-            if (c->abort_flag) return false;
+        for (int q = 0; q < 8; ++q) load(q);
+        for (int32_t k = 0; k < n_stages && !c->abort_flag;) {
+            const Stretch t(piece, k);
+            const int32_t to = t.tile / a.tiles_i;
+            const bool adds = a.db && t.tile == to * a.tiles_i;   // the first of these outputs' tiles
+            float sum[8];
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                uint32_t r[8];
-                restore4(v.code[q].x, v.scale[q], r[0], r[1]);
-                restore4(v.code[q].y, v.scale[q], r[2], r[3]);
-                restore4(v.code[q].z, v.scale[q], r[4], r[5]);
-                restore4(v.code[q].w, v.scale[q], r[6], r[7]);
-                const uint32_t d = s * kGradStage;
-                sts128(to[q][0] + d, second ? r[4] : r[0], second ? r[5] : r[1], second ? r[6] : r[2], second ? r[7] : r[3]);
-                sts128(to[q][1] + d, second ? r[0] : r[4], second ? r[1] : r[5], second ? r[2] : r[6], second ? r[3] : r[7]);
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            grad_arrive(full0 + s * 8, lane);
-            if (++s == kGradStages) { s = 0; ph ^= 1; }
-            load(v);
-            // sums of dy, where this tile is the first of its outputs
-            const int to_ = tile / a.tiles_i;
-            if (a.db && tile == to_ * a.tiles_i) {
-                const int part = (int)(at / a.stages_part);
-                const int64_t col = (int64_t)to_ * 256 + rank * 128 + 8 * (t & 15), row = (at - (int64_t)part * a.stages_part) * kTok + (t >> 4);
-                const uint16_t* src = a.dy + (part * a.rows_part + row) * a.dy_stride + col;
-                any = true;
+            for (int j = 0; j < 8; ++j) sum[j] = 0.f;
+#pragma unroll 1
+            for (; mine < k + t.len; mine += kFillPairs) {
+                const float now = scale;
+                aim(mine + kFillPairs);
+                fp8_wait(empty_s + s * 8, ph ^ 1u, c, a.status, 6u);
+                if (c->abort_flag) break;
+                const uint32_t d = to0 + s * kGradStage;
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    if (col < a.O && row + 16 * q < a.M) {
-                        const uint4 u = __ldg(reinterpret_cast<const uint4*>(src + 16 * q * a.dy_stride));
+                for (int q = 0; q < 8; ++q) {
+                    const float f = __shfl_sync(0xffffffffu, now, 4 * q + (lane >> 3));
+                    uint32_t r[8];
+                    restore4(code[q].x, f, r[0], r[1]);
+                    restore4(code[q].y, f, r[2], r[3]);
+                    restore4(code[q].z, f, r[4], r[5]);
+                    restore4(code[q].w, f, r[6], r[7]);
+                    load(q);
+                    const bool second = half != 0;
+                    sts128(d + q * 512u + column(q, 0), second ? r[4] : r[0], second ? r[5] : r[1], second ? r[6] : r[2], second ? r[7] : r[3]);
+                    sts128(d + q * 512u + column(q, 1), second ? r[0] : r[4], second ? r[1] : r[5], second ? r[2] : r[6], second ? r[3] : r[7]);
+                }
+                fp8_wait(landed_s + s * 8, ph, c, a.status, 8u);
+                if (c->abort_flag) break;
+                if (adds) {                                  // 8 outputs x 16 tokens a lane; rows behind dy's end are zero
+                    const uint32_t from = ring_s + s * kGradStage + (uint32_t)side * kGradHalf + ((uint32_t)lane >> 3) * 128u;
+#pragma unroll
+                    for (int q = 0; q < 16; ++q) {
+                        const uint32_t row = 4u * (uint32_t)q + ((uint32_t)lane >> 3);
+                        const float4 u = lds_f4(from + q * 512u + ((ch ^ (row & 7u)) << 4));
                         float f[8];
-                        widen_vec<TDQ_BF16>(u, f);
+                        widen_vec<TDQ_BF16>(make_uint4(__float_as_uint(u.x), __float_as_uint(u.y), __float_as_uint(u.z), __float_as_uint(u.w)), f);
 #pragma unroll
                         for (int j = 0; j < 8; ++j) sum[j] += f[j];
                     }
                 }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                grad_arrive(full0 + s * 8, lane);
+                s += kFillPairs;
+                if (s >= kGradStages) { s -= kGradStages; ph ^= 1u; }
             }
-            ++n;
-            ++at;
-            if (any && (at == per_tile || n == end)) {       // this cluster's part of the column sums is complete
+            if (c->abort_flag) break;
+            if (adds) {                                      // this stretch's column sums: four pairs', in order
 #pragma unroll
-                for (int j = 0; j < 8; ++j) sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 16);
-                if (lane < 16) {
+                for (int j = 0; j < 8; ++j) {
+                    sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 8);
+                    sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 16);
+                }
+                if (lane < 8) {
 #pragma unroll
                     for (int j = 0; j < 8; j += 4)
-                        *reinterpret_cast<float4*>(db_room + (warp - kFillWarp0) * 128 + 8 * lane + j) = make_float4(sum[j], sum[j + 1], sum[j + 2], sum[j + 3]);
+                        *reinterpret_cast<float4*>(db_room + pair * 128 + side * 64 + 8 * lane + j) = make_float4(sum[j], sum[j + 1], sum[j + 2], sum[j + 3]);
                 }
                 __syncwarp();
                 mbar_arrive_lane0_s(met_s, lane);
                 fp8_wait(met_s, 0u, c, a.status, 7u);
-                const int64_t first = n - at;                // the tile's first stage
-                if (t < 128) {
-                    float v2 = 0.f;
-#pragma unroll
-                    for (int i = 0; i < kFillWarps; ++i) v2 += db_room[i * 128 + t];
-                    const int64_t o = (int64_t)to_ * 256 + rank * 128 + t;
-                    if (first >= begin && at == per_tile) {
-                        if (o < a.O) a.db[o] = v2;
-                    } else {
-                        a.dbpart[(int64_t)(2 * w + (first <= begin ? 0 : 1)) * 256 + rank * 128 + t] = v2;
-                    }
+                if (fw < 4) {
+                    const int col = fw * 32 + lane;
+                    const float v = ((db_room[col] + db_room[128 + col]) + db_room[256 + col]) + db_room[384 + col];
+                    const int64_t o = (int64_t)to * 256 + rank * 128 + col;
+                    if (!t.whole) a.dbpart[(int64_t)(2 * w + t.slot) * 256 + rank * 128 + col] = v;
+                    else if (o < a.O) a.db[o] = v;
                 }
                 __syncwarp();
                 mbar_arrive_lane0_s(met_s, lane);
                 fp8_wait(met_s, 1u, c, a.status, 7u);
-                any = false;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) sum[j] = 0.f;
             }
-            if (at == per_tile) { at = 0; ++tile; }
-            return true;
-        };
-        Item u, v;
-        load(u);
-        load(v);
-        while (n < end) {
-            if (!stage(u)) break;
-            if (n >= end || !stage(v)) break;
+            k += t.len;
         }
     }
 
@@ -445,7 +470,7 @@ __global__ void __launch_bounds__(256) grad_parts_kernel(const GradArgs a) {
     pdl_wait();
     pdl_trigger();
     const int tile = (int)blockIdx.x >> 3, band = (int)blockIdx.x & 7;
-    const int64_t per_tile = (int64_t)a.stages_part * a.parts, total = per_tile * a.tiles_o * a.tiles_i, first = tile * per_tile;
+    const int32_t per_tile = a.stages_part * a.parts, total = per_tile * a.tiles_o * a.tiles_i, first = tile * per_tile;
     const int32_t w0 = piece_owner(total, a.clusters, first), w1 = piece_owner(total, a.clusters, first + per_tile - 1);
     if (w0 == w1) return;                                    // stored by the one that added it
     const int to = tile / a.tiles_i, ti = tile - to * a.tiles_i;
@@ -609,7 +634,7 @@ extern "C" tdq_status tdq_fp8_weight_grad(const void* dy, tdq_dtype dy_dtype, in
     const int n_sm = current_device_sm_count(&dev);
     if (n_sm <= 0) return TDQ_ERR_CUDA;
     const GradPlan p = grad_plan(dy, dy_dtype, dy_row_stride, M, O, I, n_sm);
-    if (p.tiles_o * p.tiles_i > INT32_MAX / 8 || p.parts * p.rows_part > kGradMax) return TDQ_ERR_UNSUPPORTED;
+    if (p.tiles_o * p.tiles_i > INT32_MAX / 8 || p.parts * p.rows_part > kGradMax || p.total > INT32_MAX) return TDQ_ERR_UNSUPPORTED;
     if (!workspace || workspace_bytes < p.bytes) return TDQ_ERR_WORKSPACE;
     uint8_t* ws = reinterpret_cast<uint8_t*>(workspace);
     GradArgs a = {};
