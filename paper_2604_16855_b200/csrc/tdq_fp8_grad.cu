@@ -23,7 +23,7 @@ namespace tdq {
 namespace {
 
 constexpr int kTok = 64;                                  // tokens a stage
-constexpr int kGradStages = 6;
+constexpr int kGradStages = 5;
 constexpr int kGroup = 8;                                 // stages whose products an accumulator adds
 constexpr uint32_t kGradOperand = kTok * 128 * 2;         // bytes: two halves of 64 columns, 128 bytes a token
 constexpr uint32_t kGradHalf = kTok * 128;
@@ -33,8 +33,9 @@ constexpr uint32_t kGradStrip = 32 * 128;
 constexpr int kSumWarp0 = 4, kSumWarps = 8, kFillWarp0 = 12, kFillWarps = 8;
 constexpr int kGradThreads = (kFillWarp0 + kFillWarps) * 32;
 constexpr int kFillPairs = kFillWarps / 2;               // two warps fill a stage, every fourth one
+constexpr uint32_t kGradCodes = kTok * 128;                // bytes of a stage's codes
 constexpr uint32_t kGradDb = kFillPairs * 128 * 4;
-constexpr uint32_t kGradSmem = kGradCtrl + kGradStages * kGradStage + kSumWarps * kGradStrip + kGradDb;
+constexpr uint32_t kGradSmem = kGradCtrl + kGradStages * kGradStage + kFillPairs * kGradCodes + kSumWarps * kGradStrip + kGradDb;
 static_assert(kGradSmem <= (uint32_t)kSmemLimit, "shared memory");
 constexpr int kGradRegsLoad = 32, kGradRegsSum = 160, kGradRegsFill = 64;   // 128 * 32 + 256 * 160 + 256 * 64 <= 640 * 96
 // D binary32, both operands bf16 with the sum's axis slow, 256 columns x 256 rows
@@ -47,8 +48,8 @@ struct GradArgs {
     const uint16_t* dy;        // bf16 [parts * rows_part][dy_stride]
     void* dw;
     float* db;                 // or null
-    float* dbpart;             // [slots][256]
-    float* part;               // [slots][256][256]
+    float* dbpart;             // [2 clusters + tiles][256]: cut tiles' parts, whole tiles'
+    float* part;               // [2 clusters][256][256]
     int64_t M, O, I, dy_stride, dw_stride, rows_part;
     int32_t Kb, tiles_o, tiles_i, stages_part, parts;   // stages of an addend, addends
     int32_t clusters;
@@ -59,6 +60,7 @@ struct GradCtrl {
     uint64_t landed[kGradStages];                            // this CTA's dy
     uint64_t full[kGradStages];                              // CTA 0: both CTAs' operands
     uint64_t empty[kGradStages];
+    uint64_t codes[kFillPairs], taken[kFillPairs];            // a pair's codes have landed; have been read
     uint64_t tfull[2], tempty[2];
     uint64_t met;                                            // the restoring warps meet, twice for each sum of db
 };
@@ -127,32 +129,34 @@ __device__ __forceinline__ void tmem_ld16_wait(uint32_t taddr, uint32_t* v) {
                  : "r"(taddr)
                  : "memory");
 }
-// four codes times their scale as four bf16, nearest even
+// Four codes times their scale as four bf16, nearest even.
 __device__ __forceinline__ void restore4(uint32_t codes, float scale, uint32_t& lo, uint32_t& hi) {
     uint32_t h0, h1;
     asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(h0), "=r"(h1) : "r"(codes));
     const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&h0)), f1 = __half22float2(*reinterpret_cast<const __half2*>(&h1));
-    lo = narrow2<TDQ_BF16>(f0.x * scale, f0.y * scale);
-    hi = narrow2<TDQ_BF16>(f1.x * scale, f1.y * scale);
+    const float2 p0 = __fmul2_rn(f0, make_float2(scale, scale)), p1 = __fmul2_rn(f1, make_float2(scale, scale));
+    lo = narrow2<TDQ_BF16>(p0.x, p0.y);
+    hi = narrow2<TDQ_BF16>(p1.x, p1.y);
 }
 
 // DT: dw's tdq_dtype
 template <int DT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGradThreads, 1)
-fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, const __grid_constant__ CUtensorMap dwmap, const __grid_constant__ CUtensorMap partmap) {
+fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap dwmap, const __grid_constant__ CUtensorMap partmap) {
     constexpr bool W16 = DT != TDQ_F32;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     Ctrl* c = reinterpret_cast<Ctrl*>(smem_raw);             // its abort flag and TMEM address; the barriers are g's
     GradCtrl* g = reinterpret_cast<GradCtrl*>(smem_raw + sizeof(Ctrl));
     const uint32_t sm_s = smem_u32(smem_raw), ring_s = sm_s + kGradCtrl;
-    const uint32_t strips_s = ring_s + kGradStages * kGradStage;
-    float* db_room = reinterpret_cast<float*>(smem_raw + kGradCtrl + kGradStages * kGradStage + kSumWarps * kGradStrip);
+    const uint32_t codes_s = ring_s + kGradStages * kGradStage, strips_s = codes_s + kFillPairs * kGradCodes;
+    float* db_room = reinterpret_cast<float*>(smem_raw + kGradSmem - kGradDb);
     const int warp = uniform_warp(), lane = threadIdx.x & 31;
     const uint32_t rank = fp8_cluster_rank();
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kGradStages; ++i) { mbar_init(&g->landed[i], 1); mbar_init(&g->full[i], 4); mbar_init(&g->empty[i], 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(&g->tfull[i], 1); mbar_init(&g->tempty[i], 2 * kSumWarps); }
+        for (int i = 0; i < kFillPairs; ++i) { mbar_init(&g->codes[i], 1); mbar_init(&g->taken[i], 2); }
         mbar_init(&g->met, kFillWarps);
         c->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -199,6 +203,26 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
                     if (++tok == a.stages_part) { tok = 0; ++part; }
                 }
                 k += t.len;
+            }
+        } else if (warp == 3) {
+            // -------------------------------------------------------- copies of codes, a slot for each pair of restoring warps
+            const uint32_t codes_bar = smem_u32(&g->codes[0]), taken_s = smem_u32(&g->taken[0]);
+            for (int32_t k = 0; k < n_stages && !c->abort_flag;) {
+                const Stretch t(piece, k);
+                const int32_t x = (2 * (t.tile % a.tiles_i) + (int32_t)rank) * 128;   // past the end: the map fills with zeros
+                int32_t tok = t.at % a.stages_part;
+#pragma unroll 1
+                for (const int32_t end = k + t.len; k < end; ++k) {
+                    const uint32_t slot = (uint32_t)k % kFillPairs;
+                    fp8_wait(taken_s + slot * 8, ((uint32_t)(k / kFillPairs) & 1u) ^ 1u, c, a.status, 9u);
+                    if (c->abort_flag) break;
+                    if (elect_one()) {
+                        mbar_expect_tx(&g->codes[slot], kGradCodes);
+                        grad_load(codes_s + slot * kGradCodes, &xmap, x, tok * kTok, codes_bar + slot * 8);
+                    }
+                    __syncwarp();
+                    if (++tok == a.stages_part) tok = 0;
+                }
             }
         } else if (warp == 1 && rank == 0) {
             // -------------------------------------------------------- instructions
@@ -349,77 +373,79 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
         const int fw = warp - kFillWarp0, pair = fw >> 1, side = fw & 1;   // a warp restores 32 tokens and sums 64 outputs of every fourth stage
         const uint32_t full0 = map_to_cta(smem_u32(&g->full[0]), 0), empty_s = smem_u32(&g->empty[0]), landed_s = smem_u32(&g->landed[0]);
         const uint32_t met_s = smem_u32(&g->met);
-        // Sixteen codes a lane and token: tokens 4 q + lane / 8, channels 16 (lane & 7) ..; eight lanes write eight different 16-byte columns at a time, the second
-        // half of them its second column first
-        const uint32_t ch = (uint32_t)lane & 7u, half = ch >> 2, row0 = (uint32_t)(side * 32 + (lane >> 3));
-        const uint32_t to0 = ring_s + kGradOperand + half * kGradHalf + row0 * 128u;
-        const auto column = [&](int q, uint32_t j) { return ((2u * (ch & 3u) + (j ^ half)) ^ ((row0 + 4u * (uint32_t)q) & 7u)) << 4; };
-        uint4 code[8];
-        float scale;                                         // of token side * 32 + lane
-        const uint8_t* src = nullptr;                        // codes of the stage to load, this lane's; null: none
-        int32_t tokens = 0;                                  // of this warp's 32, so many exist
-        const auto aim = [&](int32_t k) {                    // at the k-th stage
-            tokens = 0;
+        const uint32_t codes_bar = smem_u32(&g->codes[pair]), taken_bar = smem_u32(&g->taken[pair]);
+        // Sixteen codes a lane and token, channels 16 (lane & 7) ..: of token 4 q + lane / 8, the upper 64 channels of its neighbour, so that eight lanes
+        // read, and write, eight different 16-byte columns (the swizzle moves a row's by its number: odd and even rows never meet).
+        const uint32_t ch = (uint32_t)lane & 7u, half = ch >> 2, tok0 = ((uint32_t)lane >> 3) ^ half;
+        const uint32_t from_s = codes_s + (uint32_t)pair * kGradCodes + ((uint32_t)side * 32u + tok0) * 128u;
+        const uint32_t to_s = ring_s + kGradOperand + half * kGradHalf + ((uint32_t)side * 32u + tok0) * 128u;
+        uint32_t from[2], to[2][2];                          // of even and odd q
+#pragma unroll
+        for (uint32_t q = 0; q < 2; ++q) {
+            from[q] = from_s + ((ch ^ (tok0 + 4u * q)) << 4);
+#pragma unroll
+            for (uint32_t j = 0; j < 2; ++j) to[q][j] = to_s + (((2u * (ch & 3u) + j) ^ (tok0 + 4u * q)) << 4);
+        }
+        float scale;                                         // of token side * 32 + lane of the next stage; 0 where there is none
+        const auto load_scale = [&](int32_t k) {
             scale = 0.f;
             if (k >= n_stages) return;
-            const int32_t s = piece.stage(k), tile = s / per_tile, tok = (s - tile * per_tile) % a.stages_part;
+            const int32_t st = piece.stage(k), tile = st / per_tile, tok = (st - tile * per_tile) % a.stages_part;
             const int32_t block = 2 * (tile % a.tiles_i) + (int32_t)rank;
-            const int64_t m = (int64_t)tok * kTok + side * 32;
-            if (block >= a.Kb || m >= a.M) return;
-            tokens = (int32_t)min((int64_t)32, a.M - m);
-            src = a.xcodes + ((m + (lane >> 3)) * a.Kb + block) * 128 + ch * 16;
-            if (lane < tokens) scale = __ldg(a.xscale + (m + lane) * a.Kb + block);
-        };
-        const auto load = [&](int q) {
-            code[q] = make_uint4(0, 0, 0, 0);
-            if (4 * q + (lane >> 3) < tokens) code[q] = __ldg(reinterpret_cast<const uint4*>(src + (int64_t)(4 * q) * a.Kb * 128));
+            const int64_t m = (int64_t)tok * kTok + side * 32 + lane;
+            if (block < a.Kb && m < a.M) scale = __ldg(a.xscale + m * a.Kb + block);
         };
         int32_t mine = pair;                                 // this warp's stage, in the piece's order
         uint32_t s = (uint32_t)pair, ph = 0;                 // its place in the ring
-        aim(mine);
-#pragma unroll
-        for (int q = 0; q < 8; ++q) load(q);
+        uint32_t cph = 0;
+        load_scale(mine);
         for (int32_t k = 0; k < n_stages && !c->abort_flag;) {
             const Stretch t(piece, k);
-            const int32_t to = t.tile / a.tiles_i;
-            const bool adds = a.db && t.tile == to * a.tiles_i;   // the first of these outputs' tiles
-            float sum[8];
+            // the tiles of the same outputs take turns at the column sums
+            const int32_t ti = t.tile % a.tiles_i;
+            int32_t turn = a.db ? (t.at + mine - k) % a.tiles_i : -1;
+            float2 sum[4];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum[j] = 0.f;
+            for (int j = 0; j < 4; ++j) sum[j] = make_float2(0.f, 0.f);
 #pragma unroll 1
             for (; mine < k + t.len; mine += kFillPairs) {
                 const float now = scale;
-                aim(mine + kFillPairs);
+                load_scale(mine + kFillPairs);
+                fp8_wait(codes_bar, cph, c, a.status, 10u);
+                cph ^= 1u;
+                uint4 code[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) code[q] = lds_u4(from[q & 1] + q * 512u);
+                __syncwarp();
+                mbar_arrive_lane0_s(taken_bar, lane);
                 fp8_wait(empty_s + s * 8, ph ^ 1u, c, a.status, 6u);
                 if (c->abort_flag) break;
-                const uint32_t d = to0 + s * kGradStage;
+                const uint32_t d = s * kGradStage;
 #pragma unroll
                 for (int q = 0; q < 8; ++q) {
-                    const float f = __shfl_sync(0xffffffffu, now, 4 * q + (lane >> 3));
+                    const float f = __shfl_sync(0xffffffffu, now, 4 * q + (int)tok0);
                     uint32_t r[8];
                     restore4(code[q].x, f, r[0], r[1]);
                     restore4(code[q].y, f, r[2], r[3]);
                     restore4(code[q].z, f, r[4], r[5]);
                     restore4(code[q].w, f, r[6], r[7]);
-                    load(q);
-                    const bool second = half != 0;
-                    sts128(d + q * 512u + column(q, 0), second ? r[4] : r[0], second ? r[5] : r[1], second ? r[6] : r[2], second ? r[7] : r[3]);
-                    sts128(d + q * 512u + column(q, 1), second ? r[0] : r[4], second ? r[1] : r[5], second ? r[2] : r[6], second ? r[3] : r[7]);
+                    sts128(to[q & 1][0] + d + q * 512u, r[0], r[1], r[2], r[3]);
+                    sts128(to[q & 1][1] + d + q * 512u, r[4], r[5], r[6], r[7]);
                 }
                 fp8_wait(landed_s + s * 8, ph, c, a.status, 8u);
                 if (c->abort_flag) break;
-                if (adds) {                                  // 8 outputs x 16 tokens a lane; rows behind dy's end are zero
-                    const uint32_t from = ring_s + s * kGradStage + (uint32_t)side * kGradHalf + ((uint32_t)lane >> 3) * 128u;
+                if (turn == ti) {                            // 8 outputs x 16 tokens a lane; rows behind dy's end are zero
+                    const uint32_t at = ring_s + d + (uint32_t)side * kGradHalf + ((uint32_t)lane >> 3) * 128u;
 #pragma unroll
                     for (int q = 0; q < 16; ++q) {
-                        const uint32_t row = 4u * (uint32_t)q + ((uint32_t)lane >> 3);
-                        const float4 u = lds_f4(from + q * 512u + ((ch ^ (row & 7u)) << 4));
-                        float f[8];
-                        widen_vec<TDQ_BF16>(make_uint4(__float_as_uint(u.x), __float_as_uint(u.y), __float_as_uint(u.z), __float_as_uint(u.w)), f);
+                        const uint4 u = lds_u4(at + q * 512u + ((ch ^ (((uint32_t)lane >> 3) + 4u * (q & 1))) << 4));
+                        const uint32_t v[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) sum[j] += f[j];
+                        for (int j = 0; j < 4; ++j)
+                            sum[j] = __fadd2_rn(sum[j], make_float2(__uint_as_float(v[j] << 16), __uint_as_float(v[j] & 0xffff0000u)));
                     }
                 }
+                if (a.db) turn = (turn + kFillPairs) % a.tiles_i;
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 grad_arrive(full0 + s * 8, lane);
@@ -427,26 +453,24 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
                 if (s >= kGradStages) { s -= kGradStages; ph ^= 1u; }
             }
             if (c->abort_flag) break;
-            if (adds) {                                      // this stretch's column sums: four pairs', in order
+            if (a.db) {                                      // this stretch's column sums: four pairs', in order
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 8);
-                    sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 16);
-                }
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int x = 8; x <= 16; x <<= 1)
+                        sum[j] = __fadd2_rn(sum[j], make_float2(__shfl_xor_sync(0xffffffffu, sum[j].x, x), __shfl_xor_sync(0xffffffffu, sum[j].y, x)));
                 if (lane < 8) {
 #pragma unroll
-                    for (int j = 0; j < 8; j += 4)
-                        *reinterpret_cast<float4*>(db_room + pair * 128 + side * 64 + 8 * lane + j) = make_float4(sum[j], sum[j + 1], sum[j + 2], sum[j + 3]);
+                    for (int j = 0; j < 4; j += 2)
+                        *reinterpret_cast<float4*>(db_room + pair * 128 + side * 64 + 8 * lane + 2 * j) = make_float4(sum[j].x, sum[j].y, sum[j + 1].x, sum[j + 1].y);
                 }
                 __syncwarp();
                 mbar_arrive_lane0_s(met_s, lane);
                 fp8_wait(met_s, 0u, c, a.status, 7u);
                 if (fw < 4) {
                     const int col = fw * 32 + lane;
-                    const float v = ((db_room[col] + db_room[128 + col]) + db_room[256 + col]) + db_room[384 + col];
-                    const int64_t o = (int64_t)to * 256 + rank * 128 + col;
-                    if (!t.whole) a.dbpart[(int64_t)(2 * w + t.slot) * 256 + rank * 128 + col] = v;
-                    else if (o < a.O) a.db[o] = v;
+                    a.dbpart[(int64_t)(t.whole ? 2 * a.clusters + t.tile : 2 * w + t.slot) * 256 + rank * 128 + col] =
+                        ((db_room[col] + db_room[128 + col]) + db_room[256 + col]) + db_room[384 + col];
                 }
                 __syncwarp();
                 mbar_arrive_lane0_s(met_s, lane);
@@ -464,49 +488,59 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "n"(512) : "memory");
 }
 
-// Adds the parts of the tiles that were cut, in order of the sum: a thread block for 32 rows of a tile.
+// Adds the parts of the tiles that were cut, in order of the sum, a thread block for four rows of a tile; the blocks behind those add db, 64 outputs each.
 template <int DT>
-__global__ void __launch_bounds__(256) grad_parts_kernel(const GradArgs a) {
+__global__ void __launch_bounds__(256) grad_parts_kernel(const GradArgs a, int32_t tile_blocks) {
     pdl_wait();
     pdl_trigger();
-    const int tile = (int)blockIdx.x >> 3, band = (int)blockIdx.x & 7;
-    const int32_t per_tile = a.stages_part * a.parts, total = per_tile * a.tiles_o * a.tiles_i, first = tile * per_tile;
-    const int32_t w0 = piece_owner(total, a.clusters, first), w1 = piece_owner(total, a.clusters, first + per_tile - 1);
+    const int32_t per_tile = a.stages_part * a.parts, total = per_tile * a.tiles_o * a.tiles_i;
+    const int lane = (int)threadIdx.x & 63, y = (int)threadIdx.x >> 6;
+    if ((int32_t)blockIdx.x >= tile_blocks) {
+        __shared__ float sums[4][64];
+        const int64_t o = ((int64_t)blockIdx.x - tile_blocks) * 64 + lane;
+        const int to = (int)(o >> 8), col = (int)(o & 255);
+        float s = 0.f;
+        if (to < a.tiles_o)
+            for (int t = y; t < a.tiles_i; t += 4) {
+                const int32_t tile = to * a.tiles_i + t, first = tile * per_tile;
+                const int32_t w0 = piece_owner(total, a.clusters, first), w1 = piece_owner(total, a.clusters, first + per_tile - 1);
+                if (w0 == w1) s += a.dbpart[(int64_t)(2 * a.clusters + tile) * 256 + col];
+                else
+#pragma unroll 4
+                    for (int32_t w = w0; w <= w1; ++w) s += a.dbpart[(int64_t)(2 * w + (w == w0 && piece_begin(total, a.clusters, w) < first ? 1 : 0)) * 256 + col];
+            }
+        sums[y][lane] = s;
+        __syncthreads();
+        if (y == 0 && o < a.O) a.db[o] = ((sums[0][lane] + sums[1][lane]) + sums[2][lane]) + sums[3][lane];
+        return;
+    }
+    const int tile = (int)blockIdx.x >> 6, r = ((int)blockIdx.x & 63) * 4 + y;
+    const int32_t first = tile * per_tile, w0 = piece_owner(total, a.clusters, first), w1 = piece_owner(total, a.clusters, first + per_tile - 1);
     if (w0 == w1) return;                                    // stored by the one that added it
     const int to = tile / a.tiles_i, ti = tile - to * a.tiles_i;
-    const auto slot = [&](int32_t w) { return (int64_t)2 * w + (piece_begin(total, a.clusters, w) < first ? 1 : 0); };
-    const int64_t i = (int64_t)ti * 256 + 4 * (threadIdx.x & 63);
+    const int64_t o = (int64_t)to * 256 + r, i = (int64_t)ti * 256 + 4 * lane;
     const int left = (int)min((int64_t)4, a.I - i);
-#pragma unroll 2
-    for (int r = band * 32 + ((int)threadIdx.x >> 6); r < band * 32 + 32; r += 4) {
-        const int64_t o = (int64_t)to * 256 + r;
-        if (o >= a.O || left <= 0) break;
-        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-        for (int32_t w = w0; w <= w1; ++w) {
-            const float4 v = *reinterpret_cast<const float4*>(a.part + (slot(w) * 256 + r) * 256 + 4 * (threadIdx.x & 63));
-            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-        }
-        const float f[4] = {s.x, s.y, s.z, s.w};
-        if constexpr (DT == TDQ_F32) {
-            float* dw = reinterpret_cast<float*>(a.dw) + o * a.dw_stride + i;
-            if (a.dw_vec && left == 4) *reinterpret_cast<float4*>(dw) = s;
-            else
-                for (int j = 0; j < left; ++j) dw[j] = f[j];
-        } else {
-            uint16_t* dw = reinterpret_cast<uint16_t*>(a.dw) + o * a.dw_stride + i;
-            const uint32_t lo = narrow2<DT>(f[0], f[1]), hi = narrow2<DT>(f[2], f[3]);
-            if (a.dw_vec && left == 4) *reinterpret_cast<uint2*>(dw) = make_uint2(lo, hi);
-            else
-                for (int j = 0; j < left; ++j) dw[j] = (uint16_t)((j & 2 ? hi : lo) >> (16 * (j & 1)));
-        }
+    if (o >= a.O || left <= 0) return;
+    // the tile is the first of its clusters' pieces, but for the one whose piece begins before it
+    const float* from = a.part + (int64_t)r * 256 + 4 * lane;
+    float4 s = *reinterpret_cast<const float4*>(from + (int64_t)(2 * w0 + (piece_begin(total, a.clusters, w0) < first ? 1 : 0)) * 65536);
+#pragma unroll 8
+    for (int32_t w = w0 + 1; w <= w1; ++w) {
+        const float4 v = *reinterpret_cast<const float4*>(from + (int64_t)w * 2 * 65536);
+        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
     }
-    if (a.db && ti == 0 && threadIdx.x < 32) {
-        const int r = band * 32 + (int)threadIdx.x;
-        const int64_t o = (int64_t)to * 256 + r;
-        float s = 0.f;
-        for (int32_t w = w0; w <= w1; ++w) s += a.dbpart[slot(w) * 256 + r];
-        if (o < a.O) a.db[o] = s;
+    const float f[4] = {s.x, s.y, s.z, s.w};
+    if constexpr (DT == TDQ_F32) {
+        float* dw = reinterpret_cast<float*>(a.dw) + o * a.dw_stride + i;
+        if (a.dw_vec && left == 4) *reinterpret_cast<float4*>(dw) = s;
+        else
+            for (int j = 0; j < left; ++j) dw[j] = f[j];
+    } else {
+        uint16_t* dw = reinterpret_cast<uint16_t*>(a.dw) + o * a.dw_stride + i;
+        const uint32_t lo = narrow2<DT>(f[0], f[1]), hi = narrow2<DT>(f[2], f[3]);
+        if (a.dw_vec && left == 4) *reinterpret_cast<uint2*>(dw) = make_uint2(lo, hi);
+        else
+            for (int j = 0; j < left; ++j) dw[j] = (uint16_t)((j & 2 ? hi : lo) >> (16 * (j & 1)));
     }
 }
 
@@ -579,19 +613,20 @@ GradPlan grad_plan(const void* dy, tdq_dtype dtype, int64_t dy_stride, int64_t M
     p.cut = p.total % p.clusters != 0 || p.total / p.clusters % per_tile != 0;
     p.dy_bytes = p.copied ? (size_t)(p.parts * p.rows_part * p.dy_stride) * 2 : 0;
     p.part_bytes = p.cut ? (size_t)2 * p.clusters * 256 * 256 * 4 : 0;
-    p.db_bytes = p.cut ? (size_t)2 * p.clusters * 256 * 4 : 0;
+    p.db_bytes = (size_t)(2 * p.clusters + tiles) * 256 * 4;
     p.bytes = kWorkspaceHeader + p.part_bytes + p.db_bytes + p.dy_bytes;
     return p;
 }
 
 template <int DT>
-tdq_status launch_grad(const GradArgs& a, const GradPlan& p, const CUtensorMap& dymap, const CUtensorMap& dwmap, const CUtensorMap& partmap, int dev, cudaStream_t st) {
+tdq_status launch_grad(const GradArgs& a, const GradPlan& p, const CUtensorMap& dymap, const CUtensorMap& xmap, const CUtensorMap& dwmap, const CUtensorMap& partmap, int dev, cudaStream_t st) {
     static std::atomic<uint64_t> smem_done{0};
     if (allow_smem(fp8_grad_kernel<DT>, (int)kGradSmem, smem_done, dev) != cudaSuccess) return TDQ_ERR_CUDA;
-    if (launch_pdl(fp8_grad_kernel<DT>, dim3(2 * (unsigned)p.clusters), dim3(kGradThreads), kGradSmem, st, a, dymap, dwmap, partmap) != cudaSuccess) return TDQ_ERR_CUDA;
+    if (launch_pdl(fp8_grad_kernel<DT>, dim3(2 * (unsigned)p.clusters), dim3(kGradThreads), kGradSmem, st, a, dymap, xmap, dwmap, partmap) != cudaSuccess) return TDQ_ERR_CUDA;
     g_launch_count.fetch_add(1, std::memory_order_relaxed);
-    if (p.cut) {
-        if (launch_pdl(grad_parts_kernel<DT>, dim3((unsigned)(p.tiles_o * p.tiles_i * 8)), dim3(256), 0, st, a) != cudaSuccess) return TDQ_ERR_CUDA;
+    if (p.cut || a.db) {
+        const int32_t tile_blocks = p.cut ? (int32_t)(p.tiles_o * p.tiles_i * 64) : 0, db_blocks = a.db ? (int32_t)((a.O + 63) / 64) : 0;
+        if (launch_pdl(grad_parts_kernel<DT>, dim3((unsigned)(tile_blocks + db_blocks)), dim3(256), 0, st, a, tile_blocks) != cudaSuccess) return TDQ_ERR_CUDA;
         g_launch_count.fetch_add(1, std::memory_order_relaxed);
     }
     return TDQ_OK;
@@ -634,7 +669,7 @@ extern "C" tdq_status tdq_fp8_weight_grad(const void* dy, tdq_dtype dy_dtype, in
     const int n_sm = current_device_sm_count(&dev);
     if (n_sm <= 0) return TDQ_ERR_CUDA;
     const GradPlan p = grad_plan(dy, dy_dtype, dy_row_stride, M, O, I, n_sm);
-    if (p.tiles_o * p.tiles_i > INT32_MAX / 8 || p.parts * p.rows_part > kGradMax || p.total > INT32_MAX) return TDQ_ERR_UNSUPPORTED;
+    if (p.tiles_o * p.tiles_i > INT32_MAX / 128 || p.parts * p.rows_part > kGradMax || p.total > INT32_MAX) return TDQ_ERR_UNSUPPORTED;
     if (!workspace || workspace_bytes < p.bytes) return TDQ_ERR_WORKSPACE;
     uint8_t* ws = reinterpret_cast<uint8_t*>(workspace);
     GradArgs a = {};
@@ -656,14 +691,15 @@ extern "C" tdq_status tdq_fp8_weight_grad(const void* dy, tdq_dtype dy_dtype, in
         if (e != cudaSuccess) return TDQ_ERR_CUDA;
         g_launch_count.fetch_add(1, std::memory_order_relaxed);
     }
-    CUtensorMap dymap, dwmap, partmap;
+    CUtensorMap dymap, xmap, dwmap, partmap;
     memset(&dwmap, 0, sizeof dwmap);
     memset(&partmap, 0, sizeof partmap);
     if (!grad_operand_map(&dymap, a.dy, p.copied ? p.parts * p.rows_part : M, p.copied ? p.dy_stride : O, p.dy_stride)) return TDQ_ERR_CUDA;
+    if (!fp8_operand_map(&xmap, xcodes, M, (int64_t)a.Kb * kFp8Block, kTok)) return TDQ_ERR_CUDA;
     const int64_t w_stride = O > 1 ? dw_row_stride : (I + 7) / 8 * 8;
     if (a.dw_vec && !encode_y_map(&dwmap, dw, wsz == 2, O, I, w_stride, wsz == 2 ? 64 : 32, 32, dw_dtype == TDQ_F16)) a.dw_vec = 0;
     if (p.cut && !encode_y_map(&partmap, a.part, false, (int64_t)2 * p.clusters * 256, 256, 256, 32, 32)) return TDQ_ERR_CUDA;
-    return dw_dtype == TDQ_F32 ? launch_grad<TDQ_F32>(a, p, dymap, dwmap, partmap, dev, st)
-         : dw_dtype == TDQ_BF16 ? launch_grad<TDQ_BF16>(a, p, dymap, dwmap, partmap, dev, st)
-                                : launch_grad<TDQ_F16>(a, p, dymap, dwmap, partmap, dev, st);
+    return dw_dtype == TDQ_F32 ? launch_grad<TDQ_F32>(a, p, dymap, xmap, dwmap, partmap, dev, st)
+         : dw_dtype == TDQ_BF16 ? launch_grad<TDQ_BF16>(a, p, dymap, xmap, dwmap, partmap, dev, st)
+                                : launch_grad<TDQ_F16>(a, p, dymap, xmap, dwmap, partmap, dev, st);
 }

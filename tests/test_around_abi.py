@@ -87,7 +87,8 @@ def test_weight_grad(tdq):
     _each(f, good, [((6, 1 << 31), (2, 1 << 31), uns), ((7, 1 << 31), (10, 1 << 31), uns)])
     head = int(size(FAKE, 1, 40, 0, 40, 90))
     assert head == 256 and size(FAKE, 3, 40, 64, 40, 90) == size(FAKE, 1, 40, -1, 40, 90) == size(FAKE, 1, 40, 64, 40, 0) == 0
-    # one stage, one tile: nothing is cut; fp16 and rows off the grid pass through the workspace
-    assert size(FAKE, 1, 40, 64, 40, 90) == 256 and size(FAKE, 1, 41, 64, 40, 90) == 256 + 64 * 40 * 2
-    two = 2 * 2 * 256 * (256 + 1) * 4                        # two stages, two clusters with two places each
-    assert size(FAKE, 1, 40, 65, 40, 90) == 256 + two and size(FAKE, 2, 40, 64, 40, 90) == 256 + two + 2 * 64 * 40 * 2
+    # one stage, one tile: nothing is cut, three places for sums of dy; fp16 and rows off the grid pass through the workspace
+    one = 256 + 3 * 1024
+    assert size(FAKE, 1, 40, 64, 40, 90) == one and size(FAKE, 1, 41, 64, 40, 90) == one + 64 * 40 * 2
+    two = 256 + 2 * 2 * 256 * 256 * 4 + 5 * 1024             # two stages, two clusters with two places each
+    assert size(FAKE, 1, 40, 65, 40, 90) == two and size(FAKE, 2, 40, 64, 40, 90) == two + 2 * 64 * 40 * 2
