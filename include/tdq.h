@@ -329,6 +329,40 @@ size_t tdq_fp8_linear_workspace_bytes(int64_t M, int64_t I_pad, int64_t O);
 tdq_status tdq_fp8_linear_tiles(int64_t M, int64_t I_pad, int64_t O, int32_t sm_count, int32_t* tokens, int32_t* channels, int32_t* parts);
 
 /*
+ * Activations, of the epilogue below and of their backward pass (binary32; Phi the Gaussian distribution function, to 3e-7):
+ *   RELU max(z, 0);   GELU z Phi(z);   GELU_TANH z / 2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3)));   SILU z / (1 + exp(-z))
+ */
+typedef enum { TDQ_ACT_NONE = 0, TDQ_ACT_RELU = 1, TDQ_ACT_GELU = 2, TDQ_ACT_GELU_TANH = 3, TDQ_ACT_SILU = 4 } tdq_activation;
+
+/*
+ * tdq_fp8_linear with what follows a layer in its epilogue:
+ *   z = x W^T + bias, as there;   y = activation(z) + residual    (binary32, each output rounded once when stored)
+ *   residual   NULL or [M, O] of y_dtype, rows residual_row_stride elements apart (>= O); y itself with y's stride works in place, any other overlap with y does not.
+ *   pre        NULL or [M, O] of y_dtype, rows pre_row_stride apart (>= O): z, for the backward pass.  It overlaps neither y nor residual.  TDQ_ERR_UNSUPPORTED
+ *              together with a residual.
+ *   Everything else as for tdq_fp8_linear, whose result y is bit for bit where nothing follows.
+ */
+typedef struct {
+    int32_t activation;                        /* tdq_activation */
+    const void* residual;
+    int64_t residual_row_stride;
+    void* pre;
+    int64_t pre_row_stride;
+} tdq_fp8_epilogue;
+tdq_status tdq_fp8_linear_epilogue(const uint8_t* xcodes, const float* xscale, const uint8_t* wcodes, const float* wscale, const float* bias, int64_t M,
+                                   int64_t I_pad, int64_t O, const tdq_fp8_epilogue* e /* HOST */, void* y, tdq_dtype y_dtype, int64_t y_row_stride,
+                                   void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * An activation's backward pass from its input kept in 8 bits (tdq_quantize_act_fp8_pow2, or any codes with block scales):
+ *   dz[m,c] = dh[m,c] activation'(z[m,c]),   z = code scale    (binary32, rounded once)
+ *   dh, dz  [M, C] of dtype, each with a row stride of its own (>= C); dz may be dh with the same stride.   zcodes [M, C_pad] 16-byte aligned, C_pad = 128
+ *   ceil(C/128), zscale [M, C_pad/128].   The slope of RELU is 1 for z > 0 and else 0.  TDQ_ERR_UNSUPPORTED for more than 2^36 - 2^17 codes.
+ */
+tdq_status tdq_activation_backward_fp8(const void* dh, tdq_dtype dtype, int64_t M, int64_t C, int64_t dh_row_stride, const uint8_t* zcodes,
+                                       const float* zscale, int32_t activation, void* dz, int64_t dz_row_stride, void* cuda_stream);
+
+/*
  * The layer's backward pass from activations kept in 8 bits (the paper has no counterpart): the gradients of its weight and bias,
  *   dw[o,i] = sum_m dy[m,o] x[m,i];    db[o] = sum_m dy[m,o]        with x[m,i] = bf16(code[m,i] scale[m,i/128])
  *   on the tensor cores' bf16 instructions.  x is exact where the scales are powers of two (tdq_quantize_act_fp8_pow2, tdq_layer_norm with TDQ_NORM_POW2); other

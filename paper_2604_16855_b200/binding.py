@@ -31,7 +31,8 @@ EXPORTS = ["tdq_default_act_params", "tdq_quantize_act", "tdq_quantize_weight", 
            "tdq_quantize_status", "tdq_selftest_wait_timeout", "tdq_fold_output_affine", "tdq_measure_mma_clocks",
            "tdq_quantize_act_fp8", "tdq_quantize_weight_fp8", "tdq_fp8_linear", "tdq_fp8_linear_workspace_bytes",
            "tdq_fp8_linear_tiles", "tdq_qk_norm_rope", "tdq_quantize_act_fp8_pow2", "tdq_layer_norm", "tdq_layer_norm_backward",
-           "tdq_layer_norm_backward_workspace_bytes", "tdq_fp8_weight_grad", "tdq_fp8_weight_grad_workspace_bytes"]
+           "tdq_layer_norm_backward_workspace_bytes", "tdq_fp8_weight_grad", "tdq_fp8_weight_grad_workspace_bytes",
+           "tdq_fp8_linear_epilogue", "tdq_activation_backward_fp8"]
 
 
 class ActParams(ctypes.Structure):
@@ -47,6 +48,11 @@ class RopeParams(ctypes.Structure):
 class RopeHeads(ctypes.Structure):
     _fields_ = [("x", ctypes.c_void_p), ("out", ctypes.c_void_p), ("weight", ctypes.c_void_p)] + [
         (n, ctypes.c_int64) for n in ("heads", "row_stride", "head_stride", "out_row_stride", "out_head_stride")]
+
+
+class Fp8Epilogue(ctypes.Structure):
+    _fields_ = [("activation", ctypes.c_int32), ("residual", ctypes.c_void_p), ("residual_row_stride", ctypes.c_int64), ("pre", ctypes.c_void_p),
+                ("pre_row_stride", ctypes.c_int64)]
 
 
 _i64, _i32, _vp, _sz = ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p, ctypes.c_size_t
@@ -95,6 +101,10 @@ _lib.tdq_quantize_weight_fp8.argtypes = [_vp, ctypes.c_int, _i64, _i64, _vp, _vp
 _lib.tdq_quantize_weight_fp8.restype = ctypes.c_int
 _lib.tdq_fp8_linear.argtypes = [_vp, _vp, _vp, _vp, _vp, _i64, _i64, _i64, _vp, ctypes.c_int, _i64, _vp, _sz, _vp]
 _lib.tdq_fp8_linear.restype = ctypes.c_int
+_lib.tdq_fp8_linear_epilogue.argtypes = [_vp, _vp, _vp, _vp, _vp, _i64, _i64, _i64, ctypes.POINTER(Fp8Epilogue), _vp, ctypes.c_int, _i64, _vp, _sz, _vp]
+_lib.tdq_fp8_linear_epilogue.restype = ctypes.c_int
+_lib.tdq_activation_backward_fp8.argtypes = [_vp, ctypes.c_int, _i64, _i64, _i64, _vp, _vp, _i32, _vp, _i64, _vp]
+_lib.tdq_activation_backward_fp8.restype = ctypes.c_int
 _lib.tdq_fp8_linear_workspace_bytes.argtypes = [_i64, _i64, _i64]
 _lib.tdq_fp8_linear_workspace_bytes.restype = _sz
 _lib.tdq_fp8_linear_tiles.argtypes = [_i64, _i64, _i64, _i32] + [ctypes.POINTER(_i32)] * 3
@@ -250,10 +260,22 @@ def fp8_linear_workspace(device) -> torch.Tensor:
     return torch.zeros((FP8_WORKSPACE_BYTES,), dtype=torch.uint8, device=device)
 
 
-def fp8_linear(xcodes, xscale, wcodes, wscale, bias=None, *, out_dtype=torch.float32, y=None, workspace=None):
+ACTIVATIONS = {None: 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+
+
+def _activation(name):
+    if name not in ACTIVATIONS:
+        raise ValueError("activation must be one of %s, got %r" % (", ".join(repr(n) for n in ACTIVATIONS), name))
+    return ACTIVATIONS[name]
+
+
+def fp8_linear(xcodes, xscale, wcodes, wscale, bias=None, *, out_dtype=torch.float32, y=None, workspace=None, activation=None, residual=None, pre=None):
     """tdq_fp8_linear on codes and scales of quantize_act_fp8 and quantize_weight_fp8 (codes float8_e4m3fn, or uint8 with the same
-    bytes).  Returns y [M, O]."""
-    return _host.fp8_linear(xcodes, xscale, wcodes, wscale, bias, out_dtype, y, workspace)
+    bytes).  Returns y [M, O].
+
+    With activation ("relu", "gelu", "gelu_tanh", "silu"), residual [M, O] or pre [M, O]: tdq_fp8_linear_epilogue, y = activation(z) + residual, and the layer's
+    own output z written to pre (not together with a residual).  residual and pre are of y's type; residual may be y itself."""
+    return _host.fp8_linear(xcodes, xscale, wcodes, wscale, bias, out_dtype, y, workspace, _activation(activation), residual, pre)
 
 
 def fp8_linear_tiles(M: int, I_pad: int, O: int, sm_count: int | None = None):
@@ -309,6 +331,11 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, *, add=None, dx=None, dw
 
     add: the gradient that reaches x past the norm, added to dx.  Returns (dx like x, dweight float32 [C], dbias float32 [C])."""
     return _host.layer_norm_backward(dy, x, mean, rstd, weight, add, dx, dweight, dbias, workspace)
+
+
+def activation_backward_fp8(dh, zcodes, zscale, activation, *, dz=None):
+    """tdq_activation_backward_fp8: dh [..., C] times the activation's slope at its input, kept as codes and scales.  Returns dz like dh (dz=dh works in place)."""
+    return _host.activation_backward_fp8(dh, zcodes, zscale, _activation(activation), dz)
 
 
 def fp8_weight_grad_workspace(dy: torch.Tensor, cin: int) -> torch.Tensor:

@@ -1,0 +1,117 @@
+// The activations of the 8-bit layer's epilogue and their slopes, two elements at a time (packed binary32 multiply-adds).
+#pragma once
+#include "tdq_common.cuh"
+
+#ifdef __CUDACC__
+namespace tdq {
+namespace {
+
+__device__ __forceinline__ float ex2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float rcp(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float min_nan(float a, float b) {   // NaN where either is
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+// Gaussian tail: with a = |z|, e = exp(-a^2 / 2) and q = Phi(-a) = 1/2 erfcx(a / sqrt 2) e.  The smooth factor is a polynomial of degree 11 on [0, 5.2], fitted by
+// least squares with weights moved to the largest errors of max(a, 1) q: 6e-8 at most, roundings of its evaluation among them (behind 5.2 the factor stays what it is there, q is below
+// 1e-7).  One exponential an element and no quotient: the exponential's unit is a quarter as fast as the multiply-adds of an element in pairs.
+__device__ __forceinline__ void gauss_tail(float2 z, float2& a, float2& e, float2& q) {
+    a = make_float2(min_nan(fabsf(z.x), 20.f), min_nan(fabsf(z.y), 20.f));      // exp(-200) is 0 in binary32
+    const float2 g = __fmul2_rn(__fmul2_rn(a, a), both(-0.72134752f));          // -log2(e) / 2
+    e = make_float2(ex2(g.x), ex2(g.y));
+    const float2 b = make_float2(fminf(a.x, 5.2f), fminf(a.y, 5.2f));
+    float2 p = both(-2.29394999e-07f);
+    p = __ffma2_rn(p, b, both(5.99727082e-06f));
+    p = __ffma2_rn(p, b, both(-7.03524929e-05f));
+    p = __ffma2_rn(p, b, both(0.000496292021f));
+    p = __ffma2_rn(p, b, both(-0.00239847647f));
+    p = __ffma2_rn(p, b, both(0.00866080076f));
+    p = __ffma2_rn(p, b, both(-0.0250857733f));
+    p = __ffma2_rn(p, b, both(0.0616591349f));
+    p = __ffma2_rn(p, b, both(-0.132702291f));
+    p = __ffma2_rn(p, b, both(0.249952316f));
+    p = __ffma2_rn(p, b, both(-0.398939103f));
+    p = __ffma2_rn(p, b, both(0.49999997f));
+    q = __fmul2_rn(p, e);
+}
+// 1 / (1 + exp(-z))
+__device__ __forceinline__ float2 sigmoid(float2 z) {
+    const float2 g = __fmul2_rn(z, both(-1.44269504f));
+    const float2 d = __fadd2_rn(make_float2(ex2(g.x), ex2(g.y)), both(1.f));
+    return make_float2(rcp(d.x), rcp(d.y));
+}
+constexpr float kTanhA = 1.59576912f, kTanhB = 0.0713548163f;   // 2 sqrt(2 / pi) (1, 0.044715):  (1 + tanh u) / 2 = sigmoid(2 u)
+
+template <int ACT>
+__device__ __forceinline__ float2 activate(float2 z) {
+    if constexpr (ACT == TDQ_ACT_RELU) {
+        return make_float2(max_nan(z.x, 0.f), max_nan(z.y, 0.f));
+    } else if constexpr (ACT == TDQ_ACT_GELU) {              // z Phi(z) = max(z, 0) - |z| Phi(-|z|)
+        float2 a, e, q;
+        gauss_tail(z, a, e, q);
+        return __ffma2_rn(make_float2(-a.x, -a.y), q, make_float2(max_nan(z.x, 0.f), max_nan(z.y, 0.f)));
+    } else if constexpr (ACT == TDQ_ACT_GELU_TANH) {
+        return __fmul2_rn(z, sigmoid(__fmul2_rn(z, __ffma2_rn(__fmul2_rn(z, z), both(kTanhB), both(kTanhA)))));
+    } else if constexpr (ACT == TDQ_ACT_SILU) {
+        return __fmul2_rn(z, sigmoid(z));
+    } else {
+        return z;
+    }
+}
+template <int ACT>
+__device__ __forceinline__ float2 slope(float2 z) {
+    if constexpr (ACT == TDQ_ACT_RELU) {
+        return make_float2(z.x > 0.f ? 1.f : 0.f, z.y > 0.f ? 1.f : 0.f);
+    } else if constexpr (ACT == TDQ_ACT_GELU) {              // Phi(z) + z phi(z)
+        float2 a, e, q;
+        gauss_tail(z, a, e, q);
+        const float2 h = __ffma2_rn(__fmul2_rn(a, e), both(0.398942280f), __ffma2_rn(q, both(-1.f), both(0.5f)));   // odd part: 1/2 - q + a phi
+        return make_float2(0.5f + copysignf(h.x, z.x), 0.5f + copysignf(h.y, z.y));
+    } else if constexpr (ACT == TDQ_ACT_GELU_TANH) {         // s + z s (1 - s) (2 u)'
+        const float2 z2 = __fmul2_rn(z, z);
+        const float2 s = sigmoid(__fmul2_rn(z, __ffma2_rn(z2, both(kTanhB), both(kTanhA))));
+        const float2 d = __fmul2_rn(z, __ffma2_rn(z2, both(3.f * kTanhB), both(kTanhA)));
+        return __fmul2_rn(s, __ffma2_rn(d, __ffma2_rn(s, both(-1.f), both(1.f)), both(1.f)));
+    } else if constexpr (ACT == TDQ_ACT_SILU) {              // s (1 + z (1 - s))
+        const float2 s = sigmoid(z);
+        return __fmul2_rn(s, __ffma2_rn(z, __ffma2_rn(s, both(-1.f), both(1.f)), both(1.f)));
+    } else {
+        return both(1.f);
+    }
+}
+
+__device__ __forceinline__ float activate_by(int act, float z) {
+    switch (act) {
+        case TDQ_ACT_RELU: return activate<TDQ_ACT_RELU>(both(z)).x;
+        case TDQ_ACT_GELU: return activate<TDQ_ACT_GELU>(both(z)).x;
+        case TDQ_ACT_GELU_TANH: return activate<TDQ_ACT_GELU_TANH>(both(z)).x;
+        case TDQ_ACT_SILU: return activate<TDQ_ACT_SILU>(both(z)).x;
+        default: return z;
+    }
+}
+// all of a thread's sums
+template <int ACT, int N>
+__device__ __forceinline__ void activate_all(float2 (&v)[N]) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = activate<ACT>(v[j]);
+}
+
+}  // namespace
+}  // namespace tdq
+#endif

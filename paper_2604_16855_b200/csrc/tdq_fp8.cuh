@@ -27,11 +27,21 @@ struct Fp8Args {
     uint32_t* status;
 };
 
+// What follows the layer (tdq_fp8_linear_epilogue); the kernels without it have instances of their own.
+struct Fp8Epilogue {
+    int32_t activation;        // tdq_activation
+    int32_t residual_vec, pre_vec;   // rows on the 16-byte grid
+    const void* residual;      // [M][O] of y's type, or null
+    void* pre;                 // likewise
+    int64_t residual_stride, pre_stride;
+    bool any() const { return activation != TDQ_ACT_NONE || residual || pre; }
+};
+
 // Tensor map of a [rows][cols] byte matrix read in boxes of box_rows x 128 bytes, 128-byte swizzle (K-major operand of the
 // tensor core); false when the driver's encoder is missing or refuses.
 bool fp8_operand_map(CUtensorMap* map, const void* p, int64_t rows, int64_t cols, int box_rows);
 // Two CTAs on a tile of 256 tokens and 256 or 128 columns (tdq_fp8_pair.cu); xmap with boxes of 128 rows, wmap of half the columns.
-tdq_status launch_fp8_pair(Fp8Args a, int columns, const CUtensorMap& xmap, const CUtensorMap& wmap, int n_sm, int dev, cudaStream_t stream);
+tdq_status launch_fp8_pair(Fp8Args a, Fp8Epilogue e, int columns, const CUtensorMap& xmap, const CUtensorMap& wmap, int n_sm, int dev, cudaStream_t stream);
 
 #ifdef __CUDACC__
 namespace {

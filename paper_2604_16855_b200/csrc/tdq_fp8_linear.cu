@@ -21,6 +21,7 @@
 
 #include "tdq_tc.cuh"
 #include "tdq_fp8.cuh"
+#include "tdq_activation.cuh"
 
 namespace tdq {
 
@@ -113,9 +114,26 @@ __device__ __forceinline__ void send16(uint32_t addr_c, float2 a, float2 b, uint
                  ::"r"(addr_c), "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "r"(bar_c) : "memory");
 }
 
-template <int NT>
-__global__ void __launch_bounds__(SplitShape<NT>::kThreads, NT == 128 ? 1 : 2)
-fp8_split_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap wmap) {
+// An output with what follows the layer: z, stored where it is kept, then activation(z) + residual.
+__device__ __forceinline__ float load_as(const void* p, int64_t at, int type) {
+    if (type == TDQ_F32) return reinterpret_cast<const float*>(p)[at];
+    const uint16_t v = reinterpret_cast<const uint16_t*>(p)[at];
+    return type == TDQ_BF16 ? widen<TDQ_BF16>(v) : widen<TDQ_F16>(v);
+}
+__device__ __forceinline__ float finish(const Fp8Epilogue& e, int type, int64_t m, int64_t o, float z) {
+    if (e.pre) {
+        const int64_t at = m * e.pre_stride + o;
+        if (type == TDQ_F32) reinterpret_cast<float*>(e.pre)[at] = z;
+        else reinterpret_cast<uint16_t*>(e.pre)[at] = (uint16_t)pack16(z, 0.f, type == TDQ_F16);
+    }
+    z = activate_by(e.activation, z);
+    return e.residual ? z + load_as(e.residual, m * e.residual_stride + o, type) : z;
+}
+struct Nothing {};
+
+// EPI: with what follows the layer, in kernels of their own.
+template <int NT, bool EPI>
+__device__ __forceinline__ void split_body(const Fp8Args& a, const std::conditional_t<EPI, Fp8Epilogue, Nothing>& e, const CUtensorMap& xmap, const CUtensorMap& wmap) {
     using Sh = SplitShape<NT>;
     constexpr int CW = Sh::kCols;
     extern __shared__ __align__(128) uint8_t smem_raw[];
@@ -303,8 +321,10 @@ fp8_split_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, cons
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 if ((int)(quad * 4) + j >= n_tok) break;
-                if (a.y_type == TDQ_F32) reinterpret_cast<float*>(a.y)[at + j * a.y_stride] = r[j] + b;
-                else reinterpret_cast<uint16_t*>(a.y)[at + j * a.y_stride] = (uint16_t)pack16(r[j] + b, 0.f, a.y_type == TDQ_F16);
+                float v = r[j] + b;
+                if constexpr (EPI) v = finish(e, a.y_type, (int64_t)tt * NT + quad * 4 + j, o, v);
+                if (a.y_type == TDQ_F32) reinterpret_cast<float*>(a.y)[at + j * a.y_stride] = v;
+                else reinterpret_cast<uint16_t*>(a.y)[at + j * a.y_stride] = (uint16_t)pack16(v, 0.f, a.y_type == TDQ_F16);
             }
         }
     } else {
@@ -325,6 +345,11 @@ fp8_split_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, cons
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     if (j < left) r[j] += __ldg(a.bias + o + j);
+            }
+            if constexpr (EPI) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (j < left) r[j] = finish(e, a.y_type, (int64_t)tt * NT + (u >> 5), o + j, r[j]);
             }
             const int64_t at = ((int64_t)tt * NT + (u >> 5)) * a.y_stride + o;
             if (a.y_type == TDQ_F32) {
@@ -350,6 +375,17 @@ fp8_split_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, cons
     if (split > 1) cluster_wait();                           // no CTA leaves while another sends to it or reads from it
     if (warp == 2)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "n"(kSplitSlots * NT) : "memory");
+}
+
+template <int NT>
+__global__ void __launch_bounds__(SplitShape<NT>::kThreads, NT == 128 ? 1 : 2)
+fp8_split_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap wmap) {
+    split_body<NT, false>(a, Nothing{}, xmap, wmap);
+}
+template <int NT>
+__global__ void __launch_bounds__(SplitShape<NT>::kThreads, NT == 128 ? 1 : 2)
+fp8_split_epilogue_kernel(const Fp8Args a, const Fp8Epilogue e, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap wmap) {
+    split_body<NT, true>(a, e, xmap, wmap);
 }
 
 // Which kernel, and in how many parts: the least of these estimates in units of 10 ns, fitted to layers of 1 to 9000 tokens, 384 to 7040
@@ -395,8 +431,8 @@ Way choose_way(int64_t M, int64_t O, int K, int n_sm) {
     return best;
 }
 
-template <int NT>
-tdq_status launch_split(Fp8Args a, int split, const uint8_t* xcodes, const CUtensorMap& wmap, int n_sm, int dev, cudaStream_t stream) {
+template <int NT, bool EPI>
+tdq_status launch_split_as(Fp8Args a, const std::conditional_t<EPI, Fp8Epilogue, Nothing>& e, int split, const uint8_t* xcodes, const CUtensorMap& wmap, int n_sm, int dev, cudaStream_t stream) {
     using Sh = SplitShape<NT>;
     CUtensorMap xmap;
     if (!fp8_operand_map(&xmap, xcodes, a.M, (int64_t)a.K * kFp8Block, NT)) return TDQ_ERR_CUDA;
@@ -417,7 +453,11 @@ tdq_status launch_split(Fp8Args a, int split, const uint8_t* xcodes, const CUten
     a.n_stages = stages < per ? stages : per > least ? per : least;
     const uint32_t smem = Sh::kFixed + (uint32_t)a.n_stages * Sh::kStage;
     static std::atomic<uint64_t> smem_done{0};
-    if (allow_smem(fp8_split_kernel<NT>, kSmemLimit, smem_done, dev) != cudaSuccess) return TDQ_ERR_CUDA;
+    if constexpr (EPI) {
+        if (allow_smem(fp8_split_epilogue_kernel<NT>, kSmemLimit, smem_done, dev) != cudaSuccess) return TDQ_ERR_CUDA;
+    } else {
+        if (allow_smem(fp8_split_kernel<NT>, kSmemLimit, smem_done, dev) != cudaSuccess) return TDQ_ERR_CUDA;
+    }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(tiles * a.split));
     cfg.blockDim = dim3(Sh::kThreads);
@@ -431,9 +471,17 @@ tdq_status launch_split(Fp8Args a, int split, const uint8_t* xcodes, const CUten
     at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 2;
-    if (cudaLaunchKernelEx(&cfg, fp8_split_kernel<NT>, a, xmap, wmap) != cudaSuccess) return TDQ_ERR_CUDA;
+    cudaError_t err;
+    if constexpr (EPI) err = cudaLaunchKernelEx(&cfg, fp8_split_epilogue_kernel<NT>, a, e, xmap, wmap);
+    else err = cudaLaunchKernelEx(&cfg, fp8_split_kernel<NT>, a, xmap, wmap);
+    if (err != cudaSuccess) return TDQ_ERR_CUDA;
     g_launch_count.fetch_add(1, std::memory_order_relaxed);
     return TDQ_OK;
+}
+template <int NT>
+tdq_status launch_split(const Fp8Args& a, const Fp8Epilogue& e, int split, const uint8_t* xcodes, const CUtensorMap& wmap, int n_sm, int dev, cudaStream_t stream) {
+    if (e.any()) return launch_split_as<NT, true>(a, e, split, xcodes, wmap, n_sm, dev, stream);
+    return launch_split_as<NT, false>(a, {}, split, xcodes, wmap, n_sm, dev, stream);
 }
 
 // One warp: a fresh barrier with one expected arrival that never comes, waited on with the two kernels' own routine and a short limit.  Nothing is
@@ -473,9 +521,10 @@ extern "C" tdq_status tdq_fp8_linear_tiles(int64_t M, int64_t I_pad, int64_t O, 
     return TDQ_OK;
 }
 
-extern "C" tdq_status tdq_fp8_linear(const uint8_t* xcodes, const float* xscale, const uint8_t* wcodes, const float* wscale, const float* bias,
-                                     int64_t M, int64_t I_pad, int64_t O, void* y, tdq_dtype y_dtype, int64_t y_row_stride, void* workspace,
-                                     size_t workspace_bytes, void* cuda_stream) {
+namespace {
+tdq_status fp8_linear(const uint8_t* xcodes, const float* xscale, const uint8_t* wcodes, const float* wscale, const float* bias, int64_t M, int64_t I_pad,
+                      int64_t O, const Fp8Epilogue& e, void* y, tdq_dtype y_dtype, int64_t y_row_stride, void* workspace, size_t workspace_bytes,
+                      void* cuda_stream) {
     if (M < 0 || O < 0 || I_pad <= 0 || I_pad % kFp8Block || y_row_stride < O) return TDQ_ERR_INVALID_ARG;
     if (y_dtype != TDQ_F32 && y_dtype != TDQ_BF16 && y_dtype != TDQ_F16) return TDQ_ERR_INVALID_ARG;
     if (M == 0 || O == 0) return TDQ_OK;
@@ -483,7 +532,9 @@ extern "C" tdq_status tdq_fp8_linear(const uint8_t* xcodes, const float* xscale,
     if (!workspace || workspace_bytes < kWorkspaceHeader) return TDQ_ERR_WORKSPACE;
     const uintptr_t esz = y_dtype == TDQ_F32 ? 4 : 2;
     const auto off = [](const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; };
-    if (off(xcodes, 16) || off(wcodes, 16) || off(workspace, 16) || off(xscale, 4) || off(wscale, 4) || off(bias, 4) || off(y, esz)) return TDQ_ERR_ALIGNMENT;
+    if (off(xcodes, 16) || off(wcodes, 16) || off(workspace, 16) || off(xscale, 4) || off(wscale, 4) || off(bias, 4) || off(y, esz) ||
+        off(e.residual, esz) || off(e.pre, esz))
+        return TDQ_ERR_ALIGNMENT;
     if (M > kFp8MaxExtent || O > kFp8MaxExtent || I_pad > kFp8MaxExtent) return TDQ_ERR_UNSUPPORTED;
     int dev = 0;
     const int n_sm = current_device_sm_count(&dev);
@@ -501,14 +552,40 @@ extern "C" tdq_status tdq_fp8_linear(const uint8_t* xcodes, const float* xscale,
     a.y_vec = !off(y, 16) && (y_row_stride * (int64_t)esz) % 16 == 0;
     a.status = reinterpret_cast<uint32_t*>(workspace);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+    Fp8Epilogue f = e;
+    f.residual_vec = !off(e.residual, 16) && (e.residual_stride * (int64_t)esz) % 16 == 0;
+    f.pre_vec = !off(e.pre, 16) && (e.pre_stride * (int64_t)esz) % 16 == 0;
     const Way way = choose_way(M, O, a.K, n_sm);
     CUtensorMap wmap;
     if (!fp8_operand_map(&wmap, wcodes, O, I_pad, way.nt == 256 ? way.split / 2 : 128)) return TDQ_ERR_CUDA;
-    if (way.nt == 16) return launch_split<16>(a, way.split, xcodes, wmap, n_sm, dev, st);
-    if (way.nt == 32) return launch_split<32>(a, way.split, xcodes, wmap, n_sm, dev, st);
-    if (way.nt == 64) return launch_split<64>(a, way.split, xcodes, wmap, n_sm, dev, st);
-    if (way.nt == 128) return launch_split<128>(a, way.split, xcodes, wmap, n_sm, dev, st);
+    if (way.nt == 16) return launch_split<16>(a, f, way.split, xcodes, wmap, n_sm, dev, st);
+    if (way.nt == 32) return launch_split<32>(a, f, way.split, xcodes, wmap, n_sm, dev, st);
+    if (way.nt == 64) return launch_split<64>(a, f, way.split, xcodes, wmap, n_sm, dev, st);
+    if (way.nt == 128) return launch_split<128>(a, f, way.split, xcodes, wmap, n_sm, dev, st);
     CUtensorMap xmap;
     if (!fp8_operand_map(&xmap, xcodes, M, I_pad, 128)) return TDQ_ERR_CUDA;
-    return launch_fp8_pair(a, way.split, xmap, wmap, n_sm, dev, st);
+    return launch_fp8_pair(a, f, way.split, xmap, wmap, n_sm, dev, st);
+}
+}  // namespace
+
+extern "C" tdq_status tdq_fp8_linear(const uint8_t* xcodes, const float* xscale, const uint8_t* wcodes, const float* wscale, const float* bias,
+                                     int64_t M, int64_t I_pad, int64_t O, void* y, tdq_dtype y_dtype, int64_t y_row_stride, void* workspace,
+                                     size_t workspace_bytes, void* cuda_stream) {
+    return fp8_linear(xcodes, xscale, wcodes, wscale, bias, M, I_pad, O, Fp8Epilogue{}, y, y_dtype, y_row_stride, workspace, workspace_bytes, cuda_stream);
+}
+
+extern "C" tdq_status tdq_fp8_linear_epilogue(const uint8_t* xcodes, const float* xscale, const uint8_t* wcodes, const float* wscale, const float* bias,
+                                              int64_t M, int64_t I_pad, int64_t O, const tdq_fp8_epilogue* e, void* y, tdq_dtype y_dtype,
+                                              int64_t y_row_stride, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    if (!e || e->activation < TDQ_ACT_NONE || e->activation > TDQ_ACT_SILU || (e->residual && e->residual_row_stride < O) || (e->pre && e->pre_row_stride < O) ||
+        (e->pre && e->pre == y))
+        return TDQ_ERR_INVALID_ARG;
+    if (e->pre && e->residual) return TDQ_ERR_UNSUPPORTED;
+    Fp8Epilogue f = {};
+    f.activation = e->activation;
+    f.residual = e->residual;
+    f.residual_stride = e->residual_row_stride;
+    f.pre = e->pre;
+    f.pre_stride = e->pre_row_stride;
+    return fp8_linear(xcodes, xscale, wcodes, wscale, bias, M, I_pad, O, f, y, y_dtype, y_row_stride, workspace, workspace_bytes, cuda_stream);
 }

@@ -30,6 +30,7 @@
 
 #include "tdq_tc.cuh"
 #include "tdq_fp8.cuh"
+#include "tdq_activation.cuh"
 
 namespace tdq {
 namespace {
@@ -62,6 +63,7 @@ struct PairCtrl {
     uint64_t full[6];                                    // CTA 0: both CTAs' operands of the stage have landed
     uint64_t empty[6];
     uint64_t scales[16];                                 // a block's scales have landed in this CTA
+    uint64_t residual[kAddWarps * kStrips];              // a warp's strip holds its rows' residual
     uint64_t tfull[4], tempty[4];                        // TN = 256: accumulator 2 (a tile's block & 1) + half; 128: a block's & 3 (tempty: CTA 0 only)
 };
 
@@ -118,11 +120,56 @@ __device__ __forceinline__ void copies_arrive(uint32_t bar_s) {
     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar_s) : "memory");
 }
 
-// DT: y's tdq_dtype.
-template <int DT, int TN>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
-fp8_pair_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap wmap,
-                const __grid_constant__ CUtensorMap ymap) {
+struct PairEpilogue {
+    CUtensorMap rmap, pmap;                              // of the residual and of z, in boxes like y's
+    Fp8Epilogue e;
+};
+struct NoEpilogue {};
+
+// A warp's 32 rows x 128 bytes between a strip and a matrix of which rows or a last piece of columns are off the 16-byte grid: element by element, lanes along a
+// row, eight rows in flight (one at a time 1717 x 1464 -> 4862 bf16 took 33.5 us, 477 x 4009 -> 2809 fp32 23.6; now 18.2 and 18.1, on the grid 15.7
+// and 16.6).  Row m0 of the matrix on, `rows` of them, columns from col0 on.
+template <bool Y16, bool STORE>
+__device__ __forceinline__ void move_strip(uint32_t strip_s, void* matrix, int64_t stride, int64_t m0, int rows, int64_t col0, int64_t O, int lane) {
+    using U = std::conditional_t<Y16, uint16_t, uint32_t>;
+    constexpr int kAcross = Y16 ? 2 : 1;
+    U* y = reinterpret_cast<U*>(matrix) + m0 * stride + col0 + lane;
+    const int64_t cols = O - col0 - lane;
+    const auto place = [&](int r0, int r, int q) {
+        const uint32_t b = (uint32_t)(lane + 32 * q) * (uint32_t)sizeof(U);
+        return strip_s + (uint32_t)(r0 + r) * 128u + ((((b >> 4) ^ (uint32_t)r) << 4) | (b & 15u));
+    };
+#pragma unroll 1
+    for (int r0 = 0; r0 < rows; r0 += 8) {
+        U v[8][kAcross];
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+#pragma unroll
+            for (int q = 0; q < kAcross; ++q) {
+                if constexpr (!STORE) v[r][q] = r0 + r < rows && 32 * q < cols ? y[r * stride + 32 * q] : (U)0;
+                else if constexpr (Y16) v[r][q] = (uint16_t)lds16(place(r0, r, q));
+                else v[r][q] = lds32(place(r0, r, q));
+            }
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+#pragma unroll
+            for (int q = 0; q < kAcross; ++q) {
+                if constexpr (STORE) {
+                    if (r0 + r < rows && 32 * q < cols) y[r * stride + 32 * q] = v[r][q];
+                } else if constexpr (Y16) {
+                    asm volatile("st.shared.u16 [%0], %1;" ::"r"(place(r0, r, q)), "h"(v[r][q]) : "memory");
+                } else {
+                    sts32(place(r0, r, q), v[r][q]);
+                }
+            }
+        y += 8 * stride;
+    }
+}
+
+// DT: y's tdq_dtype.  EPI: with what follows the layer; kernels of their own, so that the layer alone costs what it did.
+template <int DT, int TN, bool EPI>
+__device__ __forceinline__ void pair_body(const Fp8Args& a, const CUtensorMap& xmap, const CUtensorMap& wmap, const CUtensorMap& ymap,
+                                          const std::conditional_t<EPI, PairEpilogue, NoEpilogue>& ep) {
     constexpr bool Y16 = DT != TDQ_F32;
     using Sh = PairShape<TN>;
     constexpr int kPairStages = Sh::kStages, kScaleSlots = Sh::kScaleSlots;
@@ -140,6 +187,8 @@ fp8_pair_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const
         for (int i = 0; i < kPairStages; ++i) { mbar_init(&g->full[i], 2); mbar_init(&g->empty[i], TN == 256 ? 2 : 1); }
         for (int i = 0; i < kScaleSlots; ++i) mbar_init(&g->scales[i], 32);
         for (int i = 0; i < 4; ++i) { mbar_init(&g->tfull[i], 1); mbar_init(&g->tempty[i], TN == 256 ? kAddWarps : 2 * kAddWarps); }
+        if constexpr (EPI)
+            for (int i = 0; i < kAddWarps * kStrips; ++i) mbar_init(&g->residual[i], 1);
         c->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -263,6 +312,8 @@ fp8_pair_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const
         const uint32_t tm0 = tmem_base + ((uint32_t)(quarter * 32) << 16) + h * (TN / 2);
         uint32_t par = 0, n = 0;                                 // phase bits of the half's two accumulators; blocks so far
         const bool ragged = a.O % (Y16 ? 8 : 4) != 0;
+        uint32_t use = 0, rpar = 0;                              // EPI: strips used so far, the strips' barriers' phases
+        const uint32_t rbar_s = smem_u32(&g->residual[aw * kStrips]);
         bool full = false, scaled = false;                       // the next block's barriers, asked ahead of their use
         for (int tile = first; tile < n_tiles && !c->abort_flag; tile += n_clusters) {
             const int mt = tile / a.tiles_n, nt = tile - mt * a.tiles_n;
@@ -273,6 +324,28 @@ fp8_pair_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const
             for (int i = 0; i < TN / 64; ++i) {
                 const int64_t col = n0 + (i >> 1) * 128 + (i & 1) * 32 + lane;
                 sts32(bias_s + (uint32_t)(i * 32 + lane) * 4u, a.bias && col < a.O ? __float_as_uint(__ldg(a.bias + col)) : 0u);
+            }
+            constexpr int kStripCols = Y16 ? 64 : 32, kPieces = TN / 2 / kStripCols;
+            const auto col_of = [&](int piece) { return n0 + (piece * kStripCols >> 6) * 128 + (piece * kStripCols & 63); };
+            // the residual's rows, one piece into the strip whose turn it will be
+            const auto load_residual = [&](int piece, uint32_t at_use) {
+                if constexpr (EPI) {
+                    const uint32_t s = at_use & 1u;
+                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(rbar_s + s * 8), "r"(kStrip) : "memory");
+                    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                                 ::"r"(strips_s + s * kStrip), "l"(reinterpret_cast<uint64_t>(&ep.rmap)), "r"((int32_t)col_of(piece)), "r"((int32_t)m0), "r"(rbar_s + s * 8)
+                                 : "memory");
+                }
+            };
+            if constexpr (EPI) {
+                if (ep.e.residual && ep.e.residual_vec) {        // the first two, on their way during the sums
+                    if (lane == 0) {
+                        bulk_wait_group_read0();
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        for (int piece = 0; piece < (kPieces < 2 ? kPieces : 2); ++piece) load_residual(piece, use + piece);
+                    }
+                    __syncwarp();
+                }
             }
             // the tensor core has run ahead during the last tile's epilogue
             full = TN == 256 ? mbar_test_s(tfull_s, par & 1u) : mbar_test_s(tfull_s + (n & 3u) * 8, (n >> 2) & 1u);
@@ -330,8 +403,106 @@ fp8_pair_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const
                 }
             }
             if (c->abort_flag) break;
+            if constexpr (EPI) {
+                constexpr int kPer = Y16 ? 8 : 4;
+                const int rows = (int)max((int64_t)0, min((int64_t)32, a.M - m0));
+                __syncwarp();
+#pragma unroll
+                for (int j = 0; j < TN / 4; j += 2) {            // biases
+                    const float4 t = lds_f4(bias_s + 8u * j);
+                    acc[j] = __fadd2_rn(acc[j], make_float2(t.x, t.y));
+                    acc[j + 1] = __fadd2_rn(acc[j + 1], make_float2(t.z, t.w));
+                }
+                const auto place = [&](uint32_t strip_s, int j) { return strip_s + (uint32_t)lane * 128u + (((uint32_t)j ^ ((uint32_t)lane & 7u)) << 4); };
+                // a piece of the sums, what the strip holds added to it or not, to the strip and on to a matrix
+                const auto put = [&](int piece, bool add, const CUtensorMap* map, bool vec, void* matrix, int64_t stride) {
+                    const uint32_t strip_s = strips_s + (use & 1u) * kStrip;
+                    const int64_t col0 = col_of(piece);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float2* v = acc + (piece * kStripCols + j * kPer) / 2;
+                        float o[kPer];
+#pragma unroll
+                        for (int q = 0; q < kPer; q += 2) { o[q] = v[q / 2].x; o[q + 1] = v[q / 2].y; }
+                        if (add) {
+                            const uint4 r = lds_u4(place(strip_s, j));
+                            const uint32_t rw[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                if constexpr (Y16) {
+                                    float lo, hi;
+                                    widen2<DT>(rw[q], lo, hi);
+                                    o[2 * q] += lo;
+                                    o[2 * q + 1] += hi;
+                                } else {
+                                    o[q] += __uint_as_float(rw[q]);
+                                }
+                            }
+                        }
+                        if constexpr (Y16)
+                            sts128(place(strip_s, j), pack16(o[0], o[1], DT == TDQ_F16), pack16(o[2], o[3], DT == TDQ_F16), pack16(o[4], o[5], DT == TDQ_F16),
+                                   pack16(o[6], o[7], DT == TDQ_F16));
+                        else
+                            sts128(place(strip_s, j), __float_as_uint(o[0]), __float_as_uint(o[1]), __float_as_uint(o[2]), __float_as_uint(o[3]));
+                    }
+                    if (vec && (!ragged || col0 + kStripCols <= a.O)) {
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) {
+                            if (m0 < a.M && col0 < a.O) tma_store_2d(map, strip_s, (int32_t)col0, (int32_t)m0);
+                            bulk_commit_group();
+                        }
+                    } else {
+                        __syncwarp();
+                        move_strip<Y16, true>(strip_s, matrix, stride, m0, rows, col0, a.O, lane);
+                        if (lane == 0) bulk_commit_group();
+                        __syncwarp();
+                    }
+                    ++use;
+                };
+                if (ep.e.pre) {
+#pragma unroll
+                    for (int piece = 0; piece < kPieces; ++piece) {
+                        if (lane == 0) bulk_wait_group_read1();  // the strip has been read: all stores but the last
+                        __syncwarp();
+                        put(piece, false, &ep.pmap, ep.e.pre_vec, ep.e.pre, ep.e.pre_stride);
+                    }
+                }
+                switch (ep.e.activation) {
+                    case TDQ_ACT_RELU: activate_all<TDQ_ACT_RELU>(acc); break;
+                    case TDQ_ACT_GELU: activate_all<TDQ_ACT_GELU>(acc); break;
+                    case TDQ_ACT_GELU_TANH: activate_all<TDQ_ACT_GELU_TANH>(acc); break;
+                    case TDQ_ACT_SILU: activate_all<TDQ_ACT_SILU>(acc); break;
+                    default: break;
+                }
+#pragma unroll
+                for (int piece = 0; piece < kPieces; ++piece) {
+                    const uint32_t st = use & 1u;
+                    if (ep.e.residual && ep.e.residual_vec) {
+                        if (piece > 0 && piece + 1 < kPieces) {  // the piece after next's turn: the strip that was stored last
+                            if (lane == 0) {
+                                bulk_wait_group_read0();
+                                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                                load_residual(piece + 1, use + 1);
+                            }
+                            __syncwarp();
+                        }
+                        fp8_wait(rbar_s + st * 8, (rpar >> st) & 1u, c, a.status, 11u);
+                        rpar ^= 1u << st;
+                        if (c->abort_flag) break;
+                    } else {
+                        if (lane == 0) bulk_wait_group_read1();
+                        __syncwarp();
+                        if (ep.e.residual) {
+                            move_strip<Y16, false>(strips_s + st * kStrip, const_cast<void*>(ep.e.residual), ep.e.residual_stride, m0, rows, col_of(piece), a.O, lane);
+                            __syncwarp();
+                        }
+                    }
+                    put(piece, ep.e.residual != nullptr, &ymap, a.y_vec, a.y, a.y_stride);
+                }
+                if (c->abort_flag) break;
+            } else {
             // 32 rows x 128 bytes at a time: 32 columns of binary32 or 64 of 16 bits
-            constexpr int kStripCols = Y16 ? 64 : 32;
             __syncwarp();
 #pragma unroll
             for (int piece = 0; piece < TN / 2 / kStripCols; ++piece) {
@@ -374,36 +545,12 @@ fp8_pair_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const
                         bulk_commit_group();
                     }
                 } else {
-                    // Rows off the 16-byte grid: element by element, lanes along a row, eight rows in flight (one at a time 1717 x 1464 -> 4862 bf16
-                    // took 33.5 us, 477 x 4009 -> 2809 fp32 23.6; now 18.2 and 18.1, on the grid 15.7 and 16.6).
-                    using U = std::conditional_t<Y16, uint16_t, uint32_t>;
-                    constexpr int kAcross = kStripCols / 32;
                     __syncwarp();
-                    U* y = reinterpret_cast<U*>(a.y) + m0 * a.y_stride + col0 + lane;
-                    const int rows = (int)max((int64_t)0, min((int64_t)32, a.M - m0));
-                    const int64_t cols = a.O - col0 - lane;
-#pragma unroll 1
-                    for (int r0 = 0; r0 < rows; r0 += 8) {
-                        U v[8][kAcross];
-#pragma unroll
-                        for (int r = 0; r < 8; ++r)
-#pragma unroll
-                            for (int q = 0; q < kAcross; ++q) {
-                                const uint32_t b = (uint32_t)(lane + 32 * q) * (uint32_t)sizeof(U);
-                                const uint32_t at = strip_s + (uint32_t)(r0 + r) * 128u + ((((b >> 4) ^ (uint32_t)r) << 4) | (b & 15u));
-                                if constexpr (Y16) v[r][q] = (uint16_t)lds16(at);
-                                else v[r][q] = lds32(at);
-                            }
-#pragma unroll
-                        for (int r = 0; r < 8; ++r)
-#pragma unroll
-                            for (int q = 0; q < kAcross; ++q)
-                                if (r0 + r < rows && 32 * q < cols) y[r * a.y_stride + 32 * q] = v[r][q];
-                        y += 8 * a.y_stride;
-                    }
+                    move_strip<Y16, true>(strip_s, a.y, a.y_stride, m0, (int)max((int64_t)0, min((int64_t)32, a.M - m0)), col0, a.O, lane);
                     if (lane == 0) bulk_commit_group();          // an empty one: a strip's turn is counted in groups
                     __syncwarp();
                 }
+            }
             }
         }
         if (lane == 0) bulk_wait_group0();                       // no store may still be reading this CTA's shared memory at exit
@@ -417,29 +564,66 @@ fp8_pair_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "n"(512) : "memory");
 }
 
-}  // namespace
+template <int DT, int TN>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+fp8_pair_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap wmap,
+                const __grid_constant__ CUtensorMap ymap) {
+    pair_body<DT, TN, false>(a, xmap, wmap, ymap, NoEpilogue{});
+}
+template <int DT, int TN>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+fp8_pair_epilogue_kernel(const Fp8Args a, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap wmap,
+                         const __grid_constant__ CUtensorMap ymap, const __grid_constant__ PairEpilogue ep) {
+    pair_body<DT, TN, true>(a, xmap, wmap, ymap, ep);
+}
 
-tdq_status launch_fp8_pair(Fp8Args a, int columns, const CUtensorMap& xmap, const CUtensorMap& wmap, int n_sm, int dev, cudaStream_t stream) {
+template <bool EPI>
+tdq_status launch_pair_as(Fp8Args a, Fp8Epilogue e, int columns, const CUtensorMap& xmap, const CUtensorMap& wmap, int n_sm, int dev, cudaStream_t stream) {
     const bool y16 = a.y_type != TDQ_F32, f16 = a.y_type == TDQ_F16;
     CUtensorMap ymap;
     memset(&ymap, 0, sizeof ymap);
     if (a.y_vec && !encode_y_map(&ymap, a.y, y16, a.M, a.O, a.y_stride, y16 ? 64 : 32, 32, f16)) a.y_vec = 0;
+    std::conditional_t<EPI, PairEpilogue, NoEpilogue> ep{};
+    if constexpr (EPI) {
+        if (e.residual && e.residual_vec && !encode_y_map(&ep.rmap, const_cast<void*>(e.residual), y16, a.M, a.O, e.residual_stride, y16 ? 64 : 32, 32, f16)) e.residual_vec = 0;
+        if (e.pre && e.pre_vec && !encode_y_map(&ep.pmap, e.pre, y16, a.M, a.O, e.pre_stride, y16 ? 64 : 32, 32, f16)) e.pre_vec = 0;
+        ep.e = e;
+    }
     a.tiles_m = (int32_t)((a.M + 255) / 256);
     a.tiles_n = (int32_t)((a.O + columns - 1) / columns);
     static_assert(PairShape<256>::kSmem <= (uint32_t)kSmemLimit && PairShape<128>::kSmem <= (uint32_t)kSmemLimit, "shared memory");
     static std::atomic<uint64_t> smem_done[2][3];
-    void (*const kernels[2][3])(Fp8Args, CUtensorMap, CUtensorMap, CUtensorMap) = {
-        {fp8_pair_kernel<TDQ_F32, 256>, fp8_pair_kernel<TDQ_BF16, 256>, fp8_pair_kernel<TDQ_F16, 256>},
-        {fp8_pair_kernel<TDQ_F32, 128>, fp8_pair_kernel<TDQ_BF16, 128>, fp8_pair_kernel<TDQ_F16, 128>}};
     const int narrow = columns == 128;
     const uint32_t smem = narrow ? PairShape<128>::kSmem : PairShape<256>::kSmem;
-    if (allow_smem(kernels[narrow][a.y_type], (int)smem, smem_done[narrow][a.y_type], dev) != cudaSuccess) return TDQ_ERR_CUDA;
     const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n;
     if (tiles > INT32_MAX / 2) return TDQ_ERR_UNSUPPORTED;
     const unsigned clusters = (unsigned)(tiles < n_sm / 2 ? tiles : n_sm / 2);
-    if (launch_pdl(kernels[narrow][a.y_type], dim3(2 * clusters), dim3(kPairThreads), smem, stream, a, xmap, wmap, ymap) != cudaSuccess) return TDQ_ERR_CUDA;
+    const auto launch = [&](const auto& kernels, const auto&... more) {
+        const auto kernel = kernels[narrow][a.y_type];
+        if (allow_smem(kernel, (int)smem, smem_done[narrow][a.y_type], dev) != cudaSuccess) return cudaErrorUnknown;
+        return launch_pdl(kernel, dim3(2 * clusters), dim3(kPairThreads), smem, stream, a, xmap, wmap, ymap, more...);
+    };
+    cudaError_t err;
+    if constexpr (EPI) {
+        void (*const kernels[2][3])(Fp8Args, CUtensorMap, CUtensorMap, CUtensorMap, PairEpilogue) = {
+            {fp8_pair_epilogue_kernel<TDQ_F32, 256>, fp8_pair_epilogue_kernel<TDQ_BF16, 256>, fp8_pair_epilogue_kernel<TDQ_F16, 256>},
+            {fp8_pair_epilogue_kernel<TDQ_F32, 128>, fp8_pair_epilogue_kernel<TDQ_BF16, 128>, fp8_pair_epilogue_kernel<TDQ_F16, 128>}};
+        err = launch(kernels, ep);
+    } else {
+        void (*const kernels[2][3])(Fp8Args, CUtensorMap, CUtensorMap, CUtensorMap) = {
+            {fp8_pair_kernel<TDQ_F32, 256>, fp8_pair_kernel<TDQ_BF16, 256>, fp8_pair_kernel<TDQ_F16, 256>},
+            {fp8_pair_kernel<TDQ_F32, 128>, fp8_pair_kernel<TDQ_BF16, 128>, fp8_pair_kernel<TDQ_F16, 128>}};
+        err = launch(kernels);
+    }
+    if (err != cudaSuccess) return TDQ_ERR_CUDA;
     g_launch_count.fetch_add(1, std::memory_order_relaxed);
     return TDQ_OK;
+}
+
+}  // namespace
+
+tdq_status launch_fp8_pair(Fp8Args a, Fp8Epilogue e, int columns, const CUtensorMap& xmap, const CUtensorMap& wmap, int n_sm, int dev, cudaStream_t stream) {
+    return e.any() ? launch_pair_as<true>(a, e, columns, xmap, wmap, n_sm, dev, stream) : launch_pair_as<false>(a, e, columns, xmap, wmap, n_sm, dev, stream);
 }
 
 }  // namespace tdq

@@ -440,11 +440,13 @@ PyObject* quantize_weight_fp8(PyObject* const* a) {
     return tuple2(codes, scale);
 }
 
-// fp8_linear(xcodes, xscale, wcodes, wscale, bias, out_dtype, y, workspace)
+// fp8_linear(xcodes, xscale, wcodes, wscale, bias, out_dtype, y, workspace, activation, residual, pre)
 PyObject* fp8_linear(PyObject* const* a) {
     const at::Tensor &xc = tensor(a[0]), &xs = tensor(a[1]), &wc = tensor(a[2]), &ws = tensor(a[3]);
-    const at::Tensor *bias = opt_tensor(a[4]), *oy = opt_tensor(a[6]), *ow = opt_tensor(a[7]);
-    need_cuda({&xc, &xs, &wc, &ws, bias, oy, ow});
+    const at::Tensor *bias = opt_tensor(a[4]), *oy = opt_tensor(a[6]), *ow = opt_tensor(a[7]), *res = opt_tensor(a[9]), *pre = opt_tensor(a[10]);
+    need_cuda({&xc, &xs, &wc, &ws, bias, oy, ow, res, pre});
+    tdq_fp8_epilogue e = {};
+    e.activation = (int32_t)int_arg(a[8]);
     if (xc.dim() != 2 || wc.dim() != 2) throw Bad{PyExc_ValueError, "xcodes and wcodes must be matrices"};
     const int64_t M = xc.size(0), I_pad = xc.size(1), O = wc.size(0), K = I_pad / kFp8Block;
     if (I_pad < 1 || I_pad % kFp8Block) throw Bad{PyExc_ValueError, "the codes' rows must be a multiple of 128 long"};
@@ -458,6 +460,14 @@ PyObject* fp8_linear(PyObject* const* a) {
     check_y(y, &xc);
     if (y.size(0) != M || y.size(1) != O) throw Bad{PyExc_ValueError, "y must be of size [" + std::to_string(M) + ", " + std::to_string(O) + "]"};
     const tdq_dtype dt = dtype_id(y);
+    const auto beside = [&](const char* name, const at::Tensor& t) {   // a matrix like y
+        if (t.scalar_type() != y.scalar_type()) throw Bad{PyExc_TypeError, std::string(name) + " must be " + dtype_name(y.scalar_type()) + ", got " + dtype_name(t.scalar_type())};
+        if (t.sizes() != y.sizes() || (O > 1 && t.stride(1) != 1) || t.device() != y.device())
+            throw Bad{PyExc_ValueError, std::string(name) + " must be of y's size and device, its columns adjacent in memory"};
+        return M > 1 ? t.stride(0) : O;
+    };
+    if (res) { e.residual = ptr(res); e.residual_row_stride = beside("residual", *res); }
+    if (pre) { e.pre = ptr(pre); e.pre_row_stride = beside("pre", *pre); }
     at::DataPtr own;
     void* wsp = ow ? ow->data_ptr() : nullptr;
     size_t wsp_bytes = ow ? (size_t)ow->numel() : 0;
@@ -467,10 +477,16 @@ PyObject* fp8_linear(PyObject* const* a) {
         own = c10::cuda::CUDACachingAllocator::get()->allocate(wsp_bytes);
         wsp = own.get();
     }
-    check(call(xc, [&](void* st) {
-              return tdq_fp8_linear(ptr<uint8_t>(xc), ptr<float>(xs), ptr<uint8_t>(wc), ptr<float>(ws), ptr<float>(bias), M, I_pad, O, ptr(y), dt,
-                                    M > 1 ? y.stride(0) : O, wsp, wsp_bytes, st);
-          }), "tdq_fp8_linear");
+    if (e.activation != TDQ_ACT_NONE || res || pre)
+        check(call(xc, [&](void* st) {
+                  return tdq_fp8_linear_epilogue(ptr<uint8_t>(xc), ptr<float>(xs), ptr<uint8_t>(wc), ptr<float>(ws), ptr<float>(bias), M, I_pad, O, &e, ptr(y), dt,
+                                                 M > 1 ? y.stride(0) : O, wsp, wsp_bytes, st);
+              }), "tdq_fp8_linear_epilogue");
+    else
+        check(call(xc, [&](void* st) {
+                  return tdq_fp8_linear(ptr<uint8_t>(xc), ptr<float>(xs), ptr<uint8_t>(wc), ptr<float>(ws), ptr<float>(bias), M, I_pad, O, ptr(y), dt,
+                                        M > 1 ? y.stride(0) : O, wsp, wsp_bytes, st);
+              }), "tdq_fp8_linear");
     return THPVariable_Wrap(y);
 }
 
@@ -699,6 +715,24 @@ PyObject* fp8_weight_grad(PyObject* const* a) {
     return tuple_of({dw, db});
 }
 
+// activation_backward_fp8(dh, zcodes, zscale, activation, dz)
+PyObject* activation_backward_fp8(PyObject* const* a) {
+    const at::Tensor &dh0 = tensor(a[0]), &zc = tensor(a[1]), &zs = tensor(a[2]);
+    const at::Tensor* odz = opt_tensor(a[4]);
+    need_cuda({&dh0, &zc, &zs, odz});
+    const Rows dh = rows_of("dh", dh0, true);
+    const tdq_dtype dt = dtype_id(dh0);
+    const int64_t act = int_arg(a[3]), K = fp8_blocks(dh.C);
+    check_tensor("zcodes", zc, {at::kFloat8_e4m3fn, at::kByte}, {dh.M, K * kFp8Block}, dh0);
+    check_tensor("zscale", zs, {at::kFloat}, {dh.M, K}, dh0);
+    const at::Tensor out = odz ? *odz : new_like(dh0, dh0.sizes(), dh0.scalar_type());
+    const Rows dz = rows_like("dz", out, dh, false);
+    check(call(dh0, [&](void* st) {
+              return tdq_activation_backward_fp8(dh.p(), dt, dh.M, dh.C, dh.stride, ptr<uint8_t>(zc), ptr<float>(zs), (int32_t)act, dz.p(), dz.stride, st);
+          }), "tdq_activation_backward_fp8");
+    return THPVariable_Wrap(out);
+}
+
 // Argument count, and C++ exceptions as Python ones.
 template <PyObject* (*F)(PyObject* const*), int N>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -726,9 +760,9 @@ PyObject* set_error_class(PyObject*, PyObject* cls) {
 PyMethodDef methods[] = {
     TDQ_ENTRY(quantize_act, 5), TDQ_ENTRY(quantize_act_fixed, 6), TDQ_ENTRY(quantize_act_nchw, 5), TDQ_ENTRY(quantize_weight, 4),
     TDQ_ENTRY(w4a4_linear, 11), TDQ_ENTRY(w4a4_linear_static, 8), TDQ_ENTRY(quant_linear_fused, 8), TDQ_ENTRY(quant_linear_host, 7),
-    TDQ_ENTRY(quantize_act_fp8, 4), TDQ_ENTRY(quantize_weight_fp8, 3), TDQ_ENTRY(fp8_linear, 8), TDQ_ENTRY(qk_norm_rope, 11),
+    TDQ_ENTRY(quantize_act_fp8, 4), TDQ_ENTRY(quantize_weight_fp8, 3), TDQ_ENTRY(fp8_linear, 11), TDQ_ENTRY(qk_norm_rope, 11),
     TDQ_ENTRY(layer_norm, 7), TDQ_ENTRY(layer_norm_fp8, 9), TDQ_ENTRY(layer_norm_backward, 10),
-    TDQ_ENTRY(fp8_weight_grad, 9),
+    TDQ_ENTRY(fp8_weight_grad, 9), TDQ_ENTRY(activation_backward_fp8, 5),
     {"set_error_class", set_error_class, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 #undef TDQ_ENTRY
 

@@ -92,3 +92,35 @@ def test_weight_grad(tdq):
     assert size(FAKE, 1, 40, 64, 40, 90) == one and size(FAKE, 1, 41, 64, 40, 90) == one + 64 * 40 * 2
     two = 256 + 2 * 2 * 256 * 256 * 4 + 5 * 1024             # two stages, two clusters with two places each
     assert size(FAKE, 1, 40, 65, 40, 90) == two and size(FAKE, 2, 40, 64, 40, 90) == two + 2 * 64 * 40 * 2
+
+
+def test_linear_epilogue(tdq):
+    inv, ali, uns = tdq.ERR_INVALID_ARG, tdq.ERR_ALIGNMENT, tdq.ERR_UNSUPPORTED
+    f = tdq.lib().tdq_fp8_linear_epilogue
+    n = tdq.FP8_WORKSPACE_BYTES
+
+    def call(e=(2, None, 0, None, 0), **kw):
+        a = dict(xc=FAKE, xs=FAKE, wc=FAKE, ws=FAKE, bias=None, M=4, I=256, O=8, e=0, y=FAKE, dt=0, st=8, wsp=FAKE, n=n, stream=None)
+        a.update(kw)
+        a["e"] = ctypes.byref(tdq.Fp8Epilogue(*e)) if e else None
+        return f(*a.values())
+    assert call(e=None) == inv and call(e=(-1, None, 0, None, 0)) == inv and call(e=(5, None, 0, None, 0)) == inv
+    assert call(e=(0, 0x2000, 7, None, 0)) == inv and call(e=(0, None, 0, 0x2000, 7)) == inv and call(e=(0, None, 0, 0x1000, 8)) == inv
+    assert call(e=(0, 0x2000, 8, 0x3000, 8)) == uns
+    assert call(e=(0, 0x2001, 8, None, 0)) == ali and call(e=(0, None, 0, 0x2002, 8)) == ali
+    assert call(xc=None) == inv and call(xc=OFF4) == ali and call(wsp=None) == tdq.ERR_WORKSPACE and call(M=1 << 31) == uns
+    assert call(M=0) == tdq.OK
+
+
+def test_activation_backward(tdq):
+    inv, ali, uns = tdq.ERR_INVALID_ARG, tdq.ERR_ALIGNMENT, tdq.ERR_UNSUPPORTED
+    _each(tdq.lib().tdq_activation_backward_fp8, [FAKE, 1, 4, 40, 40, FAKE, FAKE, 2, FAKE, 40, None],
+          [((i, v), c) for i, v, c in [(0, None, inv), (5, None, inv), (6, None, inv), (8, None, inv), (1, 3, inv), (2, -1, inv), (3, 0, inv), (4, 39, inv),
+                                       (9, 39, inv), (7, 5, inv), (7, -1, inv), (0, ODD, ali), (8, ODD, ali), (5, OFF4, ali), (6, ODD, ali), (2, 1 << 30, uns), (2, 0, tdq.OK)]])
+
+
+def test_activation_names(tdq):
+    x = torch.zeros(4, 64)
+    for f in (lambda: tdq.fp8_linear(x, x, x, x, activation="tanh"), lambda: tdq.activation_backward_fp8(x, x, x, "tanh"), lambda: tdq.activation_backward_fp8(x, x, x, "gelu")):
+        with pytest.raises(ValueError):
+            f()
