@@ -15,6 +15,7 @@
 //
 //   warps 0, 1  copies of dy; the instructions (CTA 0)      warps 4-11  sums and output      warps 12-19  restore x, sum db
 #include <algorithm>
+#include <numeric>
 
 #include "tdq_tc.cuh"
 #include "tdq_rows.cuh"
@@ -34,25 +35,35 @@ constexpr int kSumWarp0 = 4, kSumWarps = 8, kFillWarp0 = 12, kFillWarps = 8;
 constexpr int kGradThreads = (kFillWarp0 + kFillWarps) * 32;
 constexpr int kFillPairs = kFillWarps / 2;               // two warps fill a stage, every fourth one
 constexpr uint32_t kGradCodes = kTok * 128;                // bytes of a stage's codes
-constexpr uint32_t kGradDb = kFillPairs * 128 * 4;
-constexpr uint32_t kGradSmem = kGradCtrl + kGradStages * kGradStage + kFillPairs * kGradCodes + kSumWarps * kGradStrip + kGradDb;
+constexpr uint32_t kGradSmem = kGradCtrl + kGradStages * kGradStage + kFillPairs * kGradCodes + kSumWarps * kGradStrip;
 static_assert(kGradSmem <= (uint32_t)kSmemLimit, "shared memory");
 constexpr int kGradRegsLoad = 32, kGradRegsSum = 160, kGradRegsFill = 64;   // 128 * 32 + 256 * 160 + 256 * 64 <= 640 * 96
 // D binary32, both operands bf16 with the sum's axis slow, 256 columns x 256 rows
 constexpr uint32_t kGradIdesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((256u >> 3) << 17) | ((256u >> 4) << 24);
 constexpr uint32_t kGradDescLo = (kGradHalf >> 4) << 16;  // the next 64 columns; eight tokens further on are 1024 bytes (kSwDescHi)
 
+// The row of all tiles' stages, in `clusters` pieces of whole units (of a stage, or of a tile's stages where tiles are not cut).
+struct Cut {
+    int32_t units, unit, clusters;
+    // the first stage that cluster w adds
+    __host__ __device__ int32_t begin(int32_t w) const { return unit * (units / clusters * w + min(w, units % clusters)); }
+    // the cluster that adds stage s
+    __host__ __device__ int32_t owner(int32_t s) const {
+        const int32_t u = s / unit, q = units / clusters, r = units % clusters, longer = r * (q + 1);
+        return u < longer ? u / (q + 1) : r + (u - longer) / q;
+    }
+};
 struct GradArgs {
     const uint8_t* xcodes;     // [M][Kb * 128]
     const float* xscale;       // [M][Kb]
     const uint16_t* dy;        // bf16 [parts * rows_part][dy_stride]
     void* dw;
     float* db;                 // or null
-    float* dbpart;             // [2 clusters + tiles][256]: cut tiles' parts, whole tiles'
-    float* part;               // [2 clusters][256][256]
+    float* dbpart;             // [2 clusters + tiles][pairs of warps][256]: cut tiles' parts, whole tiles'
+    float4* part;              // [2 clusters][2 CTAs][8 warps][32 quads of columns][32 rows]
     int64_t M, O, I, dy_stride, dw_stride, rows_part;
     int32_t Kb, tiles_o, tiles_i, stages_part, parts;   // stages of an addend, addends
-    int32_t clusters;
+    Cut cut;
     int32_t dw_vec;            // rows of dw on the 16-byte grid
     uint32_t* status;
 };
@@ -62,24 +73,15 @@ struct GradCtrl {
     uint64_t empty[kGradStages];
     uint64_t codes[kFillPairs], taken[kFillPairs];            // a pair's codes have landed; have been read
     uint64_t tfull[2], tempty[2];
-    uint64_t met;                                            // the restoring warps meet, twice for each sum of db
 };
 static_assert(sizeof(Ctrl) + sizeof(GradCtrl) <= kGradCtrl, "control block outgrew its reservation");
 
-// the first of the row of all tiles' stages that cluster w adds
-__host__ __device__ inline int32_t piece_begin(int32_t total, int32_t clusters, int32_t w) { return total / clusters * w + min(w, total % clusters); }
-// the cluster that adds stage s
-__host__ __device__ inline int32_t piece_owner(int32_t total, int32_t clusters, int32_t s) {
-    const int32_t q = total / clusters, r = total % clusters, longer = r * (q + 1);
-    return s < longer ? s / (q + 1) : r + (s - longer) / q;
-}
 // A cluster's stages, tile by tile, in the order in which it adds them: the tile at its end first, which begins with the first tokens, then the rest, which begins in the
 // middle of a tile.  So all clusters go through the tokens at about the same time, and what several tiles read is read from memory once (from the piece's
 // begin on instead: 16384 tokens, 1024 -> 4096 bf16 TODO us).
 struct Piece {
     int32_t per_tile, begin, end, last;                      // last: where its last tile's stages begin, if it has more than one tile; else its end
-    __device__ Piece(int32_t per_tile_, int32_t total, int32_t clusters, int32_t w)
-        : per_tile(per_tile_), begin(piece_begin(total, clusters, w)), end(piece_begin(total, clusters, w + 1)) {
+    __device__ Piece(int32_t per_tile_, const Cut& cut, int32_t w) : per_tile(per_tile_), begin(cut.begin(w)), end(cut.begin(w + 1)) {
         const int32_t t = (end - 1) / per_tile * per_tile;
         last = t > begin ? t : end;
     }
@@ -142,14 +144,13 @@ __device__ __forceinline__ void restore4(uint32_t codes, float scale, uint32_t& 
 // DT: dw's tdq_dtype
 template <int DT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGradThreads, 1)
-fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap dwmap, const __grid_constant__ CUtensorMap partmap) {
+fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap dwmap) {
     constexpr bool W16 = DT != TDQ_F32;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     Ctrl* c = reinterpret_cast<Ctrl*>(smem_raw);             // its abort flag and TMEM address; the barriers are g's
     GradCtrl* g = reinterpret_cast<GradCtrl*>(smem_raw + sizeof(Ctrl));
     const uint32_t sm_s = smem_u32(smem_raw), ring_s = sm_s + kGradCtrl;
     const uint32_t codes_s = ring_s + kGradStages * kGradStage, strips_s = codes_s + kFillPairs * kGradCodes;
-    float* db_room = reinterpret_cast<float*>(smem_raw + kGradSmem - kGradDb);
     const int warp = uniform_warp(), lane = threadIdx.x & 31;
     const uint32_t rank = fp8_cluster_rank();
 
@@ -157,9 +158,12 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
         for (int i = 0; i < kGradStages; ++i) { mbar_init(&g->landed[i], 1); mbar_init(&g->full[i], 4); mbar_init(&g->empty[i], 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(&g->tfull[i], 1); mbar_init(&g->tempty[i], 2 * kSumWarps); }
         for (int i = 0; i < kFillPairs; ++i) { mbar_init(&g->codes[i], 1); mbar_init(&g->taken[i], 2); }
-        mbar_init(&g->met, kFillWarps);
         c->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (threadIdx.x == 32) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&dymap)) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&xmap)) : "memory");
     }
     if (warp == 2) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&c->tmem_base)), "n"(512) : "memory");
@@ -175,7 +179,7 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
     const uint32_t tmem_base = c->tmem_base;
     const int32_t w = (int32_t)blockIdx.x / 2;
     const int32_t per_tile = a.stages_part * a.parts;
-    const Piece piece(per_tile, per_tile * a.tiles_o * a.tiles_i, a.clusters, w);
+    const Piece piece(per_tile, a.cut, w);
     const int32_t n_stages = piece.stages();
 
     if (warp < kSumWarp0) {
@@ -295,8 +299,12 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
             const bool whole = stretch.whole;
             const int32_t slot = 2 * w + stretch.slot;
             const int64_t o0 = (int64_t)to * 256 + rank * 128 + quarter * 32, i0 = (int64_t)ti * 256 + h * 128;
-            if (!W16 || !whole) {
-                const CUtensorMap* map = whole ? &dwmap : &partmap;
+            if (!whole) {
+                // a part, as it lies in the registers: 512 bytes an instruction
+                float4* dst = a.part + ((((int64_t)slot * 2 + rank) * kSumWarps + sw) * 32) * 32 + lane;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) dst[j * 32] = make_float4(acc[2 * j].x, acc[2 * j].y, acc[2 * j + 1].x, acc[2 * j + 1].y);
+            } else if (!W16) {
 #pragma unroll
                 for (int piece = 0; piece < 4; ++piece) {
                     if (lane == 0) bulk_wait_group_read0();          // the strip has been read
@@ -308,12 +316,11 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
                                __float_as_uint(v.x), __float_as_uint(v.y));
                     }
                     const int64_t col = i0 + piece * 32;
-                    if (!whole || (a.dw_vec && (a.I % 4 == 0 || col + 32 <= a.I))) {
+                    if (a.dw_vec && (a.I % 4 == 0 || col + 32 <= a.I)) {
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         __syncwarp();
                         if (lane == 0) {
-                            if (!whole) tma_store_2d(map, strip_s, h * 128 + piece * 32, slot * 256 + (int)rank * 128 + quarter * 32);
-                            else if (o0 < a.O && col < a.I) tma_store_2d(map, strip_s, (int32_t)col, (int32_t)o0);
+                            if (o0 < a.O && col < a.I) tma_store_2d(&dwmap, strip_s, (int32_t)col, (int32_t)o0);
                             bulk_commit_group();
                         }
                     } else {
@@ -372,7 +379,6 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
         setmaxnreg_dec<kGradRegsFill>();
         const int fw = warp - kFillWarp0, pair = fw >> 1, side = fw & 1;   // a warp restores 32 tokens and sums 64 outputs of every fourth stage
         const uint32_t full0 = map_to_cta(smem_u32(&g->full[0]), 0), empty_s = smem_u32(&g->empty[0]), landed_s = smem_u32(&g->landed[0]);
-        const uint32_t met_s = smem_u32(&g->met);
         const uint32_t codes_bar = smem_u32(&g->codes[pair]), taken_bar = smem_u32(&g->taken[pair]);
         // Sixteen codes a lane and token, channels 16 (lane & 7) ..: of token 4 q + lane / 8, the upper 64 channels of its neighbour, so that eight lanes
         // read, and write, eight different 16-byte columns (the swizzle moves a row's by its number: odd and even rows never meet).
@@ -453,28 +459,17 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
                 if (s >= kGradStages) { s -= kGradStages; ph ^= 1u; }
             }
             if (c->abort_flag) break;
-            if (a.db) {                                      // this stretch's column sums: four pairs', in order
+            if (a.db) {                                      // this stretch's column sums, this warp's
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
                     for (int x = 8; x <= 16; x <<= 1)
                         sum[j] = __fadd2_rn(sum[j], make_float2(__shfl_xor_sync(0xffffffffu, sum[j].x, x), __shfl_xor_sync(0xffffffffu, sum[j].y, x)));
                 if (lane < 8) {
+                    float* to = a.dbpart + ((int64_t)(t.whole ? 2 * a.cut.clusters + t.tile : 2 * w + t.slot) * kFillPairs + pair) * 256 + rank * 128 + side * 64 + 8 * lane;
 #pragma unroll
-                    for (int j = 0; j < 4; j += 2)
-                        *reinterpret_cast<float4*>(db_room + pair * 128 + side * 64 + 8 * lane + 2 * j) = make_float4(sum[j].x, sum[j].y, sum[j + 1].x, sum[j + 1].y);
+                    for (int j = 0; j < 4; j += 2) *reinterpret_cast<float4*>(to + 2 * j) = make_float4(sum[j].x, sum[j].y, sum[j + 1].x, sum[j + 1].y);
                 }
-                __syncwarp();
-                mbar_arrive_lane0_s(met_s, lane);
-                fp8_wait(met_s, 0u, c, a.status, 7u);
-                if (fw < 4) {
-                    const int col = fw * 32 + lane;
-                    a.dbpart[(int64_t)(t.whole ? 2 * a.clusters + t.tile : 2 * w + t.slot) * 256 + rank * 128 + col] =
-                        ((db_room[col] + db_room[128 + col]) + db_room[256 + col]) + db_room[384 + col];
-                }
-                __syncwarp();
-                mbar_arrive_lane0_s(met_s, lane);
-                fp8_wait(met_s, 1u, c, a.status, 7u);
             }
             k += t.len;
         }
@@ -483,70 +478,100 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
     tc_fence_before();
     __syncthreads();
     if (c->abort_flag) __nanosleep(1000000);                 // a wait gave up: give copies and tensor core a moment
-    fp8_cluster_sync();                                      // neither CTA leaves while the other may still signal it
+    // Neither CTA leaves while the other may still signal it.  Relaxed: an arrival that releases waits for the thread's stores to memory (1400 clocks).
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (warp == 2)
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "n"(512) : "memory");
 }
 
-// Adds the parts of the tiles that were cut, in order of the sum, a thread block for four rows of a tile; the blocks behind those add db, 64 outputs each.
+// Adds the parts of the tiles that were cut, in order of the sum: a thread block for the 32 rows x 128 columns of a summing warp, which it turns to rows in shared memory.
+// The blocks behind those add db, 32 outputs each.
 template <int DT>
 __global__ void __launch_bounds__(256) grad_parts_kernel(const GradArgs a, int32_t tile_blocks) {
+    constexpr int kPitch = 132;                              // floats of a row of the turned block
+    __shared__ __align__(16) float room[32 * kPitch];
     pdl_wait();
     pdl_trigger();
-    const int32_t per_tile = a.stages_part * a.parts, total = per_tile * a.tiles_o * a.tiles_i;
-    const int lane = (int)threadIdx.x & 63, y = (int)threadIdx.x >> 6;
+    const int32_t per_tile = a.stages_part * a.parts;
     if ((int32_t)blockIdx.x >= tile_blocks) {
-        __shared__ float sums[4][64];
-        const int64_t o = ((int64_t)blockIdx.x - tile_blocks) * 64 + lane;
+        const int lane = (int)threadIdx.x & 31, y = (int)threadIdx.x >> 5;
+        const int64_t o = ((int64_t)blockIdx.x - tile_blocks) * 32 + lane;
         const int to = (int)(o >> 8), col = (int)(o & 255);
         float s = 0.f;
         if (to < a.tiles_o)
-            for (int t = y; t < a.tiles_i; t += 4) {
+            for (int t = y >> 1; t < a.tiles_i; t += 4) {        // two threads a tile, two pairs of warps each
                 const int32_t tile = to * a.tiles_i + t, first = tile * per_tile;
-                const int32_t w0 = piece_owner(total, a.clusters, first), w1 = piece_owner(total, a.clusters, first + per_tile - 1);
-                if (w0 == w1) s += a.dbpart[(int64_t)(2 * a.clusters + tile) * 256 + col];
-                else
+                const int32_t w0 = a.cut.owner(first), w1 = a.cut.owner(first + per_tile - 1);
+                const float* from = a.dbpart + (int64_t)(y & 1) * 512 + col;
 #pragma unroll 4
-                    for (int32_t w = w0; w <= w1; ++w) s += a.dbpart[(int64_t)(2 * w + (w == w0 && piece_begin(total, a.clusters, w) < first ? 1 : 0)) * 256 + col];
+                for (int32_t w = w0; w <= w1; ++w) {
+                    const int64_t slot = w0 == w1 ? 2 * a.cut.clusters + tile : 2 * w + (w == w0 && a.cut.begin(w) < first ? 1 : 0);
+                    s += from[slot * (kFillPairs * 256)] + from[slot * (kFillPairs * 256) + 256];
+                }
             }
-        sums[y][lane] = s;
+        room[y * 32 + lane] = s;
         __syncthreads();
-        if (y == 0 && o < a.O) a.db[o] = ((sums[0][lane] + sums[1][lane]) + sums[2][lane]) + sums[3][lane];
+        if (y == 0 && o < a.O) {
+#pragma unroll
+            for (int i = 1; i < 8; ++i) s += room[i * 32 + lane];
+            a.db[o] = s;
+        }
         return;
     }
-    const int tile = (int)blockIdx.x >> 6, r = ((int)blockIdx.x & 63) * 4 + y;
-    const int32_t first = tile * per_tile, w0 = piece_owner(total, a.clusters, first), w1 = piece_owner(total, a.clusters, first + per_tile - 1);
+    const int tile = (int)blockIdx.x >> 4, unit = (int)blockIdx.x & 15, lane = (int)threadIdx.x & 31, g = (int)threadIdx.x >> 5;
+    const int32_t first = tile * per_tile, w0 = a.cut.owner(first), w1 = a.cut.owner(first + per_tile - 1);
     if (w0 == w1) return;                                    // stored by the one that added it
-    const int to = tile / a.tiles_i, ti = tile - to * a.tiles_i;
-    const int64_t o = (int64_t)to * 256 + r, i = (int64_t)ti * 256 + 4 * lane;
-    const int left = (int)min((int64_t)4, a.I - i);
-    if (o >= a.O || left <= 0) return;
+    const int to = tile / a.tiles_i, ti = tile - to * a.tiles_i, sw = unit & 7;
+    const int64_t o0 = (int64_t)to * 256 + (unit >> 3) * 128 + (sw & 3) * 32, i0 = (int64_t)ti * 256 + (sw >> 2) * 128;
+    if (o0 >= a.O || i0 >= a.I) return;
     // the tile is the first of its clusters' pieces, but for the one whose piece begins before it
-    const float* from = a.part + (int64_t)r * 256 + 4 * lane;
-    float4 s = *reinterpret_cast<const float4*>(from + (int64_t)(2 * w0 + (piece_begin(total, a.clusters, w0) < first ? 1 : 0)) * 65536);
-#pragma unroll 8
-    for (int32_t w = w0 + 1; w <= w1; ++w) {
-        const float4 v = *reinterpret_cast<const float4*>(from + (int64_t)w * 2 * 65536);
-        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    const float4* from = a.part + (int64_t)unit * 1024 + g * 128 + lane;
+    float4 s[4];
+    {
+        const float4* p = from + (int64_t)(2 * w0 + (a.cut.begin(w0) < first ? 1 : 0)) * 16384;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[j] = p[j * 32];
     }
-    const float f[4] = {s.x, s.y, s.z, s.w};
-    if constexpr (DT == TDQ_F32) {
-        float* dw = reinterpret_cast<float*>(a.dw) + o * a.dw_stride + i;
-        if (a.dw_vec && left == 4) *reinterpret_cast<float4*>(dw) = s;
-        else
-            for (int j = 0; j < left; ++j) dw[j] = f[j];
-    } else {
-        uint16_t* dw = reinterpret_cast<uint16_t*>(a.dw) + o * a.dw_stride + i;
-        const uint32_t lo = narrow2<DT>(f[0], f[1]), hi = narrow2<DT>(f[2], f[3]);
-        if (a.dw_vec && left == 4) *reinterpret_cast<uint2*>(dw) = make_uint2(lo, hi);
-        else
-            for (int j = 0; j < left; ++j) dw[j] = (uint16_t)((j & 2 ? hi : lo) >> (16 * (j & 1)));
+#pragma unroll 4
+    for (int32_t w = w0 + 1; w <= w1; ++w) {
+        const float4* p = from + (int64_t)w * 2 * 16384;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float4 v = p[j * 32];
+            s[j].x += v.x; s[j].y += v.y; s[j].z += v.z; s[j].w += v.w;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) *reinterpret_cast<float4*>(room + lane * kPitch + (g * 4 + j) * 4) = s[j];
+    __syncthreads();
+    const int64_t i = i0 + 4 * lane;
+    const int left = (int)min((int64_t)4, a.I - i);
+    if (left <= 0) return;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int r = g * 4 + q;
+        const int64_t o = o0 + r;
+        if (o >= a.O) break;
+        const float4 v = *reinterpret_cast<const float4*>(room + r * kPitch + 4 * lane);
+        const float f[4] = {v.x, v.y, v.z, v.w};
+        if constexpr (DT == TDQ_F32) {
+            float* dw = reinterpret_cast<float*>(a.dw) + o * a.dw_stride + i;
+            if (a.dw_vec && left == 4) *reinterpret_cast<float4*>(dw) = v;
+            else
+                for (int j = 0; j < left; ++j) dw[j] = f[j];
+        } else {
+            uint16_t* dw = reinterpret_cast<uint16_t*>(a.dw) + o * a.dw_stride + i;
+            const uint32_t lo = narrow2<DT>(f[0], f[1]), hi = narrow2<DT>(f[2], f[3]);
+            if (a.dw_vec && left == 4) *reinterpret_cast<uint2*>(dw) = make_uint2(lo, hi);
+            else
+                for (int j = 0; j < left; ++j) dw[j] = (uint16_t)((j & 2 ? hi : lo) >> (16 * (j & 1)));
+        }
     }
 }
 
 // dy as `PARTS` bf16 addends, [PARTS][rows_part][stride], rows behind M zero: the leading eight bits of what is left, cut off, each time; exact.  A value
 // without a number goes to the first addend alone.
-template <int DT, int PARTS>
+template <int DT, int PARTS, bool VEC>
 __global__ void __launch_bounds__(256) grad_addends_kernel(const void* dy, int64_t M, int64_t O, int64_t stride, uint16_t* __restrict__ out, int64_t rows_part, int64_t out_stride) {
     using E = typename Elem<DT>::T;
     pdl_wait();
@@ -556,8 +581,13 @@ __global__ void __launch_bounds__(256) grad_addends_kernel(const void* dy, int64
         const int64_t m = u / vecs, o = (u - m * vecs) * 8;
         const E* src = reinterpret_cast<const E*>(dy) + m * stride + o;
         float f[8];
+        if constexpr (VEC) {                                 // rows on the 16-byte grid, whole vectors
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = m < M && o + j < O ? widen<DT>(src[j]) : 0.f;
+            for (int j = 0; j < 8; j += kPerVec<DT>) widen_vec<DT>(m < M ? __ldg(reinterpret_cast<const uint4*>(src + j)) : make_uint4(0, 0, 0, 0), f + j);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = m < M && o + j < O ? widen<DT>(src[j]) : 0.f;
+        }
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
             uint32_t r[4];
@@ -593,6 +623,7 @@ struct GradPlan {
     bool copied;               // dy passes through the workspace
     int64_t rows_part, dy_stride, stages_part, tiles_o, tiles_i, total;
     int32_t clusters;
+    int64_t unit;              // stages that stay together
     bool cut;                  // some tile is added by more than one cluster
     size_t dy_bytes, part_bytes, db_bytes, bytes;
 };
@@ -608,24 +639,36 @@ GradPlan grad_plan(const void* dy, tdq_dtype dtype, int64_t dy_stride, int64_t M
     p.tiles_i = (I + 255) / 256;
     const int64_t tiles = p.tiles_o * p.tiles_i, per_tile = p.stages_part * p.parts;
     p.total = tiles * per_tile;
-    const int64_t pairs = std::max(1, n_sm / 2);
-    p.clusters = (int32_t)std::min<int64_t>(pairs, std::max<int64_t>(1, p.total));
-    p.cut = p.total % p.clusters != 0 || p.total / p.clusters % per_tile != 0;
+    // Whole tiles, or pieces of any length: the least of these estimates in clocks.  A stage is 580, a tile's store hides behind the next tile's stages
+    // if there are enough.  Pieces pay for the second kernel and for every part, written once and read once; so fewer clusters than the GPU holds may be faster.
+    const int32_t pairs = std::max(1, n_sm / 2);
+    p.clusters = (int32_t)std::min<int64_t>(pairs, tiles);
+    p.unit = per_tile;
+    int64_t least = (tiles + p.clusters - 1) / p.clusters * std::max<int64_t>(580 * per_tile, 3000) + 2500;
+    const auto consider = [&](int64_t w) {
+        const int64_t cuts = w - std::gcd<int64_t>(w, tiles), parts = cuts + std::min(cuts, tiles);
+        const int64_t cost = 580 * ((p.total + w - 1) / w) + 7500 + 150 * parts;
+        if (cuts > 0 && cost < least) { least = cost; p.clusters = (int32_t)w; p.unit = 1; }
+    };
+    const int64_t most = std::min<int64_t>(pairs, p.total);
+    for (int64_t w = most; w > 1; w -= w > 32 ? 6 : w > 16 ? 3 : 1) consider(w);
+    for (int64_t w = 2 * tiles; w <= most; w += tiles) consider(w);   // equal parts of every tile: the fewest
+    p.cut = p.unit == 1 && per_tile > 1;
     p.dy_bytes = p.copied ? (size_t)(p.parts * p.rows_part * p.dy_stride) * 2 : 0;
     p.part_bytes = p.cut ? (size_t)2 * p.clusters * 256 * 256 * 4 : 0;
-    p.db_bytes = (size_t)(2 * p.clusters + tiles) * 256 * 4;
+    p.db_bytes = (size_t)(2 * p.clusters + tiles) * kFillPairs * 256 * 4;
     p.bytes = kWorkspaceHeader + p.part_bytes + p.db_bytes + p.dy_bytes;
     return p;
 }
 
 template <int DT>
-tdq_status launch_grad(const GradArgs& a, const GradPlan& p, const CUtensorMap& dymap, const CUtensorMap& xmap, const CUtensorMap& dwmap, const CUtensorMap& partmap, int dev, cudaStream_t st) {
+tdq_status launch_grad(const GradArgs& a, const GradPlan& p, const CUtensorMap& dymap, const CUtensorMap& xmap, const CUtensorMap& dwmap, int dev, cudaStream_t st) {
     static std::atomic<uint64_t> smem_done{0};
     if (allow_smem(fp8_grad_kernel<DT>, (int)kGradSmem, smem_done, dev) != cudaSuccess) return TDQ_ERR_CUDA;
-    if (launch_pdl(fp8_grad_kernel<DT>, dim3(2 * (unsigned)p.clusters), dim3(kGradThreads), kGradSmem, st, a, dymap, xmap, dwmap, partmap) != cudaSuccess) return TDQ_ERR_CUDA;
+    if (launch_pdl(fp8_grad_kernel<DT>, dim3(2 * (unsigned)p.clusters), dim3(kGradThreads), kGradSmem, st, a, dymap, xmap, dwmap) != cudaSuccess) return TDQ_ERR_CUDA;
     g_launch_count.fetch_add(1, std::memory_order_relaxed);
     if (p.cut || a.db) {
-        const int32_t tile_blocks = p.cut ? (int32_t)(p.tiles_o * p.tiles_i * 64) : 0, db_blocks = a.db ? (int32_t)((a.O + 63) / 64) : 0;
+        const int32_t tile_blocks = p.cut ? (int32_t)(p.tiles_o * p.tiles_i * 16) : 0, db_blocks = a.db ? (int32_t)((a.O + 31) / 32) : 0;
         if (launch_pdl(grad_parts_kernel<DT>, dim3((unsigned)(tile_blocks + db_blocks)), dim3(256), 0, st, a, tile_blocks) != cudaSuccess) return TDQ_ERR_CUDA;
         g_launch_count.fetch_add(1, std::memory_order_relaxed);
     }
@@ -634,7 +677,8 @@ tdq_status launch_grad(const GradArgs& a, const GradPlan& p, const CUtensorMap& 
 template <int DT, int PARTS>
 cudaError_t launch_addends(const void* dy, int64_t M, int64_t O, int64_t stride, uint16_t* out, const GradPlan& p, int n_sm, cudaStream_t st) {
     const int64_t blocks = (p.rows_part * (p.dy_stride / 8) + 255) / 256;
-    return launch_pdl(grad_addends_kernel<DT, PARTS>, dim3((unsigned)std::min<int64_t>(blocks, 16 * n_sm)), dim3(256), 0, st, dy, M, O, stride, out, p.rows_part, p.dy_stride);
+    const bool vec = O % 8 == 0 && on_grid(dy, stride, M, sizeof(typename Elem<DT>::T));
+    return launch_pdl(vec ? grad_addends_kernel<DT, PARTS, true> : grad_addends_kernel<DT, PARTS, false>, dim3((unsigned)std::min<int64_t>(blocks, 16 * n_sm)), dim3(256), 0, st, dy, M, O, stride, out, p.rows_part, p.dy_stride);
 }
 constexpr int64_t kGradMax = INT32_MAX - 512;               // coordinates of the copies are 32-bit
 
@@ -675,11 +719,11 @@ extern "C" tdq_status tdq_fp8_weight_grad(const void* dy, tdq_dtype dy_dtype, in
     GradArgs a = {};
     a.xcodes = xcodes; a.xscale = xscale; a.dw = dw; a.db = db; a.M = M; a.O = O; a.I = I;
     a.status = reinterpret_cast<uint32_t*>(ws);
-    a.part = reinterpret_cast<float*>(ws + kWorkspaceHeader);
+    a.part = reinterpret_cast<float4*>(ws + kWorkspaceHeader);
     a.dbpart = reinterpret_cast<float*>(ws + kWorkspaceHeader + p.part_bytes);
     a.dy_stride = p.dy_stride; a.dw_stride = dw_row_stride; a.rows_part = p.rows_part;
     a.Kb = (int32_t)fp8_blocks(I); a.tiles_o = (int32_t)p.tiles_o; a.tiles_i = (int32_t)p.tiles_i; a.stages_part = (int32_t)p.stages_part; a.parts = p.parts;
-    a.clusters = p.clusters;
+    a.cut = {(int32_t)(p.total / p.unit), (int32_t)p.unit, p.clusters};
     a.dw_vec = on_grid(dw, dw_row_stride, O, (int64_t)wsz);
     a.dy = reinterpret_cast<const uint16_t*>(dy);
     if (p.copied) {
@@ -691,15 +735,13 @@ extern "C" tdq_status tdq_fp8_weight_grad(const void* dy, tdq_dtype dy_dtype, in
         if (e != cudaSuccess) return TDQ_ERR_CUDA;
         g_launch_count.fetch_add(1, std::memory_order_relaxed);
     }
-    CUtensorMap dymap, xmap, dwmap, partmap;
+    CUtensorMap dymap, xmap, dwmap;
     memset(&dwmap, 0, sizeof dwmap);
-    memset(&partmap, 0, sizeof partmap);
     if (!grad_operand_map(&dymap, a.dy, p.copied ? p.parts * p.rows_part : M, p.copied ? p.dy_stride : O, p.dy_stride)) return TDQ_ERR_CUDA;
     if (!fp8_operand_map(&xmap, xcodes, M, (int64_t)a.Kb * kFp8Block, kTok)) return TDQ_ERR_CUDA;
     const int64_t w_stride = O > 1 ? dw_row_stride : (I + 7) / 8 * 8;
     if (a.dw_vec && !encode_y_map(&dwmap, dw, wsz == 2, O, I, w_stride, wsz == 2 ? 64 : 32, 32, dw_dtype == TDQ_F16)) a.dw_vec = 0;
-    if (p.cut && !encode_y_map(&partmap, a.part, false, (int64_t)2 * p.clusters * 256, 256, 256, 32, 32)) return TDQ_ERR_CUDA;
-    return dw_dtype == TDQ_F32 ? launch_grad<TDQ_F32>(a, p, dymap, xmap, dwmap, partmap, dev, st)
-         : dw_dtype == TDQ_BF16 ? launch_grad<TDQ_BF16>(a, p, dymap, xmap, dwmap, partmap, dev, st)
-                                : launch_grad<TDQ_F16>(a, p, dymap, xmap, dwmap, partmap, dev, st);
+    return dw_dtype == TDQ_F32 ? launch_grad<TDQ_F32>(a, p, dymap, xmap, dwmap, dev, st)
+         : dw_dtype == TDQ_BF16 ? launch_grad<TDQ_BF16>(a, p, dymap, xmap, dwmap, dev, st)
+                                : launch_grad<TDQ_F16>(a, p, dymap, xmap, dwmap, dev, st);
 }

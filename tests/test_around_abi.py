@@ -87,11 +87,12 @@ def test_weight_grad(tdq):
     _each(f, good, [((6, 1 << 31), (2, 1 << 31), uns), ((7, 1 << 31), (10, 1 << 31), uns)])
     head = int(size(FAKE, 1, 40, 0, 40, 90))
     assert head == 256 and size(FAKE, 3, 40, 64, 40, 90) == size(FAKE, 1, 40, -1, 40, 90) == size(FAKE, 1, 40, 64, 40, 0) == 0
-    # one stage, one tile: nothing is cut, three places for sums of dy; fp16 and rows off the grid pass through the workspace
-    one = 256 + 3 * 1024
+    # one tile of few stages: nothing is cut, three places for sums of dy; fp16 and rows off the grid pass through the workspace
+    one = 256 + 3 * 4096
     assert size(FAKE, 1, 40, 64, 40, 90) == one and size(FAKE, 1, 41, 64, 40, 90) == one + 64 * 40 * 2
-    two = 256 + 2 * 2 * 256 * 256 * 4 + 5 * 1024             # two stages, two clusters with two places each
-    assert size(FAKE, 1, 40, 65, 40, 90) == two and size(FAKE, 2, 40, 64, 40, 90) == two + 2 * 64 * 40 * 2
+    assert size(FAKE, 2, 40, 65, 40, 90) == one + 2 * 128 * 40 * 2 and size(FAKE, 0, 40, 64, 40, 90) == one + 3 * 64 * 40 * 2
+    # a long sum: two places for each of some clusters
+    assert (size(FAKE, 1, 40, 1 << 20, 40, 90) - 256 - 4096) % (2 * 256 * (256 + 4) * 4) == 0
 
 
 def test_linear_epilogue(tdq):
