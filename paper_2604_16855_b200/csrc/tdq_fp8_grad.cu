@@ -92,12 +92,15 @@ struct Piece {
 // the stages of one tile: k .. k + len - 1 of the piece's order, from stage `at` of the tile on
 struct Stretch {
     int32_t tile, at, len;
+    int32_t to, ti;                                          // the tile's outputs and channels, in tiles
     bool whole;
     int32_t slot;                                            // of the cluster's two places for parts
-    __device__ Stretch(const Piece& p, int32_t k) {
+    __device__ Stretch(const Piece& p, int32_t k, int32_t tiles_i) {
         const int32_t s = p.stage(k);
         tile = s / p.per_tile;
         at = s - tile * p.per_tile;
+        to = tile / tiles_i;
+        ti = tile - to * tiles_i;
         len = min(p.per_tile - at, (k < p.end - p.last ? p.end : p.last) - s);
         whole = len == p.per_tile;
         slot = s == p.begin ? 0 : 1;
@@ -153,6 +156,11 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
     const uint32_t codes_s = ring_s + kGradStages * kGradStage, strips_s = codes_s + kFillPairs * kGradCodes;
     const int warp = uniform_warp(), lane = threadIdx.x & 31;
     const uint32_t rank = fp8_cluster_rank();
+    // Where this cluster's work lies: a dozen quotients, ahead of the wait for the kernel before (behind it they took 2000 clocks to the first copy).
+    const int32_t w = (int32_t)blockIdx.x / 2, per_tile = a.stages_part * a.parts;
+    const Piece piece(per_tile, a.cut, w);
+    const int32_t n_stages = piece.stages();
+    const Stretch first(piece, 0, a.tiles_i);
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kGradStages; ++i) { mbar_init(&g->landed[i], 1); mbar_init(&g->full[i], 4); mbar_init(&g->empty[i], 1); }
@@ -177,10 +185,6 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
     pdl_trigger();
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = 0u;
     const uint32_t tmem_base = c->tmem_base;
-    const int32_t w = (int32_t)blockIdx.x / 2;
-    const int32_t per_tile = a.stages_part * a.parts;
-    const Piece piece(per_tile, a.cut, w);
-    const int32_t n_stages = piece.stages();
 
     if (warp < kSumWarp0) {
         setmaxnreg_dec<kGradRegsLoad>();
@@ -189,8 +193,8 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
             const uint32_t landed_s = smem_u32(&g->landed[0]), empty_s = smem_u32(&g->empty[0]);
             uint32_t s = 0, ph = 1;
             for (int32_t k = 0; k < n_stages && !c->abort_flag;) {
-                const Stretch t(piece, k);
-                const int32_t o = t.tile / a.tiles_i * 256 + (int32_t)rank * 128;   // past the end: the map fills with zeros
+                const Stretch t = k ? Stretch(piece, k, a.tiles_i) : first;
+                const int32_t o = t.to * 256 + (int32_t)rank * 128;   // past the end: the map fills with zeros
                 int32_t part = t.at / a.stages_part, tok = t.at - part * a.stages_part;
 #pragma unroll 1
                 for (int32_t i = 0; i < t.len; ++i) {
@@ -212,8 +216,8 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
             // -------------------------------------------------------- copies of codes, a slot for each pair of restoring warps
             const uint32_t codes_bar = smem_u32(&g->codes[0]), taken_s = smem_u32(&g->taken[0]);
             for (int32_t k = 0; k < n_stages && !c->abort_flag;) {
-                const Stretch t(piece, k);
-                const int32_t x = (2 * (t.tile % a.tiles_i) + (int32_t)rank) * 128;   // past the end: the map fills with zeros
+                const Stretch t = k ? Stretch(piece, k, a.tiles_i) : first;
+                const int32_t x = (2 * t.ti + (int32_t)rank) * 128;   // past the end: the map fills with zeros
                 int32_t tok = t.at % a.stages_part;
 #pragma unroll 1
                 for (const int32_t end = k + t.len; k < end; ++k) {
@@ -235,7 +239,7 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
             uint32_t s = 0, ph = 0, group = 0;
             bool on = true;
             for (int32_t k = 0; k < n_stages && on;) {
-                const Stretch t(piece, k);
+                const Stretch t = k ? Stretch(piece, k, a.tiles_i) : first;
                 for (int32_t i = 0; i < t.len && on; ++group) {
                     const int32_t len = min(kGroup, t.len - i);
                     const uint32_t slot = group & 1u;
@@ -270,7 +274,7 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
         const uint32_t tm0 = tmem_base + ((uint32_t)(quarter * 32) << 16) + h * 128;
         uint32_t group = 0;
         for (int32_t k = 0; k < n_stages && !c->abort_flag;) {
-            const Stretch stretch(piece, k);
+            const Stretch stretch = k ? Stretch(piece, k, a.tiles_i) : first;
             float2 acc[64];
 #pragma unroll
             for (int j = 0; j < 64; ++j) acc[j] = make_float2(0.f, 0.f);
@@ -295,7 +299,7 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
                 }
             }
             if (c->abort_flag) break;
-            const int to = stretch.tile / a.tiles_i, ti = stretch.tile - to * a.tiles_i;
+            const int to = stretch.to, ti = stretch.ti;
             const bool whole = stretch.whole;
             const int32_t slot = 2 * w + stretch.slot;
             const int64_t o0 = (int64_t)to * 256 + rank * 128 + quarter * 32, i0 = (int64_t)ti * 256 + h * 128;
@@ -393,30 +397,33 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
             for (uint32_t j = 0; j < 2; ++j) to[q][j] = to_s + (((2u * (ch & 3u) + j) ^ (tok0 + 4u * q)) << 4);
         }
         float scale;                                         // of token side * 32 + lane of the next stage; 0 where there is none
-        const auto load_scale = [&](int32_t k) {
-            scale = 0.f;
-            if (k >= n_stages) return;
-            const int32_t st = piece.stage(k), tile = st / per_tile, tok = (st - tile * per_tile) % a.stages_part;
-            const int32_t block = 2 * (tile % a.tiles_i) + (int32_t)rank;
+        const auto scale_at = [&](int32_t block, int32_t tok) {
             const int64_t m = (int64_t)tok * kTok + side * 32 + lane;
-            if (block < a.Kb && m < a.M) scale = __ldg(a.xscale + m * a.Kb + block);
+            return block < a.Kb && m < a.M ? __ldg(a.xscale + m * a.Kb + block) : 0.f;
+        };
+        const auto scale_of = [&](int32_t k) {               // of any stage
+            if (k >= n_stages) return 0.f;
+            const int32_t st = piece.stage(k), tile = st / per_tile;
+            return scale_at(2 * (tile % a.tiles_i) + (int32_t)rank, (st - tile * per_tile) % a.stages_part);
         };
         int32_t mine = pair;                                 // this warp's stage, in the piece's order
         uint32_t s = (uint32_t)pair, ph = 0;                 // its place in the ring
         uint32_t cph = 0;
-        load_scale(mine);
+        scale = scale_of(mine);
         for (int32_t k = 0; k < n_stages && !c->abort_flag;) {
-            const Stretch t(piece, k);
+            const Stretch t = k ? Stretch(piece, k, a.tiles_i) : first;
             // the tiles of the same outputs take turns at the column sums
-            const int32_t ti = t.tile % a.tiles_i;
-            int32_t turn = a.db ? (t.at + mine - k) % a.tiles_i : -1;
+            int32_t turn = a.db ? (t.at + mine - k) % a.tiles_i : -1, tok = (t.at + mine - k) % a.stages_part;   // of this warp's stage
+            const int32_t block = 2 * t.ti + (int32_t)rank;
             float2 sum[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) sum[j] = make_float2(0.f, 0.f);
 #pragma unroll 1
             for (; mine < k + t.len; mine += kFillPairs) {
                 const float now = scale;
-                load_scale(mine + kFillPairs);
+                tok += kFillPairs;
+                while (tok >= a.stages_part) tok -= a.stages_part;
+                scale = mine + kFillPairs < k + t.len ? scale_at(block, tok) : scale_of(mine + kFillPairs);
                 fp8_wait(codes_bar, cph, c, a.status, 10u);
                 cph ^= 1u;
                 uint4 code[8];
@@ -440,7 +447,7 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
                 }
                 fp8_wait(landed_s + s * 8, ph, c, a.status, 8u);
                 if (c->abort_flag) break;
-                if (turn == ti) {                            // 8 outputs x 16 tokens a lane; rows behind dy's end are zero
+                if (turn == t.ti) {                          // 8 outputs x 16 tokens a lane; rows behind dy's end are zero
                     const uint32_t at = ring_s + d + (uint32_t)side * kGradHalf + ((uint32_t)lane >> 3) * 128u;
 #pragma unroll
                     for (int q = 0; q < 16; ++q) {
@@ -451,7 +458,10 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
                             sum[j] = __fadd2_rn(sum[j], make_float2(__uint_as_float(v[j] << 16), __uint_as_float(v[j] & 0xffff0000u)));
                     }
                 }
-                if (a.db) turn = (turn + kFillPairs) % a.tiles_i;
+                if (a.db) {
+                    turn += kFillPairs;
+                    while (turn >= a.tiles_i) turn -= a.tiles_i;
+                }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 grad_arrive(full0 + s * 8, lane);
@@ -484,11 +494,11 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "n"(512) : "memory");
 }
 
-// Adds the parts of the tiles that were cut, in order of the sum: a thread block for the 32 rows x 128 columns of a summing warp, which it turns to rows in shared memory.
+// Adds the parts of the tiles that were cut, in order of the sum: a thread block for 32 rows x 32 columns, which it turns to rows in shared memory.
 // The blocks behind those add db, 32 outputs each.
 template <int DT>
 __global__ void __launch_bounds__(256) grad_parts_kernel(const GradArgs a, int32_t tile_blocks) {
-    constexpr int kPitch = 132;                              // floats of a row of the turned block
+    constexpr int kPitch = 36;                               // floats of a row of the turned block
     __shared__ __align__(16) float room[32 * kPitch];
     pdl_wait();
     pdl_trigger();
@@ -498,7 +508,13 @@ __global__ void __launch_bounds__(256) grad_parts_kernel(const GradArgs a, int32
         const int64_t o = ((int64_t)blockIdx.x - tile_blocks) * 32 + lane;
         const int to = (int)(o >> 8), col = (int)(o & 255);
         float s = 0.f;
-        if (to < a.tiles_o)
+        if (a.cut.unit != 1) {
+            if (to < a.tiles_o) {
+                const float* from = a.dbpart + (2 * a.cut.clusters + (int64_t)to * a.tiles_i) * (kFillPairs * 256) + (int64_t)(y & 1) * 512 + col;
+#pragma unroll 8
+                for (int t = y >> 1; t < a.tiles_i; t += 4) s += from[(int64_t)t * (kFillPairs * 256)] + from[(int64_t)t * (kFillPairs * 256) + 256];
+            }
+        } else if (to < a.tiles_o)
             for (int t = y >> 1; t < a.tiles_i; t += 4) {        // two threads a tile, two pairs of warps each
                 const int32_t tile = to * a.tiles_i + t, first = tile * per_tile;
                 const int32_t w0 = a.cut.owner(first), w1 = a.cut.owner(first + per_tile - 1);
@@ -518,54 +534,42 @@ __global__ void __launch_bounds__(256) grad_parts_kernel(const GradArgs a, int32
         }
         return;
     }
-    const int tile = (int)blockIdx.x >> 4, unit = (int)blockIdx.x & 15, lane = (int)threadIdx.x & 31, g = (int)threadIdx.x >> 5;
+    const int tile = (int)blockIdx.x >> 6, unit = ((int)blockIdx.x >> 2) & 15, lane = (int)threadIdx.x & 31, g = (int)threadIdx.x >> 5;
     const int32_t first = tile * per_tile, w0 = a.cut.owner(first), w1 = a.cut.owner(first + per_tile - 1);
     if (w0 == w1) return;                                    // stored by the one that added it
-    const int to = tile / a.tiles_i, ti = tile - to * a.tiles_i, sw = unit & 7;
-    const int64_t o0 = (int64_t)to * 256 + (unit >> 3) * 128 + (sw & 3) * 32, i0 = (int64_t)ti * 256 + (sw >> 2) * 128;
+    const int to = tile / a.tiles_i, ti = tile - to * a.tiles_i, sw = unit & 7, quarter = (int)blockIdx.x & 3;
+    const int64_t o0 = (int64_t)to * 256 + (unit >> 3) * 128 + (sw & 3) * 32, i0 = (int64_t)ti * 256 + (sw >> 2) * 128 + quarter * 32;
     if (o0 >= a.O || i0 >= a.I) return;
     // the tile is the first of its clusters' pieces, but for the one whose piece begins before it
-    const float4* from = a.part + (int64_t)unit * 1024 + g * 128 + lane;
-    float4 s[4];
-    {
-        const float4* p = from + (int64_t)(2 * w0 + (a.cut.begin(w0) < first ? 1 : 0)) * 16384;
+    const float4* from = a.part + (int64_t)unit * 1024 + quarter * 256 + g * 32 + lane;
+    float4 s = from[(int64_t)(2 * w0 + (a.cut.begin(w0) < first ? 1 : 0)) * 16384];
+    from += (int64_t)(w0 + 1) * 2 * 16384;
+    for (int32_t left = w1 - w0; left > 0; left -= 8, from += 8 * 2 * 16384) {   // eight at a time in flight
+        float4 v[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s[j] = p[j * 32];
+        for (int j = 0; j < 8; ++j) v[j] = j < left ? from[(int64_t)j * 2 * 16384] : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) { s.x += v[j].x; s.y += v[j].y; s.z += v[j].z; s.w += v[j].w; }
     }
-#pragma unroll 4
-    for (int32_t w = w0 + 1; w <= w1; ++w) {
-        const float4* p = from + (int64_t)w * 2 * 16384;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float4 v = p[j * 32];
-            s[j].x += v.x; s[j].y += v.y; s[j].z += v.z; s[j].w += v.w;
-        }
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) *reinterpret_cast<float4*>(room + lane * kPitch + (g * 4 + j) * 4) = s[j];
+    *reinterpret_cast<float4*>(room + lane * kPitch + g * 4) = s;
     __syncthreads();
-    const int64_t i = i0 + 4 * lane;
+    const int r = (int)threadIdx.x >> 3, c = ((int)threadIdx.x & 7) * 4;
+    const int64_t i = i0 + c, o = o0 + r;
     const int left = (int)min((int64_t)4, a.I - i);
-    if (left <= 0) return;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const int r = g * 4 + q;
-        const int64_t o = o0 + r;
-        if (o >= a.O) break;
-        const float4 v = *reinterpret_cast<const float4*>(room + r * kPitch + 4 * lane);
-        const float f[4] = {v.x, v.y, v.z, v.w};
-        if constexpr (DT == TDQ_F32) {
-            float* dw = reinterpret_cast<float*>(a.dw) + o * a.dw_stride + i;
-            if (a.dw_vec && left == 4) *reinterpret_cast<float4*>(dw) = v;
-            else
-                for (int j = 0; j < left; ++j) dw[j] = f[j];
-        } else {
-            uint16_t* dw = reinterpret_cast<uint16_t*>(a.dw) + o * a.dw_stride + i;
-            const uint32_t lo = narrow2<DT>(f[0], f[1]), hi = narrow2<DT>(f[2], f[3]);
-            if (a.dw_vec && left == 4) *reinterpret_cast<uint2*>(dw) = make_uint2(lo, hi);
-            else
-                for (int j = 0; j < left; ++j) dw[j] = (uint16_t)((j & 2 ? hi : lo) >> (16 * (j & 1)));
-        }
+    if (left <= 0 || o >= a.O) return;
+    const float4 v = *reinterpret_cast<const float4*>(room + r * kPitch + c);
+    const float f[4] = {v.x, v.y, v.z, v.w};
+    if constexpr (DT == TDQ_F32) {
+        float* dw = reinterpret_cast<float*>(a.dw) + o * a.dw_stride + i;
+        if (a.dw_vec && left == 4) *reinterpret_cast<float4*>(dw) = v;
+        else
+            for (int j = 0; j < left; ++j) dw[j] = f[j];
+    } else {
+        uint16_t* dw = reinterpret_cast<uint16_t*>(a.dw) + o * a.dw_stride + i;
+        const uint32_t lo = narrow2<DT>(f[0], f[1]), hi = narrow2<DT>(f[2], f[3]);
+        if (a.dw_vec && left == 4) *reinterpret_cast<uint2*>(dw) = make_uint2(lo, hi);
+        else
+            for (int j = 0; j < left; ++j) dw[j] = (uint16_t)((j & 2 ? hi : lo) >> (16 * (j & 1)));
     }
 }
 
@@ -647,7 +651,7 @@ GradPlan grad_plan(const void* dy, tdq_dtype dtype, int64_t dy_stride, int64_t M
     int64_t least = (tiles + p.clusters - 1) / p.clusters * std::max<int64_t>(580 * per_tile, 3000) + 2500;
     const auto consider = [&](int64_t w) {
         const int64_t cuts = w - std::gcd<int64_t>(w, tiles), parts = cuts + std::min(cuts, tiles);
-        const int64_t cost = 580 * ((p.total + w - 1) / w) + 7500 + 150 * parts;
+        const int64_t cost = 580 * ((p.total + w - 1) / w) + 4500 + 120 * parts;
         if (cuts > 0 && cost < least) { least = cost; p.clusters = (int32_t)w; p.unit = 1; }
     };
     const int64_t most = std::min<int64_t>(pairs, p.total);
@@ -668,7 +672,7 @@ tdq_status launch_grad(const GradArgs& a, const GradPlan& p, const CUtensorMap& 
     if (launch_pdl(fp8_grad_kernel<DT>, dim3(2 * (unsigned)p.clusters), dim3(kGradThreads), kGradSmem, st, a, dymap, xmap, dwmap) != cudaSuccess) return TDQ_ERR_CUDA;
     g_launch_count.fetch_add(1, std::memory_order_relaxed);
     if (p.cut || a.db) {
-        const int32_t tile_blocks = p.cut ? (int32_t)(p.tiles_o * p.tiles_i * 16) : 0, db_blocks = a.db ? (int32_t)((a.O + 31) / 32) : 0;
+        const int32_t tile_blocks = p.cut ? (int32_t)(p.tiles_o * p.tiles_i * 64) : 0, db_blocks = a.db ? (int32_t)((a.O + 31) / 32) : 0;
         if (launch_pdl(grad_parts_kernel<DT>, dim3((unsigned)(tile_blocks + db_blocks)), dim3(256), 0, st, a, tile_blocks) != cudaSuccess) return TDQ_ERR_CUDA;
         g_launch_count.fetch_add(1, std::memory_order_relaxed);
     }
