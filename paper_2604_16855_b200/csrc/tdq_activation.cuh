@@ -28,26 +28,25 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 }
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 
-// Gaussian tail: with a = |z|, e = exp(-a^2 / 2) and q = Phi(-a) = 1/2 erfcx(a / sqrt 2) e.  The smooth factor is a polynomial of degree 11 on [0, 5.2], fitted by
-// least squares with weights moved to the largest errors of max(a, 1) q: 6e-8 at most, roundings of its evaluation among them (behind 5.2 the factor stays what it is there, q is below
-// 1e-7).  One exponential an element and no quotient: the exponential's unit is a quarter as fast as the multiply-adds of an element in pairs.
-__device__ __forceinline__ void gauss_tail(float2 z, float2& a, float2& e, float2& q) {
-    a = make_float2(min_nan(fabsf(z.x), 20.f), min_nan(fabsf(z.y), 20.f));      // exp(-200) is 0 in binary32
-    const float2 g = __fmul2_rn(__fmul2_rn(a, a), both(-0.72134752f));          // -log2(e) / 2
+// Gaussian tail: with a = |z|, e = exp(-a^2 / 2) and q = Phi(-a) = 1/2 erfcx(a / sqrt 2) e.  The smooth factor is a polynomial of degree 10 on [0, 5], fitted by
+// least squares with weights moved to the largest errors of max(a, 1) q: 1.5e-7 at most, roundings of its evaluation among them (behind 5 the factor stays what it is there,
+// b = min(a, 5), and b q is within 8e-8 of a q).  An element costs
+// fourteen multiply-adds in all and one turn of the special functions' unit, which takes eight times as long as one.
+__device__ __forceinline__ void gauss_tail(float2 z, float2& b, float2& e, float2& q) {
+    const float2 g = __fmul2_rn(__fmul2_rn(z, z), both(-0.72134752f));          // -log2(e) / 2
     e = make_float2(ex2(g.x), ex2(g.y));
-    const float2 b = make_float2(fminf(a.x, 5.2f), fminf(a.y, 5.2f));
-    float2 p = both(-2.29394999e-07f);
-    p = __ffma2_rn(p, b, both(5.99727082e-06f));
-    p = __ffma2_rn(p, b, both(-7.03524929e-05f));
-    p = __ffma2_rn(p, b, both(0.000496292021f));
-    p = __ffma2_rn(p, b, both(-0.00239847647f));
-    p = __ffma2_rn(p, b, both(0.00866080076f));
-    p = __ffma2_rn(p, b, both(-0.0250857733f));
-    p = __ffma2_rn(p, b, both(0.0616591349f));
-    p = __ffma2_rn(p, b, both(-0.132702291f));
-    p = __ffma2_rn(p, b, both(0.249952316f));
-    p = __ffma2_rn(p, b, both(-0.398939103f));
-    p = __ffma2_rn(p, b, both(0.49999997f));
+    b = make_float2(min_nan(fabsf(z.x), 5.f), min_nan(fabsf(z.y), 5.f));
+    float2 p = both(1.23802897e-06f);
+    p = __ffma2_rn(p, b, both(-2.84340113e-05f));
+    p = __ffma2_rn(p, b, both(0.00029121447f));
+    p = __ffma2_rn(p, b, both(-0.00178629335f));
+    p = __ffma2_rn(p, b, both(0.00750757195f));
+    p = __ffma2_rn(p, b, both(-0.0237156842f));
+    p = __ffma2_rn(p, b, both(0.060663037f));
+    p = __ffma2_rn(p, b, both(-0.132287741f));
+    p = __ffma2_rn(p, b, both(0.249865487f));
+    p = __ffma2_rn(p, b, both(-0.398932129f));
+    p = __ffma2_rn(p, b, both(0.499999881f));
     q = __fmul2_rn(p, e);
 }
 // 1 / (1 + exp(-z))
@@ -63,9 +62,9 @@ __device__ __forceinline__ float2 activate(float2 z) {
     if constexpr (ACT == TDQ_ACT_RELU) {
         return make_float2(max_nan(z.x, 0.f), max_nan(z.y, 0.f));
     } else if constexpr (ACT == TDQ_ACT_GELU) {              // z Phi(z) = max(z, 0) - |z| Phi(-|z|)
-        float2 a, e, q;
-        gauss_tail(z, a, e, q);
-        return __ffma2_rn(make_float2(-a.x, -a.y), q, make_float2(max_nan(z.x, 0.f), max_nan(z.y, 0.f)));
+        float2 b, e, q;
+        gauss_tail(z, b, e, q);
+        return __ffma2_rn(make_float2(-b.x, -b.y), q, make_float2(max_nan(z.x, 0.f), max_nan(z.y, 0.f)));
     } else if constexpr (ACT == TDQ_ACT_GELU_TANH) {
         return __fmul2_rn(z, sigmoid(__fmul2_rn(z, __ffma2_rn(__fmul2_rn(z, z), both(kTanhB), both(kTanhA)))));
     } else if constexpr (ACT == TDQ_ACT_SILU) {
@@ -78,10 +77,11 @@ template <int ACT>
 __device__ __forceinline__ float2 slope(float2 z) {
     if constexpr (ACT == TDQ_ACT_RELU) {
         return make_float2(z.x > 0.f ? 1.f : 0.f, z.y > 0.f ? 1.f : 0.f);
-    } else if constexpr (ACT == TDQ_ACT_GELU) {              // Phi(z) + z phi(z)
-        float2 a, e, q;
-        gauss_tail(z, a, e, q);
-        const float2 h = __ffma2_rn(__fmul2_rn(a, e), both(0.398942280f), __ffma2_rn(q, both(-1.f), both(0.5f)));   // odd part: 1/2 - q + a phi
+    } else if constexpr (ACT == TDQ_ACT_GELU) {              // Phi(z) + z phi(z); the odd part is 1/2 - q + a phi
+        float2 b, e, q;
+        gauss_tail(z, b, e, q);
+        const float2 a = make_float2(min_nan(fabsf(z.x), 20.f), min_nan(fabsf(z.y), 20.f));   // exp(-200) is 0 in binary32
+        const float2 h = __ffma2_rn(__fmul2_rn(a, e), both(0.398942280f), __ffma2_rn(q, both(-1.f), both(0.5f)));
         return make_float2(0.5f + copysignf(h.x, z.x), 0.5f + copysignf(h.y, z.y));
     } else if constexpr (ACT == TDQ_ACT_GELU_TANH) {         // s + z s (1 - s) (2 u)'
         const float2 z2 = __fmul2_rn(z, z);
@@ -105,7 +105,9 @@ __device__ __forceinline__ float activate_by(int act, float z) {
         default: return z;
     }
 }
-// all of a thread's sums
+// All of a thread's sums.  Bound by the multiply-adds' unit (GELU fifteen an element: 2.3 us a 256 x 256 tile).  Not kept: GELU by Abramowitz and Stegun's 7.1.26, four
+// multiply-adds fewer and a quotient more, in every element's place or every other's (16384 x 1024 -> 4096 bf16 109 -> 115 us); the quotient of the
+// others by Newton's iteration (103 both ways).
 template <int ACT, int N>
 __device__ __forceinline__ void activate_all(float2 (&v)[N]) {
 #pragma unroll
