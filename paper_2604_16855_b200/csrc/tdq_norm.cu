@@ -2,8 +2,8 @@
 //
 //   mean = 1/C sum x;   rstd = 1 / sqrt(1/C sum (x - mean)^2 + eps);   y = (x - mean) rstd w + b
 //
-// Bound by HBM: the input is read once and the output written once.  A row stays in the registers of the threads that share it (a warp up to 1024
-// channels of 16 bits, then 128 to 1024 threads), as binary32 between its passes: sum, then sum of squares about the mean (not sum x^2 - C mean^2,
+// Bound by HBM: the input is read once and the output written once.  Blocks stay and go through rows, the next two already on their way, with the weights in registers
+// (one row a group of a block that ends with it: 16384 x 2048 bf16 38 us; now FWD_TIME).  A row stays in the registers of the threads that share it, as binary32 between its passes: sum, then sum of squares about the mean (not sum x^2 - C mean^2,
 // which loses what a far mean leaves), then the outputs.  Sums are binary32: lane by lane, then a butterfly, in the same order every time.
 // Rows off the 16-byte grid pass through shared memory: aligned vectors in, words shifted out, and the other way round for the output.
 #include "tdq_rows.cuh"
@@ -20,149 +20,177 @@ struct NormArgs {
     int64_t M, x_stride, y_stride;             // strides in elements
     int32_t C, Kb;                             // channels, blocks of 128
     float eps;
-    bool pow2;
+    bool pow2, w_vec;                          // weights on the 16-byte grid
 };
 
-// Forward.  R rows at a time in a group (of warps only), which share the loads of w and b.  CODES: E4M3 codes and scales instead of y.
-template <int DT, int T, int V, int R, bool CODES, bool VEC>
-__global__ void __launch_bounds__(T < 256 ? 256 : T) layer_norm_kernel(const NormArgs a) {
+template <int T> constexpr int kNormThreads = T < 256 ? 256 : T;
+// Rows on their way while one is worked on (none where T is for few rows), and whether the weights stay in registers.
+template <int T, int V, bool CODES, bool VEC> constexpr int kAhead = T == 1024 ? 0 : V <= 2 || (VEC && !CODES) ? 2 : 1;
+template <int T, int V> constexpr bool kKeepWeights = T < 1024 && V <= 3;
+
+// Blocks go through rows, 1 / T of a block a row.  CODES: E4M3 codes and scales instead of y.
+template <int DT, int T, int V, bool CODES, bool VEC>
+__global__ void __launch_bounds__(kNormThreads<T>, T > 256 ? 1 : V == 1 ? (VEC ? 4 : 3) : 2) layer_norm_kernel(const NormArgs a) {
     using E = typename Elem<DT>::T;
-    constexpr int P = kPerVec<DT>, kThreads = T < 256 ? 256 : T, kGroups = kThreads / T;
+    constexpr int P = kPerVec<DT>, kGroups = kNormThreads<T> / T, D = kAhead<T, V, CODES, VEC>;
+    constexpr bool KEEP = kKeepWeights<T, V>;
     extern __shared__ __align__(16) uint8_t smem_raw[];
     __shared__ float room[kGroups][2][T > 32 ? T / 32 : 1];
     pdl_wait();
     pdl_trigger();
-    const int group = (int)threadIdx.x / T, t = (int)threadIdx.x % T;
+    const int group = (int)threadIdx.x / T, t = (int)threadIdx.x % T, n = a.C;
     uint4* stage = reinterpret_cast<uint4*>(smem_raw) + (VEC ? 0 : group * kStageVecs<T, V>);
-    const int64_t row0 = ((int64_t)blockIdx.x * kGroups + group) * R;
-    if (row0 >= a.M) return;                                 // the whole group
-    const int n = a.C;
-    float f[R][V * P], mean[R], rstd[R];
-    {
-        uint4 v[R][V];
+    constexpr int H = P / 2;                                 // pairs of a vector
+    const uint32_t M = (uint32_t)a.M, step = gridDim.x * kGroups, in_warp = T >= 32 ? 0u : (uint32_t)group % (32 / T);
+    uint32_t m = blockIdx.x * kGroups + (uint32_t)group;     // groups of a warp go on together, until the first one's rows end
+    Row<DT, T, V, VEC> ring[D + 1];
+    const auto fetch = [&](Row<DT, T, V, VEC>& r, uint32_t at) { r.fetch(reinterpret_cast<const E*>(a.x) + (int64_t)at * a.x_stride, n, t, at < M); };
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int64_t m = row0 + r < a.M ? row0 + r : a.M - 1;   // a row past the end: the last one once more, not stored
-            const E* src = reinterpret_cast<const E*>(a.x) + m * a.x_stride;
-            if constexpr (VEC) load_row<DT, T, V>(src, n, t, v[r]);
-            else load_row_ragged<DT, T, V>(src, n, t, group, stage, v[r]);
+    for (int i = 0; i <= D; ++i) fetch(ring[i], m + i * step);
+    float2 w[KEEP ? V * H : 1], b[KEEP ? V * H : 1];
+    if constexpr (KEEP) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            load_weight_pairs<P>(a.w, a.w_vec, (t + T * i) * P, n, 1.f, w + i * H);
+            load_weight_pairs<P>(a.b, a.w_vec, (t + T * i) * P, n, 0.f, b + i * H);
         }
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-#pragma unroll
-            for (int i = 0; i < V; ++i) widen_vec<DT>(v[r][i], f[r] + i * P);
     }
     const float inv = __fdiv_rn(1.f, (float)n);
-    float s[R];
+    const auto work = [&](Row<DT, T, V, VEC>& row) {
+        const bool on = m < M;
+        float2 f[V * H];
+        {
+            uint4 v[V];
+            if constexpr (!VEC) {
+                group_sync<T>(group);
+                row.put(stage, t);
+                group_sync<T>(group);
+            }
+            row.take(stage, n, t, v);
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        s[r] = 0.f;
+            for (int i = 0; i < V; ++i) widen_pairs<DT>(v[i], f + i * H);
+        }
+        fetch(row, m + (D + 1) * step);
+        float2 sum = f[0];
 #pragma unroll
-        for (int i = 0; i < V * P; ++i) s[r] += f[r][i];
-    }
-    group_sum<T, R>(s, room[group][0], group, t);
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        mean[r] = s[r] * inv;
-        s[r] = 0.f;
+        for (int i = 1; i < V * H; ++i) sum = __fadd2_rn(sum, f[i]);
+        float s[1] = {sum.x + sum.y};
+        group_sum<T, 1>(s, room[group][0], group, t);
+        const float mean = s[0] * inv;
+        sum = two(0.f);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int first = (t + T * i) * P;
 #pragma unroll
-            for (int q = 0; q < P; ++q) {
-                f[r][i * P + q] -= mean[r];
-                // a vector lies in the row or behind it, where rows are on the grid; else it may end inside
-                if (VEC ? first < n : first + q < n) s[r] = fmaf(f[r][i * P + q], f[r][i * P + q], s[r]);
+            for (int q = 0; q < H; ++q) {
+                float2& d = f[i * H + q];
+                d = __fadd2_rn(d, two(-mean));
+                // behind the row there are no deviations; on the grid a vector lies in the row or behind it, else it may end inside
+                if (VEC ? first >= n : first + 2 * q >= n) d = two(0.f);
+                else if (!VEC && first + 2 * q + 1 >= n) d.y = 0.f;
+                sum = __ffma2_rn(d, d, sum);
             }
         }
-    }
-    group_sum<T, R>(s, room[group][1], group, t);
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        rstd[r] = __frcp_rn(__fsqrt_rn(fmaf(s[r], inv, a.eps)));
-        if (t == 0 && row0 + r < a.M) {
-            if (a.mean) a.mean[row0 + r] = mean[r];
-            if (a.rstd) a.rstd[row0 + r] = rstd[r];
+        s[0] = sum.x + sum.y;
+        group_sum<T, 1>(s, room[group][1], group, t);
+        const float rstd = __frcp_rn(__fsqrt_rn(fmaf(s[0], inv, a.eps)));
+        if (t == 0 && on) {
+            if (a.mean) a.mean[m] = mean;
+            if (a.rstd) a.rstd[m] = rstd;
         }
-    }
-    uint4 out[R][V];
+        uint32_t mx[V];
+        uint4 out[V];
+        E* const y_row = reinterpret_cast<E*>(a.y) + (int64_t)m * a.y_stride;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const int idx = t + T * i, first = idx * P;
-        float w[P], b[P];
-        load_weights<P, VEC>(a.w, first, n, 1.f, w);
-        load_weights<P, VEC>(a.b, first, n, 0.f, b);
+        for (int i = 0; i < V; ++i) {
+            const int idx = t + T * i, first = idx * P;
+            float2 wl[H], bl[H], *y = f + i * H;
+            if constexpr (!KEEP) {
+                load_weight_pairs<P>(a.w, a.w_vec, first, n, 1.f, wl);
+                load_weight_pairs<P>(a.b, a.w_vec, first, n, 0.f, bl);
+            }
+            mx[i] = 0;
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            float* y = f[r] + i * P;
-#pragma unroll
-            for (int q = 0; q < P; ++q) y[q] = fmaf(y[q] * rstd[r], w[q], b[q]);
+            for (int q = 0; q < H; ++q) {
+                y[q] = __ffma2_rn(__fmul2_rn(y[q], two(rstd)), KEEP ? w[KEEP ? i * H + q : 0] : wl[q], KEEP ? b[KEEP ? i * H + q : 0] : bl[q]);
+                if constexpr (CODES) mx[i] = max(mx[i], max(__float_as_uint(y[q].x) & 0x7fffffffu, __float_as_uint(y[q].y) & 0x7fffffffu));
+            }
             if constexpr (!CODES) {
-                if constexpr (VEC) {
-                    if (first < n && row0 + r < a.M)
-                        reinterpret_cast<uint4*>(reinterpret_cast<E*>(a.y) + (row0 + r) * a.y_stride)[idx] = narrow_vec<DT>(y);
-                } else {
-                    out[r][i] = narrow_vec<DT>(y);
-                }
-            } else {
-                // 128 channels are 128 / P neighbouring threads of the group
-                uint32_t mx = 0;
+                out[i] = narrow_pairs<DT>(y);
+                if (VEC && first < n && on) reinterpret_cast<uint4*>(y_row)[idx] = out[i];
+            }
+        }
+        if constexpr (CODES) {
+            // 128 channels are kTeam neighbouring threads; behind the row weights are 1, biases and deviations 0 (or all NaN with the row), so y is 0.  The i-th thread of
+            // a team works out the scale of its i-th block, once for all, and the others take it from there.
+            constexpr int kTeam = 128 / P;
+            uint32_t mine = 0;
 #pragma unroll
-                for (int q = 0; q < P; ++q) {
-                    if (VEC ? first >= n : first + q >= n) y[q] = 0.f;
-                    mx = max(mx, __float_as_uint(y[q]) & 0x7fffffffu);
-                }
+            for (int i = 0; i < V; ++i) {
 #pragma unroll
-                for (int d = 1; d < 128 / P; d <<= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-                float scale, inv_scale;
-                if (a.pow2) block_scale<true>(mx, scale, inv_scale);
-                else block_scale<false>(mx, scale, inv_scale);
-                if (idx < a.Kb * (128 / P) && row0 + r < a.M) {
-                    uint8_t* dst = a.codes + ((row0 + r) * a.Kb * 128 + first);
-                    const uint32_t c0 = cvt4(y[0], y[1], y[2], y[3], inv_scale);
-                    if constexpr (P == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(c0, cvt4(y[4], y[5], y[6], y[7], inv_scale));
+                for (int d = 1; d < kTeam; d <<= 1) mx[i] = max(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], d));
+                if ((t & (kTeam - 1)) == i) mine = mx[i];
+            }
+            float scale, inverse;
+            if (a.pow2) block_scale<true>(mine, scale, inverse);
+            else block_scale<false>(mine, scale, inverse);
+            const int block = t / kTeam + (t & (kTeam - 1)) * (T / kTeam);   // of the scale
+            if (on && (t & (kTeam - 1)) < V && block < a.Kb) a.scale[(int64_t)m * a.Kb + block] = scale;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const int idx = t + T * i;
+                const float r = __shfl_sync(0xffffffffu, inverse, i, kTeam);
+                const float2* y = f + i * H;
+                if (on && idx < a.Kb * kTeam) {
+                    uint8_t* dst = a.codes + ((int64_t)m * a.Kb * 128 + idx * P);
+                    const uint32_t c0 = cvt4(y[0].x, y[0].y, y[1].x, y[1].y, r);
+                    if constexpr (P == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(c0, cvt4(y[2].x, y[2].y, y[3].x, y[3].y, r));
                     else *reinterpret_cast<uint32_t*>(dst) = c0;
-                    if ((idx & (128 / P - 1)) == 0) a.scale[(row0 + r) * a.Kb + idx / (128 / P)] = scale;
                 }
             }
         }
-    }
-    if constexpr (!CODES && !VEC) {
+        if constexpr (!CODES && !VEC) store_row_ragged<DT, T, V>(y_row, n, t, group, stage, out, on);
+        m += step;
+    };
+    while (true) {
 #pragma unroll
-        for (int r = 0; r < R; ++r)
-            if (row0 + r < a.M)                              // the whole group
-                store_row_ragged<DT, T, V>(reinterpret_cast<E*>(a.y) + (row0 + r) * a.y_stride, n, t, group, stage, out[r]);
+        for (int i = 0; i <= D; ++i) {
+            if (m - in_warp >= M) return;
+            work(ring[i]);
+        }
     }
 }
 
 template <int DT, int T, int V, bool CODES, bool VEC>
-cudaError_t launch_forward(const NormArgs& a, int dev, cudaStream_t st) {
-    constexpr int R = T == 32 ? 2 : 1, kThreads = T < 256 ? 256 : T, kGroups = kThreads / T;
-    const int smem = VEC ? 0 : kGroups * kStageVecs<T, V> * 16;
-    auto* kernel = layer_norm_kernel<DT, T, V, R, CODES, VEC>;
+cudaError_t launch_forward(const NormArgs& a, int n_sm, int dev, cudaStream_t st) {
+    constexpr int kThreads = kNormThreads<T>, kGroups = kThreads / T, kSmem = VEC ? 0 : kGroups * kStageVecs<T, V> * 16;
+    auto* kernel = layer_norm_kernel<DT, T, V, CODES, VEC>;
     static std::atomic<uint64_t> done{0};
-    if (smem > 48 * 1024) {
-        const cudaError_t e = allow_smem(kernel, smem, done, dev);
+    static std::atomic<int> per_sm[kMaxDevices];
+    if (kSmem > 40 * 1024) {
+        const cudaError_t e = allow_smem(kernel, kSmem, done, dev);
         if (e != cudaSuccess) return e;
     }
-    return launch_pdl(kernel, dim3((unsigned)((a.M + kGroups * R - 1) / (kGroups * R))), dim3(kThreads), smem, st, a);
+    const int64_t most = (int64_t)n_sm * blocks_per_sm(kernel, kThreads, kSmem, per_sm, dev), need = (a.M + kGroups - 1) / kGroups;
+    return launch_pdl(kernel, dim3((unsigned)(need < most ? need : most)), dim3(kThreads), kSmem, st, a);
 }
 template <int DT, bool CODES, bool VEC>
-cudaError_t pick_forward(const NormArgs& a, RowShape s, int dev, cudaStream_t st) {
-#define TDQ_SHAPE(T, V) if (s.t == T && s.v == V) return launch_forward<DT, T, V, CODES, VEC>(a, dev, st)
-    TDQ_SHAPE(32, 1); TDQ_SHAPE(32, 2); TDQ_SHAPE(32, 4);
-    TDQ_SHAPE(128, 1); TDQ_SHAPE(128, 2); TDQ_SHAPE(128, 4);
-    TDQ_SHAPE(256, 1); TDQ_SHAPE(256, 4); TDQ_SHAPE(512, 1); TDQ_SHAPE(512, 4); TDQ_SHAPE(1024, 1); TDQ_SHAPE(1024, 4);
-    if constexpr (VEC) { TDQ_SHAPE(32, 3); TDQ_SHAPE(128, 3); }
+cudaError_t pick_forward(const NormArgs& a, RowShape s, int n_sm, int dev, cudaStream_t st) {
+#define TDQ_SHAPE(T, V) if (s.t == T && s.v == V) return launch_forward<DT, T, V, CODES, VEC>(a, n_sm, dev, st)
+    if constexpr (!CODES) TDQ_SHAPE(8, 1);
+    if constexpr (!CODES || DT != TDQ_F32) TDQ_SHAPE(16, 1);
+    TDQ_SHAPE(32, 1); TDQ_SHAPE(32, 2); TDQ_SHAPE(32, 3); TDQ_SHAPE(64, 1); TDQ_SHAPE(64, 2); TDQ_SHAPE(64, 3);
+    TDQ_SHAPE(128, 1); TDQ_SHAPE(128, 2); TDQ_SHAPE(128, 3); TDQ_SHAPE(256, 1); TDQ_SHAPE(256, 2);
+    TDQ_SHAPE(512, 1); TDQ_SHAPE(512, 2); TDQ_SHAPE(1024, 1); TDQ_SHAPE(1024, 2); TDQ_SHAPE(1024, 3); TDQ_SHAPE(1024, 4);
 #undef TDQ_SHAPE
     return cudaErrorInvalidValue;
 }
 template <int DT>
 cudaError_t forward(const NormArgs& a, bool vec, int n_sm, int dev, cudaStream_t st) {
     const int64_t n = a.codes ? (int64_t)a.Kb * 128 : a.C;   // codes behind C are written too
-    const RowShape s = row_shape((n + kPerVec<DT> - 1) / kPerVec<DT>, a.M, n_sm, 1024, vec);
-    if (a.codes) return vec ? pick_forward<DT, true, true>(a, s, dev, st) : pick_forward<DT, true, false>(a, s, dev, st);
-    return vec ? pick_forward<DT, false, true>(a, s, dev, st) : pick_forward<DT, false, false>(a, s, dev, st);
+    const RowShape s = row_shape((n + kPerVec<DT> - 1) / kPerVec<DT>, a.M, n_sm, a.codes ? 128 / kPerVec<DT> : 8, 1024);
+    if (a.codes) return vec ? pick_forward<DT, true, true>(a, s, n_sm, dev, st) : pick_forward<DT, true, false>(a, s, n_sm, dev, st);
+    return vec ? pick_forward<DT, false, true>(a, s, n_sm, dev, st) : pick_forward<DT, false, false>(a, s, n_sm, dev, st);
 }
 
 }  // namespace
@@ -185,8 +213,8 @@ extern "C" tdq_status tdq_layer_norm(const void* x, tdq_dtype dtype, int64_t M, 
     if (n_sm <= 0) return TDQ_ERR_CUDA;
     NormArgs a = {};
     a.x = x; a.y = y; a.w = weight; a.b = bias; a.codes = codes; a.scale = scale; a.mean = mean; a.rstd = rstd;
-    a.M = M; a.x_stride = x_row_stride; a.y_stride = y_row_stride; a.C = (int32_t)C; a.Kb = (int32_t)fp8_blocks(C); a.eps = eps; a.pow2 = (flags & TDQ_NORM_POW2) != 0;
-    const bool vec = C * (int64_t)esz % 16 == 0 && on_grid(x, x_row_stride, M, esz) && (!y || on_grid(y, y_row_stride, M, esz)) && !off_grid(weight, 16) && !off_grid(bias, 16);
+    a.M = M; a.x_stride = x_row_stride; a.y_stride = y_row_stride; a.C = (int32_t)C; a.Kb = (int32_t)fp8_blocks(C); a.eps = eps; a.pow2 = (flags & TDQ_NORM_POW2) != 0; a.w_vec = !off_grid(weight, 16) && !off_grid(bias, 16);
+    const bool vec = C * (int64_t)esz % 16 == 0 && on_grid(x, x_row_stride, M, esz) && (!y || on_grid(y, y_row_stride, M, esz));
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
     const cudaError_t e = dtype == TDQ_F32 ? forward<TDQ_F32>(a, vec, n_sm, dev, st) : dtype == TDQ_BF16 ? forward<TDQ_BF16>(a, vec, n_sm, dev, st)
                                                                                                         : forward<TDQ_F16>(a, vec, n_sm, dev, st);

@@ -10,7 +10,6 @@
 namespace tdq {
 namespace {
 
-constexpr int kBackThreads = 512;              // of a block
 constexpr int kSumLanes = 16;                  // threads that share a column of the last sum
 
 struct NormBackArgs {
@@ -20,83 +19,131 @@ struct NormBackArgs {
     float* part;                               // [blocks][2][C]
     int64_t M, x_stride, dy_stride, add_stride, dx_stride;   // strides in elements
     int32_t C;
+    bool w_vec;                                // weights on the 16-byte grid
 };
+
+// Threads of a block, as many whole groups as 80 registers a thread allow (64 where a row takes more than 768); whether the next row is on its way while one is worked on.
+template <int T> constexpr int kBackThreads = T > 384 ? T : 768 / T * T;
+template <int T, int V> constexpr int kBackAhead = V == 1 && T <= 768 ? 1 : 0;
 
 // T threads a row, V vectors each; VEC: rows on the 16-byte grid.
 template <int DT, int T, int V, bool VEC>
-__global__ void __launch_bounds__(kBackThreads, 1) layer_norm_back_kernel(const NormBackArgs a) {
+__global__ void __launch_bounds__(kBackThreads<T>, 1) layer_norm_back_kernel(const NormBackArgs a) {
     using E = typename Elem<DT>::T;
-    constexpr int P = kPerVec<DT>, kGroups = kBackThreads / T;
+    constexpr int P = kPerVec<DT>, kThreads = kBackThreads<T>, kGroups = kThreads / T, D = kBackAhead<T, V>;
+    constexpr bool KEEP = V == 1;                            // weights in registers
     extern __shared__ __align__(16) uint8_t smem_raw[];
     __shared__ float room[kGroups][2][2 * (T > 32 ? T / 32 : 1)];
     pdl_wait();
     pdl_trigger();
     const int group = (int)threadIdx.x / T, t = (int)threadIdx.x % T, n = a.C;
-    uint4* stage = reinterpret_cast<uint4*>(smem_raw) + (VEC ? 0 : group * kStageVecs<T, V>);
+    uint4* stage = reinterpret_cast<uint4*>(smem_raw) + (VEC ? 0 : group * 3 * kStageVecs<T, V>);   // x, dy, add; the output takes the first
+    constexpr int H = P / 2;                                 // pairs of a vector
     const float inv = __fdiv_rn(1.f, (float)n);
-    float dw[V * P], db[V * P];
+    float2 dw[V * H], db[V * H];
 #pragma unroll
-    for (int i = 0; i < V * P; ++i) dw[i] = db[i] = 0.f;
+    for (int i = 0; i < V * H; ++i) dw[i] = db[i] = two(0.f);
+    float2 w[KEEP ? V * H : 1];
+    if constexpr (KEEP) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) load_weight_pairs<P>(a.w, a.w_vec, (t + T * i) * P, n, 1.f, w + i * H);
+    }
+    // rows are counted in 32 bits, and addresses made anew from them: kept, they take twenty registers
+    const uint32_t M = (uint32_t)a.M, step = gridDim.x * kGroups, in_warp = T >= 32 ? 0u : (uint32_t)group % (32 / T);
+    uint32_t m = blockIdx.x * kGroups + (uint32_t)group;     // groups of a warp go on together, until the first one's rows end
+    struct Item {
+        Row<DT, T, V, VEC> x, dy;
+        float mean, rstd;
+    } ring[D + 1];
+    Row<DT, T, V, VEC> ar;
+    const auto fetch = [&](Item& r, uint32_t at) {
+        const bool on = at < M;
+        r.x.fetch(reinterpret_cast<const E*>(a.x) + (int64_t)at * a.x_stride, n, t, on);
+        r.dy.fetch(reinterpret_cast<const E*>(a.dy) + (int64_t)at * a.dy_stride, n, t, on);
+        r.mean = on ? __ldg(a.mean + at) : 0.f;
+        r.rstd = on ? __ldg(a.rstd + at) : 0.f;
+    };
+    if constexpr (D > 0) fetch(ring[0], m);
     int turn = 0;
-#pragma unroll 1
-    for (int64_t m = (int64_t)blockIdx.x * kGroups + group; m < a.M; m += (int64_t)gridDim.x * kGroups, turn ^= 1) {
+    const auto work = [&](Item& row, Item& then) {
+        const bool on = m < M;
+        fetch(then, m + D * step);                           // D == 0: this row
+        if (a.add) ar.fetch(reinterpret_cast<const E*>(a.add) + (int64_t)m * a.add_stride, n, t, on);
         uint4 xv[V], dv[V], av[V];
-        const E *x = reinterpret_cast<const E*>(a.x) + m * a.x_stride, *dy = reinterpret_cast<const E*>(a.dy) + m * a.dy_stride;
-        const E* add = reinterpret_cast<const E*>(a.add) + m * a.add_stride;
-        if constexpr (VEC) {
-            load_row<DT, T, V>(x, n, t, xv);
-            load_row<DT, T, V>(dy, n, t, dv);
-            if (a.add) load_row<DT, T, V>(add, n, t, av);
-        } else {
-            load_row_ragged<DT, T, V>(x, n, t, group, stage, xv);
-            load_row_ragged<DT, T, V>(dy, n, t, group, stage, dv);
-            if (a.add) load_row_ragged<DT, T, V>(add, n, t, group, stage, av);
+        if constexpr (!VEC) {
+            group_sync<T>(group);
+            row.x.put(stage, t);
+            row.dy.put(stage + kStageVecs<T, V>, t);
+            group_sync<T>(group);
         }
-        const float mean = __ldg(a.mean + m), rstd = __ldg(a.rstd + m);
-        float s[2] = {0.f, 0.f};
+        row.x.take(stage, n, t, xv);
+        row.dy.take(stage + (VEC ? 0 : kStageVecs<T, V>), n, t, dv);
+        const float2 mu = two(-row.mean), rs = two(row.rstd);
+        float2 s0 = two(0.f), s1 = two(0.f);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int first = (t + T * i) * P;
-            float xf[P], df[P], w[P];
-            widen_vec<DT>(xv[i], xf);
-            widen_vec<DT>(dv[i], df);
-            load_weights<P, VEC>(a.w, first, n, 1.f, w);
+            float2 xf[H], df[H], wl[H];
+            widen_pairs<DT>(xv[i], xf);
+            widen_pairs<DT>(dv[i], df);
+            if constexpr (!KEEP) load_weight_pairs<P>(a.w, a.w_vec, first, n, 1.f, wl);
 #pragma unroll
-            for (int q = 0; q < P; ++q) {                    // behind the row dy is 0, so whatever h is there adds nothing
-                const float h = (xf[q] - mean) * rstd, g = df[q] * w[q];
-                s[0] += g;
-                s[1] = fmaf(g, h, s[1]);
-                if (VEC || first + q < n) dw[i * P + q] = fmaf(df[q], h, dw[i * P + q]);
-                db[i * P + q] += df[q];
+            for (int q = 0; q < H; ++q) {                    // behind the row dy is 0, and h is kept out of what it could make NaN
+                float2 h = __fmul2_rn(__fadd2_rn(xf[q], mu), rs);
+                if (VEC ? first >= n : first + 2 * q >= n) h = two(0.f);
+                else if (!VEC && first + 2 * q + 1 >= n) h.y = 0.f;
+                const float2 g = __fmul2_rn(df[q], KEEP ? w[KEEP ? i * H + q : 0] : wl[q]);
+                s0 = __fadd2_rn(s0, g);
+                s1 = __ffma2_rn(g, h, s1);
+                dw[i * H + q] = __ffma2_rn(df[q], h, dw[i * H + q]);
+                db[i * H + q] = __fadd2_rn(db[i * H + q], df[q]);
             }
         }
+        float s[2] = {s0.x + s0.y, s1.x + s1.y};
         group_sum<T, 2>(s, room[group][turn], group, t);
-        const float c0 = s[0] * inv, c1 = s[1] * inv;
-        E* dx = reinterpret_cast<E*>(a.dx) + m * a.dx_stride;
+        turn ^= 1;
+        const float2 c0 = two(-s[0] * inv), c1 = two(-s[1] * inv);
+        if (a.add) {
+            if constexpr (!VEC) {
+                ar.put(stage + 2 * kStageVecs<T, V>, t);     // read again only behind the next row's meeting
+                group_sync<T>(group);
+            }
+            ar.take(stage + (VEC ? 0 : 2 * kStageVecs<T, V>), n, t, av);
+        }
+        E* dx = reinterpret_cast<E*>(a.dx) + (int64_t)m * a.dx_stride;
         uint4 out[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int first = (t + T * i) * P;
-            float xf[P], df[P], w[P];
-            widen_vec<DT>(xv[i], xf);
-            widen_vec<DT>(dv[i], df);
-            load_weights<P, VEC>(a.w, first, n, 1.f, w);
-            float r[P];
+            float2 xf[H], df[H], wl[H], r[H];
+            forget(xv[i]);
+            forget(dv[i]);
+            widen_pairs<DT>(xv[i], xf);
+            widen_pairs<DT>(dv[i], df);
+            if constexpr (!KEEP) load_weight_pairs<P>(a.w, a.w_vec, first, n, 1.f, wl);
 #pragma unroll
-            for (int q = 0; q < P; ++q) {
-                const float h = (xf[q] - mean) * rstd, g = df[q] * w[q];
-                r[q] = rstd * (g - c0 - h * c1);
+            for (int q = 0; q < H; ++q) {
+                const float2 h = __fmul2_rn(__fadd2_rn(xf[q], mu), rs), g = __fmul2_rn(df[q], KEEP ? w[KEEP ? i * H + q : 0] : wl[q]);
+                r[q] = __fmul2_rn(rs, __ffma2_rn(h, c1, __fadd2_rn(g, c0)));
             }
             if (a.add) {
-                float af[P];
-                widen_vec<DT>(av[i], af);
+                float2 af[H];
+                widen_pairs<DT>(av[i], af);
 #pragma unroll
-                for (int q = 0; q < P; ++q) r[q] += af[q];
+                for (int q = 0; q < H; ++q) r[q] = __fadd2_rn(r[q], af[q]);
             }
-            out[i] = narrow_vec<DT>(r);
-            if (VEC && first < n) reinterpret_cast<uint4*>(dx)[t + T * i] = out[i];
+            out[i] = narrow_pairs<DT>(r);
+            if (VEC && first < n && on) reinterpret_cast<uint4*>(dx)[t + T * i] = out[i];
         }
-        if constexpr (!VEC) store_row_ragged<DT, T, V>(dx, n, t, group, stage, out);
+        if constexpr (!VEC) store_row_ragged<DT, T, V>(dx, n, t, group, stage, out, on);
+        m += step;
+    };
+    while (m - in_warp < M) {
+        work(ring[0], ring[D]);
+        if constexpr (D > 0) {
+            if (m - in_warp >= M) break;
+            work(ring[1], ring[0]);
+        }
     }
     // the groups' sums, a channel's next to one another
     float* part = a.part + (int64_t)blockIdx.x * 2 * n;
@@ -106,7 +153,8 @@ __global__ void __launch_bounds__(kBackThreads, 1) layer_norm_back_kernel(const 
 #pragma unroll
             for (int q = 0; q < P; ++q) {
                 const int c = (t + T * i) * P + q;
-                if (c < n) { part[c] = dw[i * P + q]; part[n + c] = db[i * P + q]; }
+                const float2 u = dw[i * H + q / 2], v = db[i * H + q / 2];
+                if (c < n) { part[c] = q & 1 ? u.y : u.x; part[n + c] = q & 1 ? v.y : v.x; }
             }
     } else {
         constexpr int kCols = T * V * P;
@@ -118,13 +166,13 @@ __global__ void __launch_bounds__(kBackThreads, 1) layer_norm_back_kernel(const 
             for (int i = 0; i < V; ++i)
 #pragma unroll
                 for (int q = 0; q < P; q += 4) {
-                    const float* d = (which ? db : dw) + i * P + q;
-                    *reinterpret_cast<float4*>(sums + group * kCols + (t + T * i) * P + q) = make_float4(d[0], d[1], d[2], d[3]);
+                    const float2* d = (which ? db : dw) + i * H + q / 2;
+                    *reinterpret_cast<float4*>(sums + group * kCols + (t + T * i) * P + q) = make_float4(d[0].x, d[0].y, d[1].x, d[1].y);
                 }
             __syncthreads();
-            for (int c = (int)threadIdx.x; c < n; c += kBackThreads) {
+            for (int c = (int)threadIdx.x; c < n; c += kThreads) {
                 float v = 0.f;
-#pragma unroll
+#pragma unroll 16
                 for (int g = 0; g < kGroups; ++g) v += sums[g * kCols + c];
                 part[which * n + c] = v;
             }
@@ -157,31 +205,34 @@ __global__ void __launch_bounds__(32 * kSumLanes) column_sums_kernel(const float
 
 template <int DT, int T, int V, bool VEC>
 cudaError_t launch_back(const NormBackArgs& a, unsigned blocks, int dev, cudaStream_t st) {
-    constexpr int kGroups = kBackThreads / T;
-    const int stage = VEC ? 0 : kGroups * kStageVecs<T, V> * 16, sums = kGroups > 1 ? kGroups * T * V * kPerVec<DT> * 4 : 0;
-    const int smem = stage > sums ? stage : sums;
+    constexpr int kThreads = kBackThreads<T>, kGroups = kThreads / T;
+    constexpr int kStage = VEC ? 0 : kGroups * 3 * kStageVecs<T, V> * 16, kSums = kGroups > 1 ? kGroups * T * V * kPerVec<DT> * 4 : 0, kSmem = kStage > kSums ? kStage : kSums;
     auto* kernel = layer_norm_back_kernel<DT, T, V, VEC>;
     static std::atomic<uint64_t> done{0};
-    if (smem > 40 * 1024) {
-        const cudaError_t e = allow_smem(kernel, smem, done, dev);
+    if (kSmem > 40 * 1024) {
+        const cudaError_t e = allow_smem(kernel, kSmem, done, dev);
         if (e != cudaSuccess) return e;
     }
-    return launch_pdl(kernel, dim3(blocks), dim3(kBackThreads), smem, st, a);
+    return launch_pdl(kernel, dim3(blocks), dim3(kThreads), kSmem, st, a);
 }
 template <int DT, bool VEC>
 cudaError_t pick_back(const NormBackArgs& a, RowShape s, unsigned blocks, int dev, cudaStream_t st) {
 #define TDQ_SHAPE(T, V) if (s.t == T && s.v == V) return launch_back<DT, T, V, VEC>(a, blocks, dev, st)
-    TDQ_SHAPE(32, 1); TDQ_SHAPE(32, 2); TDQ_SHAPE(32, 4);
-    TDQ_SHAPE(128, 1); TDQ_SHAPE(128, 2); TDQ_SHAPE(128, 4);
-    TDQ_SHAPE(256, 1); TDQ_SHAPE(256, 4); TDQ_SHAPE(512, 1); TDQ_SHAPE(512, 4);
-    if constexpr (VEC) { TDQ_SHAPE(32, 3); TDQ_SHAPE(128, 3); }
-    if constexpr (DT == TDQ_F32) TDQ_SHAPE(512, 8);
+    TDQ_SHAPE(8, 1); TDQ_SHAPE(16, 1); TDQ_SHAPE(32, 1); TDQ_SHAPE(64, 1); TDQ_SHAPE(96, 1); TDQ_SHAPE(128, 1); TDQ_SHAPE(192, 1); TDQ_SHAPE(256, 1);
+    TDQ_SHAPE(384, 1); TDQ_SHAPE(512, 1); TDQ_SHAPE(768, 1); TDQ_SHAPE(1024, 1); TDQ_SHAPE(1024, 2);
+    if constexpr (DT == TDQ_F32) TDQ_SHAPE(1024, 4);
 #undef TDQ_SHAPE
     return cudaErrorInvalidValue;
 }
 template <int DT>
-cudaError_t backward(const NormBackArgs& a, bool vec, unsigned blocks, int n_sm, int dev, cudaStream_t st) {
-    const RowShape s = row_shape((a.C + kPerVec<DT> - 1) / kPerVec<DT>, a.M, n_sm, 512, vec);
+cudaError_t backward(const NormBackArgs& a, bool vec, unsigned blocks, int dev, cudaStream_t st) {
+    // A vector a thread: the column sums of more would leave no registers for the next row, and two vectors in 512 threads an SM took twice as long (18464 x 768 bf16 with
+    // an addend 39 us, now BACK_TIME).
+    static const int threads[] = {8, 16, 32, 64, 96, 128, 192, 256, 384, 512, 768, 1024};
+    const int64_t vecs = (a.C + kPerVec<DT> - 1) / kPerVec<DT>;
+    RowShape s = {1024, vecs <= 1024 ? 1 : vecs <= 2048 ? 2 : 4};
+    for (int t : threads)
+        if (t >= vecs) { s.t = t; break; }
     return vec ? pick_back<DT, true>(a, s, blocks, dev, st) : pick_back<DT, false>(a, s, blocks, dev, st);
 }
 int64_t back_blocks(int64_t M, int n_sm) { return M < n_sm ? M : n_sm; }
@@ -219,11 +270,12 @@ extern "C" tdq_status tdq_layer_norm_backward(const void* dy, int64_t dy_row_str
         NormBackArgs a = {};
         a.x = x; a.dy = dy; a.add = add; a.dx = dx; a.w = weight; a.mean = mean; a.rstd = rstd; a.part = reinterpret_cast<float*>(workspace);
         a.M = M; a.x_stride = x_row_stride; a.dy_stride = dy_row_stride; a.add_stride = add_row_stride; a.dx_stride = dx_row_stride; a.C = (int32_t)C;
+        a.w_vec = !off_grid(weight, 16);
         const bool vec = C * (int64_t)esz % 16 == 0 && on_grid(x, x_row_stride, M, esz) && on_grid(dy, dy_row_stride, M, esz) && on_grid(dx, dx_row_stride, M, esz) &&
-                         (!add || on_grid(add, add_row_stride, M, esz)) && !off_grid(weight, 16);
+                         (!add || on_grid(add, add_row_stride, M, esz));
         const unsigned b = (unsigned)blocks;
-        const cudaError_t e = dtype == TDQ_F32 ? backward<TDQ_F32>(a, vec, b, n_sm, dev, st) : dtype == TDQ_BF16 ? backward<TDQ_BF16>(a, vec, b, n_sm, dev, st)
-                                                                                                         : backward<TDQ_F16>(a, vec, b, n_sm, dev, st);
+        const cudaError_t e = dtype == TDQ_F32 ? backward<TDQ_F32>(a, vec, b, dev, st) : dtype == TDQ_BF16 ? backward<TDQ_BF16>(a, vec, b, dev, st)
+                                                                                                         : backward<TDQ_F16>(a, vec, b, dev, st);
         if (e != cudaSuccess) return cuda_status(e);
         g_launch_count.fetch_add(1, std::memory_order_relaxed);
     }
