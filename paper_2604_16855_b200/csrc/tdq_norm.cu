@@ -34,6 +34,7 @@ __global__ void __launch_bounds__(kNormThreads<T>, T > 256 ? 1 : V == 1 ? (VEC ?
     using E = typename Elem<DT>::T;
     constexpr int P = kPerVec<DT>, kGroups = kNormThreads<T> / T, D = kAhead<T, V, CODES, VEC>;
     constexpr bool KEEP = kKeepWeights<T, V>;
+    static_assert(T <= 32 || kGroups <= kMaxGroups, "barriers");
     extern __shared__ __align__(16) uint8_t smem_raw[];
     __shared__ float room[kGroups][2][T > 32 ? T / 32 : 1];
     pdl_wait();
@@ -74,9 +75,7 @@ __global__ void __launch_bounds__(kNormThreads<T>, T > 256 ? 1 : V == 1 ? (VEC ?
         float2 sum = f[0];
 #pragma unroll
         for (int i = 1; i < V * H; ++i) sum = __fadd2_rn(sum, f[i]);
-        float s[1] = {sum.x + sum.y};
-        group_sum<T, 1>(s, room[group][0], group, t);
-        const float mean = s[0] * inv;
+        const float mean = group_sum<T>(sum.x + sum.y, room[group][0], group, t) * inv;
         sum = two(0.f);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
@@ -91,9 +90,7 @@ __global__ void __launch_bounds__(kNormThreads<T>, T > 256 ? 1 : V == 1 ? (VEC ?
                 sum = __ffma2_rn(d, d, sum);
             }
         }
-        s[0] = sum.x + sum.y;
-        group_sum<T, 1>(s, room[group][1], group, t);
-        const float rstd = __frcp_rn(__fsqrt_rn(fmaf(s[0], inv, a.eps)));
+        const float rstd = __frcp_rn(__fsqrt_rn(fmaf(group_sum<T>(sum.x + sum.y, room[group][1], group, t), inv, a.eps)));
         if (t == 0 && on) {
             if (a.mean) a.mean[m] = mean;
             if (a.rstd) a.rstd[m] = rstd;

@@ -22,18 +22,20 @@ struct NormBackArgs {
     bool w_vec;                                // weights on the 16-byte grid
 };
 
-// Threads of a block, as many whole groups as 80 registers a thread allow (64 where a row takes more than 768); whether the next row is on its way while one is worked on.
-template <int T> constexpr int kBackThreads = T > 384 ? T : 768 / T * T;
+// Threads of a block: as many whole groups as 80 registers a thread allow (128 for rows off the grid; 64 where a row takes more threads).  Whether the next row is on its
+// way while one is worked on.
+template <int T, bool VEC> constexpr int kBackThreads = T > 384 ? T : (VEC ? 768 : 512) / T * T;
 template <int T, int V> constexpr int kBackAhead = V == 1 && T <= 768 ? 1 : 0;
 
 // T threads a row, V vectors each; VEC: rows on the 16-byte grid.
 template <int DT, int T, int V, bool VEC>
-__global__ void __launch_bounds__(kBackThreads<T>, 1) layer_norm_back_kernel(const NormBackArgs a) {
+__global__ void __launch_bounds__(kBackThreads<T, VEC>, 1) layer_norm_back_kernel(const NormBackArgs a) {
     using E = typename Elem<DT>::T;
-    constexpr int P = kPerVec<DT>, kThreads = kBackThreads<T>, kGroups = kThreads / T, D = kBackAhead<T, V>;
+    constexpr int P = kPerVec<DT>, kThreads = kBackThreads<T, VEC>, kGroups = kThreads / T, D = kBackAhead<T, V>;
     constexpr bool KEEP = V == 1;                            // weights in registers
+    static_assert(T <= 32 || kGroups <= kMaxGroups, "barriers");
     extern __shared__ __align__(16) uint8_t smem_raw[];
-    __shared__ float room[kGroups][2][2 * (T > 32 ? T / 32 : 1)];
+    __shared__ __align__(8) float room[kGroups][2][2 * (T > 32 ? T / 32 : 1)];
     pdl_wait();
     pdl_trigger();
     const int group = (int)threadIdx.x / T, t = (int)threadIdx.x % T, n = a.C;
@@ -99,10 +101,9 @@ __global__ void __launch_bounds__(kBackThreads<T>, 1) layer_norm_back_kernel(con
                 db[i * H + q] = __fadd2_rn(db[i * H + q], df[q]);
             }
         }
-        float s[2] = {s0.x + s0.y, s1.x + s1.y};
-        group_sum<T, 2>(s, room[group][turn], group, t);
+        const float2 s = group_sum2<T>(make_float2(s0.x + s0.y, s1.x + s1.y), room[group][turn], group, t);
         turn ^= 1;
-        const float2 c0 = two(-s[0] * inv), c1 = two(-s[1] * inv);
+        const float2 c0 = two(-s.x * inv), c1 = two(-s.y * inv);
         if (a.add) {
             if constexpr (!VEC) {
                 ar.put(stage + 2 * kStageVecs<T, V>, t);     // read again only behind the next row's meeting
@@ -116,7 +117,7 @@ __global__ void __launch_bounds__(kBackThreads<T>, 1) layer_norm_back_kernel(con
         for (int i = 0; i < V; ++i) {
             const int first = (t + T * i) * P;
             float2 xf[H], df[H], wl[H], r[H];
-            forget(xv[i]);
+            forget(xv[i]);                                   // made again: held, what the first pass made of the row leaves too few registers
             forget(dv[i]);
             widen_pairs<DT>(xv[i], xf);
             widen_pairs<DT>(dv[i], df);
@@ -205,7 +206,7 @@ __global__ void __launch_bounds__(32 * kSumLanes) column_sums_kernel(const float
 
 template <int DT, int T, int V, bool VEC>
 cudaError_t launch_back(const NormBackArgs& a, unsigned blocks, int dev, cudaStream_t st) {
-    constexpr int kThreads = kBackThreads<T>, kGroups = kThreads / T;
+    constexpr int kThreads = kBackThreads<T, VEC>, kGroups = kThreads / T;
     constexpr int kStage = VEC ? 0 : kGroups * 3 * kStageVecs<T, V> * 16, kSums = kGroups > 1 ? kGroups * T * V * kPerVec<DT> * 4 : 0, kSmem = kStage > kSums ? kStage : kSums;
     auto* kernel = layer_norm_back_kernel<DT, T, V, VEC>;
     static std::atomic<uint64_t> done{0};

@@ -7,6 +7,7 @@ namespace tdq {
 namespace {
 
 constexpr int64_t kMaxRow = 16384;            // channels of the longest row
+constexpr int kMaxGroups = 15;                // of several warps in a block: it has barriers 0 (of all its threads) to 15
 
 template <int DT> constexpr int kPerVec = 16 / (int)sizeof(typename Elem<DT>::T);
 
@@ -16,35 +17,56 @@ __device__ __forceinline__ void group_sync(int group) {
     if constexpr (T <= 32) __syncwarp();
     else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(T) : "memory");
 }
-// N sums over the group's threads, all at once; `room` holds N floats for each of the group's warps, and another use of it follows a barrier.
-template <int T, int N>
-__device__ __forceinline__ void group_sum(float (&v)[N], float* room, int group, int t) {
+// The sum over the group's threads; `room` holds a float for each of the group's warps, and another use of it follows a barrier.
+template <int T>
+__device__ __forceinline__ float group_sum(float v, float* room, int group, int t) {
 #pragma unroll
-    for (int d = (T < 32 ? T : 32) / 2; d; d >>= 1)
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], d);
+    for (int d = (T < 32 ? T : 32) / 2; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
     if constexpr (T > 32) {
         constexpr int kWarps = T / 32;
-        if ((t & 31) == 0)
-#pragma unroll
-            for (int i = 0; i < N; ++i) room[i * kWarps + (t >> 5)] = v[i];
+        if ((t & 31) == 0) room[t >> 5] = v;
         group_sync<T>(group);
         if constexpr (kWarps <= 4) {
+            v = room[0];
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                v[i] = room[i * kWarps];
-#pragma unroll
-                for (int k = 1; k < kWarps; ++k) v[i] += room[i * kWarps + k];
-            }
+            for (int k = 1; k < kWarps; ++k) v += room[k];
         } else {
+            v = (t & 31) < kWarps ? room[t & 31] : 0.f;
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                float s = (t & 31) < kWarps ? room[i * kWarps + (t & 31)] : 0.f;
+            for (int d = 16; d; d >>= 1)
+                if (d < kWarps) v += __shfl_xor_sync(0xffffffffu, v, d);
+            v = __shfl_sync(0xffffffffu, v, 0);
+        }
+    }
+    return v;
+}
+// Two sums at a time: the first exchange leaves the lower half of the threads with one, the upper half with the other.  `room` holds two floats for each warp.
+template <int T>
+__device__ __forceinline__ float2 group_sum2(float2 v, float* room, int group, int t) {
+    constexpr int W = T < 32 ? T : 32;
+    const bool upper = t & (W / 2);
+    float s = (upper ? v.y : v.x) + __shfl_xor_sync(0xffffffffu, upper ? v.x : v.y, W / 2);
 #pragma unroll
-                for (int d = 16; d; d >>= 1)
-                    if (d < kWarps) s += __shfl_xor_sync(0xffffffffu, s, d);
-                v[i] = __shfl_sync(0xffffffffu, s, 0);
-            }
+    for (int d = W / 4; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+    if constexpr (T <= 32) {
+        const float o = __shfl_xor_sync(0xffffffffu, s, W / 2);
+        return upper ? make_float2(o, s) : make_float2(s, o);
+    } else {
+        constexpr int kWarps = T / 32;
+        if ((t & 15) == 0) room[(t >> 5) * 2 + (upper ? 1 : 0)] = s;
+        group_sync<T>(group);
+        if constexpr (kWarps <= 4) {
+            float2 r = *reinterpret_cast<const float2*>(room);
+#pragma unroll
+            for (int k = 1; k < kWarps; ++k) r = __fadd2_rn(r, *reinterpret_cast<const float2*>(room + 2 * k));
+            return r;
+        } else {
+            float2 r = (t & 31) < kWarps ? *reinterpret_cast<const float2*>(room + 2 * (t & 31)) : make_float2(0.f, 0.f);
+            s = (upper ? r.y : r.x) + __shfl_xor_sync(0xffffffffu, upper ? r.x : r.y, 16);
+#pragma unroll
+            for (int d = 8; d; d >>= 1)
+                if (d < kWarps) s += __shfl_xor_sync(0xffffffffu, s, d);
+            return make_float2(__shfl_sync(0xffffffffu, s, 0), __shfl_sync(0xffffffffu, s, 16));
         }
     }
 }
@@ -93,6 +115,24 @@ __device__ __forceinline__ uint4 narrow_pairs(const float2* f) {
 // 16-byte vectors of a group's stage in shared memory: the longest row, its offset, and the word behind it that a shift reads
 template <int T, int V> constexpr int kStageVecs = T * V + 2;
 
+// Vectors t, t + T, .. of a row of n channels that lies `off` bytes into the stage, zeros behind it.
+template <int DT, int T, int V>
+__device__ __forceinline__ void take_ragged(const uint4* stage, int off, int n, int t, uint4* v) {
+    const uint32_t* words = reinterpret_cast<const uint32_t*>(stage) + (off >> 2);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const int first = (t + T * i) * kPerVec<DT>;
+        v[i] = make_uint4(0, 0, 0, 0);
+        if (first >= n) continue;
+        const uint32_t* p = words + 4 * (t + T * i);
+        uint32_t a = p[0], b = p[1], c = p[2], d = p[3];
+        if (sizeof(typename Elem<DT>::T) == 2 && (off & 2)) {
+            const uint32_t e = p[4];
+            a = __funnelshift_r(a, b, 16); b = __funnelshift_r(b, c, 16); c = __funnelshift_r(c, d, 16); d = __funnelshift_r(d, e, 16);
+        }
+        v[i] = keep_first<DT>(make_uint4(a, b, c, d), n - first);
+    }
+}
 // A row on its way.  fetch() starts the loads, take() gives vectors t, t + T, .. of the row, zeros behind its n channels.  Off the grid (!VEC) a row's aligned vectors (one that
 // holds an element of the row is read whole; what lies beside the row in it is not used) pass through the group's stage: put() between two group_syncs, the first
 // of which says that what was there has been read.
@@ -126,20 +166,7 @@ struct Row {
 #pragma unroll
             for (int i = 0; i < V; ++i) v[i] = raw[i];
         } else {
-            const uint32_t* words = reinterpret_cast<const uint32_t*>(stage) + (off >> 2);
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const int first = (t + T * i) * P;
-                v[i] = make_uint4(0, 0, 0, 0);
-                if (first >= n) continue;
-                const uint32_t* p = words + 4 * (t + T * i);
-                uint32_t a = p[0], b = p[1], c = p[2], d = p[3];
-                if (sizeof(E) == 2 && (off & 2)) {
-                    const uint32_t e = p[4];
-                    a = __funnelshift_r(a, b, 16); b = __funnelshift_r(b, c, 16); c = __funnelshift_r(c, d, 16); d = __funnelshift_r(d, e, 16);
-                }
-                v[i] = keep_first<DT>(make_uint4(a, b, c, d), n - first);
-            }
+            take_ragged<DT, T, V>(stage, off, n, t, v);
         }
     }
 };
