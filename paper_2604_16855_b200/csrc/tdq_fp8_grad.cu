@@ -18,7 +18,7 @@
 #include <numeric>
 
 #include "tdq_tc.cuh"
-#include "tdq_rows.cuh"
+#include "tdq_fp8_grad.cuh"
 
 namespace tdq {
 namespace {
@@ -134,16 +134,6 @@ __device__ __forceinline__ void tmem_ld16_wait(uint32_t taddr, uint32_t* v) {
                  : "r"(taddr)
                  : "memory");
 }
-// Four codes times their scale as four bf16, nearest even.
-__device__ __forceinline__ void restore4(uint32_t codes, float scale, uint32_t& lo, uint32_t& hi) {
-    uint32_t h0, h1;
-    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(h0), "=r"(h1) : "r"(codes));
-    const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&h0)), f1 = __half22float2(*reinterpret_cast<const __half2*>(&h1));
-    const float2 p0 = __fmul2_rn(f0, make_float2(scale, scale)), p1 = __fmul2_rn(f1, make_float2(scale, scale));
-    lo = narrow2<TDQ_BF16>(p0.x, p0.y);
-    hi = narrow2<TDQ_BF16>(p1.x, p1.y);
-}
-
 // DT: dw's tdq_dtype
 template <int DT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGradThreads, 1)
@@ -573,8 +563,7 @@ __global__ void __launch_bounds__(256) grad_parts_kernel(const GradArgs a, int32
     }
 }
 
-// dy as `PARTS` bf16 addends, [PARTS][rows_part][stride], rows behind M zero: the leading eight bits of what is left, cut off, each time; exact.  A value
-// without a number goes to the first addend alone.
+// dy as `PARTS` bf16 addends, [PARTS][rows_part][stride], rows behind M zero
 template <int DT, int PARTS, bool VEC>
 __global__ void __launch_bounds__(256) grad_addends_kernel(const void* dy, int64_t M, int64_t O, int64_t stride, uint16_t* __restrict__ out, int64_t rows_part, int64_t out_stride) {
     using E = typename Elem<DT>::T;
@@ -595,23 +584,7 @@ __global__ void __launch_bounds__(256) grad_addends_kernel(const void* dy, int64
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
             uint32_t r[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                uint32_t b[2];
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    float& v = f[2 * j + q];
-                    if (fabsf(v) < INFINITY) {
-                        const float lead = PARTS == 1 ? v : __uint_as_float(__float_as_uint(v) & 0xffff0000u);
-                        b[q] = __float_as_uint(lead) >> 16;
-                        v -= lead;
-                    } else {
-                        b[q] = narrow2<TDQ_BF16>(v, 0.f) & 0xffffu;
-                        v = 0.f;
-                    }
-                }
-                r[j] = b[0] | b[1] << 16;
-            }
+            grad_addend<PARTS>(f, r);
             *reinterpret_cast<uint4*>(out + (p * rows_part + m) * out_stride + o) = make_uint4(r[0], r[1], r[2], r[3]);
         }
     }
@@ -629,6 +602,8 @@ struct GradPlan {
     int32_t clusters;
     int64_t unit;              // stages that stay together
     bool cut;                  // some tile is added by more than one cluster
+    bool small;                // the kernel for little work instead
+    uint32_t split;            // its parts of the tokens
     size_t dy_bytes, part_bytes, db_bytes, bytes;
 };
 // How the work is cut, and the room that takes: the status word, parts of tiles and of db, dy's addends.
@@ -658,6 +633,12 @@ GradPlan grad_plan(const void* dy, tdq_dtype dtype, int64_t dy_stride, int64_t M
     for (int64_t w = most; w > 1; w -= w > 32 ? 6 : w > 16 ? 3 : 1) consider(w);
     for (int64_t w = 2 * tiles; w <= most; w += tiles) consider(w);   // equal parts of every tile: the fewest
     p.cut = p.unit == 1 && per_tile > 1;
+    // against the kernel for little work: launch, tensor memory and the way to the first sums, dy's addends, and the second kernel that db needs anyway
+    p.small = grad_small_cost(M, O, fp8_blocks(I), p.parts, n_sm, &p.split) < least + 7000 + (p.copied ? 5000 : 0) + (p.cut ? 0 : 4000);
+    if (p.small) {
+        p.bytes = kWorkspaceHeader;
+        return p;
+    }
     p.dy_bytes = p.copied ? (size_t)(p.parts * p.rows_part * p.dy_stride) * 2 : 0;
     p.part_bytes = p.cut ? (size_t)2 * p.clusters * 256 * 256 * 4 : 0;
     p.db_bytes = (size_t)(2 * p.clusters + tiles) * kFillPairs * 256 * 4;
@@ -717,8 +698,14 @@ extern "C" tdq_status tdq_fp8_weight_grad(const void* dy, tdq_dtype dy_dtype, in
     const int n_sm = current_device_sm_count(&dev);
     if (n_sm <= 0) return TDQ_ERR_CUDA;
     const GradPlan p = grad_plan(dy, dy_dtype, dy_row_stride, M, O, I, n_sm);
-    if (p.tiles_o * p.tiles_i > INT32_MAX / 128 || p.parts * p.rows_part > kGradMax || p.total > INT32_MAX) return TDQ_ERR_UNSUPPORTED;
+    if (!p.small && (p.tiles_o * p.tiles_i > INT32_MAX / 128 || p.parts * p.rows_part > kGradMax || p.total > INT32_MAX)) return TDQ_ERR_UNSUPPORTED;
     if (!workspace || workspace_bytes < p.bytes) return TDQ_ERR_WORKSPACE;
+    if (p.small) {
+        GradSmallArgs g = {xcodes, xscale, dy, dw, db, M, O, I, dy_row_stride, dw_row_stride, (int32_t)fp8_blocks(I), (int32_t)dw_dtype,
+                           on_grid(dw, dw_row_stride, O, (int64_t)wsz) && I % 4 == 0, p.split,
+                           reinterpret_cast<uint32_t*>(workspace)};
+        return launch_grad_small(g, dy_dtype, O % 8 == 0 && on_grid(dy, dy_row_stride, M, (int64_t)ysz), st);
+    }
     uint8_t* ws = reinterpret_cast<uint8_t*>(workspace);
     GradArgs a = {};
     a.xcodes = xcodes; a.xscale = xscale; a.dw = dw; a.db = db; a.M = M; a.O = O; a.I = I;

@@ -87,10 +87,13 @@ def test_weight_grad(tdq):
     _each(f, good, [((6, 1 << 31), (2, 1 << 31), uns), ((7, 1 << 31), (10, 1 << 31), uns)])
     head = int(size(FAKE, 1, 40, 0, 40, 90))
     assert head == 256 and size(FAKE, 3, 40, 64, 40, 90) == size(FAKE, 1, 40, -1, 40, 90) == size(FAKE, 1, 40, 64, 40, 0) == 0
-    # one tile of few stages: nothing is cut, three places for sums of dy; fp16 and rows off the grid pass through the workspace
-    one = 256 + 3 * 4096
-    assert size(FAKE, 1, 40, 64, 40, 90) == one and size(FAKE, 1, 41, 64, 40, 90) == one + 64 * 40 * 2
-    assert size(FAKE, 2, 40, 65, 40, 90) == one + 2 * 128 * 40 * 2 and size(FAKE, 0, 40, 64, 40, 90) == one + 3 * 64 * 40 * 2
+    # little work needs the status word alone
+    assert size(FAKE, 1, 40, 64, 40, 90) == size(FAKE, 0, 41, 500, 40, 90) == 256
+    # many whole tiles: a place for each tile's sums of dy; fp16 and rows off the grid pass through the workspace
+    tiles, n, o = 16 * 148, 512, 4096
+    one = 256 + (2 * 74 + tiles) * 4096
+    assert size(FAKE, 1, o, n, o, 148 * 256) == one and size(ODD, 1, o, n, o, 148 * 256) == one + n * o * 2
+    assert size(FAKE, 2, o, n, o, 148 * 256) == one + 2 * n * o * 2 and size(FAKE, 0, o, n - 1, o, 148 * 256) == one + 3 * n * o * 2
     # a long sum: two places for each of some clusters
     assert (size(FAKE, 1, 40, 1 << 20, 40, 90) - 256 - 4096) % (2 * 256 * (256 + 4) * 4) == 0
 

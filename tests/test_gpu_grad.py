@@ -152,3 +152,29 @@ def test_captured_on_another_stream(tdq):
             graph.replay()
             torch.cuda.synchronize()
             assert torch.equal(dw, want[0]) and torch.equal(db, want[1])
+
+
+def test_both_kernels_run(tdq):
+    """Little work is one launch, whatever dy's type and with db; a long or a wide sum takes the kernel for large layers, one more launch for what is cut or for db, one more
+    for dy's addends."""
+    for m, o, i, dtype, launches in [(64, 96, 200, torch.float32, 1), (500, 300, 500, torch.bfloat16, 1), (1, 4096, 1000, torch.float16, 1), (20000, 64, 64, torch.bfloat16, 2),
+                                     (4096, 2048, 1024, torch.bfloat16, 2), (4096, 2048, 1024, torch.float16, 3)]:
+        dy, xc, xs = inputs(tdq, m, o, i, dtype)
+        n0 = tdq.kernel_launch_count()
+        tdq.fp8_weight_grad(dy, xc, xs, i)
+        assert tdq.kernel_launch_count() - n0 == launches, (m, o, i, dtype)
+
+
+# every number of parts of the tokens that the kernel for little work takes, and ragged ends in each direction
+@pytest.mark.parametrize("m", [1, 31, 33, 65, 97, 129, 161, 193, 225, 400, 512, 513, 1024, 2000, 4000])
+@pytest.mark.parametrize("o,i", [(8, 128), (65, 129), (130, 40)])
+@pytest.mark.parametrize("dy_type,pitch", [("bf16", 0), ("fp32", 8), ("fp16", 1)])
+def test_little_work(tdq, m, o, i, dy_type, pitch):
+    dy, xc, xs = inputs(tdq, m, o, i, TYPES[dy_type], pitch, seed=11)
+    for dw_type in (torch.float32, torch.bfloat16):
+        whole = torch.full((o, i + 3), 55.0, dtype=dw_type, device="cuda")
+        ws = tdq.fp8_weight_grad_workspace(dy, i)
+        ws.fill_(255)
+        dw, db = tdq.fp8_weight_grad(dy, xc, xs, i, dw=whole[:, :i], workspace=ws)
+        assert tdq.workspace_status(ws) == (tdq.OK, 0) and bool((whole[:, i:] == 55.0).all())
+        check(dw, db, dy, xc, xs, i, {"bf16": 1, "fp16": 2, "fp32": 3}[dy_type])
