@@ -634,7 +634,8 @@ GradPlan grad_plan(const void* dy, tdq_dtype dtype, int64_t dy_stride, int64_t M
     for (int64_t w = 2 * tiles; w <= most; w += tiles) consider(w);   // equal parts of every tile: the fewest
     p.cut = p.unit == 1 && per_tile > 1;
     // against the kernel for little work: launch, tensor memory and the way to the first sums, dy's addends, and the second kernel that db needs anyway
-    p.small = grad_small_cost(M, O, fp8_blocks(I), p.parts, n_sm, &p.split) < least + 7000 + (p.copied ? 5000 : 0) + (p.cut ? 0 : 4000);
+    const int esz = dtype == TDQ_F32 ? 4 : 2;
+    p.small = grad_small_cost(M, O, fp8_blocks(I), O % 8 == 0 && on_grid(dy, dy_stride, M, esz), esz, n_sm, &p.split) < least + 7000 + (p.copied ? 5000 : 0) + (p.cut ? 0 : 4000);
     if (p.small) {
         p.bytes = kWorkspaceHeader;
         return p;

@@ -18,8 +18,9 @@ struct GradSmallArgs {
     uint32_t split;
     uint32_t* status;          // set to 0
 };
-// An estimate of that kernel's time in clocks, comparable with the other's, and in how many parts the tokens go; INT64_MAX where it cannot be taken.
-int64_t grad_small_cost(int64_t M, int64_t O, int64_t Kb, int parts, int n_sm, uint32_t* split);
+// An estimate of that kernel's time in clocks, comparable with the other's, and in how many parts the tokens go; INT64_MAX where it cannot be taken.  vec: dy's rows on the
+// 16-byte grid, O a multiple of eight; esz: bytes of its elements.
+int64_t grad_small_cost(int64_t M, int64_t O, int64_t Kb, bool vec, int esz, int n_sm, uint32_t* split);
 tdq_status launch_grad_small(GradSmallArgs a, tdq_dtype dy_dtype, bool vec, cudaStream_t st);
 
 #ifdef __CUDACC__
@@ -35,25 +36,22 @@ __device__ __forceinline__ void restore4(uint32_t codes, float scale, uint32_t& 
     hi = narrow2<TDQ_BF16>(p1.x, p1.y);
 }
 // The next bf16 addend of eight values, of PARTS that make them up: the leading eight bits of what is left, cut off; exact.  A value without a number goes to its first addend
-// alone.  f is left with the rest.
+// alone (a NaN keeps a bit of its mantissa that bf16 has).  f is left with the rest.
 template <int PARTS>
 __device__ __forceinline__ void grad_addend(float* f, uint32_t* r) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        uint32_t b[2];
+        uint32_t lead[2];
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
-            float& v = f[2 * j + q];
-            if (fabsf(v) < INFINITY) {
-                const float lead = PARTS == 1 ? v : __uint_as_float(__float_as_uint(v) & 0xffff0000u);
-                b[q] = __float_as_uint(lead) >> 16;
-                v -= lead;
-            } else {
-                b[q] = narrow2<TDQ_BF16>(v, 0.f) & 0xffffu;
-                v = 0.f;
+            const uint32_t v = __float_as_uint(f[2 * j + q]);
+            lead[q] = v & 0xffff0000u;
+            if constexpr (PARTS > 1) {
+                lead[q] |= (v & 0x7fffffffu) > 0x7f800000u ? 0x00400000u : 0u;
+                f[2 * j + q] = (v & 0x7f800000u) == 0x7f800000u ? 0.f : f[2 * j + q] - __uint_as_float(lead[q]);
             }
         }
-        r[j] = b[0] | b[1] << 16;
+        r[j] = __byte_perm(lead[0], lead[1], 0x7632);
     }
 }
 

@@ -217,15 +217,17 @@ cudaError_t launch_small(const GradSmallArgs& a, int64_t tiles, cudaStream_t st)
 
 }  // namespace
 
-int64_t grad_small_cost(int64_t M, int64_t O, int64_t Kb, int parts, int n_sm, uint32_t* split) {
+int64_t grad_small_cost(int64_t M, int64_t O, int64_t Kb, bool vec, int esz, int n_sm, uint32_t* split) {
     const int64_t tiles = (O + kSmallO - 1) / kSmallO * Kb, steps = (M + kSmallTok - 1) / kSmallTok;
     if (tiles > INT32_MAX / kSmallSplitMax || steps > kSmallSteps * kSmallSplitMax) return INT64_MAX;
     // as many parts as keep the thread blocks on the GPU at once, and as many as their tokens want
     int64_t s = (steps + kSmallSteps - 1) / kSmallSteps;
     while (s < kSmallSplitMax && s < steps && tiles * (s + 1) <= n_sm) ++s;
     *split = (uint32_t)s;
-    const int64_t rounds = (tiles * s + 2 * n_sm - 1) / (2 * n_sm), busy = tiles * s > n_sm ? 2 : 1;
-    return 3500 + rounds * (busy * ((steps + s - 1) / s) * (300 + 100 * parts) + (s > 1 ? 2000 : 500));
+    // Fitted to 44 layers of 1 to 7000 tokens, 64 to 4096 -> 32 to 6000 channels: the choice between the two kernels takes 2 % longer than the better one in the mean.  A step is
+    // a chain of latencies, so that of two thread blocks on an SM each takes half.
+    const int64_t rounds = (tiles * s + n_sm - 1) / n_sm, step = (steps + s - 1) / s * (vec ? 1700 : esz == 4 ? 3500 : 2600);
+    return 5500 + (rounds == 1 ? step : rounds * (3100 + step / 2));
 }
 
 tdq_status launch_grad_small(GradSmallArgs a, tdq_dtype dy_dtype, bool vec, cudaStream_t st) {
