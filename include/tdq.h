@@ -367,15 +367,16 @@ tdq_status tdq_activation_backward_fp8(const void* dh, tdq_dtype dtype, int64_t 
  *   dw[o,i] = sum_m dy[m,o] x[m,i];    db[o] = sum_m dy[m,o]        with x[m,i] = bf16(code[m,i] scale[m,i/128])
  *   on the tensor cores' bf16 instructions.  x is exact where the scales are powers of two (tdq_quantize_act_fp8_pow2, tdq_layer_norm with TDQ_NORM_POW2); other
  *   scales are taken too, with x rounded to bf16.  dy is taken exactly: bf16 as it is, fp16 and float32 as sums of two and three bf16 numbers (two and three times the
- *   work).  Sums are binary32, at most 512 tokens (of one of the addends) in the tensor core's accumulator and the rest added to them; what a tile is cut into is
- *   added in order: the same call gives the same bits on GPUs of one size.
+ *   work).  Sums are binary32, at most 512 tokens in a tensor core's accumulator at a time and their sums added in binary32; what a tile is cut into is added in order:
+ *   the same call gives the same bits on GPUs of one size.
  *   dy      [M, O] float32, bf16 or fp16, rows dy_row_stride elements apart (>= O).
  *   xcodes  [M, I_pad] E4M3, 16-byte aligned, I_pad = 128 ceil(I/128), and xscale [M, I_pad/128].  A NaN code or scale makes the gradients that it reaches NaN.
  *   dw      [O, I] dw_dtype (float32, bf16 or fp16, rounded to nearest even from binary32), rows dw_row_stride apart (>= I), overwritten.   db  NULL or [O] float32.
  *   workspace  at least tdq_fp8_weight_grad_workspace_bytes() of the same arguments (dy is looked at for its alignment only), 16-byte aligned, on the current
  *           device's size: the status word that tdq_workspace_status() reads, parts of tiles, and dy's addends where it is not bf16 on the 16-byte grid.  Not shared by
  *           calls that overlap in time.
- * O == 0 is a no-op; M == 0 gives zeros and needs no workspace.  The gradient of the layer's input is a layer of its own: tdq_fp8_linear on codes of dy and of the
+ * O == 0 is a no-op; M == 0 gives zeros and needs no workspace.  TDQ_ERR_UNSUPPORTED for M above 7 10^8, O or I above 2^31 - 513, more than 2^31 - 1 stages (of 64 tokens of an
+ * addend and 256 x 256 of dw) or 2^24 tiles.  The gradient of the layer's input is a layer of its own: tdq_fp8_linear on codes of dy and of the
  * transposed weight.
  */
 tdq_status tdq_fp8_weight_grad(const void* dy, tdq_dtype dy_dtype, int64_t dy_row_stride, const uint8_t* xcodes, const float* xscale, int64_t M, int64_t O,

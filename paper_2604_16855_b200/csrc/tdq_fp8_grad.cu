@@ -7,13 +7,18 @@
 //               64 tokens x 64 outputs a box, an operand whose slow axis is the sum's) and one block of 128 channels, written in the same layout by the
 //               restoring warps.  64 tokens a stage: 16 KB of each.
 //   sum         binary32 accumulators in TMEM (two of 256 columns), taken to binary32 registers every kGroup stages: the tensor core drops what it adds below
-//               the accumulator's last place, which over a long sum leaves more than binary32's own rounding.
-//   work        all stages of all tiles in one row, cut in equal pieces, one for every pair of SMs; a tile that is cut goes to the workspace in parts, which a second
-//               kernel adds in order.  No atomics: the same call gives the same bits.
+//               the accumulator's last place (32768 tokens in one: off by 5.3e-7 of the result, of a float32 dy 2.5e-6; so 1.6e-7 and 1.9e-7, like a product in binary32).
+//   work        whole tiles, or all stages of all tiles in one row, cut in pieces for the pairs of SMs; a tile that is cut goes to the workspace in parts, which a second kernel
+//               adds in order (several vectors a thread there: no gain).  No atomics: the same call gives the same bits.
 //   dy          bf16 on the 16-byte grid is read in place; fp16 and float32 are cut into two and three bf16 addends (exact) and rows off the grid copied,
 //               into the workspace, and the sum goes over all addends.
 //
-//   warps 0, 1  copies of dy; the instructions (CTA 0)      warps 4-11  sums and output      warps 12-19  restore x, sum db
+//   warps 0, 1  copies of dy; the instructions (CTA 0)      warp 3  copies of codes      warps 4-11  sums and output      warps 12-19  restore x, sum db
+//
+// Bound by the restoring warps' chain (codes, conversion, shared memory, notice: 580 clocks a stage, the tensor core's share 512) and by power: 16384 tokens, 1024 -> 4096 bf16
+// 122 us from a graph at 1.6 GHz (the library's product of the restored matrices, which then are in memory, 94 to 107).  Little work goes to another kernel
+// (tdq_fp8_grad_small.cu).  Not kept: arrivals that release at cluster scope (5000 clocks a stage), loads of codes and scales by the restoring warps themselves (150 us for 139 with all
+// else the same), a longer stay in the accumulator (3 % faster).
 #include <algorithm>
 #include <numeric>
 
@@ -78,7 +83,7 @@ static_assert(sizeof(Ctrl) + sizeof(GradCtrl) <= kGradCtrl, "control block outgr
 
 // A cluster's stages, tile by tile, in the order in which it adds them: the tile at its end first, which begins with the first tokens, then the rest, which begins in the
 // middle of a tile.  So all clusters go through the tokens at about the same time, and what several tiles read is read from memory once (from the piece's
-// begin on instead: 16384 tokens, 1024 -> 4096 bf16 TODO us).
+// begin on instead: 16384 tokens, 1024 -> 4096 bf16 135 us for 122, 2048 -> 4096 264 for 235).
 struct Piece {
     int32_t per_tile, begin, end, last;                      // last: where its last tile's stages begin, if it has more than one tile; else its end
     __device__ Piece(int32_t per_tile_, const Cut& cut, int32_t w) : per_tile(per_tile_), begin(cut.begin(w)), end(cut.begin(w + 1)) {

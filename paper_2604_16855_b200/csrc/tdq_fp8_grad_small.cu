@@ -4,7 +4,8 @@
 // tiles and for db, needs a second and a third kernel.  Here a thread block of eight warps has 64 outputs x one block of 128 channels in its registers (mma.sync, 32 x 32
 // a warp), 32 tokens at a time from global memory through registers, cut into bf16 addends and restored on the way to shared memory; the thread blocks of a cluster share a
 // tile's tokens, at most 512 each, and add their sums in order over distributed shared memory.
-// Measured, from a graph: SMALL_TIMES.
+// Bound by the chain of a step (loads, conversion, shared memory, instructions: 1700 clocks, with two steps on their way as well).  From a graph, db included, against the other
+// kernel: 64 x 256 -> 256 bf16 5.7 us for 8.3, 247 x 370 -> 37 fp32 5.0 for 12.2, 1000 x 300 -> 300 bf16 7.4 for 12.7, 1 x 1073 -> 208 fp16 6.0 for 10.9.
 #include <type_traits>
 
 #include "tdq_fp8_grad.cuh"

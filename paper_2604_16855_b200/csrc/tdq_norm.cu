@@ -3,7 +3,7 @@
 //   mean = 1/C sum x;   rstd = 1 / sqrt(1/C sum (x - mean)^2 + eps);   y = (x - mean) rstd w + b
 //
 // Bound by HBM: the input is read once and the output written once.  Blocks stay and go through rows, the next two already on their way, with the weights in registers
-// (one row a group of a block that ends with it: 16384 x 2048 bf16 38 us; now FWD_TIME).  A row stays in the registers of the threads that share it, as binary32 between its passes: sum, then sum of squares about the mean (not sum x^2 - C mean^2,
+// (one row a group of a block that ends with it: 16384 x 2048 bf16 38 us, now 27).  A row stays in the registers of the threads that share it, as binary32 between its passes: sum, then sum of squares about the mean (not sum x^2 - C mean^2,
 // which loses what a far mean leaves), then the outputs.  Sums are binary32: lane by lane, then a butterfly, in the same order every time.
 // Rows off the 16-byte grid pass through shared memory: aligned vectors in, words shifted out, and the other way round for the output.
 #include "tdq_rows.cuh"

@@ -22,8 +22,8 @@ struct NormBackArgs {
     bool w_vec;                                // weights on the 16-byte grid
 };
 
-// Threads of a block: as many whole groups as 80 registers a thread allow (128 for rows off the grid; 64 where a row takes more threads).  Whether the next row is on its
-// way while one is worked on.
+// Threads of a block: as many whole groups as 80 registers a thread allow (128 for rows off the grid; 64 where a row takes more threads; binary32 with 64 for all: 9000 x 768
+// 16.4 us for 15.5).  Whether the next row is on its way while one is worked on.
 template <int T, bool VEC> constexpr int kBackThreads = T > 384 ? T : (VEC ? 768 : 512) / T * T;
 template <int T, int V> constexpr int kBackAhead = V == 1 && T <= 768 ? 1 : 0;
 
@@ -227,8 +227,8 @@ cudaError_t pick_back(const NormBackArgs& a, RowShape s, unsigned blocks, int de
 }
 template <int DT>
 cudaError_t backward(const NormBackArgs& a, bool vec, unsigned blocks, int dev, cudaStream_t st) {
-    // A vector a thread: the column sums of more would leave no registers for the next row, and two vectors in 512 threads an SM took twice as long (18464 x 768 bf16 with
-    // an addend 39 us, now BACK_TIME).
+    // A vector a thread: the column sums of more would leave no registers for the next row, and two or three in 384 or 512 threads an SM took longer (18464 x 768 bf16
+    // with an addend 39 us, now 28), as rows by asynchronous copies through shared memory did (29).
     static const int threads[] = {8, 16, 32, 64, 96, 128, 192, 256, 384, 512, 768, 1024};
     const int64_t vecs = (a.C + kPerVec<DT> - 1) / kPerVec<DT>;
     RowShape s = {1024, vecs <= 1024 ? 1 : vecs <= 2048 ? 2 : 4};
