@@ -340,11 +340,13 @@ def activation_backward_fp8(dh, zcodes, zscale, activation, *, dz=None):
 
 def fp8_weight_grad_workspace(dy: torch.Tensor, cin: int) -> torch.Tensor:
     """A workspace for fp8_weight_grad with gradients laid out as dy [..., O] is."""
+    dtype = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}.get(dy.dtype)
+    if dtype is None:
+        raise TypeError("dy must be float32, bfloat16 or float16, got %s" % dy.dtype)
     rows = dy if dy.dim() == 2 else dy.reshape(-1, dy.shape[-1])
     M, O = rows.shape
     with torch.cuda.device(dy.device):
-        n = int(_lib.tdq_fp8_weight_grad_workspace_bytes(_ptr(rows), {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}[dy.dtype],
-                                                         rows.stride(0) if M > 1 else O, M, O, cin))
+        n = int(_lib.tdq_fp8_weight_grad_workspace_bytes(_ptr(rows), dtype, rows.stride(0) if M > 1 else O, M, O, cin))
     return torch.zeros((n,), dtype=torch.uint8, device=dy.device)
 
 

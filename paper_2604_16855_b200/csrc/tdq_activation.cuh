@@ -28,15 +28,15 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 }
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
 
-// Gaussian tail: with a = |z|, e = exp(-a^2 / 2) and q = Phi(-a) = 1/2 erfcx(a / sqrt 2) e.  The smooth factor is a polynomial of degree 10 on [0, 5], fitted by
+// Gaussian tail: with a = |z|, e = exp(-a^2 / 2) and q = Phi(-a) = p e, p = 1/2 erfcx(a / sqrt 2).  The smooth factor p is a polynomial of degree 10 on [0, 5], fitted by
 // least squares with weights moved to the largest errors of max(a, 1) q: 1.5e-7 at most, roundings of its evaluation among them (behind 5 the factor stays what it is there,
 // b = min(a, 5), and b q is within 8e-8 of a q).  An element costs
 // fourteen multiply-adds in all and one turn of the special functions' unit, which takes eight times as long as one.
-__device__ __forceinline__ void gauss_tail(float2 z, float2& b, float2& e, float2& q) {
+__device__ __forceinline__ void gauss_tail(float2 z, float2& b, float2& e, float2& p) {
     const float2 g = __fmul2_rn(__fmul2_rn(z, z), both(-0.72134752f));          // -log2(e) / 2
     e = make_float2(ex2(g.x), ex2(g.y));
     b = make_float2(min_nan(fabsf(z.x), 5.f), min_nan(fabsf(z.y), 5.f));
-    float2 p = both(1.23802897e-06f);
+    p = both(1.23802897e-06f);
     p = __ffma2_rn(p, b, both(-2.84340113e-05f));
     p = __ffma2_rn(p, b, both(0.00029121447f));
     p = __ffma2_rn(p, b, both(-0.00178629335f));
@@ -47,7 +47,6 @@ __device__ __forceinline__ void gauss_tail(float2 z, float2& b, float2& e, float
     p = __ffma2_rn(p, b, both(0.249865487f));
     p = __ffma2_rn(p, b, both(-0.398932129f));
     p = __ffma2_rn(p, b, both(0.499999881f));
-    q = __fmul2_rn(p, e);
 }
 // 1 / (1 + exp(-z))
 __device__ __forceinline__ float2 sigmoid(float2 z) {
@@ -62,9 +61,9 @@ __device__ __forceinline__ float2 activate(float2 z) {
     if constexpr (ACT == TDQ_ACT_RELU) {
         return make_float2(max_nan(z.x, 0.f), max_nan(z.y, 0.f));
     } else if constexpr (ACT == TDQ_ACT_GELU) {              // z Phi(z) = max(z, 0) - |z| Phi(-|z|)
-        float2 b, e, q;
-        gauss_tail(z, b, e, q);
-        return __ffma2_rn(make_float2(-b.x, -b.y), q, make_float2(max_nan(z.x, 0.f), max_nan(z.y, 0.f)));
+        float2 b, e, p;
+        gauss_tail(z, b, e, p);
+        return __ffma2_rn(make_float2(-b.x, -b.y), __fmul2_rn(p, e), make_float2(max_nan(z.x, 0.f), max_nan(z.y, 0.f)));
     } else if constexpr (ACT == TDQ_ACT_GELU_TANH) {
         return __fmul2_rn(z, sigmoid(__fmul2_rn(z, __ffma2_rn(__fmul2_rn(z, z), both(kTanhB), both(kTanhA)))));
     } else if constexpr (ACT == TDQ_ACT_SILU) {
@@ -77,11 +76,11 @@ template <int ACT>
 __device__ __forceinline__ float2 slope(float2 z) {
     if constexpr (ACT == TDQ_ACT_RELU) {
         return make_float2(z.x > 0.f ? 1.f : 0.f, z.y > 0.f ? 1.f : 0.f);
-    } else if constexpr (ACT == TDQ_ACT_GELU) {              // Phi(z) + z phi(z); the odd part is 1/2 - q + a phi
-        float2 b, e, q;
-        gauss_tail(z, b, e, q);
+    } else if constexpr (ACT == TDQ_ACT_GELU) {              // Phi(z) + z phi(z); the odd part is 1/2 - q + a phi = 1/2 + e (a / sqrt(2 pi) - p)
+        float2 b, e, p;
+        gauss_tail(z, b, e, p);
         const float2 a = make_float2(min_nan(fabsf(z.x), 20.f), min_nan(fabsf(z.y), 20.f));   // exp(-200) is 0 in binary32
-        const float2 h = __ffma2_rn(__fmul2_rn(a, e), both(0.398942280f), __ffma2_rn(q, both(-1.f), both(0.5f)));
+        const float2 h = __ffma2_rn(e, __ffma2_rn(a, both(0.398942280f), make_float2(-p.x, -p.y)), both(0.5f));
         return make_float2(0.5f + copysignf(h.x, z.x), 0.5f + copysignf(h.y, z.y));
     } else if constexpr (ACT == TDQ_ACT_GELU_TANH) {         // s + z s (1 - s) (2 u)'
         const float2 z2 = __fmul2_rn(z, z);

@@ -1,7 +1,9 @@
 // tdq_activation_backward_fp8: dz = dh activation'(z), z = code x scale kept in 8 bits.
 //
-// Bound by HBM: dh, a byte of z and dz an element.  Sixteen channels a thread, eight threads a block of 128, 16-byte accesses; rows of dh or dz off the 16-byte
-// grid go element by element, lanes along the row.
+// Bound by HBM: dh, a byte of z and dz an element; of 16 bits GELU's slope is bound by instructions as well (16384 x 4096 bf16 59 us, SiLU 51, ReLU 50; float32 GELU 88).  A vector of 16 bytes is
+// eight or four channels, neighbouring lanes have neighbouring vectors, and a thread has two or four of them, 32 lanes apart.  Sixteen channels in a row a thread, whose
+// accesses leave gaps: 62, 53, 50 and 102 us; blocks that stay and load ahead: 65, 54, 54 and 96.  Rows of dh or dz off the 16-byte grid go element by element,
+// lanes along the row.
 #include "tdq_activation.cuh"
 #include "tdq_rows.cuh"
 
@@ -27,37 +29,53 @@ __device__ __forceinline__ float2 widen_codes(uint32_t two) {
     return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 
+template <int DT> constexpr int kActVecs = DT == TDQ_F32 ? 2 : 4;   // a thread's (4 and 2: float32 88 us for 88, bf16 62 for 59)
+
 template <int DT, int ACT>
 __global__ void __launch_bounds__(kActThreads) act_back_kernel(const ActArgs a) {
     using E = typename Elem<DT>::T;
-    constexpr int P = kPerVec<DT>, kVecs = 16 / P;
+    constexpr int P = kPerVec<DT>, kLanes = 128 / P, V = kActVecs<DT>;         // lanes of a block
     pdl_wait();
     pdl_trigger();
-    const uint32_t t = blockIdx.x * kActThreads + threadIdx.x, b = t >> 3;
-    if (b >= a.n_blocks) return;
-    const uint32_t m = b / a.Kb, k = b - m * a.Kb;
-    const int c0 = (int)k * 128 + (int)(threadIdx.x & 7) * 16;
-    if (c0 >= a.C) return;
-    const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const E*>(a.dh) + (int64_t)m * a.dh_stride + c0);
-    uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<E*>(a.dz) + (int64_t)m * a.dz_stride + c0);
-    const uint4 code = __ldg(reinterpret_cast<const uint4*>(a.codes) + t);
-    uint4 v[kVecs];
+    const uint32_t b0 = (blockIdx.x * (kActThreads / 32) + (threadIdx.x >> 5)) * (V * 32 / kLanes) + (threadIdx.x & 31) / kLanes, lane = threadIdx.x % kLanes;
+    uint32_t m = b0 / a.Kb, k = b0 - m * a.Kb;
+    uint4 v[V], *dst[V];
+    uint32_t code[V][P / 4];
+    float scale[V];
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) v[i] = c0 + i * P < a.C ? src[i] : make_uint4(0, 0, 0, 0);
-    const float scale = __ldg(a.scale + b);
-    const uint32_t words[4] = {code.x, code.y, code.z, code.w};
+    for (int i = 0; i < V; ++i) {
+        const uint32_t b = b0 + i * (32 / kLanes);
+        const int c = (int)(k * 128 + lane * P);
+        dst[i] = nullptr;
+        v[i] = make_uint4(0, 0, 0, 0);
+        scale[i] = 0.f;
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i) {
+        for (int j = 0; j < P / 4; ++j) code[i][j] = 0;
+        if (b < a.n_blocks && c < a.C) {
+            v[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const E*>(a.dh) + (int64_t)m * a.dh_stride + c);
+            dst[i] = reinterpret_cast<uint4*>(reinterpret_cast<E*>(a.dz) + (int64_t)m * a.dz_stride + c);
+            const uint8_t* from = a.codes + (int64_t)b * 128 + lane * P;
+            if constexpr (P == 8) {
+                const uint2 r = __ldg(reinterpret_cast<const uint2*>(from));
+                code[i][0] = r.x;
+                code[i][P / 4 - 1] = r.y;
+            } else code[i][0] = __ldg(reinterpret_cast<const uint32_t*>(from));
+            scale[i] = __ldg(a.scale + b);
+        }
+        for (k += 32 / kLanes; k >= a.Kb; k -= a.Kb) ++m;
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
         float f[P];
         widen_vec<DT>(v[i], f);
 #pragma unroll
         for (int j = 0; j < P; j += 2) {
-            const float2 z = __fmul2_rn(widen_codes(words[(i * P + j) >> 2] >> (8 * ((i * P + j) & 3))), both(scale));
+            const float2 z = __fmul2_rn(widen_codes(code[i][j >> 2] >> (8 * (j & 3))), both(scale[i]));
             const float2 d = __fmul2_rn(make_float2(f[j], f[j + 1]), slope<ACT>(z));
             f[j] = d.x;
             f[j + 1] = d.y;
         }
-        if (c0 + i * P < a.C) dst[i] = narrow_vec<DT>(f);
+        if (dst[i]) *dst[i] = narrow_vec<DT>(f);
     }
 }
 
@@ -99,7 +117,7 @@ __global__ void __launch_bounds__(kActThreads) act_back_ragged_kernel(const ActA
 
 template <int DT, int ACT>
 cudaError_t launch_act(const ActArgs& a, bool vec, cudaStream_t st) {
-    const uint32_t per = vec ? kActThreads / 8 : kActThreads / 32;
+    const uint32_t per = vec ? kActThreads / 32 * (kActVecs<DT> * 32 * kPerVec<DT> / 128) : kActThreads / 32;
     return launch_pdl(vec ? act_back_kernel<DT, ACT> : act_back_ragged_kernel<DT, ACT>, dim3((a.n_blocks + per - 1) / per), dim3(kActThreads), 0, st, a);
 }
 template <int DT>
