@@ -4,7 +4,8 @@
  * The library quantizes token activations with token-group scales (DSTG) whose clip
  * radius is projected by two bounds (DCRP), quantizes weights per output channel, and
  * runs the W4A4 linear layer on the 4-bit codes.  Beside them stand a linear layer on 8-bit floating point
- * codes with its quantizers, and the norm and rotation of queries and keys that follows a qkv layer.
+ * codes with its quantizers, the norm and rotation of queries and keys that follows a qkv layer, and what
+ * surrounds an 8-bit layer: layer norm, activation and residual, and gradients from activations kept in 8 bits.
  *
  * Conventions shared by every call
  *   - Unless a parameter is marked HOST, pointers are DEVICE pointers owned by the caller.
