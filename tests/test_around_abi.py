@@ -128,3 +128,8 @@ def test_activation_names(tdq):
     for f in (lambda: tdq.fp8_linear(x, x, x, x, activation="tanh"), lambda: tdq.activation_backward_fp8(x, x, x, "tanh"), lambda: tdq.activation_backward_fp8(x, x, x, "gelu")):
         with pytest.raises(ValueError):
             f()
+
+
+def test_workspace_for_gradients_of_another_type(tdq):
+    with pytest.raises(TypeError, match="float64"):
+        tdq.fp8_weight_grad_workspace(torch.zeros((2, 8), dtype=torch.float64), 128)
