@@ -172,6 +172,13 @@ def test_activation_backward(tdq, m, n, pitch, x_type, act):
     assert tdq.activation_backward_fp8(e, zc[:0], zs[:0], act).shape == (0, n)
 
 
+@pytest.mark.parametrize("x_type", list(TYPES))
+@pytest.mark.parametrize("m,n", [(301, 128), (1, 256), (100, 384), (65, 640), (9, 72), (33, 896)])
+def test_activation_backward_of_few_blocks_a_row(tdq, m, n, x_type):
+    """A thread's vectors lie in several rows."""
+    test_activation_backward(tdq, m, n, 0, x_type, "gelu")
+
+
 @pytest.mark.parametrize("act", ACTS)
 def test_slopes_are_the_values_differences(tdq, act):
     """The epilogue's values at z - d and z + d against the slope at z, both as the kernels compute them."""
