@@ -368,7 +368,7 @@ tdq_status tdq_activation_backward_fp8(const void* dh, tdq_dtype dtype, int64_t 
  *   dw[o,i] = sum_m dy[m,o] x[m,i];    db[o] = sum_m dy[m,o]        with x[m,i] = bf16(code[m,i] scale[m,i/128])
  *   on the tensor cores' bf16 instructions.  x is exact where the scales are powers of two (tdq_quantize_act_fp8_pow2, tdq_layer_norm with TDQ_NORM_POW2); other
  *   scales are taken too, with x rounded to bf16.  dy is taken exactly: bf16 as it is, fp16 and float32 as sums of two and three bf16 numbers (two and three times the
- *   work).  Sums are binary32, at most 512 tokens in a tensor core's accumulator at a time and their sums added in binary32; what a tile is cut into is added in order:
+ *   work; what a float32 number has below 2^-133, bf16's smallest, is lost).  Sums are binary32, at most 512 tokens in a tensor core's accumulator at a time and their sums added in binary32; what a tile is cut into is added in order:
  *   the same call gives the same bits on GPUs of one size.
  *   dy      [M, O] float32, bf16 or fp16, rows dy_row_stride elements apart (>= O).
  *   xcodes  [M, I_pad] E4M3, 16-byte aligned, I_pad = 128 ceil(I/128), and xscale [M, I_pad/128].  A NaN code or scale makes the gradients that it reaches NaN.
