@@ -72,6 +72,7 @@ __device__ __forceinline__ float2 activate(float2 z) {
         return z;
     }
 }
+// For |z| < 10^13: products of larger ones leave binary32's range in the tanh form, SiLU's at an infinity, and inf 0 is no slope.
 template <int ACT>
 __device__ __forceinline__ float2 slope(float2 z) {
     if constexpr (ACT == TDQ_ACT_RELU) {
