@@ -1,4 +1,4 @@
-// tdq_fp8_weight_grad for little work: dw[o,i] = sum_m dy[m,o] x[m,i], db[o] = sum_m dy[m,o] in one kernel, without a workspace.
+// tdq_fp8_weight_grad for little work: dw[o,i] = sum_m dy[m,o] x[m,i], db[o] = sum_m dy[m,o] in one kernel; of the workspace only the status word.
 //
 // What counts is the way from launch to result: the kernel for large layers (tdq_fp8_grad.cu) sets up tensor memory and copy engine and, for a dy that is not bf16, for cut
 // tiles and for db, needs a second and a third kernel.  Here a thread block of eight warps has 64 outputs x one block of 128 channels in its registers (mma.sync, 32 x 32
@@ -195,8 +195,13 @@ __global__ void __launch_bounds__(kSmallThreads, 2) fp8_grad_small_kernel(const 
             a.db[o] = d;
         }
     }
-    if (split > 1)                                           // no block leaves while another reads from it
+    // No block leaves while another reads from it.  The lanes meet first: the barrier's instruction is the whole warp's, and the rows' loops are not.  Relaxed: what a warp has read from
+    // other blocks is there by then, as it has gone into a store (a row's first lane has a channel, so that every load of the warp has been waited for); an
+    // arrival that releases waits for those stores themselves (64 x 256 -> 256 bf16 6.1 us for 5.7).
+    if (split > 1) {
+        __syncwarp();
         asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
 }
 
 template <int DT, bool VEC>
