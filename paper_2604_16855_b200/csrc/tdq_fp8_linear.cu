@@ -369,9 +369,11 @@ __device__ __forceinline__ void split_body(const Fp8Args& a, const std::conditio
                         if (j < left) y[j] = (uint16_t)((j & 2 ? w1 : w0) >> (16 * (j & 1)));
             }
         }
+        __syncwarp();
         if (split > 1) cluster_arrive_relaxed();                 // nothing more is read
     }
     if (c->abort_flag) __nanosleep(1000000);                 // a wait gave up: give copies and tensor core a moment
+    __syncwarp();                                            // out of the loops over outputs: what follows is the whole warp's
     if (split > 1) cluster_wait();                           // no CTA leaves while another sends to it or reads from it
     if (warp == 2)
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "n"(kSplitSlots * NT) : "memory");
