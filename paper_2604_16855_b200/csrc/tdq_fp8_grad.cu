@@ -207,6 +207,12 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
                 }
                 k += t.len;
             }
+            // the last stages' commits reach this CTA too: waited for, so that none is under way when it leaves
+#pragma unroll 1
+            for (int i = 0; i < kGradStages; ++i) {
+                fp8_wait(empty_s + s * 8, ph, c, a.status, 5u);
+                if (++s == kGradStages) { s = 0; ph ^= 1; }
+            }
         } else if (warp == 3) {
             // -------------------------------------------------------- copies of codes, a slot for each pair of restoring warps
             const uint32_t codes_bar = smem_u32(&g->codes[0]), taken_s = smem_u32(&g->taken[0]);
@@ -259,6 +265,9 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
                 }
                 k += t.len;
             }
+            // and so do the other CTA's arrivals, of the last two accumulators' readers
+#pragma unroll 1
+            for (int i = 0; i < 2; ++i, ++group) fp8_wait(tempty_s + (group & 1u) * 8, ((group >> 1) & 1u) ^ 1u, c, a.status, 3u);
         }
     } else if (warp < kFillWarp0) {
         // ------------------------------------------------------------ sums and output
@@ -483,7 +492,8 @@ fp8_grad_kernel(const GradArgs a, const __grid_constant__ CUtensorMap dymap, con
     tc_fence_before();
     __syncthreads();
     if (c->abort_flag) __nanosleep(1000000);                 // a wait gave up: give copies and tensor core a moment
-    // Neither CTA leaves while the other may still signal it.  Relaxed: an arrival that releases waits for the thread's stores to memory (1400 clocks).
+    // Neither CTA leaves while the tensor core may still read its operands; signals from the other have been waited for, each by one of the warps above.  Relaxed: an arrival
+    // that releases waits for the thread's stores to memory (1400 clocks).
     asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (warp == 2)
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "n"(512) : "memory");

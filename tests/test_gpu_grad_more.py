@@ -30,3 +30,19 @@ def test_launches_that_follow_at_once(tdq, m, o, i, dy_type):
     for (dy, xc, xs), out in zip(sets, outs):
         check(*out[0], dy, xc, xs, i, {"bf16": 1, "fp16": 2, "fp32": 3}[dy_type])
         assert all(torch.equal(dw, out[0][0]) and torch.equal(db, out[0][1]) for dw, db in out)
+
+
+# pieces of one stage and of a few, with and without addends: the last commits and arrivals come when there is little left to do
+@pytest.mark.parametrize("m,o,i", [(9217, 63, 147), (64, 5000, 2100), (4617, 960, 320), (20000, 8, 8)])
+@pytest.mark.parametrize("dy_type", ["bf16", "fp32"])
+def test_large_layers_that_follow_at_once(tdq, m, o, i, dy_type):
+    sets = [inputs(tdq, m, o, i, TYPES[dy_type], seed=s) for s in (3, 4)]
+    outs = [[(torch.zeros((o, i), device="cuda"), torch.zeros((o,), device="cuda")) for _ in range(20)] for _ in sets]
+    ws = tdq.fp8_weight_grad_workspace(sets[0][0], i)
+    for n in range(20):
+        for (dy, xc, xs), out in zip(sets, outs):
+            tdq.fp8_weight_grad(dy, xc, xs, i, dw=out[n][0], db=out[n][1], workspace=ws)
+    assert tdq.workspace_status(ws) == (tdq.OK, 0)
+    for (dy, xc, xs), out in zip(sets, outs):
+        check(*out[0], dy, xc, xs, i, {"bf16": 1, "fp32": 3}[dy_type])
+        assert all(torch.equal(dw, out[0][0]) and torch.equal(db, out[0][1]) for dw, db in out)
