@@ -135,7 +135,7 @@ __device__ __forceinline__ void take_ragged(const uint4* stage, int off, int n, 
 }
 // A row on its way.  fetch() starts the loads, take() gives vectors t, t + T, .. of the row, zeros behind its n channels.  Off the grid (!VEC) a row's aligned vectors (one that
 // holds an element of the row is read whole; what lies beside the row in it is not used) pass through the group's stage: put() between two group_syncs, the first
-// of which says that what was there has been read.
+// of which says that what was there has been read.  Plain loads: the output may be an input, and the read-only path is for what nobody writes meanwhile.
 template <int DT, int T, int V, bool VEC>
 struct Row {
     using E = typename Elem<DT>::T;
@@ -146,14 +146,14 @@ struct Row {
         if constexpr (VEC) {
 #pragma unroll
             for (int i = 0; i < V; ++i)
-                raw[i] = on && (t + T * i) * P < n ? __ldg(reinterpret_cast<const uint4*>(row) + t + T * i) : make_uint4(0, 0, 0, 0);
+                raw[i] = on && (t + T * i) * P < n ? reinterpret_cast<const uint4*>(row)[t + T * i] : make_uint4(0, 0, 0, 0);
         } else {
             const uintptr_t at = reinterpret_cast<uintptr_t>(row);
             off = (int)(at & 15);
             const int n_vec = on ? (off + n * (int)sizeof(E) + 15) >> 4 : 0;
             const uint4* src = reinterpret_cast<const uint4*>(at & ~(uintptr_t)15);
 #pragma unroll
-            for (int i = 0; i < N; ++i) raw[i] = t + T * i < n_vec ? __ldg(src + t + T * i) : make_uint4(0, 0, 0, 0);
+            for (int i = 0; i < N; ++i) raw[i] = t + T * i < n_vec ? src[t + T * i] : make_uint4(0, 0, 0, 0);
         }
     }
     __device__ __forceinline__ void put(uint4* stage, int t) const {
