@@ -234,8 +234,7 @@ inline RowShape row_shape(int64_t vecs, int64_t M, int n_sm, int least, int most
     int t = least;
     const bool few = M < 2 * (int64_t)n_sm;
     while (t < most && vecs > (int64_t)t * (few || t < 32 ? 1 : t < 256 ? 3 : 2)) t *= 2;
-    const int v = (int)((vecs + t - 1) / t);
-    return {t, v <= 3 ? v : v <= 4 ? 4 : 8};
+    return {t, (int)((vecs + t - 1) / t)};
 }
 inline bool on_grid(const void* p, int64_t stride, int64_t M, int64_t esz) {
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (M <= 1 || stride * esz % 16 == 0);
