@@ -288,8 +288,8 @@ tdq_status tdq_quantize_act_fp8(const void* x, tdq_dtype x_dtype, int64_t B, int
 
 /*
  * The same quantizer with scales that are powers of two, for activations kept for the backward pass: scale = the smallest 2^s (s integer) with
- * a <= 448 2^s, r = 1 / scale.  code x scale is then exact in bf16, as tdq_fp8_weight_grad takes it.  Everything else as above; tdq_fp8_linear takes
- * these codes and scales like any others.
+ * a <= 448 2^s, r = 1 / scale.  code x scale is then exact in bf16, as tdq_fp8_weight_grad takes it (from |x| = 248 x 2^120 on it is 2^128, an infinity of bf16 and
+ * float32).  Everything else as above; tdq_fp8_linear takes these codes and scales like any others.
  */
 tdq_status tdq_quantize_act_fp8_pow2(const void* x, tdq_dtype x_dtype, int64_t B, int64_t N, int64_t C, int64_t row_stride_elems, uint8_t* codes,
                                      float* scale, void* cuda_stream);

@@ -3,7 +3,7 @@
 // Bound by HBM: dh, a byte of z and dz an element; of 16 bits GELU's slope is bound by instructions as well (16384 x 4096 bf16 59 us, SiLU 51, ReLU 50; float32 GELU 88).  A vector of 16 bytes is
 // eight or four channels, neighbouring lanes have neighbouring vectors, and a thread has two or four of them, 32 lanes apart.  Sixteen channels in a row a thread, whose
 // accesses leave gaps: 62, 53, 50 and 102 us; blocks that stay and load ahead: 65, 54, 54 and 96.  Rows of dh or dz off the 16-byte grid go element by element,
-// lanes along the row.
+// lanes along the row: twice the time in 16 bits (16384 x 4096 with a pitch of 4097 bf16 GELU 99 us, SiLU 85, float32 GELU 106).
 #include "tdq_activation.cuh"
 #include "tdq_rows.cuh"
 

@@ -2,9 +2,11 @@
 //
 //   mean = 1/C sum x;   rstd = 1 / sqrt(1/C sum (x - mean)^2 + eps);   y = (x - mean) rstd w + b
 //
-// Bound by HBM: the input is read once and the output written once.  Blocks stay and go through rows, the next two already on their way, with the weights in registers
-// (one row a group of a block that ends with it: 16384 x 2048 bf16 38 us, now 27).  A row stays in the registers of the threads that share it, as binary32 between its passes: sum, then sum of squares about the mean (not sum x^2 - C mean^2,
-// which loses what a far mean leaves), then the outputs.  Sums are binary32: lane by lane, then a butterfly, in the same order every time.
+// Bound by HBM: the input is read once and the output written once.  Blocks stay and go through rows, the next two already on their way (one, or none, where a row's
+// vectors or threads are many: kAhead), with the weights in registers (one row a group of a block that ends with it: 16384 x 2048 bf16 38 us, now 26).  To codes it is bound by
+// latency: 16 warps an SM, at 128 registers a thread, behind a row's two sums, its blocks' maxima and their quotients (56 % of the issue slots; 18464 x 768 bf16 13 us where the
+// bytes take 7).  A row stays in the registers of the threads that share it, as binary32 between its passes: sum, then sum of squares about the mean (not
+// sum x^2 - C mean^2, which loses what a far mean leaves), then the outputs.  Sums are binary32: lane by lane, then a butterfly, in the same order every time.
 // Rows off the 16-byte grid pass through shared memory: aligned vectors in, words shifted out, and the other way round for the output.
 #include "tdq_rows.cuh"
 
